@@ -72,6 +72,21 @@ def lib() -> ctypes.CDLL:
     L.fq_kv4_output_workspace_bytes.argtypes = [ci, ci, ci]
     L.fq_kv4_output_ws.restype = ci
     L.fq_kv4_output_ws.argtypes = [vp, vp, vp, vp, vp, ci, ci, ci, ci, vp, ctypes.c_size_t, vp]
+    c64 = ctypes.c_int64
+    L.fq_rmsnorm.restype = ci
+    L.fq_rmsnorm.argtypes = [vp, vp, vp, cf, vp, vp, ci, ci, vp]
+    L.fq_rmsnorm_quant_ws.restype = ci
+    L.fq_rmsnorm_quant_ws.argtypes = [vp, vp, vp, cf, vp, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
+    L.fq_kv4_append.restype = ci
+    L.fq_kv4_append.argtypes = [vp, c64, vp, ci, vp, vp, ci, vp, vp, vp, c64, c64, ci, ci, ci, ci, ci, vp]
+    L.fq_kv4_read.restype = ci
+    L.fq_kv4_read.argtypes = [vp, c64, c64, ci, ci, vp, vp, vp, ci, ci, vp]
+    L.fq_kv4_attention_workspace_bytes.restype = ctypes.c_size_t
+    L.fq_kv4_attention_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+    L.fq_kv4_attention_ws.restype = ci
+    L.fq_kv4_attention_ws.argtypes = [vp, vp, vp, c64, c64, ci, ci, vp, ci, vp, cf, vp, ci, ci, ci, ci, vp, ctypes.c_size_t, vp]
+    L.fq_kv4_attention_prefix_ws.restype = ci
+    L.fq_kv4_attention_prefix_ws.argtypes = [vp, vp, vp, c64, c64, ci, ci, vp, ci, vp, ci, vp, cf, vp, ci, ci, ci, ci, vp, ctypes.c_size_t, vp]
     L.fq_w4a8_gemm_ws.restype = ci
     L.fq_w4a8_gemm_ws.argtypes = [vp, vp, vp, vp, cf, vp, ci, ci, ci, vp, ctypes.c_size_t, ci, vp]
     L.fq_w4a8_gemm_add_ws.restype = ci
@@ -640,3 +655,195 @@ def fq_kv4_output(P: torch.Tensor, p_scale: torch.Tensor, V_packed: torch.Tensor
     if rc != 0:
         raise FireqError(rc, "fq_kv4_output")
     return O
+
+
+def _norm_arguments(X, weight, residual, out):
+    X = _dev(X, torch.bfloat16, "X")
+    weight = _dev(weight, torch.bfloat16, "weight")
+    if X.dim() != 2 or weight.numel() != X.shape[1]:
+        raise FireqError(-2, "fq_rmsnorm")
+    if residual is None:
+        if out is not None:
+            raise FireqError(-2, "fq_rmsnorm")
+        return X, weight, None, None
+    residual = _dev(residual, torch.bfloat16, "residual")
+    out = torch.empty_like(X) if out is None else _dev(out, torch.bfloat16, "out")
+    if residual.shape != X.shape or out.shape != X.shape:
+        raise FireqError(-2, "fq_rmsnorm")
+    return X, weight, residual, out
+
+
+def _ptr(t):
+    return 0 if t is None else t.data_ptr()
+
+
+def fq_rmsnorm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None):
+    """bf16 [M,K] RMS norm of X, or of H = bf16(X + residual): (Y, H) then.  `out` receives H and may be the residual itself
+    (the residual stream updated in place)."""
+    X, weight, residual, H = _norm_arguments(X, weight, residual, out)
+    M, K = X.shape
+    Y = torch.empty_like(X)
+    rc = lib().fq_rmsnorm(X.data_ptr(), _ptr(residual), weight.data_ptr(), ctypes.c_float(float(eps)), _ptr(H), Y.data_ptr(), M, K, _stream())
+    if rc != 0:
+        raise FireqError(rc, "fq_rmsnorm")
+    return Y if H is None else (Y, H)
+
+
+def fq_rmsnorm_quant(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: Optional[torch.Tensor] = None,
+                     out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(uint8 [M,K] E4M3 codes, float32 [M] row scales) of the RMS norm of X [M,K], the operands of fq_w4a8_gemm; with a
+    residual (codes, scales, H = bf16(X + residual)).  `out` receives H and may be the residual itself; `workspace`
+    (fq_w4a8_gemm_workspace_bytes(M, N, K) bytes or more) is prepared for fq_w4a8_gemm(..., workspace_prepared=True)."""
+    X, weight, residual, H = _norm_arguments(X, weight, residual, out)
+    M, K = X.shape
+    A = torch.empty((M, K), dtype=torch.uint8, device=X.device)
+    s = torch.empty((M,), dtype=torch.float32, device=X.device)
+    ws, nbytes = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
+    rc = lib().fq_rmsnorm_quant_ws(X.data_ptr(), _ptr(residual), weight.data_ptr(), ctypes.c_float(float(eps)), _ptr(H), A.data_ptr(),
+                                   s.data_ptr(), M, K, ws, nbytes, _stream())
+    if rc != 0:
+        raise FireqError(rc, "fq_rmsnorm_quant")
+    return (A, s) if H is None else (A, s, H)
+
+
+KV4_TILE_TOKENS, KV4_TILE_BYTES = 16, 2080
+
+
+def fq_kv4_cache(pages: int, heads: int, page: int, device=None) -> torch.Tensor:
+    """uint8 [pages, heads, page / 16, 2080]: an empty paged INT4 key/value cache (one layer's) for tokens of `heads` key/value
+    heads, `page` (a multiple of 16) to a page.  A slice of a larger tensor of that form serves too, as long as its last two
+    dimensions are contiguous."""
+    if page <= 0 or page % KV4_TILE_TOKENS:
+        raise FireqError(-2, "fq_kv4_cache")
+    return torch.zeros((pages, heads, page // KV4_TILE_TOKENS, KV4_TILE_BYTES), dtype=torch.uint8,
+                       device=torch.device("cuda", torch.cuda.current_device()) if device is None else device)
+
+
+def _cache(cache):
+    """(pointer, page stride, head stride, pages, tokens of a page), heads"""
+    if not isinstance(cache, torch.Tensor) or not cache.is_cuda:
+        raise TypeError("cache must be a GPU tensor")
+    if cache.dtype != torch.uint8:
+        raise TypeError("cache must have dtype %s, got %s" % (torch.uint8, cache.dtype))
+    if cache.dim() != 4 or cache.shape[3] != KV4_TILE_BYTES or cache.shape[2] == 0:
+        raise FireqError(-2, "cache")
+    if cache.stride(3) != 1 or (cache.shape[2] > 1 and cache.stride(2) != KV4_TILE_BYTES):
+        raise ValueError("cache must have its pages contiguous")
+    pages, heads, tiles, _ = cache.shape
+    per = tiles * KV4_TILE_BYTES
+    head_stride = cache.stride(1) if heads > 1 else per
+    page_stride = cache.stride(0) if pages > 1 else heads * head_stride
+    return (cache.data_ptr(), page_stride, head_stride, pages, tiles * KV4_TILE_TOKENS), heads
+
+
+def fq_kv4_append(QKV: torch.Tensor, cos_sin: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor,
+                  interleaved: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(uint8 [T,Hq,128] E4M3 codes, float32 [T,Hq] scales) of the rotated queries of the fused projections' output QKV
+    bf16 [T, (Hq + 2 Hkv) * 128] (rows may be strided); rotated keys and values go to `slots` (int64 [T], negative: padding) of
+    the paged cache as INT4.  cos_sin: float32 [positions, 64, 2]; positions: int32 [T]."""
+    if not isinstance(QKV, torch.Tensor) or not QKV.is_cuda:
+        raise TypeError("QKV must be a GPU tensor")
+    if QKV.dtype != torch.bfloat16:
+        raise TypeError("QKV must have dtype %s, got %s" % (torch.bfloat16, QKV.dtype))
+    cos_sin = _dev(cos_sin, torch.float32, "cos_sin")
+    positions = _dev(positions, torch.int32, "positions")
+    slots = _dev(slots, torch.int64, "slots")
+    geometry, Hkv = _cache(cache)
+    if QKV.dim() != 2:
+        raise FireqError(-2, "fq_kv4_append")
+    T, width = QKV.shape
+    if (width > 1 and QKV.stride(1) != 1) or (T > 1 and QKV.stride(0) < width):
+        raise ValueError("QKV must have contiguous rows")
+    if width % 128 or cos_sin.dim() != 3 or tuple(cos_sin.shape[1:]) != (64, 2):
+        raise FireqError(-2, "fq_kv4_append")
+    Hq = width // 128 - 2 * Hkv
+    if Hq <= 0 or positions.numel() != T or slots.numel() != T:
+        raise FireqError(-2, "fq_kv4_append")
+    Q = torch.empty((T, Hq, 128), dtype=torch.uint8, device=QKV.device)
+    s = torch.empty((T, Hq), dtype=torch.float32, device=QKV.device)
+    rc = lib().fq_kv4_append(QKV.data_ptr(), QKV.stride(0) if T > 1 else width, cos_sin.data_ptr(), cos_sin.shape[0], positions.data_ptr(),
+                             slots.data_ptr(), 1 if interleaved else 0, Q.data_ptr(), s.data_ptr(), *geometry, T, Hq, Hkv, _stream())
+    if rc != 0:
+        raise FireqError(rc, "fq_kv4_append")
+    return Q, s
+
+
+def fq_kv4_read(cache: torch.Tensor, slots: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(K, V) bf16 [n,Hkv,128]: the cached tokens in `slots` (int64 [n]; zeros for a negative slot)."""
+    geometry, Hkv = _cache(cache)
+    slots = _dev(slots, torch.int64, "slots")
+    n = slots.numel()
+    K = torch.empty((n, Hkv, 128), dtype=torch.bfloat16, device=cache.device)
+    V = torch.empty((n, Hkv, 128), dtype=torch.bfloat16, device=cache.device)
+    rc = lib().fq_kv4_read(*geometry, slots.data_ptr(), K.data_ptr(), V.data_ptr(), n, Hkv, _stream())
+    if rc != 0:
+        raise FireqError(rc, "fq_kv4_read")
+    return K, V
+
+
+def fq_kv4_attention_workspace_bytes(B: int, Hq: int, Hkv: int, max_len: int, prefix_len: int = 0) -> int:
+    return int(lib().fq_kv4_attention_workspace_bytes(int(B), int(Hq), int(Hkv), int(max_len), int(prefix_len)))
+
+
+def _attention(where, Q, q_scale, cache, prefix_pages, prefix_len, block_table, seq_lens, out_scale, max_len, out, workspace):
+    Q = _dev(Q, torch.uint8, "Q")
+    q_scale = _dev(q_scale, torch.float32, "q_scale")
+    geometry, Hkv = _cache(cache)
+    block_table = _dev(block_table, torch.int32, "block_table")
+    seq_lens = _dev(seq_lens, torch.int32, "seq_lens")
+    if Q.dim() != 3 or Q.shape[2] != 128 or block_table.dim() != 2:
+        raise FireqError(-2, where)
+    B, Hq, _ = Q.shape
+    width = block_table.shape[1]
+    if q_scale.numel() != B * Hq or block_table.shape[0] != B or seq_lens.numel() != B or Hq % Hkv:
+        raise FireqError(-2, where)
+    max_len = min(width * geometry[4], 0x7FFFFFFF) if max_len is None else int(max_len)
+    shared = 0
+    if prefix_pages is not None:
+        prefix_pages = _dev(prefix_pages, torch.int32, "prefix_pages")
+        prefix_len = int(prefix_len)
+        if prefix_len < 0 or prefix_pages.numel() * geometry[4] < prefix_len:
+            raise FireqError(-2, where)
+        shared = prefix_pages.data_ptr()
+    if out is None:
+        out = torch.empty((B, Hq, 128), dtype=torch.bfloat16, device=Q.device)
+    else:
+        out = _dev(out, torch.bfloat16, "out")
+        if tuple(out.shape) not in ((B, Hq, 128), (B, Hq * 128)):
+            raise FireqError(-2, where)
+    if workspace is None:
+        need = fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) if max_len >= 0 else 0
+        workspace = torch.empty((need,), dtype=torch.uint8, device=Q.device) if need else None
+    ws, nbytes = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
+    args = (block_table.data_ptr(), width, seq_lens.data_ptr(), ctypes.c_float(float(out_scale)), out.data_ptr(), B, Hq, Hkv, max_len, ws, nbytes,
+            _stream())
+    if prefix_pages is None:
+        rc = lib().fq_kv4_attention_ws(Q.data_ptr(), q_scale.data_ptr(), *geometry, *args)
+    else:
+        rc = lib().fq_kv4_attention_prefix_ws(Q.data_ptr(), q_scale.data_ptr(), *geometry, shared, prefix_len, *args)
+    if rc != 0:
+        raise FireqError(rc, where)
+    return out
+
+
+def fq_kv4_attention(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, seq_lens: torch.Tensor,
+                     out_scale: float, max_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """bf16 [B,Hq,128]: attention of one query token per sequence (codes and scales from fq_kv4_append) over its seq_lens[b]
+    (int32 [B]) cached tokens, in the pages block_table[b] (int32 [B, pages of a sequence]) of a paged cache.
+
+    `max_len`: an upper bound of seq_lens that the host knows, by default what the table has room for (it only decides how the
+    work is split); `workspace` of fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len) bytes is allocated here when not given."""
+    return _attention("fq_kv4_attention", Q, q_scale, cache, None, 0, block_table, seq_lens, out_scale, max_len, out, workspace)
+
+
+def fq_kv4_attention_prefix(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch.Tensor, prefix_pages: torch.Tensor, prefix_len: int,
+                            block_table: torch.Tensor, seq_lens: torch.Tensor, out_scale: float, max_len: Optional[int] = None,
+                            out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """fq_kv4_attention for sequences that share a prefix: each attends to prefix_len tokens in prefix_pages (int32 [pages]) and
+    then to its own seq_lens[b] tokens in block_table[b].  The prefix is read once for all of them."""
+    if prefix_pages is None:
+        raise TypeError("prefix_pages must be a GPU tensor")
+    return _attention("fq_kv4_attention_prefix", Q, q_scale, cache, prefix_pages, prefix_len, block_table, seq_lens, out_scale, max_len, out,
+                      workspace)

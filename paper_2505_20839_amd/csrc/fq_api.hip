@@ -2,6 +2,8 @@
 // Declarations and the contract of every call are in include/fireq.h.
 #include "../../include/fireq.h"
 #include "../../include/fireq_kv4_ws.h"
+#include "../../include/fireq_norm.h"
+#include "../../include/fireq_paged.h"
 #include "../../include/fireq_wquant_ws.h"
 #include "fq_common.h"
 #include "fq_kernels.h"
@@ -496,6 +498,146 @@ int fq_kv4_output_ws(const uint8_t* P_fp8, const float* p_scale, const uint8_t* 
 int fq_kv4_output(const uint8_t* P_fp8, const float* p_scale, const uint8_t* V_packed, const uint8_t* v_scale,
                   uint16_t* O_bf16, int H, int R, int T, int ldp, void* stream) {
     return fq_kv4_output_ws(P_fp8, p_scale, V_packed, v_scale, O_bf16, H, R, T, ldp, nullptr, 0, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+    return p < q + nb && q < p + na;
+}
+
+// Checks shared by the norms; `out`: Y_bf16 or A_fp8, `per`: its bytes per number.
+int check_norm(const uint16_t* X, const uint16_t* R, const uint16_t* w, float eps, const uint16_t* H, const void* out, size_t per, int M, int K) {
+    // (a grid holds fewer than 2^32 threads, 1024 of them for a long row)
+    if (M < 0 || M >= 1 << 22 || K <= 0 || (K % 8) != 0 || !(eps > 0.f) || !(eps <= 3.402823466e38f)) return FQ_ERR_SHAPE;
+    if (M == 0) return FQ_OK;
+    if (!X || !w || !out || (R != nullptr) != (H != nullptr)) return FQ_ERR_NULL;
+    if (!aligned16(X) || !aligned16(w) || !aligned16(out) || !aligned16(R) || !aligned16(H)) return FQ_ERR_ALIGN;
+    const size_t n = (size_t)M * K * 2, no = (size_t)M * K * per;
+    if (H && ((H != X && overlap(H, n, X, n)) || (H != R && overlap(H, n, R, n)) || overlap(H, n, w, (size_t)K * 2) || overlap(H, n, out, no)))
+        return FQ_ERR_SHAPE;
+    const bool whole = per == 2;                          // a bf16 output may take an input's place
+    if (overlap(out, no, w, (size_t)K * 2) || (!(whole && out == X) && overlap(out, no, X, n)) || (R && !(whole && out == R) && overlap(out, no, R, n)))
+        return FQ_ERR_SHAPE;
+    return FQ_OK;
+}
+
+// A paged cache's geometry.
+int check_paged(const uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages, int page, int heads) {
+    if (pages < 0 || page <= 0 || page % FQ_KV4_TILE_TOKENS != 0 || heads <= 0 || heads > 65535) return FQ_ERR_SHAPE;
+    const int64_t per = (int64_t)(page / FQ_KV4_TILE_TOKENS) * FQ_KV4_TILE_BYTES;
+    if (page_stride <= 0 || head_stride <= 0 || page_stride % 16 != 0 || head_stride % 16 != 0) return FQ_ERR_SHAPE;
+    if ((heads > 1 && head_stride < per) || (pages > 1 && page_stride < per)) return FQ_ERR_SHAPE;
+    if (pages > 0 && !cache) return FQ_ERR_NULL;
+    if (!aligned16(cache)) return FQ_ERR_ALIGN;
+    return FQ_OK;
+}
+
+int attend(const uint8_t* Q_fp8, const float* q_scale, const uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages, int page,
+           const int32_t* prefix_pages, int prefix_len, const int32_t* block_table, int table_width, const int32_t* seq_lens,
+           float out_scale, uint16_t* O_bf16, int B, int Hq, int Hkv, int max_len, void* workspace, size_t workspace_bytes, void* stream) {
+    if (B < 0 || B > 65535 || Hq <= 0 || Hq > 65535 || Hkv <= 0 || Hq % Hkv != 0 || table_width < 0 || max_len < 0 || prefix_len < 0 ||
+        !(out_scale > 0.f) || !(out_scale <= 3.402823466e38f))
+        return FQ_ERR_SHAPE;
+    const int rc = check_paged(cache, page_stride, head_stride, pages, page, Hkv);
+    if (rc != FQ_OK) return rc;
+    if ((int64_t)Hkv * ((Hq / Hkv + 15) / 16) > 65535 || (int64_t)B * Hq > 1 << 23) return FQ_ERR_SHAPE;
+    if (B == 0) return FQ_OK;
+    if (!Q_fp8 || !q_scale || !seq_lens || !O_bf16 || (table_width > 0 && !block_table) || (prefix_len > 0 && !prefix_pages)) return FQ_ERR_NULL;
+    if (!aligned16(Q_fp8) || !aligned16(O_bf16)) return FQ_ERR_ALIGN;
+    if (pages == 0 && (prefix_len > 0 || (table_width > 0 && max_len > 0))) return FQ_ERR_SHAPE;   // no page to fall back on
+    const size_t need = fq_attend_scratch_bytes(B, Hq, Hkv, max_len, prefix_len);
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need) return FQ_ERR_MEMORY;
+        if (!aligned16(workspace)) return FQ_ERR_ALIGN;
+    }
+    const fq_attend_args a = {Q_fp8, q_scale, {const_cast<uint8_t*>(cache), page_stride, head_stride, pages, page}, prefix_pages, block_table,
+                              seq_lens, prefix_len, table_width, out_scale, O_bf16, B, Hq, Hkv, max_len};
+    fq_launch_attend(a, workspace, static_cast<hipStream_t>(stream));
+    return after_launch();
+}
+
+}  // namespace
+
+extern "C" {
+
+int fq_rmsnorm(const uint16_t* X_bf16, const uint16_t* R_bf16, const uint16_t* w_bf16, float eps, uint16_t* H_bf16, uint16_t* Y_bf16,
+               int M, int K, void* stream) {
+    const int rc = check_norm(X_bf16, R_bf16, w_bf16, eps, H_bf16, Y_bf16, 2, M, K);
+    if (rc != FQ_OK || M == 0) return rc;
+    fq_launch_rmsnorm(X_bf16, R_bf16, w_bf16, eps, H_bf16, Y_bf16, M, K, static_cast<hipStream_t>(stream));
+    return after_launch();
+}
+
+int fq_rmsnorm_quant_ws(const uint16_t* X_bf16, const uint16_t* R_bf16, const uint16_t* w_bf16, float eps, uint16_t* H_bf16,
+                        uint8_t* A_fp8, float* a_scale, int M, int K, void* workspace, size_t workspace_bytes, void* stream) {
+    const int rc = check_norm(X_bf16, R_bf16, w_bf16, eps, H_bf16, A_fp8, 1, M, K);
+    if (rc != FQ_OK || M == 0) return rc;
+    if (!a_scale) return FQ_ERR_NULL;
+    void* planes = nullptr;
+    if (workspace && choose_kernel(M) == GemmKernel::Large) {
+        if (!fq_quantize_can_write_zero_point(K)) return FQ_ERR_SHAPE;
+        if (workspace_bytes < fq_gemm_large_workspace_bytes(M, K)) return FQ_ERR_MEMORY;
+        if (!aligned16(workspace)) return FQ_ERR_ALIGN;
+        planes = workspace;
+    }
+    fq_launch_rmsnorm_quant(X_bf16, R_bf16, w_bf16, eps, H_bf16, A_fp8, a_scale, M, K, planes, static_cast<hipStream_t>(stream));
+    return after_launch();
+}
+
+int fq_kv4_append(const uint16_t* QKV_bf16, int64_t ld, const float* cos_sin, int max_positions, const int32_t* positions,
+                  const int64_t* slots, int interleaved, uint8_t* Q_fp8, float* q_scale, uint8_t* cache, int64_t page_stride,
+                  int64_t head_stride, int pages, int page, int T, int Hq, int Hkv, void* stream) {
+    if (T < 0 || Hq <= 0 || Hq > 65535 || Hkv <= 0 || Hq % Hkv != 0 || max_positions < 0) return FQ_ERR_SHAPE;
+    const int rc = check_paged(cache, page_stride, head_stride, pages, page, Hkv);
+    if (rc != FQ_OK) return rc;
+    const int64_t heads = (int64_t)Hq + 2 * (int64_t)Hkv;
+    if (ld < heads * 128 || ld % 8 != 0 || (int64_t)T * heads > (int64_t)0x0FFFFFF0) return FQ_ERR_SHAPE;
+    if (T == 0) return FQ_OK;
+    if (!QKV_bf16 || !positions || !slots || !Q_fp8 || !q_scale || (max_positions > 0 && !cos_sin)) return FQ_ERR_NULL;
+    if (!aligned16(QKV_bf16) || !aligned16(cos_sin) || !aligned16(Q_fp8)) return FQ_ERR_ALIGN;
+    const fq_paged_cache c = {cache, page_stride, head_stride, pages, page};
+    fq_launch_kv4_append(QKV_bf16, ld, cos_sin, max_positions, positions, slots, interleaved != 0, Q_fp8, q_scale, c, T, Hq, Hkv,
+                         static_cast<hipStream_t>(stream));
+    return after_launch();
+}
+
+int fq_kv4_read(const uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages, int page, const int64_t* slots,
+                uint16_t* K_bf16, uint16_t* V_bf16, int n, int Hkv, void* stream) {
+    if (n < 0) return FQ_ERR_SHAPE;
+    const int rc = check_paged(cache, page_stride, head_stride, pages, page, Hkv);
+    if (rc != FQ_OK) return rc;
+    if ((int64_t)n * Hkv > (int64_t)0x0FFFFFF0) return FQ_ERR_SHAPE;
+    if (n == 0) return FQ_OK;
+    if (!slots || !K_bf16 || !V_bf16) return FQ_ERR_NULL;
+    if (!aligned16(K_bf16) || !aligned16(V_bf16)) return FQ_ERR_ALIGN;
+    const fq_paged_cache c = {const_cast<uint8_t*>(cache), page_stride, head_stride, pages, page};
+    fq_launch_kv4_read(c, slots, K_bf16, V_bf16, n, Hkv, static_cast<hipStream_t>(stream));
+    return after_launch();
+}
+
+size_t fq_kv4_attention_workspace_bytes(int B, int Hq, int Hkv, int max_len, int prefix_len) {
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_len < 0 || prefix_len < 0) return 0;
+    return fq_attend_scratch_bytes(B, Hq, Hkv, max_len, prefix_len);
+}
+
+int fq_kv4_attention_ws(const uint8_t* Q_fp8, const float* q_scale, const uint8_t* cache, int64_t page_stride, int64_t head_stride,
+                        int pages, int page, const int32_t* block_table, int table_width, const int32_t* seq_lens, float out_scale,
+                        uint16_t* O_bf16, int B, int Hq, int Hkv, int max_len, void* workspace, size_t workspace_bytes, void* stream) {
+    return attend(Q_fp8, q_scale, cache, page_stride, head_stride, pages, page, nullptr, 0, block_table, table_width, seq_lens, out_scale,
+                  O_bf16, B, Hq, Hkv, max_len, workspace, workspace_bytes, stream);
+}
+
+int fq_kv4_attention_prefix_ws(const uint8_t* Q_fp8, const float* q_scale, const uint8_t* cache, int64_t page_stride,
+                               int64_t head_stride, int pages, int page, const int32_t* prefix_pages, int prefix_len,
+                               const int32_t* block_table, int table_width, const int32_t* seq_lens, float out_scale,
+                               uint16_t* O_bf16, int B, int Hq, int Hkv, int max_len, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+    return attend(Q_fp8, q_scale, cache, page_stride, head_stride, pages, page, prefix_pages, prefix_len, block_table, table_width, seq_lens,
+                  out_scale, O_bf16, B, Hq, Hkv, max_len, workspace, workspace_bytes, stream);
 }
 
 size_t fq_w4a8_gemm_static_max_workspace(void) { return FQ_STATIC_SCRATCH_BYTES; }

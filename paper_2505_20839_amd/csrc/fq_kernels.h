@@ -125,3 +125,34 @@ void fq_launch_gemm_ksplit64(const uint8_t* A, const float* a_scale, const uint8
 void fq_launch_gemm_ksplit(int choice, const uint8_t* A, const float* a_scale, const uint8_t* wp, const uint8_t* gs,
                            float tscale, uint16_t* Y, int M, int N, int K, void* workspace, bool prepared,
                            const uint16_t* R, hipStream_t stream);
+
+// Residual addition and RMS norm (fq_norm.hip).  R == NULL: H = X, not written.  workspace: NULL, or the GEMM's (a shape that
+// fq_quantize_can_write_zero_point(K) accepts).
+void fq_launch_rmsnorm(const uint16_t* X, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint16_t* Y, int M, int K,
+                       hipStream_t stream);
+void fq_launch_rmsnorm_quant(const uint16_t* X, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint8_t* A, float* a_scale,
+                             int M, int K, void* workspace, hipStream_t stream);
+
+// Paged INT4 key/value cache (fq_paged.hip, fq_attend.hip; layout in include/fireq_paged.h).
+#define FQP_TILE 2080                                     // bytes of 16 tokens of a head
+struct fq_paged_cache {
+    uint8_t* base;
+    long long page_stride, head_stride;                   // bytes
+    int pages, page;                                      // number of pages, tokens of one
+};
+void fq_launch_kv4_append(const uint16_t* QKV, long long ld, const float* cos_sin, int max_positions, const int32_t* positions,
+                          const int64_t* slots, bool interleaved, uint8_t* Q, float* q_scale, const fq_paged_cache& c, int T, int Hq,
+                          int Hkv, hipStream_t stream);
+void fq_launch_kv4_read(const fq_paged_cache& c, const int64_t* slots, uint16_t* K, uint16_t* V, int n, int Hkv, hipStream_t stream);
+struct fq_attend_args {
+    const uint8_t* Q;
+    const float* q_scale;
+    fq_paged_cache c;
+    const int32_t *shared, *table, *lens;                 // pages of the prefix (or NULL), of the sequences; their lengths
+    int prefix, width;
+    float out_scale;
+    uint16_t* O;
+    int B, Hq, Hkv, max_len;
+};
+size_t fq_attend_scratch_bytes(int B, int Hq, int Hkv, int max_len, int prefix);
+void fq_launch_attend(const fq_attend_args& a, void* scratch, hipStream_t stream);
