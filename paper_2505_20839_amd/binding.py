@@ -32,7 +32,8 @@ _MARSHALLED = ("fq_quantize_act", "fq_quantize_act_ws", "fq_packed_weight_bytes"
                "fq_w4a8_gemm_swiglu_ws", "fq_w4a8_gemm_add_ws", "fq_w4a8_gemm_swiglu_quant_ws", "fq_w4a8_linear_workspace_bytes",
                "fq_w4a8_linear_ws", "fq_kv4_packed_bytes", "fq_kv4_scores", "fq_kv4_output_workspace_bytes", "fq_kv4_output_ws",
                "fq_kv4_pack", "fq_pack_weights", "fq_cas_scales_workspace_bytes", "fq_cas_scales_ws", "fq_pts_exponent_workspace_bytes",
-               "fq_pts_exponent_ws", "fq_quantize_weights")
+               "fq_pts_exponent_ws", "fq_quantize_weights", "fq_rmsnorm", "fq_rmsnorm_quant_ws", "fq_kv4_append", "fq_kv4_read",
+               "fq_kv4_attention_workspace_bytes", "fq_kv4_attention_ws", "fq_kv4_attention_prefix_ws")
 
 
 class FireqError(RuntimeError):
@@ -681,6 +682,11 @@ def fq_rmsnorm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: Opti
                out: Optional[torch.Tensor] = None):
     """bf16 [M,K] RMS norm of X, or of H = bf16(X + residual): (Y, H) then.  `out` receives H and may be the residual itself
     (the residual stream updated in place)."""
+    r = (_marshal or marshal()).rmsnorm(X, weight, eps, residual, out)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, "fq_rmsnorm")
+        return r
     X, weight, residual, H = _norm_arguments(X, weight, residual, out)
     M, K = X.shape
     Y = torch.empty_like(X)
@@ -695,6 +701,11 @@ def fq_rmsnorm_quant(X: torch.Tensor, weight: torch.Tensor, eps: float, residual
     """(uint8 [M,K] E4M3 codes, float32 [M] row scales) of the RMS norm of X [M,K], the operands of fq_w4a8_gemm; with a
     residual (codes, scales, H = bf16(X + residual)).  `out` receives H and may be the residual itself; `workspace`
     (fq_w4a8_gemm_workspace_bytes(M, N, K) bytes or more) is prepared for fq_w4a8_gemm(..., workspace_prepared=True)."""
+    r = (_marshal or marshal()).rmsnorm_quant(X, weight, eps, residual, out, workspace)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, "fq_rmsnorm_quant")
+        return r
     X, weight, residual, H = _norm_arguments(X, weight, residual, out)
     M, K = X.shape
     A = torch.empty((M, K), dtype=torch.uint8, device=X.device)
@@ -742,6 +753,11 @@ def fq_kv4_append(QKV: torch.Tensor, cos_sin: torch.Tensor, positions: torch.Ten
     """(uint8 [T,Hq,128] E4M3 codes, float32 [T,Hq] scales) of the rotated queries of the fused projections' output QKV
     bf16 [T, (Hq + 2 Hkv) * 128] (rows may be strided); rotated keys and values go to `slots` (int64 [T], negative: padding) of
     the paged cache as INT4.  cos_sin: float32 [positions, 64, 2]; positions: int32 [T]."""
+    r = (_marshal or marshal()).kv4_append(QKV, cos_sin, positions, slots, cache, interleaved)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, "fq_kv4_append")
+        return r
     if not isinstance(QKV, torch.Tensor) or not QKV.is_cuda:
         raise TypeError("QKV must be a GPU tensor")
     if QKV.dtype != torch.bfloat16:
@@ -771,6 +787,11 @@ def fq_kv4_append(QKV: torch.Tensor, cos_sin: torch.Tensor, positions: torch.Ten
 
 def fq_kv4_read(cache: torch.Tensor, slots: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """(K, V) bf16 [n,Hkv,128]: the cached tokens in `slots` (int64 [n]; zeros for a negative slot)."""
+    r = (_marshal or marshal()).kv4_read(cache, slots)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, "fq_kv4_read")
+        return r
     geometry, Hkv = _cache(cache)
     slots = _dev(slots, torch.int64, "slots")
     n = slots.numel()
@@ -787,6 +808,11 @@ def fq_kv4_attention_workspace_bytes(B: int, Hq: int, Hkv: int, max_len: int, pr
 
 
 def _attention(where, Q, q_scale, cache, prefix_pages, prefix_len, block_table, seq_lens, out_scale, max_len, out, workspace):
+    r = (_marshal or marshal()).kv4_attention(Q, q_scale, cache, prefix_pages, prefix_len, block_table, seq_lens, out_scale, max_len, out, workspace)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, where)
+        return r
     Q = _dev(Q, torch.uint8, "Q")
     q_scale = _dev(q_scale, torch.float32, "q_scale")
     geometry, Hkv = _cache(cache)

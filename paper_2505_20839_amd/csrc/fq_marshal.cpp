@@ -17,6 +17,8 @@
 
 #include "../../include/fireq.h"
 #include "../../include/fireq_kv4_ws.h"
+#include "../../include/fireq_norm.h"
+#include "../../include/fireq_paged.h"
 #include "../../include/fireq_wquant_ws.h"
 
 namespace {
@@ -43,6 +45,13 @@ struct Api {
     decltype(&fq_pts_exponent_workspace_bytes) pts_exponent_workspace_bytes;
     decltype(&fq_pts_exponent_ws) pts_exponent_ws;
     decltype(&fq_quantize_weights) quantize_weights;
+    decltype(&fq_rmsnorm) rmsnorm;
+    decltype(&fq_rmsnorm_quant_ws) rmsnorm_quant_ws;
+    decltype(&fq_kv4_append) kv4_append;
+    decltype(&fq_kv4_read) kv4_read;
+    decltype(&fq_kv4_attention_workspace_bytes) attention_workspace_bytes;
+    decltype(&fq_kv4_attention_ws) attention_ws;
+    decltype(&fq_kv4_attention_prefix_ws) attention_prefix_ws;
 };
 Api api = {};
 bool bound = false;
@@ -401,6 +410,151 @@ PyObject* quantize_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// rmsnorm(X, weight, eps, residual, out), rmsnorm_quant(X, weight, eps, residual, out, workspace)
+template <bool QUANT>
+PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n == (QUANT ? 6 : 5));
+        const at::Tensor &X = dev(a[0], at::kBFloat16), &w = dev(a[1], at::kBFloat16);
+        want(X.dim() == 2 && X.size(0) > 0 && X.size(0) <= INT_LIMIT && X.size(1) > 0 && X.size(1) <= INT_LIMIT && w.numel() == X.size(1));
+        const float eps = number(a[2]);
+        const int M = (int)X.size(0), K = (int)X.size(1);
+        at::Tensor H;
+        const uint16_t* r = nullptr;
+        if (a[3] != Py_None) {
+            const at::Tensor& R = dev(a[3], at::kBFloat16);
+            want(R.sizes() == X.sizes());
+            r = (const uint16_t*)R.data_ptr();
+            H = output(a[4], X.sizes(), X);
+        } else {
+            want(a[4] == Py_None);
+        }
+        const uint16_t *x = (const uint16_t*)X.data_ptr(), *pw = (const uint16_t*)w.data_ptr();
+        uint16_t* h = r ? (uint16_t*)H.data_ptr() : nullptr;
+        void* st = stream();
+        if (!QUANT) {
+            at::Tensor Y = fresh({M, K}, at::kBFloat16, X);
+            uint16_t* y = (uint16_t*)Y.data_ptr();
+            const int rc = call([&] { return api.rmsnorm(x, r, pw, eps, h, y, M, K, st); });
+            return r ? wrap(rc, {Y, H}) : wrap(rc, Y);
+        }
+        at::Tensor A = fresh({M, K}, at::kByte, X), s = fresh({M}, at::kFloat, X);
+        const Scratch ws(a[QUANT ? 5 : 0], 0, X);
+        uint8_t* pa = (uint8_t*)A.data_ptr();
+        float* ps = (float*)s.data_ptr();
+        const bool with = a[QUANT ? 5 : 0] != Py_None;
+        const int rc = call([&] { return api.rmsnorm_quant_ws(x, r, pw, eps, h, pa, ps, M, K, with ? ws.p : nullptr, with ? ws.bytes : 0, st); });
+        return r ? wrap(rc, {A, s, H}) : wrap(rc, {A, s});
+    });
+}
+
+struct Paged {                                            // a paged cache [pages, heads, page / 16, 2080], its pages contiguous
+    const at::Tensor& c;
+    int pages, heads, page;
+    int64_t page_stride, head_stride;
+    explicit Paged(PyObject* o) : c(tensor(o)) {
+        want(c.is_cuda() && c.scalar_type() == at::kByte && c.dim() == 4 && c.size(3) == FQ_KV4_TILE_BYTES && c.stride(3) == 1 && c.size(2) > 0 &&
+             (c.size(2) == 1 || c.stride(2) == FQ_KV4_TILE_BYTES));
+        want(c.size(0) > 0 && c.size(0) <= INT_LIMIT && c.size(1) > 0 && c.size(1) <= INT_LIMIT && c.size(2) <= INT_LIMIT / FQ_KV4_TILE_TOKENS);
+        pages = (int)c.size(0);
+        heads = (int)c.size(1);
+        page = (int)c.size(2) * FQ_KV4_TILE_TOKENS;
+        head_stride = heads > 1 ? c.stride(1) : c.size(2) * FQ_KV4_TILE_BYTES;
+        page_stride = pages > 1 ? c.stride(0) : heads * head_stride;
+    }
+    uint8_t* p() const { return (uint8_t*)c.data_ptr(); }
+};
+
+// kv4_append(QKV, cos_sin, positions, slots, cache, interleaved)
+PyObject* kv4_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n == 6);
+        const at::Tensor &X = tensor(a[0]), &rot = dev(a[1], at::kFloat), &pos = dev(a[2], at::kInt), &slots = dev(a[3], at::kLong);
+        want(X.is_cuda() && X.scalar_type() == at::kBFloat16 && X.dim() == 2 && X.stride(1) == 1);
+        const Paged c(a[4]);
+        const int interleaved = truth(a[5]) ? 1 : 0;
+        const int64_t T = X.size(0), width = X.size(1), Hq = width / 128 - 2 * (int64_t)c.heads, ld = T > 1 ? X.stride(0) : width;
+        want(T > 0 && T <= INT_LIMIT && width % 128 == 0 && Hq > 0 && Hq <= INT_LIMIT && ld >= width && pos.numel() == T && slots.numel() == T &&
+             rot.dim() == 3 && rot.size(0) <= INT_LIMIT && rot.size(1) == 64 && rot.size(2) == 2);
+        at::Tensor Q = fresh({T, Hq, 128}, at::kByte, X), s = fresh({T, Hq}, at::kFloat, X);
+        const uint16_t* x = (const uint16_t*)X.data_ptr();
+        const float* cs = (const float*)rot.data_ptr();
+        const int32_t* pp = (const int32_t*)pos.data_ptr();
+        const int64_t* sl = (const int64_t*)slots.data_ptr();
+        uint8_t* q = (uint8_t*)Q.data_ptr();
+        float* qs = (float*)s.data_ptr();
+        const int positions = (int)rot.size(0);
+        void* st = stream();
+        const int rc = call([&] {
+            return api.kv4_append(x, ld, cs, positions, pp, sl, interleaved, q, qs, c.p(), c.page_stride, c.head_stride, c.pages, c.page, (int)T, (int)Hq, c.heads, st);
+        });
+        return wrap(rc, {Q, s});
+    });
+}
+
+// kv4_read(cache, slots)
+PyObject* kv4_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n == 2);
+        const Paged c(a[0]);
+        const at::Tensor& slots = dev(a[1], at::kLong);
+        const int64_t count = slots.numel();
+        want(count > 0 && count <= INT_LIMIT);
+        at::Tensor K = fresh({count, c.heads, 128}, at::kBFloat16, c.c), V = fresh({count, c.heads, 128}, at::kBFloat16, c.c);
+        const int64_t* sl = (const int64_t*)slots.data_ptr();
+        uint16_t *k = (uint16_t*)K.data_ptr(), *v = (uint16_t*)V.data_ptr();
+        void* st = stream();
+        const int rc = call([&] { return api.kv4_read(c.p(), c.page_stride, c.head_stride, c.pages, c.page, sl, k, v, (int)count, c.heads, st); });
+        return wrap(rc, {K, V});
+    });
+}
+
+// kv4_attention(Q, q_scale, cache, prefix_pages, prefix_len, block_table, seq_lens, out_scale, max_len, out, workspace)
+PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n == 11);
+        const at::Tensor &Q = dev(a[0], at::kByte), &qs = dev(a[1], at::kFloat);
+        const Paged c(a[2]);
+        const at::Tensor &table = dev(a[5], at::kInt), &lens = dev(a[6], at::kInt);
+        want(Q.dim() == 3 && Q.size(2) == 128 && table.dim() == 2);
+        const int64_t B = Q.size(0), Hq = Q.size(1), width = table.size(1);
+        want(B > 0 && B <= INT_LIMIT && Hq > 0 && Hq <= INT_LIMIT && Hq % c.heads == 0 && width <= INT_LIMIT && qs.numel() == B * Hq && table.size(0) == B &&
+             lens.numel() == B);
+        const float out_scale = number(a[7]);
+        const int64_t most = width * c.page < INT_LIMIT ? width * c.page : INT_LIMIT;
+        const int max_len = a[8] == Py_None ? (int)most : whole(a[8]);
+        const int32_t* shared = nullptr;
+        int prefix = 0;
+        const bool with = a[3] != Py_None;
+        if (with) {
+            const at::Tensor& p = dev(a[3], at::kInt);
+            prefix = whole(a[4]);
+            want(p.numel() * c.page >= prefix);
+            shared = (const int32_t*)p.data_ptr();
+        }
+        at::Tensor O;
+        if (a[9] == Py_None) {
+            O = fresh({B, Hq, 128}, at::kBFloat16, Q);
+        } else {
+            O = dev(a[9], at::kBFloat16);
+            want(O.sizes() == at::IntArrayRef({B, Hq, 128}) || O.sizes() == at::IntArrayRef({B, Hq * 128}));
+        }
+        const Scratch ws(a[10], a[10] == Py_None ? api.attention_workspace_bytes((int)B, (int)Hq, c.heads, max_len, prefix) : 0, Q);
+        const uint8_t* q = (const uint8_t*)Q.data_ptr();
+        const float* s = (const float*)qs.data_ptr();
+        const int32_t *tb = (const int32_t*)table.data_ptr(), *ln = (const int32_t*)lens.data_ptr();
+        uint16_t* o = (uint16_t*)O.data_ptr();
+        void* st = stream();
+        const int rc = call([&] {
+            return with ? api.attention_prefix_ws(q, s, c.p(), c.page_stride, c.head_stride, c.pages, c.page, shared, prefix, tb, (int)width, ln, out_scale, o,
+                                                  (int)B, (int)Hq, c.heads, max_len, ws.p, ws.bytes, st)
+                        : api.attention_ws(q, s, c.p(), c.page_stride, c.head_stride, c.pages, c.page, tb, (int)width, ln, out_scale, o, (int)B, (int)Hq,
+                                           c.heads, max_len, ws.p, ws.bytes, st);
+        });
+        return wrap(rc, O);
+    });
+}
+
 // gemm_workspace_bytes(M, N, K)
 PyObject* gemm_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&] {
@@ -445,6 +599,11 @@ PyMethodDef methods[] = {
     FQ_METHOD("cas_scales", cas_scales),
     FQ_METHOD("pts_exponent", pts_exponent),
     FQ_METHOD("quantize_weights", quantize_weights),
+    FQ_METHOD("rmsnorm", rmsnorm<false>),
+    FQ_METHOD("rmsnorm_quant", rmsnorm<true>),
+    FQ_METHOD("kv4_append", kv4_append),
+    FQ_METHOD("kv4_read", kv4_read),
+    FQ_METHOD("kv4_attention", kv4_attention),
     FQ_METHOD("gemm_workspace_bytes", gemm_workspace_bytes),
     {nullptr, nullptr, 0, nullptr}};
 

@@ -493,3 +493,66 @@ def test_a_decode_step_in_a_graph_and_on_another_stream(fq):
         torch.cuda.synchronize()
         for a, b, c in zip(got, want, other):
             assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_native_and_python_forms_agree(fq):
+    """Every call through the native marshalling and through its Python form: the same outputs, the same refusals."""
+    from test_gpu_marshal import _same
+    x = torch.randn((5, 1024), device="cuda").bfloat16()
+    r, w = torch.randn_like(x), torch.ones(1024, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    for name in ("fq_rmsnorm", "fq_rmsnorm_quant"):
+        for kw in ({}, {"residual": r}, {"residual": r, "out": torch.empty_like(x)}):
+            _same(fq, name, lambda: ((x, w, 1e-5), dict(kw)), native=True)
+        for bad, exc in (((x.float(), w, 1e-5), TypeError), ((x, w[:-8], 1e-5), fq.FireqError), ((x, w, 0.0), fq.FireqError), ((x[:, ::2], w[::2].contiguous(), 1e-5), ValueError)):
+            _same(fq, name, lambda: (bad, {}), exc)
+        _same(fq, name, lambda: ((x, w, 1e-5), {"out": x}), fq.FireqError)
+        _same(fq, name, lambda: ((x, w, 1e-5), {"residual": r[:4]}), fq.FireqError)
+        _same(fq, name, lambda: ((x[:0], w, 1e-5), {}), native=False)
+    _same(fq, "fq_rmsnorm_quant", lambda: ((x, w, 1e-5), {"workspace": ws}), native=True)
+    Hq, Hkv, page = 4, 2, 32
+    qkv = torch.randn((6, 8 * 128), device="cuda").bfloat16()
+    rot = torch.from_numpy(_rotation(20)).cuda()
+    pos, slots = torch.arange(6, dtype=torch.int32, device="cuda"), torch.arange(6, device="cuda") + 20
+    cache = fq.fq_kv4_cache(3, Hkv, page)
+    ok = (qkv, rot, pos, slots, cache)
+    _same(fq, "fq_kv4_append", lambda: (ok, {}), native=True)
+    _same(fq, "fq_kv4_append", lambda: (ok, {"interleaved": True}), native=True)
+    _same(fq, "fq_kv4_append", lambda: ((qkv[:, :1024], rot, pos, slots, cache), {}), native=True)
+    for bad, exc in (((qkv.float(),) + ok[1:], TypeError), ((qkv, rot, pos[:5], slots, cache), fq.FireqError), ((qkv, rot, pos, slots, cache[:, :, :, :2064]), fq.FireqError),
+                     ((qkv[:, : 4 * 128], rot, pos, slots, cache), fq.FireqError)):
+        _same(fq, "fq_kv4_append", lambda: (bad, {}), exc)
+    _same(fq, "fq_kv4_read", lambda: ((cache, slots), {}), native=True)
+    _same(fq, "fq_kv4_read", lambda: ((cache, pos), {}), TypeError)
+    Q, qs = fq.fq_kv4_append(*ok)
+    table = torch.arange(6, dtype=torch.int32, device="cuda").reshape(6, 1) % 3
+    lens = torch.tensor([26, 0, 21, 26, 1, 22], dtype=torch.int32, device="cuda")
+    slots2 = torch.arange(96, device="cuda")
+    fq.fq_kv4_append(torch.randn((96, 8 * 128), device="cuda").bfloat16(), rot, (slots2 % 20).to(torch.int32), slots2, cache)
+    args = (Q, qs, cache, table, lens, 0.1)
+    need = fq.fq_kv4_attention_workspace_bytes(6, Hq, Hkv, 32)
+    for kw in ({}, {"max_len": 30}, {"out": torch.empty((6, Hq * 128), dtype=torch.bfloat16, device="cuda")}, {"workspace": torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")}):
+        _same(fq, "fq_kv4_attention", lambda: (args, dict(kw)), native=True)
+    shared = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    _same(fq, "fq_kv4_attention_prefix", lambda: ((Q, qs, cache, shared, 50, table, lens, 0.1), {}), native=True)
+    for bad, exc in (((Q, qs, cache, shared, 65, table, lens, 0.1), fq.FireqError), ((Q, qs, cache, shared, 50, table, lens, -0.1), fq.FireqError),
+                     ((Q, qs, cache, shared.long(), 50, table, lens, 0.1), TypeError)):
+        _same(fq, "fq_kv4_attention_prefix", lambda: (bad, {}), exc)
+    for bad, exc in (((Q[:, :3].contiguous(), qs, cache, table, lens, 0.1), fq.FireqError), ((Q, qs, cache, table.long(), lens, 0.1), TypeError), ((Q, qs, cache, table, lens, 0.0), fq.FireqError)):
+        _same(fq, "fq_kv4_attention", lambda: (bad, {}), exc)
+    _same(fq, "fq_kv4_attention", lambda: (args, {"max_len": -1}), fq.FireqError)
+
+
+def test_attention_negative_and_zero_query_scales(fq):
+    """A query's scale of 0 weighs all tokens alike; a negative one turns its scores round."""
+    rng = np.random.default_rng(8)
+    lens = [77, 300]
+    ref, table, _ = _filled(rng, lens, 1, 16)
+    q, qs = _queries(rng, 2, 4, 2)
+    qs[0, 1] = 0.0
+    qs[1, 2] *= -1
+    got = fq.fq_kv4_attention(torch.from_numpy(q).cuda(), torch.from_numpy(qs).cuda(), torch.from_numpy(ref.b).cuda(), torch.from_numpy(table).cuda(),
+                              torch.tensor(lens, dtype=torch.int32).cuda(), 0.1)
+    flipped, fs = q.copy(), np.abs(qs)
+    flipped[1, 2] ^= 0x80
+    _check_attention(ref, table, lens, flipped, fs, 1, got, 0.1)
