@@ -11,7 +11,7 @@
  *   values  byte 1024 + 256 p + 16 n + 4 m + b
  *                                        token 4 p + (0, 2, 1, 3)[b], channel n + 32 m (low) and n + 32 m + 16 (high)
  *   scales  byte 2048 + 8 p + i          E4M3 scale of the key of token 4 p + i; + 4: of its value
- * page_stride and head_stride are in bytes, positive multiples of 16 (a page of a head is contiguous; head_stride is at least
+ * page_stride (below 2^36) and head_stride are in bytes, positive multiples of 16 (a page of a head is contiguous; head_stride is at least
  * page / 16 * 2080 and pages do not overlap).  Slot s is token s % page of page s / page.  A fresh cache may hold anything: no
  * call reads a token that was not appended, or lets its bytes count.
  *
@@ -33,7 +33,7 @@
  * fq_kv4_attention_ws   O[b,h,:] = bf16( sum_t p_t v_t / sum_t p_t ), p_t = exp(out_scale q . k_t), over the tokens
  *                 t < seq_lens[b], token t in page block_table[b][t / page] (row b at block_table + b * table_width).  A
  *                 sequence with no token (a length <= 0) gets zeros.  Scores are FP32 sums of exact products; probabilities,
- *                 relative to a running maximum, are summed in FP32 and enter the product with V as fp16 numbers times sigma.
+ *                 relative to a running maximum, enter the FP32 sums as fp16 numbers; sigma * code is exact.
  *                 out_scale > 0; max_len is an upper bound of seq_lens that the caller knows (it decides how the work is
  *                 split).  A sequence longer than it, or than table_width * page, or a page number outside the cache
  *                 within a sequence's length, gives NaN for that sequence.

@@ -529,7 +529,8 @@ int check_norm(const uint16_t* X, const uint16_t* R, const uint16_t* w, float ep
 int check_paged(const uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages, int page, int heads) {
     if (pages < 0 || page <= 0 || page % FQ_KV4_TILE_TOKENS != 0 || heads <= 0 || heads > 65535) return FQ_ERR_SHAPE;
     const int64_t per = (int64_t)(page / FQ_KV4_TILE_TOKENS) * FQ_KV4_TILE_BYTES;
-    if (page_stride <= 0 || head_stride <= 0 || page_stride % 16 != 0 || head_stride % 16 != 0) return FQ_ERR_SHAPE;
+    if (page_stride <= 0 || head_stride <= 0 || page_stride % 16 != 0 || head_stride % 16 != 0 || per > 0x7FFFFFFF) return FQ_ERR_SHAPE;
+    if (page_stride >> 36) return FQ_ERR_SHAPE;           // (the kernels count pages in 16 bytes, 32 bits)
     if ((heads > 1 && head_stride < per) || (pages > 1 && page_stride < per)) return FQ_ERR_SHAPE;
     if (pages > 0 && !cache) return FQ_ERR_NULL;
     if (!aligned16(cache)) return FQ_ERR_ALIGN;

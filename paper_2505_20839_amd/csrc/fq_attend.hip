@@ -6,15 +6,15 @@
 //                   queries.  Code + 8 as an E4M3 number is the code times 2^-9 (fq_common.h); the zero point is the same for all
 //                   tokens of a query, -2^-6 sum q, and the product starts from it.
 //     P^T           a lane has 4 tokens (4 g + i, g = lane / 16) of one query (lane % 16): scaled by the keys' sigmas, exponentiated against the
-//                   query's maximum so far, multiplied by the values' sigmas and rounded to fp16 (11 bits; 2^7 times the probability, so
-//                   that sigma * p stays below 2^16 and reaches 2^-31 of the largest).  Two tiles give the 8 fp16 numbers that a
-//                   lane of the B operand of v_mfma_f32_16x16x32_f16 holds, tokens in this order on both sides.
+//                   query's maximum so far and rounded to fp16 (11 bits).  Two tiles give the 8 fp16 numbers that a lane of the B
+//                   operand of v_mfma_f32_16x16x32_f16 holds, tokens in this order on both sides.
 //     O^T = V^T P^T per 16 channels.  A value's code c, shifted to the top of an fp16 mantissa under the exponent of 16, is the number
-//                   16 + c: unpacking is a shift and an and-or for two of them.  24 sum p sigma (16 and the zero point) is one more
-//                   such product against a constant, taken off at the end.  (As a subnormal fp16 number, c * 2^-24, it would save a
-//                   shift, but the matrix cores align products by their factors' exponents, and a subnormal's is far above its value: sums came
-//                   out 2^-18 off.)
-// O stays in registers and is rescaled where a query's maximum has moved.
+//                   16 + c; one packed fused multiply-add with the token's sigma and -24 sigma makes it sigma * (c - 8), exact in fp16 (8 bits).
+//                   (As subnormal fp16 numbers, c * 2^-24, the codes would save a shift, but the matrix cores align products by their
+//                   factors' exponents, and a subnormal's is far above its value: sums came out 2^-18 off.)
+//     sum p         one more such product, against ones: the sum of the same rounded numbers.
+// O stays in registers.  A query's maximum moves only when a score passes it by more than FQA_SLACK powers of two, which fp16 has room
+// for: the lanes of a query compare their own scores with it, and only then with each other.
 #include "fq_common.h"
 #include "fq_kernels.h"
 
@@ -23,8 +23,8 @@ namespace {
 typedef _Float16 fqa_v8h __attribute__((ext_vector_type(8)));
 typedef _Float16 fqa_v2h __attribute__((ext_vector_type(2)));
 
-#define FQA_ZERO (-__builtin_inff())
-#define FQA_LIFT 7.0f                                     // log2 of the factor on the probabilities
+#define FQA_LIFT 7.0f                                     // log2 of the factor on the probabilities: down to 2^-31 above fp16's smallest
+#define FQA_SLACK 6.0f                                    // ... and 2^(7 + 6) is the largest
 
 #define FQA_MFMA_QK(a, b, c) __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4((a), (b), (c), 0, 0, 0, 0, 0, 0)
 
@@ -32,13 +32,20 @@ __device__ __forceinline__ float fqa_over_groups_max(float v) {   // over the fo
     v = fmaxf(v, __shfl_xor(v, 16, 64));
     return fmaxf(v, __shfl_xor(v, 32, 64));
 }
-__device__ __forceinline__ float fqa_over_groups_sum(float v) {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
+// The lane's values for channel j of 16 (word j / 2 of each of two tiles) as eight fp16 numbers sigma * (code - 8): a word holds, for j
+// even and odd, nibbles 0 / 1 (tokens 0, 1 of four) and 2 / 3 (tokens 2, 3) of both halves.  `mask` and `base` are 0x03C003C0 and
+// 0x4C004C00 held in registers, for one and-or instead of an and and an or with a literal each.
+struct fqa_sigmas { fqa_v2h s[2], n[2]; };                // sigma and -24 sigma of tokens 0, 1 and 2, 3
+__device__ __forceinline__ fqa_v2h fqa_value_pair(unsigned w, unsigned mask, unsigned base, fqa_v2h s, fqa_v2h n) {
+    return __builtin_elementwise_fma(__builtin_bit_cast(fqa_v2h, (w & mask) | base), s, n);
 }
-
-// Two codes at bits 6 .. 9 of the halves -> two fp16 numbers 16 + code.
-__device__ __forceinline__ int fqa_value_pair(unsigned w) { return (int)((w & 0x03C003C0u) | 0x4C004C00u); }
+template <int ODD>
+__device__ __forceinline__ fqa_v8h fqa_values(int w0, int w1, unsigned mask, unsigned base, const fqa_sigmas& a, const fqa_sigmas& b) {
+    const unsigned x = (unsigned)w0, y = (unsigned)w1;
+    const fqa_v2h r0 = fqa_value_pair(ODD ? x << 2 : x << 6, mask, base, a.s[0], a.n[0]), r1 = fqa_value_pair(ODD ? x >> 6 : x >> 2, mask, base, a.s[1], a.n[1]);
+    const fqa_v2h r2 = fqa_value_pair(ODD ? y << 2 : y << 6, mask, base, b.s[0], b.n[0]), r3 = fqa_value_pair(ODD ? y >> 6 : y >> 2, mask, base, b.s[1], b.n[1]);
+    return (fqa_v8h){r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
+}
 
 struct fqa_tile { fq_v4i k, v; fq_v2i s; };
 
@@ -46,7 +53,7 @@ struct fqa_tile { fq_v4i k, v; fq_v2i s; };
 struct fqa_cursor {
     const int* pages_of;                                  // the sequence's pages
     const uint8_t* head;                                  // the head's part of page 0
-    long long page_stride;
+    unsigned page_stride;                                 // in 16 bytes
     int last;                                             // the range's last tile
     int tile, page, within, tiles_per_page, first, pages;
     int ids;                                              // lane l: page number first + l
@@ -66,142 +73,176 @@ struct fqa_cursor {
         within = t0 - page * tiles_per_page;
         fetch(lane);
     }
-    // the next tile's bytes; behind the range its last tile again
-    __device__ __forceinline__ fqa_tile next(int lane) {
-        const int id = __builtin_amdgcn_readlane(ids, page - first);
-        const uint8_t* p = head + id * page_stride + within * FQP_TILE;
-        fqa_tile t;
-        t.k = *reinterpret_cast<const fq_v4i*>(p + 16 * lane);
-        t.v = *reinterpret_cast<const fq_v4i*>(p + 1024 + 16 * lane);
-        t.s = *reinterpret_cast<const fq_v2i*>(p + 2048 + 8 * (lane >> 4));
-        if (tile < last) {
-            ++tile;
-            if (++within == tiles_per_page) {
-                within = 0;
-                if (++page - first == 64) {
-                    first = page;
-                    fetch(lane);
-                }
-            }
+    // the bytes of the next NT tiles; behind the range its last tile again
+    template <int NT>
+    __device__ __forceinline__ void next(fqa_tile (&t)[NT], int lane) {
+        if (page - first > 64 - NT) {
+            first = page;
+            fetch(lane);
         }
-        return t;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int id = __builtin_amdgcn_readlane(ids, page - first);
+            const uint8_t* p = head + (((unsigned long long)(unsigned)id * page_stride) << 4) + (unsigned)(within * FQP_TILE);
+            t[i].k = *reinterpret_cast<const fq_v4i*>(p + 16 * lane);
+            t[i].v = *reinterpret_cast<const fq_v4i*>(p + 1024 + 16 * lane);
+            t[i].s = *reinterpret_cast<const fq_v2i*>(p + 2048 + 8 * (lane >> 4));
+            const int on = tile < last ? 1 : 0;
+            tile += on;
+            within += on;
+            const int over = within == tiles_per_page ? 1 : 0;
+            page += over;
+            within = over ? 0 : within;
+        }
     }
+};
+
+#define FQA_LOWEST (-3.0e38f)                             // below every score, and finite: times a scale of 0 it is 0
+
+// A query tile's state.  Scores are kept before the query's factor: s = sum q k * sigma_k, probability 2^(qs * (s - m)).
+template <int RT>
+struct fqa_state {
+    float m[RT], sub[RT];                                 // the reference score (within the slack of the largest so far), LIFT - qs * m
+    fq_v4f o[RT][8], l[RT];                               // O^T; sum p, the same in all four
 };
 
 template <int RT>
-struct fqa_state {
-    float m[RT], l[RT];                                   // maximum (in log2), this lane's part of the sum
-    fq_v4f o[RT][8], z[RT];                               // O^T and its zero-point part
+struct fqa_queries {
+    fq_v8i q[RT];                                         // codes, as the B operand
+    fq_v4f zp[RT];                                        // -2^-6 sum of the codes
+    float qs[RT];                                         // factor of a score in log2, not negative
 };
 
-// Tiles t0 .. t1 of a head's tokens below `len`, NT (even) tiles a step.
-template <int RT, int NT>
-__device__ __forceinline__ void fqa_range(fqa_cursor& cur, int t0, int t1, int len, const fq_v8i (&q)[RT], const float (&qs)[RT],
-                                          fqa_state<RT>& st, int lane) {
+// One query (16 lanes of a query tile: 32 bytes each): a negative factor turns the codes' signs instead.
+template <int RT>
+__device__ __forceinline__ void fqa_take_query(fqa_queries<RT>& Q, int r, const uint8_t* codes, float scale, float out_scale, int g) {
+    const fq_v4i* p = reinterpret_cast<const fq_v4i*>(codes + 32 * g);
+    const fq_v4i a = p[0], b = p[1];
+    const int flip = scale < 0.f ? (int)0x80808080 : 0;
+    Q.q[r] = (fq_v8i){a[0] ^ flip, a[1] ^ flip, a[2] ^ flip, a[3] ^ flip, b[0] ^ flip, b[1] ^ flip, b[2] ^ flip, b[3] ^ flip};
+    Q.qs[r] = fabsf(scale) * out_scale * (512.0f * 1.44269504088896340736f);
+    constexpr int E = (int)FQ_ZP_BYTES;
+    const fq_v8i eights = {E, E, E, E, E, E, E, E};
+    Q.zp[r] = FQA_MFMA_QK(eights, Q.q[r], ((fq_v4f){0.f, 0.f, 0.f, 0.f}));
+}
+
+// NT (even) tiles from tile tb on.  TAIL: tokens from `len` on are masked.
+template <int RT, int NT, bool TAIL>
+__device__ __forceinline__ void fqa_step(const fqa_tile (&now)[NT], int tb, int len, const fqa_queries<RT>& Q, fqa_state<RT>& st, unsigned mask,
+                                         unsigned base, int g) {
+    fq_v8i k[NT];
+    float ks[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        k[i] = fq_unpack_chunk(now[i].k);
+        const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[0], false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[0], true);
+        ks[i][0] = s01[0]; ks[i][1] = s01[1]; ks[i][2] = s23[0]; ks[i][3] = s23[1];
+    }
+    auto masked = [&](int i, int e) __attribute__((always_inline)) { return TAIL && (tb + i) * 16 + 4 * g + e >= len; };
+    fq_v4i pt[RT][NT / 2];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        float s[NT][4], top = FQA_LOWEST;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const fq_v4f c = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[i][e] = masked(i, e) ? FQA_LOWEST : c[e] * ks[i][e];
+                top = fmaxf(top, s[i][e]);
+            }
+        }
+        if (__any((top - st.m[r]) * Q.qs[r] > FQA_SLACK)) {
+            const float m = fmaxf(st.m[r], fqa_over_groups_max(top)), f = __builtin_amdgcn_exp2f((st.m[r] - m) * Q.qs[r]);
+            st.m[r] = m;
+            st.sub[r] = fmaf(m, -Q.qs[r], FQA_LIFT);
+            st.l[r] *= f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) st.o[r][j] *= f;
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                float p[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) p[u] = masked(i, e + u) ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i][e + u], Q.qs[r], st.sub[r]));
+                pt[r][i / 2][2 * (i & 1) + e / 2] = __builtin_bit_cast(int, __builtin_convertvector((fq_v2f){p[0], p[1]}, fqa_v2h));
+            }
+    }
+    constexpr int ONE = 0x3C003C00;
+    const fq_v4i ones = {ONE, ONE, ONE, ONE};
+#pragma unroll
+    for (int i = 0; i < NT / 2; ++i) {
+        fqa_sigmas sg[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int w = now[2 * i + u].s[1];
+            fq_v2f v01 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {                 // (whatever the bytes behind the end are)
+                v01[e] = masked(2 * i + u, e) ? 0.f : v01[e];
+                v23[e] = masked(2 * i + u, 2 + e) ? 0.f : v23[e];
+            }
+            sg[u].s[0] = __builtin_convertvector(v01, fqa_v2h);
+            sg[u].s[1] = __builtin_convertvector(v23, fqa_v2h);
+            sg[u].n[0] = sg[u].s[0] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
+            sg[u].n[1] = sg[u].s[1] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+            st.l[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fqa_v8h, ones), __builtin_bit_cast(fqa_v8h, pt[r][i]), st.l[r], 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const fqa_v8h even = fqa_values<0>(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1]);
+            const fqa_v8h odd = fqa_values<1>(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                st.o[r][2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, __builtin_bit_cast(fqa_v8h, pt[r][i]), st.o[r][2 * w], 0, 0, 0);
+                st.o[r][2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odd, __builtin_bit_cast(fqa_v8h, pt[r][i]), st.o[r][2 * w + 1], 0, 0, 0);
+            }
+        }
+    }
+}
+
+// Tiles t0 .. t1 of a head's tokens below `len`, NT tiles a step, the next AHEAD steps' bytes on their way meanwhile (buffers that
+// change roles in an unrolled loop, so that no register is copied).
+template <int RT, int NT, int AHEAD>
+__device__ __forceinline__ void fqa_range(fqa_cursor& cur, int t0, int t1, int len, const fqa_queries<RT>& Q, fqa_state<RT>& st, int lane) {
     const int g = lane >> 4;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        st.m[r] = FQA_ZERO;
-        st.l[r] = 0.f;
-        st.z[r] = (fq_v4f){0.f, 0.f, 0.f, 0.f};
+        st.m[r] = FQA_LOWEST;
+        st.sub[r] = fmaf(FQA_LOWEST, -Q.qs[r], FQA_LIFT);
+        st.l[r] = (fq_v4f){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 8; ++j) st.o[r][j] = (fq_v4f){0.f, 0.f, 0.f, 0.f};
     }
-    fq_v4f zp[RT];
-    constexpr int E = (int)FQ_ZP_BYTES;
-    const fq_v8i eights = {E, E, E, E, E, E, E, E};
+    unsigned mask = 0x03C003C0u, base = 0x4C004C00u;
+    asm("" : "+s"(mask));
+    asm("" : "+v"(base));
+    fqa_tile buf[AHEAD + 1][NT];
+    const int whole = len >> 4 < t1 ? len >> 4 : t1;      // tiles below need no mask
+    int tb = t0;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) zp[r] = FQA_MFMA_QK(eights, q[r], ((fq_v4f){0.f, 0.f, 0.f, 0.f}));
-    const fq_v4i offset = {0x4E004E00, 0x4E004E00, 0x4E004E00, 0x4E004E00};   // 24 in fp16
-    fqa_tile buf[NT];
-    cur.start(t0, t1, lane);
+    for (int u = 0; u < AHEAD; ++u)
+        if (u == 0 || tb + u * NT < t1) cur.next(buf[u], lane);
+    while (tb + (AHEAD + 1) * NT <= whole) {
 #pragma unroll
-    for (int i = 0; i < NT; ++i) buf[i] = cur.next(lane);
-    for (int tb = t0; tb < t1; tb += NT) {
-        fqa_tile now[NT];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) now[i] = buf[i];
-        if (tb + NT < t1) {
-#pragma unroll
-            for (int i = 0; i < NT; ++i) buf[i] = cur.next(lane);
+        for (int u = 0; u <= AHEAD; ++u) {
+            cur.next(buf[(u + AHEAD) % (AHEAD + 1)], lane);
+            fqa_step<RT, NT, false>(buf[u], tb + u * NT, len, Q, st, mask, base, g);
         }
-        const bool tail = (tb + NT) * 16 > len;
-        fq_v4f p[RT][NT];
-        float vs[NT][4];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const fq_v8i a = fq_unpack_chunk(now[i].k);
-            const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[0], false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[0], true);
-            const fq_v2f v01 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[1], false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[1], true);
-            const float ks[4] = {s01[0], s01[1], s23[0], s23[1]};
-            vs[i][0] = v01[0]; vs[i][1] = v01[1]; vs[i][2] = v23[0]; vs[i][3] = v23[1];
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const fq_v4f c = FQA_MFMA_QK(a, q[r], zp[r]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) p[r][i][e] = c[e] * ks[e] * qs[r];
-            }
-        }
-        if (tail) {
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if ((tb + i) * 16 + 4 * g + e >= len) {
-                        vs[i][e] = 0.f;
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) p[r][i][e] = FQA_ZERO;
-                    }
-        }
-        fq_v4i pt[RT][NT / 2];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            float top = p[r][0][0];
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top = fmaxf(top, p[r][i][e]);
-            top = fqa_over_groups_max(top);
-            if (__any(top > st.m[r])) {
-                const float m = fmaxf(st.m[r], top), f = __builtin_amdgcn_exp2f(st.m[r] - m);
-                st.m[r] = m;
-                st.l[r] *= f;
-                st.z[r] *= f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) st.o[r][j] *= f;
-            }
-            const float sub = st.m[r] - FQA_LIFT;
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    const float a = __builtin_amdgcn_exp2f(p[r][i][e] - sub), b = __builtin_amdgcn_exp2f(p[r][i][e + 1] - sub);
-                    st.l[r] += a + b;
-                    pt[r][i / 2][2 * (i & 1) + e / 2] = __builtin_bit_cast(int, __builtin_convertvector((fq_v2f){a * vs[i][e], b * vs[i][e + 1]}, fqa_v2h));
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < NT / 2; ++i) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-                st.z[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fqa_v8h, offset), __builtin_bit_cast(fqa_v8h, pt[r][i]), st.z[r], 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const unsigned w0 = (unsigned)now[2 * i].v[j >> 1], w1 = (unsigned)now[2 * i + 1].v[j >> 1];
-                const fq_v4i a = j & 1 ? (fq_v4i){fqa_value_pair(w0 << 2), fqa_value_pair(w0 >> 6), fqa_value_pair(w1 << 2), fqa_value_pair(w1 >> 6)}
-                                       : (fq_v4i){fqa_value_pair(w0 << 6), fqa_value_pair(w0 >> 2), fqa_value_pair(w1 << 6), fqa_value_pair(w1 >> 2)};
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-                    st.o[r][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fqa_v8h, a), __builtin_bit_cast(fqa_v8h, pt[r][i]), st.o[r][j], 0, 0, 0);
-            }
-        }
+        tb += (AHEAD + 1) * NT;
     }
+    if (tb + AHEAD * NT < t1) cur.next(buf[AHEAD], lane);
+#pragma unroll
+    for (int u = 0; u <= AHEAD; ++u)
+        if (tb + u * NT < t1) fqa_step<RT, NT, true>(buf[u], tb + u * NT, len, Q, st, mask, base, g);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        st.l[r] = fqa_over_groups_sum(st.l[r]);
-        if (cur.bad) st.l[r] = __builtin_nanf("");
-#pragma unroll
-        for (int j = 0; j < 8; ++j) st.o[r][j] -= st.z[r];
+        st.m[r] *= Q.qs[r];
+        if (cur.bad) st.l[r][0] = __builtin_nanf("");
     }
 }
 
@@ -212,86 +253,73 @@ struct fqa_parts {
     int slots;
 };
 
-// Own tokens: a workgroup takes `chunk` tiles of one sequence for 16 query rows of a key/value head, its waves share them.
-template <int WAVES, int NT>
-__global__ __launch_bounds__(64 * WAVES) void fqa_own_kernel(fq_attend_args a, fqa_parts parts, int chunk, int first_slot, int row_tiles) {
-    __shared__ float wm[WAVES][16], wl[WAVES][16];
-    __shared__ float wo[WAVES][16][132];
+// A workgroup's work: tiles c0 .. c1 of one key/value head for `rows` (up to 16 RT) query rows, numbered by row_of(0 .. rows - 1).  Its waves
+// share the tiles out and join their sums through LDS; the result is a part of each row, or, with one part, the row's output.
+template <int RT, int WAVES>
+struct fqa_shared {
+    float m[WAVES][16 * RT], l[WAVES][16 * RT], o[WAVES][16 * RT][132];
+};
+template <int RT, int WAVES, int NT, int AHEAD, class F>
+__device__ __forceinline__ void fqa_group(const fq_attend_args& a, const fqa_parts& parts, fqa_shared<RT, WAVES>& sh, int c0, int c1, int len,
+                                          const int* pages_of, bool bad, int kv, int rows, F row_of, int slot) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-    const int b = blockIdx.z, kv = blockIdx.y / row_tiles, rt = blockIdx.y % row_tiles, G = a.Hq / a.Hkv;
-    const int raw = a.lens[b];
-    const long long most = (long long)a.width * a.c.page;
-    const int cap = a.max_len < most ? a.max_len : (int)most;
-    const bool too_long = raw > cap;
-    const int len = raw > cap ? cap : raw < 0 ? 0 : raw, tiles = (len + 15) >> 4;
-    const int c0 = (int)blockIdx.x * chunk;
-    const int rows = G - 16 * rt < 16 ? G - 16 * rt : 16;
-    const int row0 = b * a.Hq + kv * G + 16 * rt;
-    const bool direct = parts.slots == 1;
-    if (c0 >= tiles) {
-        if (direct) {                                     // no tokens at all
-            for (int i = threadIdx.x; i < rows * 16; i += 64 * WAVES)
-                reinterpret_cast<fq_v4i*>(a.O)[(size_t)row0 * 16 + i] = too_long ? (fq_v4i){0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0, 0x7FC07FC0} : (fq_v4i){0, 0, 0, 0};
-        } else if ((int)threadIdx.x < rows) {
-            float* ml = parts.ml + ((size_t)(row0 + threadIdx.x) * parts.slots + first_slot + blockIdx.x) * 2;
-            ml[0] = FQA_ZERO;
-            ml[1] = too_long ? __builtin_nanf("") : 0.f;
-        }
-        return;
-    }
-    const int c1 = c0 + chunk < tiles ? c0 + chunk : tiles;
     // the waves' shares: steps of NT tiles
     const int steps = (c1 - c0 + NT - 1) / NT, per = (steps + WAVES - 1) / WAVES * NT;
     const int t0 = c0 + wave * per, t1 = t0 + per < c1 ? t0 + per : c1;
     if (t0 < t1) {
-        const size_t row = (size_t)row0 + (n < rows ? n : 0);
-        const fq_v4i* qp = reinterpret_cast<const fq_v4i*>(a.Q + row * 128 + 32 * g);
-        const fq_v4i qa = qp[0], qb = qp[1];
-        const fq_v8i q[1] = {{qa[0], qa[1], qa[2], qa[3], qb[0], qb[1], qb[2], qb[3]}};
-        const float qs[1] = {a.q_scale[row] * a.out_scale * (512.0f * 1.44269504088896340736f)};
         fqa_cursor cur;
-        cur.pages_of = a.table + (size_t)b * a.width;
+        cur.pages_of = pages_of;
         cur.head = a.c.base + kv * a.c.head_stride;
-        cur.page_stride = a.c.page_stride;
+        cur.page_stride = (unsigned)(a.c.page_stride >> 4);
         cur.tiles_per_page = a.c.page >> 4;
         cur.pages = a.c.pages;
-        cur.bad = too_long;
-        fqa_state<1> st;
-        fqa_range<1, NT>(cur, t0, t1, len, q, qs, st, lane);
-        if (g == 0) {
-            wm[wave][n] = st.m[0];
-            wl[wave][n] = st.l[0];
-        }
+        cur.bad = bad;
+        cur.start(t0, t1, lane);
+        fqa_queries<RT> Q;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            *reinterpret_cast<fq_v4f*>(&wo[wave][n][16 * j + 4 * g]) = st.o[0][j];
-    } else if (g == 0) {
-        wm[wave][n] = FQA_ZERO;
-        wl[wave][n] = 0.f;
+        for (int r = 0; r < RT; ++r) {
+            const size_t row = row_of(16 * r + n < rows ? 16 * r + n : 0);
+            fqa_take_query(Q, r, a.Q + row * 128, a.q_scale[row], a.out_scale, g);
+        }
+        fqa_state<RT> st;
+        fqa_range<RT, NT, AHEAD>(cur, t0, t1, len, Q, st, lane);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            if (g == 0) {
+                sh.m[wave][16 * r + n] = st.m[r];
+                sh.l[wave][16 * r + n] = st.l[r][0];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(&sh.o[wave][16 * r + n][16 * j + 4 * g]) = st.o[r][j];
+        }
+    } else if (lane < 16 * RT) {
+        sh.m[wave][lane] = FQA_LOWEST;
+        sh.l[wave][lane] = 0.f;
     }
     __syncthreads();
+    const bool direct = parts.slots == 1;
     for (int i = threadIdx.x; i < rows * 32; i += 64 * WAVES) {   // four channels of a row
         const int r = i >> 5, c = 4 * (i & 31);
-        float top = FQA_ZERO, l = 0.f;
+        float top = FQA_LOWEST, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, wm[w][r]);
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sh.m[w][r]);
         fq_v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            if (wl[w][r] == 0.f) continue;                // (a wave without tokens; a NaN is kept)
-            const float f = __builtin_amdgcn_exp2f(wm[w][r] - top);
-            l += wl[w][r] * f;
-            o += *reinterpret_cast<const fq_v4f*>(&wo[w][r][c]) * f;
+            if (sh.l[w][r] == 0.f) continue;              // (a wave without tokens; a NaN is kept)
+            const float f = __builtin_amdgcn_exp2f(sh.m[w][r] - top);
+            l += sh.l[w][r] * f;
+            o += *reinterpret_cast<const fq_v4f*>(&sh.o[w][r][c]) * f;
         }
+        const size_t row = row_of(r);
         if (direct) {
-            const float inv = 1.0f / l;
-            o *= inv;
+            o *= 1.0f / l;
             uint2 out;
             out.x = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[0], o[1]}, fq_v2bf));
             out.y = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[2], o[3]}, fq_v2bf));
-            *reinterpret_cast<uint2*>(a.O + (size_t)(row0 + r) * 128 + c) = out;
+            *reinterpret_cast<uint2*>(a.O + row * 128 + c) = out;
         } else {
-            const size_t at = (size_t)(row0 + r) * parts.slots + first_slot + blockIdx.x;
+            const size_t at = row * parts.slots + slot;
             *reinterpret_cast<fq_v4f*>(parts.o + at * 128 + c) = o;
             if (c == 0) {
                 parts.ml[at * 2] = top;
@@ -301,71 +329,111 @@ __global__ __launch_bounds__(64 * WAVES) void fqa_own_kernel(fq_attend_args a, f
     }
 }
 
-// The shared prefix: a wave takes `chunk` tiles for RT * 16 of a key/value head's B * G query rows.
-template <int RT, int NT>
-__global__ __launch_bounds__(256) void fqa_prefix_kernel(fq_attend_args a, fqa_parts parts, int chunk) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-    const int kv = blockIdx.z, G = a.Hq / a.Hkv, rows = a.B * G;
-    const int first = ((int)blockIdx.y * 4 + wave) * RT * 16;
-    if (first >= rows) return;
-    const int tiles = (a.prefix + 15) >> 4, t0 = (int)blockIdx.x * chunk, t1 = t0 + chunk < tiles ? t0 + chunk : tiles;
-    fq_v8i q[RT];
-    float qs[RT];
-    size_t at[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int i = first + 16 * r + n, k = i < rows ? i : rows - 1;
-        at[r] = (size_t)(k / G) * a.Hq + kv * G + k % G;
-        const fq_v4i* qp = reinterpret_cast<const fq_v4i*>(a.Q + at[r] * 128 + 32 * g);
-        const fq_v4i qa = qp[0], qb = qp[1];
-        q[r] = (fq_v8i){qa[0], qa[1], qa[2], qa[3], qb[0], qb[1], qb[2], qb[3]};
-        qs[r] = a.q_scale[at[r]] * a.out_scale * (512.0f * 1.44269504088896340736f);
-    }
-    fqa_cursor cur;
-    cur.pages_of = a.shared;
-    cur.head = a.c.base + kv * a.c.head_stride;
-    cur.page_stride = a.c.page_stride;
-    cur.tiles_per_page = a.c.page >> 4;
-    cur.pages = a.c.pages;
-    cur.bad = false;
-    fqa_state<RT> st;
-    fqa_range<RT, NT>(cur, t0, t1, a.prefix, q, qs, st, lane);
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        if (first + 16 * r + n >= rows) continue;
-        const size_t s = at[r] * parts.slots + blockIdx.x;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(parts.o + s * 128 + 16 * j + 4 * g) = st.o[r][j];
-        if (g == 0) {
-            parts.ml[s * 2] = st.m[r];
-            parts.ml[s * 2 + 1] = st.l[r];
+// Own tokens: a workgroup takes `chunk` tiles of one sequence for 16 query rows of a key/value head.  Heads are the fastest index and chunks the
+// slowest: workgroup i runs on XCD i % 8, and with chunks (of which a short sequence has the first ones only) or sequences fastest some
+// XCDs got most of the work (37 sequences of 0 to 6000 tokens 37.0 us, 31.9 with a number of chunks that happened to spread them).
+template <int WAVES, int NT, int AHEAD>
+__global__ __launch_bounds__(64 * WAVES, 4) void fqa_own_kernel(fq_attend_args a, fqa_parts parts, int chunk, int first_slot, int row_tiles) {
+    __shared__ fqa_shared<1, WAVES> sh;
+    const int heads = a.Hkv * row_tiles, b = (int)blockIdx.x / heads, kv = (int)blockIdx.x % heads / row_tiles, rt = (int)blockIdx.x % row_tiles;
+    const int G = a.Hq / a.Hkv, raw = a.lens[b];
+    const long long most = (long long)a.width * a.c.page;
+    const int cap = a.max_len < most ? a.max_len : (int)most;
+    const bool too_long = raw > cap;
+    const int len = raw > cap ? cap : raw < 0 ? 0 : raw, tiles = (len + 15) >> 4;
+    const int c0 = (int)blockIdx.y * chunk, c1 = c0 + chunk < tiles ? c0 + chunk : tiles;
+    const int rows = G - 16 * rt < 16 ? G - 16 * rt : 16;
+    const int row0 = b * a.Hq + kv * G + 16 * rt, slot = first_slot + (int)blockIdx.y;
+    if (c0 >= tiles) {                                    // no tokens
+        if (parts.slots == 1) {
+            constexpr int N = 0x7FC07FC0;
+            for (int i = threadIdx.x; i < rows * 16; i += 64 * WAVES)
+                reinterpret_cast<fq_v4i*>(a.O)[(size_t)row0 * 16 + i] = too_long ? (fq_v4i){N, N, N, N} : (fq_v4i){0, 0, 0, 0};
+        } else if ((int)threadIdx.x < rows) {
+            float* ml = parts.ml + ((size_t)(row0 + threadIdx.x) * parts.slots + slot) * 2;
+            ml[0] = FQA_LOWEST;
+            ml[1] = too_long ? __builtin_nanf("") : 0.f;
         }
+        return;
     }
+    fqa_group<1, WAVES, NT, AHEAD>(a, parts, sh, c0, c1, len, a.table + (size_t)b * a.width, too_long, kv, rows, [=](int i) { return (size_t)row0 + i; }, slot);
 }
 
-// One wave per row: the parts' sums, each brought to the largest maximum.
-__global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t* __restrict__ O, int rows) {
-    const int lane = threadIdx.x & 63, row = (int)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= rows) return;
-    const float* ml = parts.ml + (size_t)row * parts.slots * 2;
-    const float* po = parts.o + (size_t)row * parts.slots * 128;
-    float top = FQA_ZERO;
-    for (int s = lane; s < parts.slots; s += 64) top = fmaxf(top, ml[2 * s]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    float l = 0.f, x = 0.f, y = 0.f;
-    for (int s = 0; s < parts.slots; ++s) {
-        const float pl = ml[2 * s + 1];
-        if (pl == 0.f) continue;
-        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - top);
-        l += pl * f;
-        const fq_v2f o = *reinterpret_cast<const fq_v2f*>(po + (size_t)s * 128 + 2 * lane);
-        x += o[0] * f;
-        y += o[1] * f;
-    }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-    reinterpret_cast<unsigned*>(O)[(size_t)row * 64 + lane] = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){x * inv, y * inv}, fq_v2bf));
+// The shared prefix: a workgroup takes `chunk` tiles for 16 RT of a key/value head's B * G query rows.  Workgroups with the same tiles of a
+// head follow each other at a distance of Hkv, so that with 8 heads (or a multiple) they run on one XCD and find them in its L2.
+template <int RT, int WAVES, int NT, int AHEAD>
+__global__ __launch_bounds__(64 * WAVES, 2) void fqa_prefix_kernel(fq_attend_args a, fqa_parts parts, int chunk, int row_groups) {
+    __shared__ fqa_shared<RT, WAVES> sh;
+    const int kv = (int)(blockIdx.x % a.Hkv), group = (int)(blockIdx.x / a.Hkv % row_groups), slot = (int)(blockIdx.x / a.Hkv / row_groups);
+    const int G = a.Hq / a.Hkv, all = a.B * G, first = group * 16 * RT, rows = all - first < 16 * RT ? all - first : 16 * RT;
+    const int tiles = (a.prefix + 15) >> 4, c0 = slot * chunk, c1 = c0 + chunk < tiles ? c0 + chunk : tiles;
+    fqa_group<RT, WAVES, NT, AHEAD>(a, parts, sh, c0, c1, a.prefix, a.shared, false, kv, rows,
+                                    [&](int i) { return (size_t)((first + i) / G) * a.Hq + kv * G + (first + i) % G; }, slot);
 }
+
+// The parts' sums, each brought to the largest maximum.  A workgroup per row: 32 lanes hold the 128 channels, its 8 groups of 32 lanes
+// take every eighth part, four requested at a time.
+__global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t* __restrict__ O) {
+    __shared__ float wm[8], wl[8];
+    __shared__ fq_v4f wo[8][32];
+    const int c = threadIdx.x & 31, grp = threadIdx.x >> 5, row = blockIdx.x, n = parts.slots;
+    const fq_v2f* ml = reinterpret_cast<const fq_v2f*>(parts.ml) + (size_t)row * n;
+    const fq_v4f* po = reinterpret_cast<const fq_v4f*>(parts.o) + (size_t)row * n * 32 + c;
+    float m = FQA_LOWEST, l = 0.f;
+    fq_v4f o = {0.f, 0.f, 0.f, 0.f};
+    for (int s0 = grp; s0 < n; s0 += 32) {
+        fq_v2f pm[4];
+        fq_v4f x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int s = s0 + 8 * u < n ? s0 + 8 * u : s0;
+            pm[u] = ml[s];
+            x[u] = po[(size_t)s * 32];
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (s0 + 8 * u >= n) pm[u][1] = 0.f;
+            if (pm[u][1] != 0.f) top = fmaxf(top, pm[u][0]);   // (an empty part has no sums)
+        }
+        const float f = __builtin_amdgcn_exp2f(m - top);
+        l *= f;
+        o *= f;
+        m = top;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (pm[u][1] == 0.f) continue;
+            const float fu = __builtin_amdgcn_exp2f(pm[u][0] - top);
+            l += pm[u][1] * fu;
+            o += x[u] * fu;
+        }
+    }
+    if (c == 0) {
+        wm[grp] = m;
+        wl[grp] = l;
+    }
+    wo[grp][c] = o;
+    __syncthreads();
+    if (grp) return;
+#pragma unroll
+    for (int i = 1; i < 8; ++i) m = fmaxf(m, wm[i]);
+    l = 0.f;
+    o = (fq_v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float f = __builtin_amdgcn_exp2f(wm[i] - m);
+        l += wl[i] * f;
+        o += wo[i][c] * f;
+    }
+    o *= l == 0.f ? 0.f : 1.0f / l;
+    uint2 out;
+    out.x = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[0], o[1]}, fq_v2bf));
+    out.y = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[2], o[3]}, fq_v2bf));
+    reinterpret_cast<uint2*>(O)[(size_t)row * 32 + c] = out;
+}
+
+constexpr int FQA_OWN_WAVES = 4, FQA_OWN_NT = 2, FQA_OWN_AHEAD = 1, FQA_PREFIX_RT = 2, FQA_PREFIX_WAVES = 4, FQA_PREFIX_NT = 2, FQA_PREFIX_AHEAD = 1;
+constexpr int FQA_OWN_WANT = 6, FQA_OWN_MIN = 16, FQA_OWN_MAX = 128, FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16;
 
 struct fqa_plan { int own_chunk, own_slots, prefix_chunk, prefix_slots; };
 
@@ -376,18 +444,29 @@ fqa_plan fqa_choose(int B, int Hq, int Hkv, int max_len, int prefix) {
     {
         // workgroups of four waves, about four for each compute unit
         const long long heads = (long long)B * Hkv * row_tiles;
-        long long want = (4ll * cus + heads - 1) / heads;
+        const long long want = (FQA_OWN_WANT * cus + heads - 1) / heads;
         long long chunk = (tiles + want - 1) / want;
-        chunk = chunk < 16 ? 16 : chunk > 128 ? 128 : (chunk + 15) / 16 * 16;
+        chunk = chunk < FQA_OWN_MIN ? FQA_OWN_MIN : chunk > FQA_OWN_MAX ? FQA_OWN_MAX : (chunk + 15) / 16 * 16;
+        if (chunk < tiles / 65535 + 1) chunk = tiles / 65535 + 1;   // (a grid's second dimension)
         p.own_chunk = (int)chunk;
         p.own_slots = (int)((tiles + chunk - 1) / chunk);
     }
     if (prefix > 0) {
         const int pt = (int)(((long long)prefix + 15) / 16);
-        const long long groups = ((long long)B * G + 127) / 128 * Hkv;
-        long long want = (2ll * cus + groups - 1) / groups;
+        const long long groups = ((long long)B * G + 16 * FQA_PREFIX_RT - 1) / (16 * FQA_PREFIX_RT) * Hkv;
+        const long long room = FQA_PREFIX_WANT * (long long)cus;   // workgroups that run at once
+        // as few parts as fill whole rounds of them to seven eighths, up to 16 parts
+        long long want = 1;
+        for (long long w = 1, best = 0; w <= 16 && best < 14; ++w) {
+            const long long used = 16 * groups * w / ((groups * w + room - 1) / room * room);
+            if (used > best) {
+                best = used;
+                want = w;
+            }
+        }
+        if (want < room / groups) want = room / groups;
         long long chunk = (pt + want - 1) / want;
-        chunk = chunk < 8 ? 8 : chunk > 64 ? 64 : (chunk + 3) / 4 * 4;
+        chunk = chunk < FQA_PREFIX_MIN ? FQA_PREFIX_MIN : (chunk + 7) / 8 * 8;
         p.prefix_chunk = (int)chunk;
         p.prefix_slots = (int)((pt + chunk - 1) / chunk);
     }
@@ -407,9 +486,12 @@ void fq_launch_attend(const fq_attend_args& a, void* scratch, hipStream_t stream
     const int slots = p.own_slots + p.prefix_slots, G = a.Hq / a.Hkv, row_tiles = (G + 15) / 16;
     const bool join = slots > 1 || a.prefix > 0;
     fqa_parts parts = {static_cast<float*>(scratch), static_cast<float*>(scratch) + (size_t)slots * a.B * a.Hq * 128, join ? slots : 1};
-    if (p.prefix_slots)
-        hipLaunchKernelGGL((fqa_prefix_kernel<2, 4>), dim3(p.prefix_slots, (a.B * G + 127) / 128, a.Hkv), dim3(256), 0, stream, a, parts, p.prefix_chunk);
-    hipLaunchKernelGGL((fqa_own_kernel<4, 4>), dim3(p.own_slots, a.Hkv * row_tiles, a.B), dim3(256), 0, stream, a, parts, p.own_chunk, p.prefix_slots, row_tiles);
-    if (join)
-        hipLaunchKernelGGL(fqa_join_kernel, dim3((unsigned)((a.B * a.Hq + 3) / 4)), dim3(256), 0, stream, parts, a.O, a.B * a.Hq);
+    if (p.prefix_slots) {
+        const int groups = (a.B * G + 16 * FQA_PREFIX_RT - 1) / (16 * FQA_PREFIX_RT);
+        hipLaunchKernelGGL((fqa_prefix_kernel<FQA_PREFIX_RT, FQA_PREFIX_WAVES, FQA_PREFIX_NT, FQA_PREFIX_AHEAD>), dim3((unsigned)(p.prefix_slots * groups * a.Hkv)),
+                           dim3(64 * FQA_PREFIX_WAVES), 0, stream, a, parts, p.prefix_chunk, groups);
+    }
+    hipLaunchKernelGGL((fqa_own_kernel<FQA_OWN_WAVES, FQA_OWN_NT, FQA_OWN_AHEAD>), dim3((unsigned)(a.B * a.Hkv * row_tiles), p.own_slots), dim3(64 * FQA_OWN_WAVES), 0, stream, a,
+                       parts, p.own_chunk, p.prefix_slots, row_tiles);
+    if (join) hipLaunchKernelGGL(fqa_join_kernel, dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, stream, parts, a.O);
 }
