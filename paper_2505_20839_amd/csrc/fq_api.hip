@@ -530,7 +530,8 @@ int check_paged(const uint8_t* cache, int64_t page_stride, int64_t head_stride, 
     if (pages < 0 || page <= 0 || page % FQ_KV4_TILE_TOKENS != 0 || heads <= 0 || heads > 65535) return FQ_ERR_SHAPE;
     const int64_t per = (int64_t)(page / FQ_KV4_TILE_TOKENS) * FQ_KV4_TILE_BYTES;
     if (page_stride <= 0 || head_stride <= 0 || page_stride % 16 != 0 || head_stride % 16 != 0 || per > 0x7FFFFFFF) return FQ_ERR_SHAPE;
-    if (page_stride >> 36) return FQ_ERR_SHAPE;           // (the kernels count pages in 16 bytes, 32 bits)
+    // (the kernels count a page's 16-byte units and a cache's tiles in 32 bits)
+    if ((page_stride >> 36) != 0 || (int64_t)pages * (page / FQ_KV4_TILE_TOKENS) > 0xFFFFFFFFll) return FQ_ERR_SHAPE;
     if ((heads > 1 && head_stride < per) || (pages > 1 && page_stride < per)) return FQ_ERR_SHAPE;
     if (pages > 0 && !cache) return FQ_ERR_NULL;
     if (!aligned16(cache)) return FQ_ERR_ALIGN;
@@ -596,7 +597,7 @@ int fq_kv4_append(const uint16_t* QKV_bf16, int64_t ld, const float* cos_sin, in
     const int rc = check_paged(cache, page_stride, head_stride, pages, page, Hkv);
     if (rc != FQ_OK) return rc;
     const int64_t heads = (int64_t)Hq + 2 * (int64_t)Hkv;
-    if (ld < heads * 128 || ld % 8 != 0 || (int64_t)T * heads > (int64_t)0x0FFFFFF0) return FQ_ERR_SHAPE;
+    if (ld < heads * 128 || ld % 8 != 0 || (int64_t)T * heads > (int64_t)0x0FFFFFF0 || T >= 1 << 23) return FQ_ERR_SHAPE;
     if (T == 0) return FQ_OK;
     if (!QKV_bf16 || !positions || !slots || !Q_fp8 || !q_scale || (max_positions > 0 && !cos_sin)) return FQ_ERR_NULL;
     if (!aligned16(QKV_bf16) || !aligned16(cos_sin) || !aligned16(Q_fp8)) return FQ_ERR_ALIGN;
