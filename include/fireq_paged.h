@@ -38,7 +38,8 @@
  *                 split).  A sequence longer than it, or than table_width * page, or a page number outside the cache
  *                 within a sequence's length, gives NaN for that sequence.
  * fq_kv4_attention_prefix_ws   the same where every sequence attends to prefix_len tokens in prefix_pages first, and then
- *                 to its own seq_lens[b] tokens: the prefix is read once for all sequences.
+ *                 to its own seq_lens[b] tokens: the prefix is read and unpacked for up to 32 query rows at a time, not for
+ *                 every sequence (unless that is less work than sharing it).
  * Scratch: fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) bytes, 16-byte aligned (prefix_len 0: without prefix).
  *
  * Q_fp8, cache, QKV_bf16, cos_sin, K, V, O: 16-byte aligned.  Conventions and status codes are those of fireq.h; T, n or B = 0

@@ -868,7 +868,7 @@ def fq_kv4_attention_prefix(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch
                             block_table: torch.Tensor, seq_lens: torch.Tensor, out_scale: float, max_len: Optional[int] = None,
                             out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """fq_kv4_attention for sequences that share a prefix: each attends to prefix_len tokens in prefix_pages (int32 [pages]) and
-    then to its own seq_lens[b] tokens in block_table[b].  The prefix is read once for all of them."""
+    then to its own seq_lens[b] tokens in block_table[b].  The prefix is worked on for many sequences at a time."""
     if prefix_pages is None:
         raise TypeError("prefix_pages must be a GPU tensor")
     return _attention("fq_kv4_attention_prefix", Q, q_scale, cache, prefix_pages, prefix_len, block_table, seq_lens, out_scale, max_len, out,

@@ -332,16 +332,19 @@ __device__ __forceinline__ void fqa_group(const fq_attend_args& a, const fqa_par
 // Own tokens: a workgroup takes `chunk` tiles of one sequence for 16 query rows of a key/value head.  Heads are the fastest index and chunks the
 // slowest: workgroup i runs on XCD i % 8, and with chunks (of which a short sequence has the first ones only) or sequences fastest some
 // XCDs got most of the work (37 sequences of 0 to 6000 tokens 37.0 us, 31.9 with a number of chunks that happened to spread them).
+// With shared_slots, the first workgroups of a sequence take a shared prefix instead, in chunks of shared_chunk tiles.
 template <int WAVES, int NT, int AHEAD>
-__global__ __launch_bounds__(64 * WAVES, 4) void fqa_own_kernel(fq_attend_args a, fqa_parts parts, int chunk, int first_slot, int row_tiles) {
+__global__ __launch_bounds__(64 * WAVES, 4) void fqa_own_kernel(fq_attend_args a, fqa_parts parts, int chunk, int first_slot, int row_tiles, int shared_slots,
+                                                                int shared_chunk) {
     __shared__ fqa_shared<1, WAVES> sh;
     const int heads = a.Hkv * row_tiles, b = (int)blockIdx.x / heads, kv = (int)blockIdx.x % heads / row_tiles, rt = (int)blockIdx.x % row_tiles;
-    const int G = a.Hq / a.Hkv, raw = a.lens[b];
+    const bool shared = (int)blockIdx.y < shared_slots;
+    const int G = a.Hq / a.Hkv, raw = shared ? a.prefix : a.lens[b];
     const long long most = (long long)a.width * a.c.page;
-    const int cap = a.max_len < most ? a.max_len : (int)most;
+    const int cap = shared ? raw : a.max_len < most ? a.max_len : (int)most;
     const bool too_long = raw > cap;
-    const int len = raw > cap ? cap : raw < 0 ? 0 : raw, tiles = (len + 15) >> 4;
-    const int c0 = (int)blockIdx.y * chunk, c1 = c0 + chunk < tiles ? c0 + chunk : tiles;
+    const int len = raw > cap ? cap : raw < 0 ? 0 : raw, tiles = (len + 15) >> 4, per = shared ? shared_chunk : chunk;
+    const int c0 = (shared ? (int)blockIdx.y : (int)blockIdx.y - shared_slots) * per, c1 = c0 + per < tiles ? c0 + per : tiles;
     const int rows = G - 16 * rt < 16 ? G - 16 * rt : 16;
     const int row0 = b * a.Hq + kv * G + 16 * rt, slot = first_slot + (int)blockIdx.y;
     if (c0 >= tiles) {                                    // no tokens
@@ -356,7 +359,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void fqa_own_kernel(fq_attend_args a
         }
         return;
     }
-    fqa_group<1, WAVES, NT, AHEAD>(a, parts, sh, c0, c1, len, a.table + (size_t)b * a.width, too_long, kv, rows, [=](int i) { return (size_t)row0 + i; }, slot);
+    fqa_group<1, WAVES, NT, AHEAD>(a, parts, sh, c0, c1, len, shared ? a.shared : a.table + (size_t)b * a.width, too_long, kv, rows, [=](int i) { return (size_t)row0 + i; }, slot);
 }
 
 // The shared prefix: a workgroup takes `chunk` tiles for 16 RT of a key/value head's B * G query rows.  Workgroups with the same tiles of a
@@ -433,28 +436,53 @@ __global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t
 }
 
 constexpr int FQA_OWN_WAVES = 4, FQA_OWN_NT = 2, FQA_OWN_AHEAD = 1, FQA_PREFIX_RT = 2, FQA_PREFIX_WAVES = 4, FQA_PREFIX_NT = 2, FQA_PREFIX_AHEAD = 1;
-constexpr int FQA_OWN_WANT = 6, FQA_OWN_MIN = 16, FQA_OWN_MAX = 128, FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16;
+constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 36000;
 
-struct fqa_plan { int own_chunk, own_slots, prefix_chunk, prefix_slots; };
+// own_chunk and own_slots: tiles of a part of a sequence, and parts of the longest; the same for the prefix, which is worked on for
+// row_groups groups of rows together, or (row_groups 0) for each sequence apart, like its own tokens.
+struct fqa_plan { int own_chunk, own_slots, prefix_chunk, prefix_slots, row_groups; };
+
+// Tiles of a part, for `heads` (sequence, key/value head, 16 query rows) of up to `tiles` each.  A wave of a part's four takes about 0.25 us a
+// tile beyond 4; a second part costs the joining kernel, 2 us.  us, from a graph, 32 query and 8 key/value heads unless said otherwise:
+//     one workgroup per compute unit           1 x 32001 tokens, parts of 64 (256 workgroups) 12.4; 32 (504) 13.7; 16 (1008) 16.2; 128 (128) 16.0
+//                                              1 x 8000, 16 (256) 8.5; 32 9.2; 64 11.3     16 x 4000, 128 (256) 16.8; 64 (512) 18.1; 32 18.5
+//     ... but at least 16 tiles                1 x 1000, 16 7.2; 64 8.1
+//     ... and up to 64 parts                   1 x 32001, 8 / 1 heads, 32 (63 parts) 10.0; 16 (126) 10.9
+//     one part of a short sequence             1 x 600, 7.2 -> 6.4;  with many heads 16 x 1000, 16 9.6; 64 8.8    30 x 700 of 32 heads 17.3 -> 13.8
+//     more workgroups than compute units: sequences differ in length, and short parts even that out
+//                                              37 x 0 .. 6000, 64 30.0; 128 35.1           128 x 0 .. 1500 (1024 heads), 94 28.9; 48 30.0
+int fqa_part(long long heads, int tiles) {
+    const long long cus = fq_device_cus();
+    if (tiles <= 40 || (tiles <= 64 && 2 * heads >= cus)) return tiles;
+    const long long want = heads < cus ? cus / heads : 1;
+    long long chunk = (tiles + want - 1) / want;
+    if (chunk < (tiles + 63) / 64) chunk = (tiles + 63) / 64;
+    chunk = chunk < 16 ? 16 : (chunk + 15) / 16 * 16;
+    const long long cap = heads < 2 * cus ? 64 : 128;
+    if (chunk > cap && heads * ((tiles + chunk - 1) / chunk) > cus) chunk = cap;
+    if (chunk < tiles / 60000 + 1) chunk = tiles / 60000 + 1;     // (a grid has 65535 in its second dimension)
+    return (int)(chunk < tiles ? chunk : tiles);
+}
 
 fqa_plan fqa_choose(int B, int Hq, int Hkv, int max_len, int prefix) {
-    fqa_plan p = {0, 0, 0, 0};
-    const int G = Hq / Hkv, row_tiles = (G + 15) / 16, cus = fq_device_cus();
+    fqa_plan p = {0, 0, 0, 0, 0};
+    const int G = Hq / Hkv, row_tiles = (G + 15) / 16;
+    const long long heads = (long long)B * Hkv * row_tiles;
     const int tiles = max_len > 0 ? (int)(((long long)max_len + 15) / 16) : 1;   // (one empty part says so where a length passes 0)
-    {
-        // workgroups of four waves, about four for each compute unit
-        const long long heads = (long long)B * Hkv * row_tiles;
-        const long long want = (FQA_OWN_WANT * cus + heads - 1) / heads;
-        long long chunk = (tiles + want - 1) / want;
-        chunk = chunk < FQA_OWN_MIN ? FQA_OWN_MIN : chunk > FQA_OWN_MAX ? FQA_OWN_MAX : (chunk + 15) / 16 * 16;
-        if (chunk < tiles / 65535 + 1) chunk = tiles / 65535 + 1;   // (a grid's second dimension)
-        p.own_chunk = (int)chunk;
-        p.own_slots = (int)((tiles + chunk - 1) / chunk);
-    }
+    p.own_chunk = fqa_part(heads, tiles);
+    p.own_slots = (tiles + p.own_chunk - 1) / p.own_chunk;
     if (prefix > 0) {
-        const int pt = (int)(((long long)prefix + 15) / 16);
-        const long long groups = ((long long)B * G + 16 * FQA_PREFIX_RT - 1) / (16 * FQA_PREFIX_RT) * Hkv;
-        const long long room = FQA_PREFIX_WANT * (long long)cus;   // workgroups that run at once
+        const int pt = (int)(((long long)prefix + 15) / 16), cus = fq_device_cus();
+        // Apart: one kernel less, no groups of rows to gather, but every sequence unpacks the prefix again.  us, apart / together (32 query, 8 key/value
+        // heads): 8 x 1100 8.5 / 14.8, 64 x 300 12.5 / 18.0, 16 x 4000 (32000 tiles) 16.3 / 17.8, 64 x 1000 (32256) 16.8 / 19.9; 96 x 1000 of 8 query
+        // heads (48384) 19.3 / 15.0, 30 x 8000 (120000) 42.4 / 26.7
+        if (heads * pt <= FQA_APART) {
+            p.prefix_chunk = fqa_part(heads, pt);
+            p.prefix_slots = (pt + p.prefix_chunk - 1) / p.prefix_chunk;
+            return p;
+        }
+        p.row_groups = (int)(((long long)B * G + 16 * FQA_PREFIX_RT - 1) / (16 * FQA_PREFIX_RT));
+        const long long groups = (long long)p.row_groups * Hkv, room = FQA_PREFIX_WANT * (long long)cus;   // workgroups, and how many run at once
         // as few parts as fill whole rounds of them to seven eighths, up to 16 parts
         long long want = 1;
         for (long long w = 1, best = 0; w <= 16 && best < 14; ++w) {
@@ -486,12 +514,11 @@ void fq_launch_attend(const fq_attend_args& a, void* scratch, hipStream_t stream
     const int slots = p.own_slots + p.prefix_slots, G = a.Hq / a.Hkv, row_tiles = (G + 15) / 16;
     const bool join = slots > 1 || a.prefix > 0;
     fqa_parts parts = {static_cast<float*>(scratch), static_cast<float*>(scratch) + (size_t)slots * a.B * a.Hq * 128, join ? slots : 1};
-    if (p.prefix_slots) {
-        const int groups = (a.B * G + 16 * FQA_PREFIX_RT - 1) / (16 * FQA_PREFIX_RT);
-        hipLaunchKernelGGL((fqa_prefix_kernel<FQA_PREFIX_RT, FQA_PREFIX_WAVES, FQA_PREFIX_NT, FQA_PREFIX_AHEAD>), dim3((unsigned)(p.prefix_slots * groups * a.Hkv)),
-                           dim3(64 * FQA_PREFIX_WAVES), 0, stream, a, parts, p.prefix_chunk, groups);
-    }
-    hipLaunchKernelGGL((fqa_own_kernel<FQA_OWN_WAVES, FQA_OWN_NT, FQA_OWN_AHEAD>), dim3((unsigned)(a.B * a.Hkv * row_tiles), p.own_slots), dim3(64 * FQA_OWN_WAVES), 0, stream, a,
-                       parts, p.own_chunk, p.prefix_slots, row_tiles);
+    if (p.row_groups)
+        hipLaunchKernelGGL((fqa_prefix_kernel<FQA_PREFIX_RT, FQA_PREFIX_WAVES, FQA_PREFIX_NT, FQA_PREFIX_AHEAD>), dim3((unsigned)(p.prefix_slots * p.row_groups * a.Hkv)),
+                           dim3(64 * FQA_PREFIX_WAVES), 0, stream, a, parts, p.prefix_chunk, p.row_groups);
+    const int apart = p.row_groups ? 0 : p.prefix_slots;
+    hipLaunchKernelGGL((fqa_own_kernel<FQA_OWN_WAVES, FQA_OWN_NT, FQA_OWN_AHEAD>), dim3((unsigned)(a.B * a.Hkv * row_tiles), apart + p.own_slots),
+                       dim3(64 * FQA_OWN_WAVES), 0, stream, a, parts, p.own_chunk, p.prefix_slots - apart, row_tiles, apart, p.prefix_chunk);
     if (join) hipLaunchKernelGGL(fqa_join_kernel, dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, stream, parts, a.O);
 }

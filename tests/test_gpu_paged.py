@@ -289,11 +289,12 @@ def _queries(rng, B, Hq, spread):
     return pu.to_e4m3((x / s[..., None]).astype(np.float32)), s
 
 
-def _check_attention(ref, table, lens, q, qs, Hkv, got, scale, pre=(), prefix=0, skip=()):
+def _check_attention(ref, table, lens, q, qs, Hkv, got, scale, pre=(), prefix=0, skip=(), only=None):
     B, Hq = q.shape[:2]
     page, G = ref.page, Hq // Hkv
     got = got.double().cpu().numpy()
-    for b in range(B):
+    assert np.isfinite(got).all() or skip
+    for b in range(B) if only is None else only:
         if b in skip:
             assert np.isnan(got[b]).all(), b
             continue
@@ -556,3 +557,29 @@ def test_attention_negative_and_zero_query_scales(fq):
     flipped, fs = q.copy(), np.abs(qs)
     flipped[1, 2] ^= 0x80
     _check_attention(ref, table, lens, flipped, fs, 1, got, 0.1)
+
+
+@pytest.mark.parametrize("B, Hq, Hkv, page, prefix, longest", [
+    (40, 4, 1, 16, 3000, 4), (130, 1, 1, 48, 1203, 1), (32, 8, 2, 128, 2047, 20), (65, 2, 1, 16, 17, 2), (100, 16, 8, 16, 130, 1),
+    (200, 2, 1, 16, 3201, 3), (130, 12, 4, 48, 1303, 20), (20, 40, 8, 128, 4000, 9), (1000, 1, 1, 16, 700, 1), (300, 20, 1, 32, 999, 2)])
+def test_attention_of_many_rows_behind_a_prefix(fq, B, Hq, Hkv, page, prefix, longest):
+    """The prefix apart for each sequence (the first five) and together for groups of rows: last groups of few rows, chunks and waves without
+    tokens, tiles that the prefix ends in.  A sample of the sequences is checked."""
+    rng = np.random.default_rng(B + prefix)
+    lens = [int(n) for n in rng.integers(0, longest + 1, B)]
+    ref, table, pre = _filled(rng, lens, Hkv, page, prefix=prefix)
+    q, qs = _queries(rng, B, Hq, 1.5)
+    got = fq.fq_kv4_attention_prefix(torch.from_numpy(q).cuda(), torch.from_numpy(qs).cuda(), torch.from_numpy(ref.b).cuda(), torch.from_numpy(pre).cuda(), prefix,
+                                     torch.from_numpy(table).cuda(), torch.tensor(lens, dtype=torch.int32).cuda(), 0.1, max_len=longest)
+    _check_attention(ref, table, lens, q, qs, Hkv, got, 0.1, pre, prefix, only=sorted({0, B - 1} | set(rng.integers(0, B, 12).tolist())))
+
+
+@pytest.mark.parametrize("B", [3, 30, 900])
+def test_a_bad_prefix_page_is_everybodys(fq, B):
+    rng = np.random.default_rng(B)
+    ref, table, pre = _filled(rng, [5] * B, 1, 16, prefix=700)
+    q, qs = _queries(rng, B, 4, 1)
+    pre[17] = ref.b.shape[0] + 5
+    got = fq.fq_kv4_attention_prefix(torch.from_numpy(q).cuda(), torch.from_numpy(qs).cuda(), torch.from_numpy(ref.b).cuda(), torch.from_numpy(pre).cuda(), 700,
+                                     torch.from_numpy(table).cuda(), torch.full((B,), 5, dtype=torch.int32, device="cuda"), 0.1)
+    assert bool(torch.isnan(got.float()).all())
