@@ -374,29 +374,34 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fqa_prefix_kernel(fq_attend_arg
                                     [&](int i) { return (size_t)((first + i) / G) * a.Hq + kv * G + (first + i) % G; }, slot);
 }
 
-// The parts' sums, each brought to the largest maximum.  A workgroup per row: 32 lanes hold the 128 channels, its 8 groups of 32 lanes
-// take every eighth part, four requested at a time.
-__global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t* __restrict__ O) {
-    __shared__ float wm[8], wl[8];
-    __shared__ fq_v4f wo[8][32];
-    const int c = threadIdx.x & 31, grp = threadIdx.x >> 5, row = blockIdx.x, n = parts.slots;
+// The parts' sums, each brought to the largest maximum.  32 lanes hold the 128 channels of a row; GROUPS of 32 lanes share its parts, four
+// requested at a time.  A wave per row for up to 8 parts (no LDS, no barrier; 96 sequences behind a prefix, 3072 rows of 6 parts, the whole
+// call 46.8 us, 50.1 with a workgroup each; 1 x 1000 tokens 6.9 and 7.3), a workgroup for more (12 parts 7.9 us, 8.3 with a wave; 32 parts
+// 12.4 and 14.0).
+template <int GROUPS>
+__global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t* __restrict__ O, int rows) {
+    constexpr int ROWS = 8 / GROUPS;                      // of a workgroup
+    __shared__ float wm[GROUPS], wl[GROUPS];
+    __shared__ fq_v4f wo[GROUPS][32];
+    const int c = threadIdx.x & 31, grp = (int)(threadIdx.x >> 5) % GROUPS, row = (int)blockIdx.x * ROWS + (int)(threadIdx.x >> 5) / GROUPS, n = parts.slots;
+    if (row >= rows) return;                              // (one row a workgroup where there is a barrier)
     const fq_v2f* ml = reinterpret_cast<const fq_v2f*>(parts.ml) + (size_t)row * n;
     const fq_v4f* po = reinterpret_cast<const fq_v4f*>(parts.o) + (size_t)row * n * 32 + c;
     float m = FQA_LOWEST, l = 0.f;
     fq_v4f o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = grp; s0 < n; s0 += 32) {
+    for (int s0 = grp; s0 < n; s0 += 4 * GROUPS) {
         fq_v2f pm[4];
         fq_v4f x[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int s = s0 + 8 * u < n ? s0 + 8 * u : s0;
+            const int s = s0 + GROUPS * u < n ? s0 + GROUPS * u : s0;
             pm[u] = ml[s];
             x[u] = po[(size_t)s * 32];
         }
         float top = m;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            if (s0 + 8 * u >= n) pm[u][1] = 0.f;
+            if (s0 + GROUPS * u >= n) pm[u][1] = 0.f;
             if (pm[u][1] != 0.f) top = fmaxf(top, pm[u][0]);   // (an empty part has no sums)
         }
         const float f = __builtin_amdgcn_exp2f(m - top);
@@ -411,22 +416,34 @@ __global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t
             o += x[u] * fu;
         }
     }
-    if (c == 0) {
-        wm[grp] = m;
-        wl[grp] = l;
-    }
-    wo[grp][c] = o;
-    __syncthreads();
-    if (grp) return;
+    if (GROUPS == 2) {                                    // the other half of the wave
+        const float top = fmaxf(m, __shfl_xor(m, 32, 64)), f = __builtin_amdgcn_exp2f(m - top);
+        l *= f;
+        l += __shfl_xor(l, 32, 64);
 #pragma unroll
-    for (int i = 1; i < 8; ++i) m = fmaxf(m, wm[i]);
-    l = 0.f;
-    o = (fq_v4f){0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < 4; ++i) {
+            o[i] *= f;
+            o[i] += __shfl_xor(o[i], 32, 64);
+        }
+        if (grp) return;
+    } else {
+        if (c == 0) {
+            wm[grp] = m;
+            wl[grp] = l;
+        }
+        wo[grp][c] = o;
+        __syncthreads();
+        if (grp) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float f = __builtin_amdgcn_exp2f(wm[i] - m);
-        l += wl[i] * f;
-        o += wo[i][c] * f;
+        for (int i = 1; i < GROUPS; ++i) m = fmaxf(m, wm[i]);
+        l = 0.f;
+        o = (fq_v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+            const float f = __builtin_amdgcn_exp2f(wm[i] - m);
+            l += wl[i] * f;
+            o += wo[i][c] * f;
+        }
     }
     o *= l == 0.f ? 0.f : 1.0f / l;
     uint2 out;
@@ -436,7 +453,7 @@ __global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t
 }
 
 constexpr int FQA_OWN_WAVES = 4, FQA_OWN_NT = 2, FQA_OWN_AHEAD = 1, FQA_PREFIX_RT = 2, FQA_PREFIX_WAVES = 4, FQA_PREFIX_NT = 2, FQA_PREFIX_AHEAD = 1;
-constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 36000;
+constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 36000, FQA_JOIN_FEW = 8;
 
 // own_chunk and own_slots: tiles of a part of a sequence, and parts of the longest; the same for the prefix, which is worked on for
 // row_groups groups of rows together, or (row_groups 0) for each sequence apart, like its own tokens.
@@ -451,8 +468,7 @@ struct fqa_plan { int own_chunk, own_slots, prefix_chunk, prefix_slots, row_grou
 //     one part of a short sequence             1 x 600, 7.2 -> 6.4;  with many heads 16 x 1000, 16 9.6; 64 8.8    30 x 700 of 32 heads 17.3 -> 13.8
 //     more workgroups than compute units: sequences differ in length, and short parts even that out
 //                                              37 x 0 .. 6000, 64 30.0; 128 35.1           128 x 0 .. 1500 (1024 heads), 94 28.9; 48 30.0
-int fqa_part(long long heads, int tiles) {
-    const long long cus = fq_device_cus();
+int fqa_part(long long heads, int tiles, long long cus) {
     if (tiles <= 40 || (tiles <= 64 && 2 * heads >= cus)) return tiles;
     const long long want = heads < cus ? cus / heads : 1;
     long long chunk = (tiles + want - 1) / want;
@@ -466,18 +482,18 @@ int fqa_part(long long heads, int tiles) {
 
 fqa_plan fqa_choose(int B, int Hq, int Hkv, int max_len, int prefix) {
     fqa_plan p = {0, 0, 0, 0, 0};
-    const int G = Hq / Hkv, row_tiles = (G + 15) / 16;
+    const int G = Hq / Hkv, row_tiles = (G + 15) / 16, cus = fq_device_cus();
     const long long heads = (long long)B * Hkv * row_tiles;
     const int tiles = max_len > 0 ? (int)(((long long)max_len + 15) / 16) : 1;   // (one empty part says so where a length passes 0)
-    p.own_chunk = fqa_part(heads, tiles);
+    p.own_chunk = fqa_part(heads, tiles, cus);
     p.own_slots = (tiles + p.own_chunk - 1) / p.own_chunk;
     if (prefix > 0) {
-        const int pt = (int)(((long long)prefix + 15) / 16), cus = fq_device_cus();
+        const int pt = (int)(((long long)prefix + 15) / 16);
         // Apart: one kernel less, no groups of rows to gather, but every sequence unpacks the prefix again.  us, apart / together (32 query, 8 key/value
         // heads): 8 x 1100 8.5 / 14.8, 64 x 300 12.5 / 18.0, 16 x 4000 (32000 tiles) 16.3 / 17.8, 64 x 1000 (32256) 16.8 / 19.9; 96 x 1000 of 8 query
         // heads (48384) 19.3 / 15.0, 30 x 8000 (120000) 42.4 / 26.7
         if (heads * pt <= FQA_APART) {
-            p.prefix_chunk = fqa_part(heads, pt);
+            p.prefix_chunk = fqa_part(heads, pt, cus);
             p.prefix_slots = (pt + p.prefix_chunk - 1) / p.prefix_chunk;
             return p;
         }
@@ -520,5 +536,9 @@ void fq_launch_attend(const fq_attend_args& a, void* scratch, hipStream_t stream
     const int apart = p.row_groups ? 0 : p.prefix_slots;
     hipLaunchKernelGGL((fqa_own_kernel<FQA_OWN_WAVES, FQA_OWN_NT, FQA_OWN_AHEAD>), dim3((unsigned)(a.B * a.Hkv * row_tiles), apart + p.own_slots),
                        dim3(64 * FQA_OWN_WAVES), 0, stream, a, parts, p.own_chunk, p.prefix_slots - apart, row_tiles, apart, p.prefix_chunk);
-    if (join) hipLaunchKernelGGL(fqa_join_kernel, dim3((unsigned)(a.B * a.Hq)), dim3(256), 0, stream, parts, a.O);
+    if (join) {
+        const int rows = a.B * a.Hq;
+        if (slots <= FQA_JOIN_FEW) hipLaunchKernelGGL(fqa_join_kernel<2>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, parts, a.O, rows);
+        else hipLaunchKernelGGL(fqa_join_kernel<8>, dim3((unsigned)rows), dim3(256), 0, stream, parts, a.O, rows);
+    }
 }

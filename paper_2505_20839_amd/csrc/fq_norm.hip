@@ -215,6 +215,13 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
     }
 }
 
+// Waves per row and chunks per thread, us with residual from a graph, the choice here first:
+//     1 x 4096      <4, 2> 2.9; <8, 1> 2.8; <2, 4> 3.3; <1, 8> 4.3      8192 x 4096   <4, 2> 42.5 (5.5 TB/s); <8, 1> 43.1; <2, 4> 43.7; <1, 8> 46.4
+//     1000 x 5120   <8, 2> 8.2; <4, 3> 8.1; <4, 4> 8.5; <16, 1> 9.3     6000 x 5120   <8, 2> 39.7; <4, 3> 40.3; <4, 4> 40.5; <16, 1> 44.1
+//     1000 x 8192   <8, 2> 10.5; <4, 4> 10.9; <16, 1> 11.7              4096 x 8192   <8, 2> 42.7; <4, 4> 43.8; <16, 1> 44.9
+//     64 x 11008    <16, 2> 4.2; <8, 4> 4.4; <4, 8> 4.9                 2000 x 11008  <16, 2> 30.3; <8, 4> 29.6; <4, 8> 31.0
+//     1 x 16384     <16, 2> 3.9; <8, 4> 4.1; <4, 8> 4.6                 2048 x 16384  <16, 2> 44.9; <8, 4> 45.0; <4, 8> 45.8
+//     8192 x 2048   <1, 4> 21.1 and 8192 x 1024 11.8 (one wave a row); 300 x 2048 <4, 2> 3.5; <2, 4> 3.6; <1, 8> 4.5
 template <bool RES, int OUT>
 void fqn_launch(const uint16_t* X, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint16_t* Y, uint8_t* A, float* a_scale,
                 int M, int K, uint16_t* planes, hipStream_t stream) {
