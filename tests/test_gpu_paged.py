@@ -583,3 +583,47 @@ def test_a_bad_prefix_page_is_everybodys(fq, B):
     got = fq.fq_kv4_attention_prefix(torch.from_numpy(q).cuda(), torch.from_numpy(qs).cuda(), torch.from_numpy(ref.b).cuda(), torch.from_numpy(pre).cuda(), 700,
                                      torch.from_numpy(table).cuda(), torch.full((B,), 5, dtype=torch.int32, device="cuda"), 0.1)
     assert bool(torch.isnan(got.float()).all())
+
+
+def test_the_decoding_example(fq):
+    """The blocks of examples/paged_decode.py: a prompt and tokens behind it, with the prefix shared and with a copy of it in every sequence's
+    own pages; the same prompt decoded token by token; and the command itself, eager and from a graph."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_decode.py")
+    spec = importlib.util.spec_from_file_location("paged_decode", path)
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    T, B, page = 70, 3, 16
+    g = torch.Generator(device="cuda").manual_seed(3)
+    prompt = torch.randn((T, 512), generator=g, device="cuda").bfloat16()
+    tokens = torch.randn((4, B, 512), generator=g, device="cuda").bfloat16()
+
+    def decoder():
+        return ex.Decoder(blocks=2, hidden=512, ffn=768, Hq=4, Hkv=2, page=page, pages=64, positions=256)
+
+    def pages(lo, n):
+        return torch.arange(lo, lo + n, dtype=torch.int32, device="cuda")
+
+    one, two = decoder(), decoder()
+    one.prefill(prompt, pages(0, 5))
+    table = torch.stack([pages(10 * (b + 1), 2) for b in range(B)])
+    long = torch.stack([pages(10 * (b + 1), 6) for b in range(B)])
+    for b in range(B):
+        two.prefill(prompt, long[b])
+    for i in range(4):
+        shared = one.step(tokens[i], table, torch.full((B,), i + 1, dtype=torch.int32, device="cuda"), pages(0, 5), T, max_len=8)
+        apart = two.step(tokens[i], long, torch.full((B,), T + i + 1, dtype=torch.int32, device="cuda"), None, 0, max_len=96)
+        # both caches hold the same numbers; the sums are split otherwise, and a bf16 step in the first block can move codes behind it
+        rel = (shared.float() - apart.float()).norm() / apart.float().norm()
+        assert bool(torch.isfinite(shared.float()).all()) and float(rel) < 0.1, float(rel)
+    three = decoder()
+    last = None
+    for t in range(T):
+        last = three.step(prompt[t:t + 1], pages(0, 5)[None].contiguous(), torch.full((1,), t + 1, dtype=torch.int32, device="cuda"), None, 0, max_len=T)
+    whole = decoder().prefill(prompt, pages(0, 5))[-1:]
+    rel = (last.float() - whole.float()).norm() / whole.float().norm()
+    assert float(rel) < 0.1, float(rel)
+    a = ex.main(["--batch", "3", "--prefix", "100", "--steps", "5", "--blocks", "1"])
+    b = ex.main(["--batch", "3", "--prefix", "100", "--steps", "5", "--blocks", "1", "--no-graph"])
+    assert a.shape == b.shape and bool(torch.isfinite(a.float()).all())
