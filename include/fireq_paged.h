@@ -43,7 +43,7 @@
  * Scratch: fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) bytes, 16-byte aligned (prefix_len 0: without prefix).
  *
  * Q_fp8, cache, QKV_bf16, cos_sin, K, V, O: 16-byte aligned.  Conventions and status codes are those of fireq.h; T, n or B = 0
- * is a successful no-op.  Hq is a multiple of Hkv; B, Hq <= 65535, B * Hq <= 2^23, T < 2^23, T * (Hq + 2 Hkv) and n * Hkv below 2^28 - 16, fewer than 2^32 tiles a head.
+ * is a successful no-op.  Hq is a multiple of Hkv; B, Hq <= 65535, B * Hq <= 2^23, max_len and prefix_len <= 2^30, T < 2^23, T * (Hq + 2 Hkv) and n * Hkv below 2^28 - 16, fewer than 2^32 tiles a head.
  */
 #ifndef FIREQ_PAGED_H
 #define FIREQ_PAGED_H

@@ -824,7 +824,7 @@ def _attention(where, Q, q_scale, cache, prefix_pages, prefix_len, block_table, 
     width = block_table.shape[1]
     if q_scale.numel() != B * Hq or block_table.shape[0] != B or seq_lens.numel() != B or Hq % Hkv:
         raise FireqError(-2, where)
-    max_len = min(width * geometry[4], 0x7FFFFFFF) if max_len is None else int(max_len)
+    max_len = min(width * geometry[4], 1 << 30) if max_len is None else int(max_len)
     shared = 0
     if prefix_pages is not None:
         prefix_pages = _dev(prefix_pages, torch.int32, "prefix_pages")

@@ -253,15 +253,57 @@ struct fqa_parts {
     int slots;
 };
 
+// Parts first, first + STEP, .. of n of a row added to (m, l, o), four requested at a time (po: at the lane's four channels).
+template <int STEP>
+__device__ __forceinline__ void fqa_add_parts(const fq_v2f* ml, const fq_v4f* po, int first, int n, float& m, float& l, fq_v4f& o) {
+    for (int s0 = first; s0 < n; s0 += 4 * STEP) {
+        fq_v2f pm[4];
+        fq_v4f x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int s = s0 + STEP * u < n ? s0 + STEP * u : s0;
+            pm[u] = ml[s];
+            x[u] = po[(size_t)s * 32];
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (s0 + STEP * u >= n) pm[u][1] = 0.f;
+            if (pm[u][1] != 0.f) top = fmaxf(top, pm[u][0]);   // (an empty part has no sums)
+        }
+        const float f = __builtin_amdgcn_exp2f(m - top);
+        l *= f;
+        o *= f;
+        m = top;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (pm[u][1] == 0.f) continue;
+            const float fu = __builtin_amdgcn_exp2f(pm[u][0] - top);
+            l += pm[u][1] * fu;
+            o += x[u] * fu;
+        }
+    }
+}
+
+// o / l as four bf16 (a row without tokens: zeros).
+__device__ __forceinline__ uint2 fqa_output(fq_v4f o, float l) {
+    o *= l == 0.f ? 0.f : 1.0f / l;
+    uint2 out;
+    out.x = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[0], o[1]}, fq_v2bf));
+    out.y = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[2], o[3]}, fq_v2bf));
+    return out;
+}
+
 // A workgroup's work: tiles c0 .. c1 of one key/value head for `rows` (up to 16 RT) query rows, numbered by row_of(0 .. rows - 1).  Its waves
-// share the tiles out and join their sums through LDS; the result is a part of each row, or, with one part, the row's output.
+// share the tiles out and join their sums through LDS; the result is a part of each row, or (finish) its output, with the `earlier` parts that a
+// kernel before has left added.
 template <int RT, int WAVES>
-struct fqa_shared {
-    float m[WAVES][16 * RT], l[WAVES][16 * RT], o[WAVES][16 * RT][132];
+struct __attribute__((aligned(16))) fqa_shared {
+    float o[WAVES][16 * RT][132], m[WAVES][16 * RT], l[WAVES][16 * RT];
 };
 template <int RT, int WAVES, int NT, int AHEAD, class F>
 __device__ __forceinline__ void fqa_group(const fq_attend_args& a, const fqa_parts& parts, fqa_shared<RT, WAVES>& sh, int c0, int c1, int len,
-                                          const int* pages_of, bool bad, int kv, int rows, F row_of, int slot) {
+                                          const int* pages_of, bool bad, int kv, int rows, F row_of, int slot, bool finish, int earlier) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     // the waves' shares: steps of NT tiles
     const int steps = (c1 - c0 + NT - 1) / NT, per = (steps + WAVES - 1) / WAVES * NT;
@@ -294,10 +336,9 @@ __device__ __forceinline__ void fqa_group(const fq_attend_args& a, const fqa_par
         }
     } else if (lane < 16 * RT) {
         sh.m[wave][lane] = FQA_LOWEST;
-        sh.l[wave][lane] = 0.f;
+        sh.l[wave][lane] = bad ? __builtin_nanf("") : 0.f;
     }
     __syncthreads();
-    const bool direct = parts.slots == 1;
     for (int i = threadIdx.x; i < rows * 32; i += 64 * WAVES) {   // four channels of a row
         const int r = i >> 5, c = 4 * (i & 31);
         float top = FQA_LOWEST, l = 0.f;
@@ -312,12 +353,10 @@ __device__ __forceinline__ void fqa_group(const fq_attend_args& a, const fqa_par
             o += *reinterpret_cast<const fq_v4f*>(&sh.o[w][r][c]) * f;
         }
         const size_t row = row_of(r);
-        if (direct) {
-            o *= 1.0f / l;
-            uint2 out;
-            out.x = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[0], o[1]}, fq_v2bf));
-            out.y = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[2], o[3]}, fq_v2bf));
-            *reinterpret_cast<uint2*>(a.O + row * 128 + c) = out;
+        if (finish) {
+            fqa_add_parts<1>(reinterpret_cast<const fq_v2f*>(parts.ml) + row * parts.slots, reinterpret_cast<const fq_v4f*>(parts.o) + row * parts.slots * 32 + (i & 31), 0,
+                             earlier, top, l, o);
+            *reinterpret_cast<uint2*>(a.O + row * 128 + c) = fqa_output(o, l);
         } else {
             const size_t at = row * parts.slots + slot;
             *reinterpret_cast<fq_v4f*>(parts.o + at * 128 + c) = o;
@@ -332,10 +371,11 @@ __device__ __forceinline__ void fqa_group(const fq_attend_args& a, const fqa_par
 // Own tokens: a workgroup takes `chunk` tiles of one sequence for 16 query rows of a key/value head.  Heads are the fastest index and chunks the
 // slowest: workgroup i runs on XCD i % 8, and with chunks (of which a short sequence has the first ones only) or sequences fastest some
 // XCDs got most of the work (37 sequences of 0 to 6000 tokens 37.0 us, 31.9 with a number of chunks that happened to spread them).
-// With shared_slots, the first workgroups of a sequence take a shared prefix instead, in chunks of shared_chunk tiles.
+// With shared_slots, the first workgroups of a sequence take a shared prefix instead, in chunks of shared_chunk tiles.  finish: a sequence's tokens
+// are one part, whose workgroup writes the output, with the `earlier` parts of the prefix's kernel added.
 template <int WAVES, int NT, int AHEAD>
 __global__ __launch_bounds__(64 * WAVES, 4) void fqa_own_kernel(fq_attend_args a, fqa_parts parts, int chunk, int first_slot, int row_tiles, int shared_slots,
-                                                                int shared_chunk) {
+                                                                int shared_chunk, int finish, int earlier) {
     __shared__ fqa_shared<1, WAVES> sh;
     const int heads = a.Hkv * row_tiles, b = (int)blockIdx.x / heads, kv = (int)blockIdx.x % heads / row_tiles, rt = (int)blockIdx.x % row_tiles;
     const bool shared = (int)blockIdx.y < shared_slots;
@@ -347,8 +387,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void fqa_own_kernel(fq_attend_args a
     const int c0 = (shared ? (int)blockIdx.y : (int)blockIdx.y - shared_slots) * per, c1 = c0 + per < tiles ? c0 + per : tiles;
     const int rows = G - 16 * rt < 16 ? G - 16 * rt : 16;
     const int row0 = b * a.Hq + kv * G + 16 * rt, slot = first_slot + (int)blockIdx.y;
-    if (c0 >= tiles) {                                    // no tokens
-        if (parts.slots == 1) {
+    if (c0 >= tiles && earlier == 0) {                    // no tokens
+        if (finish) {
             constexpr int N = 0x7FC07FC0;
             for (int i = threadIdx.x; i < rows * 16; i += 64 * WAVES)
                 reinterpret_cast<fq_v4i*>(a.O)[(size_t)row0 * 16 + i] = too_long ? (fq_v4i){N, N, N, N} : (fq_v4i){0, 0, 0, 0};
@@ -359,7 +399,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void fqa_own_kernel(fq_attend_args a
         }
         return;
     }
-    fqa_group<1, WAVES, NT, AHEAD>(a, parts, sh, c0, c1, len, shared ? a.shared : a.table + (size_t)b * a.width, too_long, kv, rows, [=](int i) { return (size_t)row0 + i; }, slot);
+    fqa_group<1, WAVES, NT, AHEAD>(a, parts, sh, c0, c1, len, shared ? a.shared : a.table + (size_t)b * a.width, too_long, kv, rows, 
+                                    [=](int i) { return (size_t)row0 + i; }, slot, finish != 0, earlier);
 }
 
 // The shared prefix: a workgroup takes `chunk` tiles for 16 RT of a key/value head's B * G query rows.  Workgroups with the same tiles of a
@@ -371,7 +412,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fqa_prefix_kernel(fq_attend_arg
     const int G = a.Hq / a.Hkv, all = a.B * G, first = group * 16 * RT, rows = all - first < 16 * RT ? all - first : 16 * RT;
     const int tiles = (a.prefix + 15) >> 4, c0 = slot * chunk, c1 = c0 + chunk < tiles ? c0 + chunk : tiles;
     fqa_group<RT, WAVES, NT, AHEAD>(a, parts, sh, c0, c1, a.prefix, a.shared, false, kv, rows,
-                                    [&](int i) { return (size_t)((first + i) / G) * a.Hq + kv * G + (first + i) % G; }, slot);
+                                    [&](int i) { return (size_t)((first + i) / G) * a.Hq + kv * G + (first + i) % G; }, slot, false, 0);
 }
 
 // The parts' sums, each brought to the largest maximum.  32 lanes hold the 128 channels of a row; GROUPS of 32 lanes share its parts, four
@@ -389,33 +430,7 @@ __global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t
     const fq_v4f* po = reinterpret_cast<const fq_v4f*>(parts.o) + (size_t)row * n * 32 + c;
     float m = FQA_LOWEST, l = 0.f;
     fq_v4f o = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = grp; s0 < n; s0 += 4 * GROUPS) {
-        fq_v2f pm[4];
-        fq_v4f x[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int s = s0 + GROUPS * u < n ? s0 + GROUPS * u : s0;
-            pm[u] = ml[s];
-            x[u] = po[(size_t)s * 32];
-        }
-        float top = m;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (s0 + GROUPS * u >= n) pm[u][1] = 0.f;
-            if (pm[u][1] != 0.f) top = fmaxf(top, pm[u][0]);   // (an empty part has no sums)
-        }
-        const float f = __builtin_amdgcn_exp2f(m - top);
-        l *= f;
-        o *= f;
-        m = top;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (pm[u][1] == 0.f) continue;
-            const float fu = __builtin_amdgcn_exp2f(pm[u][0] - top);
-            l += pm[u][1] * fu;
-            o += x[u] * fu;
-        }
-    }
+    fqa_add_parts<GROUPS>(ml, po, grp, n, m, l, o);
     if (GROUPS == 2) {                                    // the other half of the wave
         const float top = fmaxf(m, __shfl_xor(m, 32, 64)), f = __builtin_amdgcn_exp2f(m - top);
         l *= f;
@@ -445,19 +460,20 @@ __global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t
             o += wo[i][c] * f;
         }
     }
-    o *= l == 0.f ? 0.f : 1.0f / l;
-    uint2 out;
-    out.x = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[0], o[1]}, fq_v2bf));
-    out.y = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[2], o[3]}, fq_v2bf));
-    reinterpret_cast<uint2*>(O)[(size_t)row * 32 + c] = out;
+    reinterpret_cast<uint2*>(O)[(size_t)row * 32 + c] = fqa_output(o, l);
 }
 
 constexpr int FQA_OWN_WAVES = 4, FQA_OWN_NT = 2, FQA_OWN_AHEAD = 1, FQA_PREFIX_RT = 2, FQA_PREFIX_WAVES = 4, FQA_PREFIX_NT = 2, FQA_PREFIX_AHEAD = 1;
-constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 36000, FQA_JOIN_FEW = 8;
+constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 36000, FQA_JOIN_FEW = 8, FQA_FINISH = 16;
 
 // own_chunk and own_slots: tiles of a part of a sequence, and parts of the longest; the same for the prefix, which is worked on for
-// row_groups groups of rows together, or (row_groups 0) for each sequence apart, like its own tokens.
-struct fqa_plan { int own_chunk, own_slots, prefix_chunk, prefix_slots, row_groups; };
+// row_groups groups of rows together, or (row_groups 0) for each sequence apart, like its own tokens.  finish: the kernel of a sequence's own
+// tokens, where they are one part, adds the prefix's up to FQA_FINISH parts itself and writes the output; otherwise a third kernel joins all.
+struct fqa_plan {
+    int own_chunk, own_slots, prefix_chunk, prefix_slots, row_groups;
+    bool finish() const { return own_slots == 1 && (prefix_slots == 0 || (row_groups != 0 && prefix_slots <= FQA_FINISH)); }
+    int slots() const { return prefix_slots + (finish() ? 0 : own_slots); }   // parts of a row that go through memory
+};
 
 // Tiles of a part, for `heads` (sequence, key/value head, 16 query rows) of up to `tiles` each.  A wave of a part's four takes about 0.25 us a
 // tile beyond 4; a second part costs the joining kernel, 2 us.  us, from a graph, 32 query and 8 key/value heads unless said otherwise:
@@ -520,23 +536,21 @@ fqa_plan fqa_choose(int B, int Hq, int Hkv, int max_len, int prefix) {
 }  // namespace
 
 size_t fq_attend_scratch_bytes(int B, int Hq, int Hkv, int max_len, int prefix) {
-    const fqa_plan p = fqa_choose(B, Hq, Hkv, max_len, prefix);
-    const size_t slots = (size_t)p.own_slots + p.prefix_slots;
-    return slots <= 1 && prefix <= 0 ? 0 : slots * B * Hq * 130 * sizeof(float);
+    return (size_t)fqa_choose(B, Hq, Hkv, max_len, prefix).slots() * B * Hq * 130 * sizeof(float);
 }
 
 void fq_launch_attend(const fq_attend_args& a, void* scratch, hipStream_t stream) {
     const fqa_plan p = fqa_choose(a.B, a.Hq, a.Hkv, a.max_len, a.prefix);
-    const int slots = p.own_slots + p.prefix_slots, G = a.Hq / a.Hkv, row_tiles = (G + 15) / 16;
-    const bool join = slots > 1 || a.prefix > 0;
-    fqa_parts parts = {static_cast<float*>(scratch), static_cast<float*>(scratch) + (size_t)slots * a.B * a.Hq * 128, join ? slots : 1};
+    const int slots = p.slots(), row_tiles = (a.Hq / a.Hkv + 15) / 16;
+    const fqa_parts parts = {static_cast<float*>(scratch), static_cast<float*>(scratch) + (size_t)slots * a.B * a.Hq * 128, slots};
     if (p.row_groups)
         hipLaunchKernelGGL((fqa_prefix_kernel<FQA_PREFIX_RT, FQA_PREFIX_WAVES, FQA_PREFIX_NT, FQA_PREFIX_AHEAD>), dim3((unsigned)(p.prefix_slots * p.row_groups * a.Hkv)),
                            dim3(64 * FQA_PREFIX_WAVES), 0, stream, a, parts, p.prefix_chunk, p.row_groups);
     const int apart = p.row_groups ? 0 : p.prefix_slots;
     hipLaunchKernelGGL((fqa_own_kernel<FQA_OWN_WAVES, FQA_OWN_NT, FQA_OWN_AHEAD>), dim3((unsigned)(a.B * a.Hkv * row_tiles), apart + p.own_slots),
-                       dim3(64 * FQA_OWN_WAVES), 0, stream, a, parts, p.own_chunk, p.prefix_slots - apart, row_tiles, apart, p.prefix_chunk);
-    if (join) {
+                       dim3(64 * FQA_OWN_WAVES), 0, stream, a, parts, p.own_chunk, p.prefix_slots - apart, row_tiles, apart, p.prefix_chunk, p.finish() ? 1 : 0,
+                       p.finish() ? p.prefix_slots : 0);
+    if (!p.finish()) {
         const int rows = a.B * a.Hq;
         if (slots <= FQA_JOIN_FEW) hipLaunchKernelGGL(fqa_join_kernel<2>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, parts, a.O, rows);
         else hipLaunchKernelGGL(fqa_join_kernel<8>, dim3((unsigned)rows), dim3(256), 0, stream, parts, a.O, rows);

@@ -521,7 +521,7 @@ PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         want(B > 0 && B <= INT_LIMIT && Hq > 0 && Hq <= INT_LIMIT && Hq % c.heads == 0 && width <= INT_LIMIT && qs.numel() == B * Hq && table.size(0) == B &&
              lens.numel() == B);
         const float out_scale = number(a[7]);
-        const int64_t most = width * c.page < INT_LIMIT ? width * c.page : INT_LIMIT;
+        const int64_t most = std::min<int64_t>(width * c.page, 1 << 30);
         const int max_len = a[8] == Py_None ? (int)most : whole(a[8]);
         const int32_t* shared = nullptr;
         int prefix = 0;

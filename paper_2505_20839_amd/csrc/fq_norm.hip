@@ -1,7 +1,7 @@
 // Residual addition and root-mean-square norm in front of a quantised layer (include/fireq_norm.h):
 //     h = bf16(x + r),  y = h * w / sqrt(mean h^2 + eps),  codes = E4M3(y / beta),  beta = max |y| / 448
 // in one pass over the row: with t = max |h w| the row's two statistics, sum h^2 and t, come out of one reduction, beta is
-// t * rstd / 448 and a code is E4M3(h w * (448 / t)) -- rstd cancels, so no value waits for it.
+// t * rstd / 448 and a code is E4M3(448 h w / t) -- rstd cancels, so no value waits for it, and adds no rounding.
 // Bound by HBM: 7 bytes per element with the residual, 3 without (bf16 output: 8 and 4).
 #include <type_traits>
 #include "fq_common.h"
@@ -170,13 +170,18 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
     }
     if (t == 0 && on) a_scale[m] = bad ? __builtin_nanf("") : top == 0u ? 1.0f : tf * rstd / 448.0f;
     fq_v2i* a = reinterpret_cast<fq_v2i*>(A + at);
-    // 448 / t passes FP32's range for a t below 2^-119: those rows divide by t first, exactly as far as it matters
-    const float mul = bad || top == 0u ? 0.f : 448.0f / tf;
+    // h w is exact in FP32 (8 bits each); 448 h w / t by one exact residual step behind h w * (448 / t), as a correctly rounded quotient.
+    // Rows whose t lies outside [2^-100, 2^110] divide by t first: 448 / t or 448 h w may pass FP32's range there.
+    const float mul = bad || top == 0u ? 0.f : 448.0f / tf, rt = bad || top == 0u ? 0.f : 1.0f / tf;
     auto put = [&](auto tiny, int i, int c, fq_v4i h, fq_v4i g) __attribute__((always_inline)) {
         fq_v2i o = {0, 0};
         if (!bad) {
             if constexpr (decltype(tiny)::value) o = fqn_codes8(h, g, [&](float v) { return tf > 0.f ? v / tf * 448.0f : 0.f; });
-            else o = fqn_codes8(h, g, [&](float v) { return v * mul; });
+            else
+                o = fqn_codes8(h, g, [&](float v) {
+                    const float q = v * mul;
+                    return fmaf(fmaf(q, tf, -448.0f * v), -rt, q);
+                });
         }
         if (on) a[c] = o;
         if (ZP) {
@@ -200,7 +205,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
                 if (t + i * T < nchunk) put(tiny, i, t + i * T, keep[i], wt[i]);
         }
     };
-    if (__builtin_amdgcn_readfirstlane((int)(tf < 0x1p-100f))) convert(std::true_type());
+    if (__builtin_amdgcn_readfirstlane((int)(top != 0u && !(tf >= 0x1p-100f && tf <= 0x1p110f)))) convert(std::true_type());
     else convert(std::false_type());
     if (ZP) {
         const int G = K >> 7, C2 = 2 * ((G + 15) >> 4);
@@ -230,8 +235,14 @@ void fqn_launch(const uint16_t* X, const uint16_t* R, const uint16_t* W, float e
                        dim3(WPR_ > 4 ? 64 * WPR_ : 256), 0, stream, X, R, W, eps, H, Y, A, a_scale, K, planes, M)
     if (K > 16384) {
         if constexpr (OUT != FQN_CODES_ZP) {              // (no zero-point terms for rows this long)
-            if (K > 65536) FQN_LAUNCH(16, 1, true);
-            else if (K > 32768) FQN_LAUNCH(16, 8, false);
+            // (row, residual and weights of more than 32768 numbers do not fit the registers where bf16 leaves: 512 x 40960
+            // 68.3 us held, 40.2 read twice; the codes' kernel 33.5 held, 36.0 read twice)
+            constexpr int HELD = RES && OUT == FQN_BF16 ? 32768 : 65536;
+            if (K > HELD) FQN_LAUNCH(16, 1, true);
+            else if constexpr (HELD > 32768) {
+                if (K > 32768) FQN_LAUNCH(16, 8, false);
+                else FQN_LAUNCH(16, 4, false);
+            }
             else FQN_LAUNCH(16, 4, false);
         }
     } else if (K > 8192) FQN_LAUNCH(16, 2, false);

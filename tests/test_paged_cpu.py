@@ -88,7 +88,7 @@ def test_read_refusals(change, status):
 @pytest.mark.parametrize("prefix", [False, True])
 @pytest.mark.parametrize("change, status", PAGED + [
     (dict(B=0, Q=0, O=0), OK), (dict(B=-1), SHAPE), (dict(B=65536), SHAPE), (dict(Hq=5), SHAPE), (dict(B=65535, Hq=256), SHAPE), (dict(width=-1), SHAPE),
-    (dict(max_len=-1), SHAPE), (dict(prefix_len=-1), SHAPE), (dict(scale=0.0), SHAPE), (dict(scale=-1.0), SHAPE), (dict(scale=float("nan")), SHAPE),
+    (dict(max_len=-1), SHAPE), (dict(prefix_len=-1), SHAPE), (dict(max_len=(1 << 30) + 1), SHAPE), (dict(prefix_len=(1 << 30) + 1), SHAPE), (dict(scale=0.0), SHAPE), (dict(scale=-1.0), SHAPE), (dict(scale=float("nan")), SHAPE),
     (dict(scale=float("inf")), SHAPE), (dict(pages=0), SHAPE), (dict(Q=0), NULL), (dict(qs=0), NULL), (dict(lens=0), NULL), (dict(table=0), NULL), (dict(O=0), NULL),
     (dict(shared=0), NULL), (dict(Q=ODD), ALIGN), (dict(O=ODD), ALIGN), (dict(ws=0), MEMORY), (dict(nbytes=64), MEMORY), (dict(ws=ODD), ALIGN)])
 def test_attention_refusals(change, status, prefix):
