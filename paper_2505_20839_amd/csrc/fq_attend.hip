@@ -464,7 +464,7 @@ __global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t
 }
 
 constexpr int FQA_OWN_WAVES = 4, FQA_OWN_NT = 2, FQA_OWN_AHEAD = 1, FQA_PREFIX_RT = 2, FQA_PREFIX_WAVES = 4, FQA_PREFIX_NT = 2, FQA_PREFIX_AHEAD = 1;
-constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 36000, FQA_JOIN_FEW = 8, FQA_FINISH = 16;
+constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 24000, FQA_APART_FEW = 48000, FQA_JOIN_FEW = 8, FQA_FINISH = 16;
 
 // own_chunk and own_slots: tiles of a part of a sequence, and parts of the longest; the same for the prefix, which is worked on for
 // row_groups groups of rows together, or (row_groups 0) for each sequence apart, like its own tokens.  finish: the kernel of a sequence's own
@@ -505,10 +505,10 @@ fqa_plan fqa_choose(int B, int Hq, int Hkv, int max_len, int prefix) {
     p.own_slots = (tiles + p.own_chunk - 1) / p.own_chunk;
     if (prefix > 0) {
         const int pt = (int)(((long long)prefix + 15) / 16);
-        // Apart: one kernel less, no groups of rows to gather, but every sequence unpacks the prefix again.  us, apart / together (32 query, 8 key/value
-        // heads): 8 x 1100 8.5 / 14.8, 64 x 300 12.5 / 18.0, 16 x 4000 (32000 tiles) 16.3 / 17.8, 64 x 1000 (32256) 16.8 / 19.9; 96 x 1000 of 8 query
-        // heads (48384) 19.3 / 15.0, 30 x 8000 (120000) 42.4 / 26.7
-        if (heads * pt <= FQA_APART) {
+        // Apart: no groups of rows to gather and half the start of a kernel, but every sequence unpacks the prefix again.  us, apart / together (32
+        // query, 8 key/value heads): 8 x 1100 (4416 tiles) 8.2 / 12.7, 64 x 300 (9728) 11.7 / 14.2, 16 x 2000 (16000) 11.3 / 12.6, 32 x 2000 (32000)
+        // 15.6 / 13.5, 16 x 4000 15.7 / 14.4, 64 x 1000 15.9 / 14.5; rows that fill no group: 4 x 16000 (32000 tiles, 16 rows) 16.8 / 19.2
+        if (heads * pt <= ((long long)B * G <= 8 * FQA_PREFIX_RT ? FQA_APART_FEW : FQA_APART)) {
             p.prefix_chunk = fqa_part(heads, pt, cus);
             p.prefix_slots = (pt + p.prefix_chunk - 1) / p.prefix_chunk;
             return p;
