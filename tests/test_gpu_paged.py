@@ -627,3 +627,28 @@ def test_the_decoding_example(fq):
     a = ex.main(["--batch", "3", "--prefix", "100", "--steps", "5", "--blocks", "1"])
     b = ex.main(["--batch", "3", "--prefix", "100", "--steps", "5", "--blocks", "1", "--no-graph"])
     assert a.shape == b.shape and bool(torch.isfinite(a.float()).all())
+
+
+@pytest.mark.parametrize("T, Hq, Hkv, page", [(300, 2, 1, 16), (129, 5, 1, 48), (3, 64, 16, 16), (2, 130, 2, 32)])
+def test_append_of_many_rows_and_many_heads(fq, T, Hq, Hkv, page):
+    """Rows that change places between the XCDs, and rows whose heads take more than one workgroup."""
+    test_append_and_read(fq, T, Hq, Hkv, page, False, 0)
+
+
+def test_read_of_many_tokens(fq):
+    rng = np.random.default_rng(12)
+    ref = pu.Cache(70, 2, 32, rng, stale_nan=False)
+    ref.b[..., 2048:] = rng.integers(0, 0x7F, ref.b[..., 2048:].shape, dtype=np.uint8)
+    slots = rng.integers(-1, 70 * 32, 2113)
+    K, V = (t.double().cpu().numpy() for t in fq.fq_kv4_read(torch.from_numpy(ref.b).cuda(), torch.from_numpy(slots).cuda()))
+    for i in list(range(0, 2113, 37)) + [2112]:
+        for h in range(2):
+            for got, value in ((K, False), (V, True)):
+                if slots[i] < 0:
+                    assert not got[i, h].any()
+                    continue
+                c, sc = ref.get(int(slots[i]), h, value)
+                assert np.array_equal(got[i, h], c * pu.E4M3[sc])
+    again = fq.fq_kv4_read(torch.from_numpy(ref.b).cuda(), torch.from_numpy(np.sort(slots)).cuda())
+    order = np.argsort(slots, kind="stable")
+    assert np.array_equal(again[0].double().cpu().numpy(), K[order]) and np.array_equal(again[1].double().cpu().numpy(), V[order])
