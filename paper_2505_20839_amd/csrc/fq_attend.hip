@@ -498,7 +498,7 @@ int fqa_part(long long heads, int tiles, long long cus) {
     chunk = chunk < 16 ? 16 : (chunk + 15) / 16 * 16;
     const long long cap = heads < 2 * cus ? 64 : 128;
     if (chunk > cap && heads * ((tiles + chunk - 1) / chunk) > cus) chunk = cap;
-    if (chunk < tiles / 60000 + 1) chunk = tiles / 60000 + 1;     // (a grid has 65535 in its second dimension)
+    if (chunk < tiles / 60000 + 1) chunk = (tiles / 60000 + 16) / 16 * 16;   // (a grid has 65535 in its second dimension; a step may not pass a part's end)
     return (int)(chunk < tiles ? chunk : tiles);
 }
 

@@ -342,6 +342,17 @@ def test_attention_behind_a_prefix(fq, B, Hq, Hkv, page, prefix, longest):
     assert torch.equal(none.view(torch.int16), fq.fq_kv4_attention(*args, *own).view(torch.int16))
 
 
+def test_attention_with_a_bound_far_above_the_lengths(fq):
+    """Parts are long then (a grid has 65535 of them at most): whole steps, nothing counted twice at their ends."""
+    rng = np.random.default_rng(5)
+    lens = [2500] + [0] * 258 + [17]
+    ref, table, _ = _filled(rng, lens, 1, 32)
+    q, qs = _queries(rng, len(lens), 1, 0.1)
+    got = fq.fq_kv4_attention(torch.from_numpy(q).cuda(), torch.from_numpy(qs).cuda(), torch.from_numpy(ref.b).cuda(), torch.from_numpy(table).cuda(),
+                              torch.tensor(lens, dtype=torch.int32).cuda(), 0.1, max_len=131072016)
+    _check_attention(ref, table, lens, q, qs, 1, got, 0.1)
+
+
 def test_attention_what_cannot_be_done_shows(fq):
     rng = np.random.default_rng(4)
     lens = [40, 40, 40, 70, 20, -3]

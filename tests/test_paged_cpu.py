@@ -112,6 +112,15 @@ def test_attention_workspace_sizes():
     assert size(4, 32, 8, 10, 5000) % (4 * 32 * 130 * 4) == 0 and size(4, 32, 8, 10, 5000) > 0
 
 
+@pytest.mark.parametrize("max_len", [1 << 30, (1 << 30) - 5, 300000001, 131072000, 5000000])
+@pytest.mark.parametrize("B, heads", [(8, 1), (1, 8), (64, 8), (600, 1)])
+def test_parts_of_long_bounds_are_whole_steps(B, heads, max_len):
+    """A step takes two tiles and may not pass the end of its part: some even number of tiles gives this number of parts."""
+    parts, tiles = binding.fq_kv4_attention_workspace_bytes(B, heads, heads, max_len) // (B * heads * 130 * 4), (max_len + 15) // 16
+    assert 1 < parts <= 60000
+    assert any((tiles + n - 1) // n == parts for n in range(16, tiles + 16, 16) if abs(n * parts - tiles) <= n + 16 * parts)
+
+
 def test_binding_wants_gpu_tensors():
     t = torch.zeros((2, 128))
     for call in (lambda: binding.fq_rmsnorm(t, t, 1e-5), lambda: binding.fq_rmsnorm_quant(t, t, 1e-5), lambda: binding.fq_kv4_read(t, t),
