@@ -40,7 +40,7 @@
  * fq_kv4_attention_prefix_ws   the same where every sequence attends to prefix_len tokens in prefix_pages first, and then
  *                 to its own seq_lens[b] tokens: the prefix is read and unpacked for up to 32 query rows at a time, not for
  *                 every sequence (unless that is less work than sharing it).
- * Scratch: fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) bytes, 16-byte aligned (prefix_len 0: without prefix); it may be
+ * Scratch: fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) bytes, 16-byte aligned (prefix_len 0: without prefix; 0 bytes for sizes that the calls refuse); it may be
  * reused or freed once the work enqueued by the call has finished, and calls that overlap in time need scratch of their own.
  *
  * Q_fp8, cache, QKV_bf16, cos_sin, K, V, O: 16-byte aligned.  Conventions and status codes are those of fireq.h; T, n or B = 0

@@ -538,15 +538,18 @@ int check_paged(const uint8_t* cache, int64_t page_stride, int64_t head_stride, 
     return FQ_OK;
 }
 
+// The sizes that the attention takes.
+bool attention_sizes(int B, int Hq, int Hkv, int max_len, int prefix_len) {
+    return B >= 0 && B <= 65535 && Hq > 0 && Hq <= 65535 && Hkv > 0 && Hq % Hkv == 0 && (int64_t)B * Hq <= 1 << 23 &&
+           (int64_t)Hkv * ((Hq / Hkv + 15) / 16) <= 65535 && max_len >= 0 && max_len <= 1 << 30 && prefix_len >= 0 && prefix_len <= 1 << 30;
+}
+
 int attend(const uint8_t* Q_fp8, const float* q_scale, const uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages, int page,
            const int32_t* prefix_pages, int prefix_len, const int32_t* block_table, int table_width, const int32_t* seq_lens,
            float out_scale, uint16_t* O_bf16, int B, int Hq, int Hkv, int max_len, void* workspace, size_t workspace_bytes, void* stream) {
-    if (B < 0 || B > 65535 || Hq <= 0 || Hq > 65535 || Hkv <= 0 || Hq % Hkv != 0 || table_width < 0 || max_len < 0 || max_len > 1 << 30 || prefix_len < 0 || prefix_len > 1 << 30 ||
-        !(out_scale > 0.f) || !(out_scale <= 3.402823466e38f))
-        return FQ_ERR_SHAPE;
+    if (!attention_sizes(B, Hq, Hkv, max_len, prefix_len) || table_width < 0 || !(out_scale > 0.f) || !(out_scale <= 3.402823466e38f)) return FQ_ERR_SHAPE;
     const int rc = check_paged(cache, page_stride, head_stride, pages, page, Hkv);
     if (rc != FQ_OK) return rc;
-    if ((int64_t)Hkv * ((Hq / Hkv + 15) / 16) > 65535 || (int64_t)B * Hq > 1 << 23) return FQ_ERR_SHAPE;
     if (B == 0) return FQ_OK;
     if (!Q_fp8 || !q_scale || !seq_lens || !O_bf16 || (table_width > 0 && !block_table) || (prefix_len > 0 && !prefix_pages)) return FQ_ERR_NULL;
     if (!aligned16(Q_fp8) || !aligned16(O_bf16)) return FQ_ERR_ALIGN;
@@ -622,7 +625,7 @@ int fq_kv4_read(const uint8_t* cache, int64_t page_stride, int64_t head_stride, 
 }
 
 size_t fq_kv4_attention_workspace_bytes(int B, int Hq, int Hkv, int max_len, int prefix_len) {
-    if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv != 0 || max_len < 0 || max_len > 1 << 30 || prefix_len < 0 || prefix_len > 1 << 30) return 0;
+    if (B <= 0 || !attention_sizes(B, Hq, Hkv, max_len, prefix_len)) return 0;
     return fq_attend_scratch_bytes(B, Hq, Hkv, max_len, prefix_len);
 }
 

@@ -2,6 +2,8 @@
 import ctypes
 import os
 import re
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -110,6 +112,17 @@ def test_attention_workspace_sizes():
     # whole rows of 128 sums, a maximum and a sum in FP32 for each part of each query head
     assert size(4, 32, 8, 100000, 0) % (4 * 32 * 130 * 4) == 0 and size(4, 32, 8, 100000, 0) > 0
     assert size(4, 32, 8, 10, 5000) % (4 * 32 * 130 * 4) == 0 and size(4, 32, 8, 10, 5000) > 0
+
+
+def test_no_workspace_for_sizes_that_are_refused():
+    """In a process of its own: such sizes must not end the caller."""
+    code = """from paper_2505_20839_amd import binding
+for B, Hq, Hkv in ((2 ** 31 - 1, 64, 1), (65536, 8, 8), (1, 2 ** 31 - 1, 1), (65535, 256, 1), (2 ** 31 - 1, 2 ** 31 - 1, 1), (2 ** 30, 2 ** 30, 2 ** 30)):
+    for prefix in (0, 1, 5000, 1 << 30):
+        assert binding.fq_kv4_attention_workspace_bytes(B, Hq, Hkv, 100, prefix) == 0, (B, Hq, Hkv, prefix)
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=os.path.dirname(INCLUDE))
+    assert r.returncode == 0, (r.returncode, r.stderr[-300:])
 
 
 @pytest.mark.parametrize("max_len", [1 << 30, (1 << 30) - 5, 300000001, 131072000, 5000000])
