@@ -829,9 +829,11 @@ def _attention(where, Q, q_scale, cache, prefix_pages, prefix_len, block_table, 
     if prefix_pages is not None:
         prefix_pages = _dev(prefix_pages, torch.int32, "prefix_pages")
         prefix_len = int(prefix_len)
-        if prefix_len < 0 or prefix_pages.numel() * geometry[4] < prefix_len:
+        if prefix_len < 0 or prefix_len > 1 << 30 or prefix_pages.numel() * geometry[4] < prefix_len:
             raise FireqError(-2, where)
         shared = prefix_pages.data_ptr()
+    if max_len < 0 or max_len > 1 << 30:                  # (a C int would take its low bits)
+        raise FireqError(-2, where)
     if out is None:
         out = torch.empty((B, Hq, 128), dtype=torch.bfloat16, device=Q.device)
     else:
@@ -839,7 +841,7 @@ def _attention(where, Q, q_scale, cache, prefix_pages, prefix_len, block_table, 
         if tuple(out.shape) not in ((B, Hq, 128), (B, Hq * 128)):
             raise FireqError(-2, where)
     if workspace is None:
-        need = fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) if max_len >= 0 else 0
+        need = fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len)
         workspace = torch.empty((need,), dtype=torch.uint8, device=Q.device) if need else None
     ws, nbytes = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
     args = (block_table.data_ptr(), width, seq_lens.data_ptr(), ctypes.c_float(float(out_scale)), out.data_ptr(), B, Hq, Hkv, max_len, ws, nbytes,

@@ -460,6 +460,20 @@ def test_attention_refusals(fq):
     assert fq.fq_kv4_attention(**good, out=flat).data_ptr() == flat.data_ptr() and not bool(flat.any())
 
 
+@pytest.mark.parametrize("more", [1 << 32, (1 << 32) + 5, (1 << 33) + (1 << 20), (1 << 30) + 1])
+def test_attention_refuses_bounds_past_its_integers(fq, more):
+    """Not taken for their low 32 bits."""
+    cache = fq.fq_kv4_cache(2, 1, 16)
+    Q, qs = torch.zeros((1, 1, 128), dtype=torch.uint8, device="cuda"), torch.ones((1, 1), device="cuda")
+    table, lens = torch.zeros((1, 2), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(fq.FireqError):
+        fq.fq_kv4_attention(Q, qs, cache, table, lens, 0.1, max_len=more)
+    with pytest.raises(fq.FireqError):
+        fq.fq_kv4_attention_prefix(Q, qs, cache, table[0], 3, table, lens, 0.1, max_len=more)
+    with pytest.raises(fq.FireqError):
+        fq.fq_kv4_attention_prefix(Q, qs, cache, table[0], more, table, lens, 0.1)
+
+
 def test_a_decode_step_in_a_graph_and_on_another_stream(fq):
     """Norm, append and attention captured once, replayed on new inputs with eager work in between, and on a side stream."""
     torch.manual_seed(0)
