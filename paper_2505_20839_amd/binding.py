@@ -674,6 +674,17 @@ def _norm_arguments(X, weight, residual, out):
     return X, weight, residual, out
 
 
+def _scratch(t):
+    """(pointer, bytes) of a caller's workspace, or of none"""
+    if t is None:
+        return 0, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError("workspace must be a GPU tensor")
+    if not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _ptr(t):
     return 0 if t is None else t.data_ptr()
 
@@ -710,7 +721,7 @@ def fq_rmsnorm_quant(X: torch.Tensor, weight: torch.Tensor, eps: float, residual
     M, K = X.shape
     A = torch.empty((M, K), dtype=torch.uint8, device=X.device)
     s = torch.empty((M,), dtype=torch.float32, device=X.device)
-    ws, nbytes = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
+    ws, nbytes = _scratch(workspace)
     rc = lib().fq_rmsnorm_quant_ws(X.data_ptr(), _ptr(residual), weight.data_ptr(), ctypes.c_float(float(eps)), _ptr(H), A.data_ptr(),
                                    s.data_ptr(), M, K, ws, nbytes, _stream())
     if rc != 0:
@@ -843,7 +854,7 @@ def _attention(where, Q, q_scale, cache, prefix_pages, prefix_len, block_table, 
     if workspace is None:
         need = fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len)
         workspace = torch.empty((need,), dtype=torch.uint8, device=Q.device) if need else None
-    ws, nbytes = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (0, 0)
+    ws, nbytes = _scratch(workspace)
     args = (block_table.data_ptr(), width, seq_lens.data_ptr(), ctypes.c_float(float(out_scale)), out.data_ptr(), B, Hq, Hkv, max_len, ws, nbytes,
             _stream())
     if prefix_pages is None:

@@ -410,6 +410,14 @@ PyObject* quantize_weights(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// a workspace that the Python form does not refuse
+void scratch_or_none(PyObject* o) {
+    if (o != Py_None) {
+        const at::Tensor& t = tensor(o);
+        want(t.is_cuda() && t.is_contiguous());
+    }
+}
+
 // rmsnorm(X, weight, eps, residual, out), rmsnorm_quant(X, weight, eps, residual, out, workspace)
 template <bool QUANT>
 PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -439,6 +447,7 @@ PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n) {
             return r ? wrap(rc, {Y, H}) : wrap(rc, Y);
         }
         at::Tensor A = fresh({M, K}, at::kByte, X), s = fresh({M}, at::kFloat, X);
+        scratch_or_none(a[QUANT ? 5 : 0]);
         const Scratch ws(a[QUANT ? 5 : 0], 0, X);
         uint8_t* pa = (uint8_t*)A.data_ptr();
         float* ps = (float*)s.data_ptr();
@@ -539,6 +548,7 @@ PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
             O = dev(a[9], at::kBFloat16);
             want(O.sizes() == at::IntArrayRef({B, Hq, 128}) || O.sizes() == at::IntArrayRef({B, Hq * 128}));
         }
+        scratch_or_none(a[10]);
         const Scratch ws(a[10], a[10] == Py_None ? api.attention_workspace_bytes((int)B, (int)Hq, c.heads, max_len, prefix) : 0, Q);
         const uint8_t* q = (const uint8_t*)Q.data_ptr();
         const float* s = (const float*)qs.data_ptr();

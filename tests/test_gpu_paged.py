@@ -474,6 +474,20 @@ def test_attention_refuses_bounds_past_its_integers(fq, more):
         fq.fq_kv4_attention_prefix(Q, qs, cache, table[0], more, table, lens, 0.1)
 
 
+def test_workspaces_that_are_refused(fq):
+    """Host memory, and a view whose numbers do not lie together."""
+    x, w = torch.zeros((128, 512), dtype=torch.bfloat16, device="cuda"), torch.ones(512, dtype=torch.bfloat16, device="cuda")
+    cache = fq.fq_kv4_cache(2, 1, 16)
+    Q, qs = torch.zeros((1, 1, 128), dtype=torch.uint8, device="cuda"), torch.ones((1, 1), device="cuda")
+    table, lens = torch.zeros((1, 2000), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    n = max(fq.fq_w4a8_gemm_workspace_bytes(128, 256, 512), fq.fq_kv4_attention_workspace_bytes(1, 1, 1, 32000, 20))
+    for ws, e in ((torch.empty(n, dtype=torch.uint8), TypeError), (n, TypeError), (torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2], ValueError)):
+        for call in (lambda: fq.fq_rmsnorm_quant(x, w, 1e-5, workspace=ws), lambda: fq.fq_kv4_attention(Q, qs, cache, table, lens, 0.1, workspace=ws),
+                     lambda: fq.fq_kv4_attention_prefix(Q, qs, cache, table[0], 20, table, lens, 0.1, workspace=ws)):
+            with pytest.raises(e, match="workspace"):
+                call()
+
+
 def test_a_decode_step_in_a_graph_and_on_another_stream(fq):
     """Norm, append and attention captured once, replayed on new inputs with eager work in between, and on a side stream."""
     torch.manual_seed(0)

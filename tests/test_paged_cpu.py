@@ -141,6 +141,8 @@ def test_binding_wants_gpu_tensors():
                  lambda: binding.fq_kv4_attention_prefix(t, t, t, t, 1, t, t, 1.0), lambda: binding.fq_kv4_attention_prefix(t, t, t, None, 1, t, t, 1.0)):
         with pytest.raises(TypeError, match="GPU tensor"):
             call()
+    with pytest.raises(TypeError, match="workspace must be a GPU tensor"):
+        binding._scratch(t)
     with pytest.raises(binding.FireqError):
         binding.fq_kv4_cache(4, 2, 24, device="cpu")
     assert tuple(binding.fq_kv4_cache(4, 2, 48, device="cpu").shape) == (4, 2, 3, 2080)
