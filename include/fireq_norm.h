@@ -13,8 +13,9 @@
  *                        (workspace_prepared = 1 there), as fq_quantize_act_ws does; where that size is 0 (M <= 64) it may
  *                        be NULL.
  *
- * A row with a number that is not finite, or whose squares, sum or products with w pass FP32's range, gets the scale NaN and
- * codes of zero: every output of the layer behind it is NaN in that row, and no code is.  (fq_rmsnorm: NaN throughout.)
+ * A row with a number that is not finite, or whose squares, sum, products with w or y pass FP32's range, gets the scale NaN and
+ * codes of zero: every output of the layer behind it is NaN in that row, and no code is.  (fq_rmsnorm: NaN throughout, and
+ * infinity for a single y past the range.)
  *
  *   X_bf16, R_bf16, H_bf16, Y_bf16 [M,K] row-major, 16-byte aligned; w_bf16 [K], 16-byte aligned; eps > 0, finite.
  *   K a positive multiple of 8; M < 2^22.  H_bf16 is written where R_bf16 is given (both or none, FQ_ERR_NULL) and may be R_bf16 or

@@ -146,8 +146,8 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
             top = red_top[first + i] > top ? red_top[first + i] : top;
         }
     }
-    const bool bad = !(ss < __builtin_inff()) || top >= 0x7F800000u;
-    const float rstd = 1.0f / sqrtf(ss / (float)K + eps), tf = __uint_as_float(top);
+    const float rstd = 1.0f / sqrtf(ss / (float)K + eps), tf = __uint_as_float(top), ymax = tf * rstd;
+    const bool bad = !(ss < __builtin_inff()) || top >= 0x7F800000u || (OUT != FQN_BF16 && !(ymax < __builtin_inff()));
     if (OUT == FQN_BF16) {
         fq_v4i* y = reinterpret_cast<fq_v4i*>(Y + at);
         const float f = bad ? __builtin_nanf("") : rstd;
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
         }
         return;
     }
-    if (t == 0 && on) a_scale[m] = bad ? __builtin_nanf("") : top == 0u ? 1.0f : tf * rstd / 448.0f;
+    if (t == 0 && on) a_scale[m] = bad ? __builtin_nanf("") : top == 0u ? 1.0f : ymax / 448.0f;
     fq_v2i* a = reinterpret_cast<fq_v2i*>(A + at);
     // h w is exact in FP32 (8 bits each); 448 h w / t by one exact residual step behind h w * (448 / t), as a correctly rounded quotient.
     // Rows whose t lies outside [2^-100, 2^110] divide by t first: 448 / t or 448 h w may pass FP32's range there.

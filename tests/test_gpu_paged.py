@@ -131,6 +131,20 @@ def test_norm_rows_that_are_not_finite(fq, bad):
     assert bool(torch.isnan(s).all()) and not bool(A.any())
 
 
+@pytest.mark.parametrize("K", [1024, 4096, 70000])
+def test_norm_results_past_the_range(fq, K):
+    """h w fits FP32 and y does not: a row with one number is brought to sqrt(K) times the weight."""
+    x, w = torch.zeros((3, K)), torch.ones(K)
+    x[:, 9], w[9] = 1.0, 1e38
+    x[1, 9], x[1, 10], x[2, 9] = 0.0, 1.0, 0.0
+    x, w = x.bfloat16(), w.bfloat16()
+    A, s = fq.fq_rmsnorm_quant(x.cuda(), w.cuda(), 1e-5)
+    assert torch.isnan(s[0]) and not bool(A[0].any())
+    _check_norm(fq, x[1:], None, w, 1e-5, [A.cpu()[1:], s.cpu()[1:]], True)
+    y = fq.fq_rmsnorm(x.cuda(), w.cuda(), 1e-5).cpu()
+    assert float(y[0, 9]) == float("inf") and int((y[0] != 0).sum()) == 1
+
+
 def test_norm_refusals(fq):
     x = torch.zeros((4, 512), dtype=torch.bfloat16, device="cuda")
     w = torch.ones(512, dtype=torch.bfloat16, device="cuda")
