@@ -422,7 +422,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fqa_prefix_kernel(fq_attend_arg
 }
 
 // The parts' sums, each brought to the largest maximum.  32 lanes hold the 128 channels of a row; GROUPS of 32 lanes share its parts, four
-// requested at a time.  A wave per row for up to 8 parts (no LDS, no barrier; 96 sequences behind a prefix, 3072 rows of 6 parts, the whole
+// requested at a time.  A wave per row for up to 8 parts (no LDS, no barrier; 96 sequences behind a prefix, 32 query heads, 6 parts, the whole
 // call 46.8 us, 50.1 with a workgroup each; 1 x 1000 tokens 6.9 and 7.3), a workgroup for more (12 parts 7.9 us, 8.3 with a wave; 32 parts
 // 12.4 and 14.0).
 template <int GROUPS>
