@@ -43,6 +43,9 @@
  * Scratch: fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) bytes, 16-byte aligned (prefix_len 0: without prefix; 0 bytes for sizes that the calls refuse); it may be
  * reused or freed once the work enqueued by the call has finished, and calls that overlap in time need scratch of their own.
  *
+ * Outputs (Q_fp8, q_scale, the cache of an append, K, V, O) and scratch overlap neither each other nor anything that the call reads
+ * (FQ_ERR_SHAPE).  A cache is its tiles: what lies between them, other layers of one pool say, may be an output.
+ *
  * Q_fp8, cache, QKV_bf16, cos_sin, K, V, O: 16-byte aligned.  Conventions and status codes are those of fireq.h; T, n or B = 0
  * is a successful no-op.  Hq is a multiple of Hkv; B, Hq <= 65535, B * Hq <= 2^23, max_len and prefix_len <= 2^30, T < 2^23, T * (Hq + 2 Hkv) and n * Hkv below 2^28 - 16, fewer than 2^32 tiles a head.
  */

@@ -509,6 +509,38 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
     return p < q + nb && q < p + na;
 }
 
+// The bytes of a paged cache's tiles: n1 x n2 blocks of `per` bytes at two strides.  What lies between them is somebody else's (other layers
+// of a pool).
+struct blocks {
+    const void* base;
+    int64_t n1, s1, n2, s2, per;
+};
+bool overlap(const void* p, size_t n, const blocks& c) {
+    if (n == 0 || c.n1 <= 0 || c.n2 <= 0) return false;
+    const bool first = c.n1 > 1 && (c.n2 == 1 || c.s1 >= c.s2);                       // the larger stride outside
+    const __int128 N = first ? c.n1 : c.n2, S = first ? c.s1 : c.s2, m = first ? c.n2 : c.n1, s = first ? c.s2 : c.s1, per = c.per;
+    const __int128 a = (__int128)reinterpret_cast<uintptr_t>(p) - (__int128)reinterpret_cast<uintptr_t>(c.base), b = a + (__int128)n, w = (m - 1) * s + per;
+    if (b <= 0 || a >= (N - 1) * S + w) return false;
+    if (N > 1 && w > S) return true;                      // (not one inside the other: the whole span)
+    const __int128 i0 = a < w ? 0 : (a - w) / S + 1, i1 = N == 1 ? 0 : (b - 1) / S;
+    for (__int128 i = i0; i <= i1 && i < N; ++i) {        // (one that is not the first or the last lies in the range as a whole)
+        const __int128 x = a - i * S, y = b - i * S, j0 = x < per ? 0 : (x - per) / s + 1;
+        if (y > 0 && j0 < m && j0 * s < y) return true;
+    }
+    return false;
+}
+
+// Whether an array meets one of `n` others; empty ones do not.
+struct bytes {
+    const void* p;
+    size_t n;
+};
+bool meet(const bytes& out, const bytes* others, int n) {
+    for (int i = 0; i < n; ++i)
+        if (out.n > 0 && others[i].n > 0 && overlap(out.p, out.n, others[i].p, others[i].n)) return true;
+    return false;
+}
+
 // Checks shared by the norms; `out`: Y_bf16 or A_fp8, `per`: its bytes per number.
 int check_norm(const uint16_t* X, const uint16_t* R, const uint16_t* w, float eps, const uint16_t* H, const void* out, size_t per, int M, int K) {
     // (a grid holds fewer than 2^32 threads, 1024 of them for a long row)
@@ -538,6 +570,10 @@ int check_paged(const uint8_t* cache, int64_t page_stride, int64_t head_stride, 
     return FQ_OK;
 }
 
+blocks paged_blocks(const uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages, int page, int heads) {
+    return {cache, pages, page_stride, heads, head_stride, (int64_t)(page / FQ_KV4_TILE_TOKENS) * FQ_KV4_TILE_BYTES};
+}
+
 // The sizes that the attention takes.
 bool attention_sizes(int B, int Hq, int Hkv, int max_len, int prefix_len) {
     return B >= 0 && B <= 65535 && Hq > 0 && Hq <= 65535 && Hkv > 0 && Hq % Hkv == 0 && (int64_t)B * Hq <= 1 << 23 &&
@@ -559,6 +595,12 @@ int attend(const uint8_t* Q_fp8, const float* q_scale, const uint8_t* cache, int
         if (!workspace || workspace_bytes < need) return FQ_ERR_MEMORY;
         if (!aligned16(workspace)) return FQ_ERR_ALIGN;
     }
+    // (workgroups that have not begun still read what an output would have changed)
+    const size_t rows = (size_t)B * Hq;
+    const bytes in[] = {{Q_fp8, rows * 128}, {q_scale, rows * 4}, {block_table, (size_t)B * table_width * 4}, {seq_lens, (size_t)B * 4},
+                        {prefix_pages, ((size_t)prefix_len + page - 1) / page * 4}, {workspace, need}};
+    const blocks c = paged_blocks(cache, page_stride, head_stride, pages, page, Hkv);
+    if (meet({O_bf16, rows * 256}, in, 6) || overlap(O_bf16, rows * 256, c) || meet({workspace, need}, in, 5) || overlap(workspace, need, c)) return FQ_ERR_SHAPE;
     const fq_attend_args a = {Q_fp8, q_scale, {const_cast<uint8_t*>(cache), page_stride, head_stride, pages, page}, prefix_pages, block_table,
                               seq_lens, prefix_len, table_width, out_scale, O_bf16, B, Hq, Hkv, max_len};
     fq_launch_attend(a, workspace, static_cast<hipStream_t>(stream));
@@ -604,6 +646,14 @@ int fq_kv4_append(const uint16_t* QKV_bf16, int64_t ld, const float* cos_sin, in
     if (T == 0) return FQ_OK;
     if (!QKV_bf16 || !positions || !slots || !Q_fp8 || !q_scale || (max_positions > 0 && !cos_sin)) return FQ_ERR_NULL;
     if (!aligned16(QKV_bf16) || !aligned16(cos_sin) || !aligned16(Q_fp8)) return FQ_ERR_ALIGN;
+    const size_t rows = (size_t)T * Hq;
+    const bytes in[] = {{cos_sin, (size_t)max_positions * 512}, {positions, (size_t)T * 4}, {slots, (size_t)T * 8}, {Q_fp8, rows * 128}, {q_scale, rows * 4}};
+    const blocks all = paged_blocks(cache, page_stride, head_stride, pages, page, Hkv), tokens = {QKV_bf16, T, ld * 2, 1, 0, heads * 256};
+    if (meet(in[3], in, 3) || meet(in[4], in, 4) || overlap(Q_fp8, rows * 128, tokens) || overlap(q_scale, rows * 4, tokens) ||
+        overlap(QKV_bf16, ((size_t)(T - 1) * ld + heads * 128) * 2, all))
+        return FQ_ERR_SHAPE;
+    for (const bytes& x : in)
+        if (overlap(x.p, x.n, all)) return FQ_ERR_SHAPE;
     const fq_paged_cache c = {cache, page_stride, head_stride, pages, page};
     fq_launch_kv4_append(QKV_bf16, ld, cos_sin, max_positions, positions, slots, interleaved != 0, Q_fp8, q_scale, c, T, Hq, Hkv,
                          static_cast<hipStream_t>(stream));
@@ -619,6 +669,10 @@ int fq_kv4_read(const uint8_t* cache, int64_t page_stride, int64_t head_stride, 
     if (n == 0) return FQ_OK;
     if (!slots || !K_bf16 || !V_bf16) return FQ_ERR_NULL;
     if (!aligned16(K_bf16) || !aligned16(V_bf16)) return FQ_ERR_ALIGN;
+    const size_t out = (size_t)n * Hkv * 256;
+    const bytes in[] = {{slots, (size_t)n * 8}, {K_bf16, out}};
+    const blocks all = paged_blocks(cache, page_stride, head_stride, pages, page, Hkv);
+    if (meet({K_bf16, out}, in, 1) || meet({V_bf16, out}, in, 2) || overlap(K_bf16, out, all) || overlap(V_bf16, out, all)) return FQ_ERR_SHAPE;
     const fq_paged_cache c = {const_cast<uint8_t*>(cache), page_stride, head_stride, pages, page};
     fq_launch_kv4_read(c, slots, K_bf16, V_bf16, n, Hkv, static_cast<hipStream_t>(stream));
     return after_launch();
