@@ -19,7 +19,8 @@
  *
  *   X_bf16, R_bf16, H_bf16, Y_bf16 [M,K] row-major, 16-byte aligned; w_bf16 [K], 16-byte aligned; eps > 0, finite.
  *   K a positive multiple of 8; M < 2^22.  H_bf16 is written where R_bf16 is given (both or none, FQ_ERR_NULL) and may be R_bf16 or
- *   X_bf16 itself; any other overlap of H or Y with an input is FQ_ERR_SHAPE (Y_bf16 may be X_bf16 or R_bf16).
+ *   X_bf16 itself; any other overlap of H or Y with an input is FQ_ERR_SHAPE (Y_bf16 may be X_bf16 or R_bf16), and so
+ *   is any of a_scale or of the workspace with another array of the call.
  * Conventions and status codes are those of fireq.h; M = 0 is a successful no-op.
  */
 #ifndef FIREQ_NORM_H

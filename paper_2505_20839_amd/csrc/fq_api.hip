@@ -631,6 +631,10 @@ int fq_rmsnorm_quant_ws(const uint16_t* X_bf16, const uint16_t* R_bf16, const ui
         if (!aligned16(workspace)) return FQ_ERR_ALIGN;
         planes = workspace;
     }
+    const size_t n = (size_t)M * K;
+    const bytes in[] = {{X_bf16, n * 2}, {R_bf16, R_bf16 ? n * 2 : 0}, {w_bf16, (size_t)K * 2}, {H_bf16, H_bf16 ? n * 2 : 0}, {A_fp8, n},
+                        {planes, planes ? fq_gemm_large_workspace_bytes(M, K) : 0}};
+    if (meet({a_scale, (size_t)M * 4}, in, 6) || meet(in[5], in, 5)) return FQ_ERR_SHAPE;
     fq_launch_rmsnorm_quant(X_bf16, R_bf16, w_bf16, eps, H_bf16, A_fp8, a_scale, M, K, planes, static_cast<hipStream_t>(stream));
     return after_launch();
 }

@@ -119,3 +119,28 @@ def test_gaps_of_any_layout():
         at = CACHE + 16 * rng.randrange(-n // 16 - 2, (4 * page + head + PER) // 16 + 2)
         meets = any(at < CACHE + p * page + h * head + PER and CACHE + p * page + h * head < at + n for p in range(PAGES) for h in range(2))
         assert read(page_stride=page, head_stride=head, K=at) == (SHAPE if meets else LAUNCH), (page, head, at - CACHE)
+
+
+def norm(residual=False, **change):
+    M, K = 100, 256
+    need = binding.lib().fq_w4a8_gemm_workspace_bytes(M, 256, K)
+    a = dict(X=1 * MB, R=2 * MB, w=3 * MB, H=4 * MB, A=5 * MB, s=6 * MB, ws=7 * MB)
+    a.update(change)
+    return binding.lib().fq_rmsnorm_quant_ws(a["X"], a["R"] if residual else 0, a["w"], ctypes.c_float(1e-5), a["H"] if residual else 0, a["A"], a["s"], M, K,
+                                             a["ws"], need, 0), need
+
+
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm_scales_and_workspace_over_the_rest(residual):
+    rc, need = norm(residual)
+    assert rc == LAUNCH and need > 0 and need % 16 == 0
+    arrays = dict(X=100 * 512, w=512, A=100 * 256, **(dict(R=100 * 512, H=100 * 512) if residual else {}))
+    for out, no in (("s", 400), ("ws", need)):
+        for name, n in arrays.items():
+            for at in (0, n - 16, 16 - no):
+                assert norm(residual, **{out: 32 * MB, name: 32 * MB - at})[0] == SHAPE, (out, name, at)
+            for at in (n, -no):
+                assert norm(residual, **{out: 32 * MB, name: 32 * MB - at})[0] == LAUNCH, (out, name, at)
+    assert norm(residual, s=32 * MB, ws=32 * MB)[0] == norm(residual, s=32 * MB + need - 4, ws=32 * MB)[0] == SHAPE
+    if residual:                                          # the stream in place is still taken
+        assert norm(True, H=1 * MB)[0] == norm(True, H=2 * MB)[0] == LAUNCH
