@@ -658,10 +658,17 @@ def fq_kv4_output(P: torch.Tensor, p_scale: torch.Tensor, V_packed: torch.Tensor
     return O
 
 
+def _fits(*sizes):
+    """Whether C ints hold them (ctypes would pass the low bits on)."""
+    return all(-(1 << 31) <= n < 1 << 31 for n in sizes)
+
+
 def _norm_arguments(X, weight, residual, out):
     X = _dev(X, torch.bfloat16, "X")
     weight = _dev(weight, torch.bfloat16, "weight")
     if X.dim() != 2 or weight.numel() != X.shape[1]:
+        raise FireqError(-2, "fq_rmsnorm")
+    if not _fits(*X.shape):
         raise FireqError(-2, "fq_rmsnorm")
     if residual is None:
         if out is not None:
@@ -753,6 +760,8 @@ def _cache(cache):
     if cache.stride(3) != 1 or (cache.shape[2] > 1 and cache.stride(2) != KV4_TILE_BYTES):
         raise ValueError("cache must have its pages contiguous")
     pages, heads, tiles, _ = cache.shape
+    if not _fits(pages, heads, tiles * KV4_TILE_TOKENS):
+        raise FireqError(-2, "cache")
     per = tiles * KV4_TILE_BYTES
     head_stride = cache.stride(1) if heads > 1 else per
     page_stride = cache.stride(0) if pages > 1 else heads * head_stride
@@ -787,6 +796,8 @@ def fq_kv4_append(QKV: torch.Tensor, cos_sin: torch.Tensor, positions: torch.Ten
     Hq = width // 128 - 2 * Hkv
     if Hq <= 0 or positions.numel() != T or slots.numel() != T:
         raise FireqError(-2, "fq_kv4_append")
+    if not _fits(T, Hq, cos_sin.shape[0]):
+        raise FireqError(-2, "fq_kv4_append")
     Q = torch.empty((T, Hq, 128), dtype=torch.uint8, device=QKV.device)
     s = torch.empty((T, Hq), dtype=torch.float32, device=QKV.device)
     rc = lib().fq_kv4_append(QKV.data_ptr(), QKV.stride(0) if T > 1 else width, cos_sin.data_ptr(), cos_sin.shape[0], positions.data_ptr(),
@@ -806,6 +817,8 @@ def fq_kv4_read(cache: torch.Tensor, slots: torch.Tensor) -> Tuple[torch.Tensor,
     geometry, Hkv = _cache(cache)
     slots = _dev(slots, torch.int64, "slots")
     n = slots.numel()
+    if not _fits(n):
+        raise FireqError(-2, "fq_kv4_read")
     K = torch.empty((n, Hkv, 128), dtype=torch.bfloat16, device=cache.device)
     V = torch.empty((n, Hkv, 128), dtype=torch.bfloat16, device=cache.device)
     rc = lib().fq_kv4_read(*geometry, slots.data_ptr(), K.data_ptr(), V.data_ptr(), n, Hkv, _stream())
@@ -815,7 +828,9 @@ def fq_kv4_read(cache: torch.Tensor, slots: torch.Tensor) -> Tuple[torch.Tensor,
 
 
 def fq_kv4_attention_workspace_bytes(B: int, Hq: int, Hkv: int, max_len: int, prefix_len: int = 0) -> int:
-    return int(lib().fq_kv4_attention_workspace_bytes(int(B), int(Hq), int(Hkv), int(max_len), int(prefix_len)))
+    """Bytes of scratch that the attention of these sizes needs; 0 for sizes that it refuses, as the C function answers."""
+    sizes = [int(n) for n in (B, Hq, Hkv, max_len, prefix_len)]
+    return int(lib().fq_kv4_attention_workspace_bytes(*sizes)) if _fits(*sizes) else 0
 
 
 def _attention(where, Q, q_scale, cache, prefix_pages, prefix_len, block_table, seq_lens, out_scale, max_len, out, workspace):
@@ -834,6 +849,8 @@ def _attention(where, Q, q_scale, cache, prefix_pages, prefix_len, block_table, 
     B, Hq, _ = Q.shape
     width = block_table.shape[1]
     if q_scale.numel() != B * Hq or block_table.shape[0] != B or seq_lens.numel() != B or Hq % Hkv:
+        raise FireqError(-2, where)
+    if not _fits(B, Hq, width):
         raise FireqError(-2, where)
     max_len = min(width * geometry[4], 1 << 30) if max_len is None else int(max_len)
     shared = 0
