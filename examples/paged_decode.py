@@ -127,24 +127,28 @@ def main(argv=None):
         lens.add_(1)
         return y
 
-    y = step()
+    step()
     torch.cuda.synchronize()
     run = step
     if not a.no_graph:
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             y = step()
-        run = graph.replay
-    run()
+
+        def run():
+            graph.replay()
+            return y
+
+    last = run()
     torch.cuda.synchronize()
     began = time.perf_counter()
     for _ in range(steps):
-        run()
+        last = run()
     torch.cuda.synchronize()
     took = (time.perf_counter() - began) / steps
     print("%d sequences behind %d shared tokens, %d blocks: %.1f us a step, %.0f tokens/s; finite: %s"
-          % (B, a.prefix, a.blocks, took * 1e6, B / took, bool(torch.isfinite(y.float()).all())))
-    return y
+          % (B, a.prefix, a.blocks, took * 1e6, B / took, bool(torch.isfinite(last.float()).all())))
+    return last
 
 
 if __name__ == "__main__":
