@@ -117,7 +117,8 @@ def main(argv=None):
     g = torch.Generator(device="cuda").manual_seed(1)
     order = torch.randperm(B * width + shared, generator=g, device="cuda").to(torch.int32)
     table, prefix_pages = order[: B * width].reshape(B, width).contiguous(), order[B * width:].contiguous()
-    d.prefill(torch.randn((a.prefix, 4096), generator=g, device="cuda").bfloat16(), prefix_pages)
+    if a.prefix:
+        d.prefill(torch.randn((a.prefix, 4096), generator=g, device="cuda").bfloat16(), prefix_pages)
     x = torch.randn((B, 4096), generator=g, device="cuda").bfloat16()
     lens = torch.ones(B, dtype=torch.int32, device="cuda")
 

@@ -26,3 +26,9 @@ def test_eager_and_graph_end_alike(example):
     graph, eager = example.main(args + ["5"]), example.main(args + ["5", "--no-graph"])
     assert bool(torch.isfinite(eager.float()).all()) and torch.equal(graph.view(torch.int16), eager.view(torch.int16))
     assert not torch.equal(eager.view(torch.int16), example.main(args + ["4", "--no-graph"]).view(torch.int16))
+
+
+def test_without_a_shared_prompt(example):
+    args = ["--batch", "2", "--prefix", "0", "--steps", "2", "--blocks", "1"]
+    graph, eager = example.main(args), example.main(args + ["--no-graph"])
+    assert bool(torch.isfinite(eager.float()).all()) and torch.equal(graph.view(torch.int16), eager.view(torch.int16))
