@@ -113,7 +113,7 @@ def main(argv=None):
     a = ap.parse_args(argv)
     B, page, steps = a.batch, 32, a.steps
     width, shared = -(-(steps + 4) // page), -(-a.prefix // page)
-    d = Decoder(blocks=a.blocks, pages=B * width + shared, page=page)
+    d = Decoder(blocks=a.blocks, pages=B * width + shared, page=page, positions=a.prefix + steps + 2)
     g = torch.Generator(device="cuda").manual_seed(1)
     order = torch.randperm(B * width + shared, generator=g, device="cuda").to(torch.int32)
     table, prefix_pages = order[: B * width].reshape(B, width).contiguous(), order[B * width:].contiguous()
