@@ -23,6 +23,9 @@
  *                     queries         q_scale = max |q| / 448 (1 for zeros), Q_fp8 = E4M3 nearest-even of q / q_scale
  *                     keys, values    sigma = E4M3 nearest-even of min(max |x| / 7, 448), code = clamp(round_half_even(x / sigma),
  *                                     -8, 7), 0 where sigma is 0; FP32 quotients
+ *                 (sigma's least steps are 2^-9 and there is no further factor: a key or value head of max |x| <= 7 * 2^-10,
+ *                 0.0068, is kept as zeros, and one below about 0.05 coarsely.  Layers with heads that small scale their key projection by
+ *                 a power of two and out_scale back, their value projection and the output layer's w_tscale)
  *                 and key and value go to slot slots[i].  A negative slot is padding: nothing is cached.  Two rows with one slot
  *                 leave either's bytes.  What cannot be done shows: a head with a number that is not finite gets the scale NaN
  *                 (codes 0); a position outside the table, or a slot behind the cache's end (nothing is cached), gives
@@ -32,8 +35,12 @@
  *                 slot, NaN for one behind the cache's end.
  * fq_kv4_attention_ws   O[b,h,:] = bf16( sum_t p_t v_t / sum_t p_t ), p_t = exp(out_scale q . k_t), over the tokens
  *                 t < seq_lens[b], token t in page block_table[b][t / page] (row b at block_table + b * table_width).  A
- *                 sequence with no token (a length <= 0) gets zeros.  Scores are FP32 sums of exact products; probabilities,
- *                 relative to a running maximum, enter the FP32 sums as fp16 numbers; sigma * code is exact.
+ *                 sequence with no token (a length <= 0) gets zeros.  Scores are sums q_scale sigma out_scale
+ *                 (sum_d q_d (code_d + 8) - 8 sum_d q_d) on the FP8 matrix cores, whose products are exact and are aligned to the
+ *                 largest of an instruction before they are added: a score lies within 2^-12 of the largest
+ *                 |q_scale q_d sigma out_scale| max(code_d + 8, 8) of its token (measured: 2^-13), and within FP32's
+ *                 roundings of its factors, of the exact one.  A query with one channel far above the others feels it in the
+ *                 others.  Probabilities, relative to a running maximum, enter the FP32 sums as fp16 numbers; sigma * code is exact.
  *                 out_scale > 0; max_len is an upper bound of seq_lens that the caller knows (it decides how the work is
  *                 split).  A sequence longer than it, or than table_width * page, or a page number outside the cache
  *                 within a sequence's length, gives NaN for that sequence.

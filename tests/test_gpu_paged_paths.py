@@ -34,3 +34,39 @@ def test_outputs_over_inputs_are_refused_and_between_tiles_are_not(fq):
     other = pool[1, 2].view(-1)[:2048].view(torch.bfloat16).view(2, 4, 128)    # another layer's page
     assert torch.equal(fq.fq_kv4_attention(Q, S, cache, T, L, 0.1, out=other).view(torch.int16), want.view(torch.int16))
     assert np.array_equal(cache.cpu().numpy(), ref.b)
+
+
+def _attention_within(q, q_scale, K, V, kc, ks, vs, out_scale):
+    """pu.attention with the score's error counted as include/fireq_paged.h states it: 2^-12 of the largest term of the zero-point form, the
+    zero point's own 8 |q| among them (a channel of code -8 has no product)."""
+    o, tol = pu.attention(q, q_scale, K, V, kc, ks, vs, out_scale)
+    f = float(q_scale) * out_scale
+    s = K @ pu.E4M3[q] * f
+    p = np.exp(s - s.max())
+    e = 2.0 ** -12 * (np.abs(pu.E4M3[q])[None, :] * np.maximum(kc + 8, 8)).max(1) * np.abs(ks[:, 0]) * f
+    return o, tol + ((p * e) @ np.abs(V) + (p * e).sum() * np.abs(o)) / p.sum()
+
+
+@pytest.mark.parametrize("low", [3, 7, 11])
+def test_scores_of_queries_with_an_outlier(fq, low):
+    """One channel 2^low above the others: the others' products lose their last bits, by no more than the header says."""
+    rng = np.random.default_rng(low)
+    lens = [2, 40, 333, 17, 64, 9]
+    ref, table, _ = _filled(rng, lens, 1, 16)
+    for b, n in enumerate(lens):                          # the outlier's codes are one number in all tokens, the lowest or the highest too
+        for t in range(n):
+            slot = int(table[b, t // 16]) * 16 + t % 16
+            codes, sc = ref.get(slot, 0, False)
+            codes[77] = (-8, 7, 0)[b % 3]
+            ref.put(slot, 0, False, codes, 0x38)
+    x = rng.standard_normal((len(lens), 16, 128)) * 2.0 ** -low
+    x[..., 77] = np.sign(x[..., 77])
+    qs = (np.abs(x).max(-1) / 448).astype(np.float32)
+    q = pu.to_e4m3((x / qs[..., None]).astype(np.float32))
+    qs *= np.float32(2.0 ** low)
+    got = fq.fq_kv4_attention(*_gpu(q, qs, ref.b, table, np.array(lens, np.int32)), 0.02).double().cpu().numpy()
+    for b, n in enumerate(lens):
+        kv = list(ref.tokens([int(table[b, t // 16]) * 16 + t % 16 for t in range(n)], 0))
+        for r in range(16):
+            o, tol = _attention_within(q[b, r], qs[b, r], *kv, 0.02)
+            assert (np.abs(got[b, r] - o) <= tol).all(), (b, r)
