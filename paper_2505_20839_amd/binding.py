@@ -889,8 +889,8 @@ def fq_kv4_attention(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch.Tensor
     """bf16 [B,Hq,128]: attention of one query token per sequence (codes and scales from fq_kv4_append) over its seq_lens[b]
     (int32 [B]) cached tokens, in the pages block_table[b] (int32 [B, pages of a sequence]) of a paged cache.
 
-    `max_len`: an upper bound of seq_lens that the host knows, by default what the table has room for (it only decides how the
-    work is split); `workspace` of fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len) bytes is allocated here when not given."""
+    `max_len`: an upper bound of seq_lens that the host knows, by default what the table has room for (it decides how the work is
+    split: one far above the lengths costs up to several times the time); `workspace` of fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len) bytes is allocated here when not given."""
     return _attention("fq_kv4_attention", Q, q_scale, cache, None, 0, block_table, seq_lens, out_scale, max_len, out, workspace)
 
 
