@@ -108,6 +108,23 @@ __device__ __forceinline__ unsigned fq_dpp_umax(unsigned v) {
     return o > v ? o : v;
 }
 
+// Sum of the eight E4M3 values of two words of codes.
+__device__ __forceinline__ float fq_sum8(fq_v2i o) {
+    const fq_v2f a = __builtin_amdgcn_cvt_pk_f32_fp8(o[0], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(o[0], true);
+    const fq_v2f c = __builtin_amdgcn_cvt_pk_f32_fp8(o[1], false), d = __builtin_amdgcn_cvt_pk_f32_fp8(o[1], true);
+    return ((a[0] + a[1]) + (b[0] + b[1])) + ((c[0] + c[1]) + (d[0] + d[1]));
+}
+
+template <int CTRL>
+__device__ __forceinline__ float fq_dpp_add(float v) {
+    return v + __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, false));
+}
+
+// The sum of 16 neighbouring lanes, in each of them: pairs, quads, eights, sixteens.
+__device__ __forceinline__ float fq_row16_sum(float v) {
+    return fq_dpp_add<0x140>(fq_dpp_add<0x141>(fq_dpp_add<0x4E>(fq_dpp_add<0xB1>(v))));
+}
+
 // The largest value of 16 neighbouring lanes, in each of them: pairs, quads, eights, sixteens.
 __device__ __forceinline__ unsigned fq_row16_max(unsigned v) {
     v = fq_dpp_umax<0xB1, 0xF>(v);

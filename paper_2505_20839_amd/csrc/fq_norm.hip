@@ -11,17 +11,9 @@ namespace {
 
 enum { FQN_BF16 = 0, FQN_CODES = 1, FQN_CODES_ZP = 2 };   // what leaves: bf16, codes and scale, and the GEMM's zero-point terms too
 
-template <int CTRL>
-__device__ __forceinline__ float fqn_dpp_add(float v) {
-    return v + __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, false));
-}
-
-// The sum of 16 neighbouring lanes, in each of them; of a wave, in every lane.
-__device__ __forceinline__ float fqn_row16_sum(float v) {
-    return fqn_dpp_add<0x140>(fqn_dpp_add<0x141>(fqn_dpp_add<0x4E>(fqn_dpp_add<0xB1>(v))));
-}
+// The sum of a wave, in every lane.
 __device__ __forceinline__ float fqn_wave_sum(float v) {
-    v = fqn_row16_sum(v);
+    v = fq_row16_sum(v);
     const int b = (int)__float_as_uint(v);
     return (__uint_as_float((unsigned)__builtin_amdgcn_readlane(b, 0)) + __uint_as_float((unsigned)__builtin_amdgcn_readlane(b, 16))) +
            (__uint_as_float((unsigned)__builtin_amdgcn_readlane(b, 32)) + __uint_as_float((unsigned)__builtin_amdgcn_readlane(b, 48)));
@@ -66,12 +58,6 @@ __device__ __forceinline__ fq_v2i fqn_codes8(fq_v4i h, fq_v4i w, F quotient) {
         o[j] = r;
     }
     return o;
-}
-
-__device__ __forceinline__ float fqn_sum8(fq_v2i o) {     // of eight E4M3 values
-    const fq_v2f a = __builtin_amdgcn_cvt_pk_f32_fp8(o[0], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(o[0], true);
-    const fq_v2f c = __builtin_amdgcn_cvt_pk_f32_fp8(o[1], false), d = __builtin_amdgcn_cvt_pk_f32_fp8(o[1], true);
-    return ((a[0] + a[1]) + (b[0] + b[1])) + ((c[0] + c[1]) + (d[0] + d[1]));
 }
 
 // WPR waves per row with up to CH chunks (16 bytes, 8 numbers) of it per thread; workgroups of max(4, WPR) waves.  The row and
@@ -173,7 +159,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
     // h w is exact in FP32 (8 bits each); 448 h w / t by one exact residual step behind h w * (448 / t), as a correctly rounded quotient.
     // Rows whose t lies outside [2^-100, 2^110] divide by t first: 448 / t or 448 h w may pass FP32's range there.
     const float mul = bad || top == 0u ? 0.f : 448.0f / tf, rt = bad || top == 0u ? 0.f : 1.0f / tf;
-    auto put = [&](auto tiny, int i, int c, fq_v4i h, fq_v4i g) __attribute__((always_inline)) {
+    auto put = [&](auto tiny, int c, fq_v4i h, fq_v4i g) __attribute__((always_inline)) {
         fq_v2i o = {0, 0};
         if (!bad) {
             if constexpr (decltype(tiny)::value) o = fqn_codes8(h, g, [&](float v) { return tf > 0.f ? v / tf * 448.0f : 0.f; });
@@ -186,7 +172,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
         if (on) a[c] = o;
         if (ZP) {
             // a group is 16 consecutive chunks = 16 consecutive lanes, all here or all absent (K is a multiple of 128)
-            float z = fqn_row16_sum(fqn_sum8(o));
+            float z = fq_row16_sum(fq_sum8(o));
             if ((t & 15) == 0) {
                 z *= -0.015625f;
                 const _Float16 hi = (_Float16)z, lo = (_Float16)(z - (float)hi);
@@ -198,11 +184,11 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
     auto convert = [&](auto tiny) __attribute__((always_inline)) {
         if (REREAD) {
             if (on)
-                for (int c = t; c < nchunk; c += T) put(tiny, 0, c, RES ? hs[c] : x[c], w[c]);
+                for (int c = t; c < nchunk; c += T) put(tiny, c, RES ? hs[c] : x[c], w[c]);
         } else {
 #pragma unroll
             for (int i = 0; i < CH; ++i)
-                if (t + i * T < nchunk) put(tiny, i, t + i * T, keep[i], wt[i]);
+                if (t + i * T < nchunk) put(tiny, t + i * T, keep[i], wt[i]);
         }
     };
     if (__builtin_amdgcn_readfirstlane((int)(top != 0u && !(tf >= 0x1p-100f && tf <= 0x1p110f)))) convert(std::true_type());

@@ -11,19 +11,6 @@
 #include "fq_common.h"
 #include "fq_kernels.h"
 
-
-// Sum of the eight E4M3 values of two words of codes.
-__device__ __forceinline__ float fq_sum8(fq_v2i o) {
-    const fq_v2f a = __builtin_amdgcn_cvt_pk_f32_fp8(o[0], false), b = __builtin_amdgcn_cvt_pk_f32_fp8(o[0], true);
-    const fq_v2f c = __builtin_amdgcn_cvt_pk_f32_fp8(o[1], false), d = __builtin_amdgcn_cvt_pk_f32_fp8(o[1], true);
-    return ((a[0] + a[1]) + (b[0] + b[1])) + ((c[0] + c[1]) + (d[0] + d[1]));
-}
-
-template <int CTRL>
-__device__ __forceinline__ float fq_dpp_add(float v) {
-    return v + __uint_as_float((unsigned)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xF, 0xF, false));
-}
-
 // WPR waves per row, up to CH chunks (of 16 bytes, 8 bf16) of it per thread in registers between the search for the
 // largest magnitude and the conversion, so that the row is read once; longer rows are read a second time (REREAD).
 // Bound by HBM (3 bytes per element); what keeps it from there is the latency of a row (load, maximum, conversion, store one
@@ -122,11 +109,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fq_quantize_kernel(c
                 if (ZP) {
                     // a group is 16 consecutive chunks = 16 consecutive lanes (nchunk is a multiple of 16,
                     // so a group's lanes are all here or all absent)
-                    float z = fq_sum8(o);
-                    z = fq_dpp_add<0xB1>(z);              // pairs, quads, eights, sixteens
-                    z = fq_dpp_add<0x4E>(z);
-                    z = fq_dpp_add<0x141>(z);
-                    z = fq_dpp_add<0x140>(z);
+                    float z = fq_row16_sum(fq_sum8(o));
                     if ((t & 15) == 0) {
                         z *= -0.015625f;
                         const _Float16 hi = (_Float16)z;                  // round to nearest even
