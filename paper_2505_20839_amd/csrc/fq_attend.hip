@@ -371,7 +371,8 @@ __device__ __forceinline__ void fqa_group(const fq_attend_args& a, const fqa_par
 // Own tokens: a workgroup takes `chunk` tiles of one sequence for 16 query rows of a key/value head.  Heads are the fastest index and chunks the
 // slowest: workgroup i runs on XCD i % 8, and with chunks (of which a short sequence has the first ones only) or sequences fastest some
 // XCDs got most of the work (37 sequences of 0 to 6000 tokens 37.0 us, 31.9 with a number of chunks that happened to spread them).
-// Bound by HBM where there is enough to read: 64 x 8192 tokens (545 MB) 102 us, 5.3 TB/s, the rate of a large copy; 37 x 0 .. 6000 (105 MB) 24.
+// Where there is enough to read, between HBM and issue: 64 x 8192 tokens (545 MB, 547 fetched) 102 us, 5.3 TB/s (a large copy 5.1, a kernel that only
+// reads 7), vector and matrix instructions 55 and 13 % of the busy cycles; 37 x 0 .. 6000 (105 MB) 24.
 // One workgroup per compute unit and less is bound by a wave's chain: start, length, page table and first tiles 3 us, then 0.5 us for two tiles (1 x
 // 32001 tokens 10.0, 33 MB).  Two or eight waves a workgroup, four tiles a step, bytes two steps ahead were slower on most lengths.
 // With shared_slots, the first workgroups of a sequence take a shared prefix instead, in chunks of shared_chunk tiles.  finish: a sequence's tokens
@@ -408,8 +409,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void fqa_own_kernel(fq_attend_args a
 
 // The shared prefix: a workgroup takes `chunk` tiles for 16 RT of a key/value head's B * G query rows.  Workgroups with the same tiles of a
 // head follow each other at a distance of Hkv, so that with 8 heads (or a multiple) they run on one XCD and find them in its L2.
-// 384 rows of each of 8 heads x 12000 tokens (18.9 GFLOP) 32.4 us: 1.83 us per 1000 tokens (880 TFLOP/s, vector and matrix instructions in about
-// equal parts behind each other in two waves per SIMD) and 10.5 for the start, gathering the rows, and 8 MB of parts.  The whole call at an earlier
+// 384 rows of each of 8 heads x 12000 tokens (18.9 GFLOP) 32.4 us: 1.83 us per 1000 tokens (880 TFLOP/s; vector instructions 67 %, matrix instructions
+// 23 % of the busy cycles, behind each other in two waves per SIMD) and 10.5 for the start, gathering the rows, and 8 MB of parts.  The whole call at an earlier
 // state: RT = 2 54.0, 1 60.9, 3 56.1 (one wave per SIMD).
 template <int RT, int WAVES, int NT, int AHEAD>
 __global__ __launch_bounds__(64 * WAVES, 2) void fqa_prefix_kernel(fq_attend_args a, fqa_parts parts, int chunk, int row_groups) {
