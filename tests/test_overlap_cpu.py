@@ -33,10 +33,10 @@ def attention(prefix=False, **change):
 
 
 def append(**change):
-    a = dict(QKV=1 * MB, ld=1600, cos_sin=2 * MB, positions=3 * MB, slots=4 * MB, Q=5 * MB, qs=6 * MB, cache=CACHE, page_stride=PAGE, head_stride=HEAD)
+    a = dict(QKV=1 * MB, ld=1856, cos_sin=2 * MB, positions=3 * MB, slots=4 * MB, Q=5 * MB, qs=6 * MB, cache=CACHE, page_stride=PAGE, head_stride=HEAD)
     a.update(change)
     return binding.lib().fq_kv4_append(a["QKV"], a["ld"], a["cos_sin"], 40, a["positions"], a["slots"], 0, a["Q"], a["qs"], a["cache"], a["page_stride"],
-                                       a["head_stride"], PAGES, 32, 6, 8, 2, 0)
+                                       a["head_stride"], PAGES, 32, 6, 10, 2, 0)
 
 
 def read(**change):
@@ -75,7 +75,7 @@ def test_attention_outputs_over_inputs(prefix):
 
 
 def test_append_outputs_over_inputs():
-    q, s, rows = 6 * 8 * 128, 6 * 8 * 4, 12 * 256
+    q, s, rows = 6 * 10 * 128, 6 * 10 * 4, 14 * 256
     for name, n in dict(cos_sin=40 * 512, positions=24, slots=48).items():
         n16 = (n + 15) // 16 * 16
         for out, no in (("Q", q), ("qs", s)):
@@ -84,12 +84,12 @@ def test_append_outputs_over_inputs():
             assert append(**{out: 32 * MB, name: 32 * MB - n16}) == append(**{out: 32 * MB, name: 32 * MB + no}) == LAUNCH
     assert append(Q=32 * MB, qs=32 * MB + 16) == append(Q=32 * MB, qs=32 * MB + q - 16) == SHAPE
     X = 32 * MB
-    for i in (0, 1, 5):                                   # strided rows of 3072 bytes: Q over a row
-        for at in (X + i * 3200, X + i * 3200 + rows - 16):
+    for i in (0, 1, 5):                                   # strided rows of 14 heads: Q over a row
+        for at in (X + i * 3712, X + i * 3712 + rows - 16):
             assert append(QKV=X, Q=at) == append(QKV=X, qs=at) == SHAPE
-    assert append(QKV=X, qs=X + 3 * 3200 - 64) == SHAPE
+    assert append(QKV=X, qs=X + 3 * 3712 - 64) == SHAPE
     assert append(QKV=X, ld=16384, Q=X + 2 * 32768 + rows) == LAUNCH     # between two rows
-    assert append(QKV=X, Q=X + 5 * 3200 + rows) == append(QKV=X, Q=X - q) == LAUNCH
+    assert append(QKV=X, Q=X + 5 * 3712 + rows) == append(QKV=X, Q=X - q) == LAUNCH
     for name in ("QKV", "cos_sin", "positions", "slots", "Q", "qs"):
         for at in (CACHE, CACHE + HEAD, CACHE + 3 * PAGE, END - 16):
             assert append(**{name: at}) == SHAPE, (name, at)
