@@ -43,12 +43,14 @@
  *                 others.  Probabilities, relative to a running maximum, enter the FP32 sums as fp16 numbers; sigma * code is exact.
  *                 out_scale > 0; max_len is an upper bound of seq_lens that the caller knows.  It decides how the work is
  *                 split, and parts that no sequence has are dispatched and joined all the same: 64 sequences of 1000 tokens
- *                 (32 / 8 heads) take 16 us with max_len 1000, 24 with 32768, 54 with 131072; 32 of them 9.9, 13.7 and 13.7.  A sequence longer than it, or than table_width * page, or a page number outside the cache
- *                 within a sequence's length, gives NaN for that sequence.
+ *                 (32 / 8 heads) take 16 us with max_len 1000, 24 with 32768, 54 with 131072; 32 of them 9.9, 13.7 and 13.7.
+ *                 A sequence longer than it, or than table_width * page, or a page number outside the cache within a sequence's
+ *                 length, gives NaN for that sequence.
  * fq_kv4_attention_prefix_ws   the same where every sequence attends to prefix_len tokens in prefix_pages first, and then
  *                 to its own seq_lens[b] tokens: the prefix is read and unpacked for up to 32 query rows at a time, not for
  *                 every sequence (unless that is less work than sharing it).
- * Scratch: fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) bytes, 16-byte aligned (prefix_len 0: without prefix; 0 bytes for sizes that the calls refuse); it may be
+ * Scratch: fq_kv4_attention_workspace_bytes(B, Hq, Hkv, max_len, prefix_len) bytes, 16-byte aligned (prefix_len 0: without
+ * prefix; 0 bytes for sizes that the calls refuse); it may be
  * reused or freed once the work enqueued by the call has finished, and calls that overlap in time need scratch of their own.
  *
  * Outputs (Q_fp8, q_scale, the cache of an append, K, V, O) and scratch overlap neither each other nor anything that the call reads
