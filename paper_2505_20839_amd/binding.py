@@ -33,7 +33,9 @@ _MARSHALLED = ("fq_quantize_act", "fq_quantize_act_ws", "fq_packed_weight_bytes"
                "fq_w4a8_linear_ws", "fq_kv4_packed_bytes", "fq_kv4_scores", "fq_kv4_output_workspace_bytes", "fq_kv4_output_ws",
                "fq_kv4_pack", "fq_pack_weights", "fq_cas_scales_workspace_bytes", "fq_cas_scales_ws", "fq_pts_exponent_workspace_bytes",
                "fq_pts_exponent_ws", "fq_quantize_weights", "fq_rmsnorm", "fq_rmsnorm_quant_ws", "fq_kv4_append", "fq_kv4_read",
-               "fq_kv4_attention_workspace_bytes", "fq_kv4_attention_ws", "fq_kv4_attention_prefix_ws")
+               "fq_kv4_attention_workspace_bytes", "fq_kv4_attention_ws", "fq_kv4_attention_prefix_ws", "fq_rmsnorm_block",
+               "fq_rmsnorm_block_quant_ws", "fq_kv4_append_axes", "fq_kv4_attention_chunk_workspace_bytes", "fq_kv4_attention_chunk_ws",
+               "fq_sample_workspace_bytes", "fq_sample_bf16_ws", "fq_sample_fp32_ws")
 
 
 class FireqError(RuntimeError):
@@ -88,6 +90,22 @@ def lib() -> ctypes.CDLL:
     L.fq_kv4_attention_ws.argtypes = [vp, vp, vp, c64, c64, ci, ci, vp, ci, vp, cf, vp, ci, ci, ci, ci, vp, ctypes.c_size_t, vp]
     L.fq_kv4_attention_prefix_ws.restype = ci
     L.fq_kv4_attention_prefix_ws.argtypes = [vp, vp, vp, c64, c64, ci, ci, vp, ci, vp, ci, vp, cf, vp, ci, ci, ci, ci, vp, ctypes.c_size_t, vp]
+    L.fq_rmsnorm_block.restype = ci
+    L.fq_rmsnorm_block.argtypes = [vp, vp, vp, vp, ci, cf, vp, vp, cf, vp, vp, ci, ci, vp]
+    L.fq_rmsnorm_block_quant_ws.restype = ci
+    L.fq_rmsnorm_block_quant_ws.argtypes = [vp, vp, vp, vp, ci, cf, vp, vp, cf, vp, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
+    L.fq_kv4_append_axes.restype = ci
+    L.fq_kv4_append_axes.argtypes = [vp, c64, vp, ci, vp, ci, vp, vp, ci, vp, vp, vp, c64, c64, ci, ci, ci, ci, ci, vp]
+    L.fq_kv4_attention_chunk_workspace_bytes.restype = ctypes.c_size_t
+    L.fq_kv4_attention_chunk_workspace_bytes.argtypes = [ci, ci, ci, ci, ci, ci]
+    L.fq_kv4_attention_chunk_ws.restype = ci
+    L.fq_kv4_attention_chunk_ws.argtypes = [vp, vp, vp, c64, c64, ci, ci, vp, ci, vp, vp, vp, vp, ci, cf, vp, cf, vp, ci, ci, ci, ci, ci, ci, vp,
+                                            ctypes.c_size_t, vp]
+    L.fq_sample_workspace_bytes.restype = ctypes.c_size_t
+    L.fq_sample_workspace_bytes.argtypes = [ci, ci]
+    for name in ("fq_sample_bf16_ws", "fq_sample_fp32_ws"):
+        getattr(L, name).restype = ci
+        getattr(L, name).argtypes = [vp, c64, vp, vp, vp, vp, vp, vp, vp, ci, ci, vp, ctypes.c_size_t, vp]
     L.fq_w4a8_gemm_ws.restype = ci
     L.fq_w4a8_gemm_ws.argtypes = [vp, vp, vp, vp, cf, vp, ci, ci, ci, vp, ctypes.c_size_t, ci, vp]
     L.fq_w4a8_gemm_add_ws.restype = ci
@@ -196,6 +214,13 @@ def _dev(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
     return t
+
+
+def _here(*tensors) -> None:
+    """All of them on the current device, whose stream the call takes."""
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError("tensors must be on the current device, %d, got %s" % (torch.cuda.current_device(), t.device))
 
 
 def _stream() -> ctypes.c_void_p:
@@ -736,6 +761,77 @@ def fq_rmsnorm_quant(X: torch.Tensor, weight: torch.Tensor, eps: float, residual
     return (A, s) if H is None else (A, s, H)
 
 
+def _block_arguments(where, X, weight, residual, post, gate, gate_rows, scale, out):
+    if residual is None:
+        raise TypeError("residual must be a GPU tensor")
+    X, weight, residual, H = _norm_arguments(X, weight, residual, out)
+    M, K = X.shape
+    if post is not None:
+        post = _dev(post, torch.bfloat16, "post")
+        if post.numel() != K:
+            raise FireqError(-2, where)
+    gates = 1
+    if gate is None:
+        if gate_rows is not None:
+            raise FireqError(-1, where)
+    else:
+        gate = _dev(gate, torch.bfloat16, "gate")
+        if gate.numel() != K and (gate.dim() != 2 or gate.shape[1] != K):
+            raise FireqError(-2, where)
+        gates = gate.shape[0] if gate.dim() == 2 else 1
+        if not _fits(gates):
+            raise FireqError(-2, where)
+        if gate_rows is not None:
+            gate_rows = _dev(gate_rows, torch.int32, "gate_rows")
+            if gate_rows.numel() != M:
+                raise FireqError(-2, where)
+    _here(X, weight, residual, H, post, gate, gate_rows)
+    return X, H, (X.data_ptr(), _ptr(post), _ptr(gate), _ptr(gate_rows), gates, ctypes.c_float(float(scale)), residual.data_ptr(), weight.data_ptr())
+
+
+def fq_rmsnorm_block(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor, post: Optional[torch.Tensor] = None,
+                     gate: Optional[torch.Tensor] = None, gate_rows: Optional[torch.Tensor] = None, scale: float = 1.0,
+                     out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(Y, H) bf16 [M,K] between two blocks with a norm on both sides: H = bf16(residual + scale * gate * p), p the RMS norm of X with the weights
+    `post` (bf16 [K]; None: X itself), and Y the RMS norm of H with `weight`.  gate: bf16 [K] or [1,K] for all rows, [M,K] for each its own, or
+    [gates,K] with gate_rows (int32 [M]) naming each row's.  `out` receives H and may be the residual itself."""
+    r = (_marshal or marshal()).rmsnorm_block(X, weight, eps, residual, post, gate, gate_rows, scale, out)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, "fq_rmsnorm_block")
+        return r
+    X, H, args = _block_arguments("fq_rmsnorm_block", X, weight, residual, post, gate, gate_rows, scale, out)
+    M, K = X.shape
+    Y = torch.empty_like(X)
+    rc = lib().fq_rmsnorm_block(*args, ctypes.c_float(float(eps)), H.data_ptr(), Y.data_ptr(), M, K, _stream())
+    if rc != 0:
+        raise FireqError(rc, "fq_rmsnorm_block")
+    return Y, H
+
+
+def fq_rmsnorm_block_quant(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor, post: Optional[torch.Tensor] = None,
+                           gate: Optional[torch.Tensor] = None, gate_rows: Optional[torch.Tensor] = None, scale: float = 1.0,
+                           out: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """fq_rmsnorm_block with its Y as the operands of the next layer: (uint8 [M,K] E4M3 codes, float32 [M] row scales, H).  `workspace` as in
+    fq_rmsnorm_quant."""
+    r = (_marshal or marshal()).rmsnorm_block_quant(X, weight, eps, residual, post, gate, gate_rows, scale, out, workspace)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, "fq_rmsnorm_block_quant")
+        return r
+    X, H, args = _block_arguments("fq_rmsnorm_block_quant", X, weight, residual, post, gate, gate_rows, scale, out)
+    M, K = X.shape
+    A = torch.empty((M, K), dtype=torch.uint8, device=X.device)
+    s = torch.empty((M,), dtype=torch.float32, device=X.device)
+    ws, nbytes = _scratch(workspace)
+    _here(workspace)
+    rc = lib().fq_rmsnorm_block_quant_ws(*args, ctypes.c_float(float(eps)), H.data_ptr(), A.data_ptr(), s.data_ptr(), M, K, ws, nbytes, _stream())
+    if rc != 0:
+        raise FireqError(rc, "fq_rmsnorm_block_quant")
+    return A, s, H
+
+
 KV4_TILE_TOKENS, KV4_TILE_BYTES = 16, 2080
 
 
@@ -768,6 +864,31 @@ def _cache(cache):
     return (cache.data_ptr(), page_stride, head_stride, pages, tiles * KV4_TILE_TOKENS), heads
 
 
+def _append_arguments(where, QKV, cos_sin, positions, slots, cache, axes):
+    """(T, Hq, Hkv, geometry, row stride) after the checks; positions of `axes` axes (0: one, of any shape)."""
+    if not isinstance(QKV, torch.Tensor) or not QKV.is_cuda:
+        raise TypeError("QKV must be a GPU tensor")
+    if QKV.dtype != torch.bfloat16:
+        raise TypeError("QKV must have dtype %s, got %s" % (torch.bfloat16, QKV.dtype))
+    _dev(cos_sin, torch.float32, "cos_sin")
+    _dev(positions, torch.int32, "positions")
+    _dev(slots, torch.int64, "slots")
+    geometry, Hkv = _cache(cache)
+    if QKV.dim() != 2:
+        raise FireqError(-2, where)
+    T, width = QKV.shape
+    if (width > 1 and QKV.stride(1) != 1) or (T > 1 and QKV.stride(0) < width):
+        raise ValueError("QKV must have contiguous rows")
+    if width % 128 or cos_sin.dim() != 3 or tuple(cos_sin.shape[1:]) != (64, 2):
+        raise FireqError(-2, where)
+    Hq = width // 128 - 2 * Hkv
+    if Hq <= 0 or positions.numel() != T * max(axes, 1) or slots.numel() != T:
+        raise FireqError(-2, where)
+    if not _fits(T, Hq, cos_sin.shape[0]):
+        raise FireqError(-2, where)
+    return T, Hq, Hkv, geometry, QKV.stride(0) if T > 1 else width
+
+
 def fq_kv4_append(QKV: torch.Tensor, cos_sin: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache: torch.Tensor,
                   interleaved: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
     """(uint8 [T,Hq,128] E4M3 codes, float32 [T,Hq] scales) of the rotated queries of the fused projections' output QKV
@@ -778,32 +899,39 @@ def fq_kv4_append(QKV: torch.Tensor, cos_sin: torch.Tensor, positions: torch.Ten
         if type(r) is int:
             raise FireqError(r, "fq_kv4_append")
         return r
-    if not isinstance(QKV, torch.Tensor) or not QKV.is_cuda:
-        raise TypeError("QKV must be a GPU tensor")
-    if QKV.dtype != torch.bfloat16:
-        raise TypeError("QKV must have dtype %s, got %s" % (torch.bfloat16, QKV.dtype))
-    cos_sin = _dev(cos_sin, torch.float32, "cos_sin")
-    positions = _dev(positions, torch.int32, "positions")
-    slots = _dev(slots, torch.int64, "slots")
-    geometry, Hkv = _cache(cache)
-    if QKV.dim() != 2:
-        raise FireqError(-2, "fq_kv4_append")
-    T, width = QKV.shape
-    if (width > 1 and QKV.stride(1) != 1) or (T > 1 and QKV.stride(0) < width):
-        raise ValueError("QKV must have contiguous rows")
-    if width % 128 or cos_sin.dim() != 3 or tuple(cos_sin.shape[1:]) != (64, 2):
-        raise FireqError(-2, "fq_kv4_append")
-    Hq = width // 128 - 2 * Hkv
-    if Hq <= 0 or positions.numel() != T or slots.numel() != T:
-        raise FireqError(-2, "fq_kv4_append")
-    if not _fits(T, Hq, cos_sin.shape[0]):
-        raise FireqError(-2, "fq_kv4_append")
+    T, Hq, Hkv, geometry, ld = _append_arguments("fq_kv4_append", QKV, cos_sin, positions, slots, cache, 0)
     Q = torch.empty((T, Hq, 128), dtype=torch.uint8, device=QKV.device)
     s = torch.empty((T, Hq), dtype=torch.float32, device=QKV.device)
-    rc = lib().fq_kv4_append(QKV.data_ptr(), QKV.stride(0) if T > 1 else width, cos_sin.data_ptr(), cos_sin.shape[0], positions.data_ptr(),
+    rc = lib().fq_kv4_append(QKV.data_ptr(), ld, cos_sin.data_ptr(), cos_sin.shape[0], positions.data_ptr(),
                              slots.data_ptr(), 1 if interleaved else 0, Q.data_ptr(), s.data_ptr(), *geometry, T, Hq, Hkv, _stream())
     if rc != 0:
         raise FireqError(rc, "fq_kv4_append")
+    return Q, s
+
+
+def fq_kv4_append_axes(QKV: torch.Tensor, cos_sin: torch.Tensor, positions: torch.Tensor, axis_of_pair, slots: torch.Tensor,
+                       cache: torch.Tensor, interleaved: bool = False) -> Tuple[torch.Tensor, torch.Tensor]:
+    """fq_kv4_append with positions on several axes (time, height, width): positions int32 [axes, T]; axis_of_pair: 64 whole numbers on the host,
+    the axis that each pair of dimensions turns by, -1 for one that does not turn."""
+    r = (_marshal or marshal()).kv4_append_axes(QKV, cos_sin, positions, axis_of_pair, slots, cache, interleaved)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, "fq_kv4_append_axes")
+        return r
+    if not isinstance(positions, torch.Tensor) or not positions.is_cuda:
+        raise TypeError("positions must be a GPU tensor")
+    pairs = [int(x) for x in axis_of_pair]
+    if positions.dim() != 2 or len(pairs) != 64 or not 1 <= positions.shape[0] <= 127 or not all(-1 <= x < positions.shape[0] for x in pairs):
+        raise FireqError(-2, "fq_kv4_append_axes")
+    axes = positions.shape[0]
+    T, Hq, Hkv, geometry, ld = _append_arguments("fq_kv4_append_axes", QKV, cos_sin, positions, slots, cache, axes)
+    _here(QKV, cos_sin, positions, slots, cache)
+    Q = torch.empty((T, Hq, 128), dtype=torch.uint8, device=QKV.device)
+    s = torch.empty((T, Hq), dtype=torch.float32, device=QKV.device)
+    rc = lib().fq_kv4_append_axes(QKV.data_ptr(), ld, cos_sin.data_ptr(), cos_sin.shape[0], positions.data_ptr(), axes, (ctypes.c_int8 * 64)(*pairs),
+                                  slots.data_ptr(), 1 if interleaved else 0, Q.data_ptr(), s.data_ptr(), *geometry, T, Hq, Hkv, _stream())
+    if rc != 0:
+        raise FireqError(rc, "fq_kv4_append_axes")
     return Q, s
 
 
@@ -903,3 +1031,119 @@ def fq_kv4_attention_prefix(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch
         raise TypeError("prefix_pages must be a GPU tensor")
     return _attention("fq_kv4_attention_prefix", Q, q_scale, cache, prefix_pages, prefix_len, block_table, seq_lens, out_scale, max_len, out,
                       workspace)
+
+
+def fq_kv4_attention_chunk_workspace_bytes(T: int, B: int, Hq: int, Hkv: int, max_new: int, max_len: int) -> int:
+    """Bytes of scratch that the attention of these sizes needs (often 0); 0 for sizes that it refuses, as the C function answers."""
+    sizes = [int(n) for n in (T, B, Hq, Hkv, max_new, max_len)]
+    return int(lib().fq_kv4_attention_chunk_workspace_bytes(*sizes)) if _fits(*sizes) else 0
+
+
+def fq_kv4_attention_chunk(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch.Tensor, block_table: torch.Tensor, starts: torch.Tensor,
+                           seq_lens: torch.Tensor, out_scale: float, max_new: Optional[int] = None, max_len: Optional[int] = None,
+                           first: Optional[torch.Tensor] = None, end: Optional[torch.Tensor] = None, window: int = 0, cap: float = 0.0,
+                           slopes: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """bf16 [T,Hq,128]: attention of the new tokens of several sequences, a whole prompt, a chunk of one or a single token each, over their cached
+    tokens.  Rows starts[b] .. starts[b + 1] - 1 (int32 [B + 1]) of Q belong to sequence b and are the last of its seq_lens[b] (int32 [B]) tokens in
+    the pages block_table[b] (int32 [B, pages of a sequence]).
+
+    A row at place pos attends to first[i] <= t < end[i] (int32 [T]; by default 0 and pos + 1: causal), t > pos - window (0: no window), with the
+    scores cap * tanh(s / cap) (0: s) - slopes[h] * |pos - t| (float32 [Hq]).  Rows without a token are zeros; rows of no sequence are left as
+    `out` had them.
+
+    `max_new`, `max_len`: upper bounds of a sequence's rows and of seq_lens that the host knows, by default T and what the table has room for;
+    `workspace` of fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len) bytes is allocated here when not given."""
+    where = "fq_kv4_attention_chunk"
+    r = (_marshal or marshal()).kv4_attention_chunk(Q, q_scale, cache, block_table, starts, seq_lens, out_scale, max_new, max_len, first, end, window, cap,
+                                                    slopes, out, workspace)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, where)
+        return r
+    Q = _dev(Q, torch.uint8, "Q")
+    q_scale = _dev(q_scale, torch.float32, "q_scale")
+    geometry, Hkv = _cache(cache)
+    block_table = _dev(block_table, torch.int32, "block_table")
+    starts = _dev(starts, torch.int32, "starts")
+    seq_lens = _dev(seq_lens, torch.int32, "seq_lens")
+    if Q.dim() != 3 or Q.shape[2] != 128 or block_table.dim() != 2:
+        raise FireqError(-2, where)
+    T, Hq, _ = Q.shape
+    B, width = block_table.shape
+    if q_scale.numel() != T * Hq or starts.numel() != B + 1 or seq_lens.numel() != B or Hq % Hkv:
+        raise FireqError(-2, where)
+    for name, t, n, dtype in (("first", first, T, torch.int32), ("end", end, T, torch.int32), ("slopes", slopes, Hq, torch.float32)):
+        if t is not None and _dev(t, dtype, name).numel() != n:
+            raise FireqError(-2, where)
+    max_new = T if max_new is None else int(max_new)
+    max_len = min(width * geometry[4], 1 << 30) if max_len is None else int(max_len)
+    window = int(window)
+    if not _fits(T, Hq, B, width, max_new, window) or max_len < 0 or max_len > 1 << 30:
+        raise FireqError(-2, where)
+    if out is None:
+        out = torch.empty((T, Hq, 128), dtype=torch.bfloat16, device=Q.device)
+    else:
+        out = _dev(out, torch.bfloat16, "out")
+        if tuple(out.shape) not in ((T, Hq, 128), (T, Hq * 128)):
+            raise FireqError(-2, where)
+    _here(Q, q_scale, cache, block_table, starts, seq_lens, first, end, slopes, out)
+    if workspace is None:
+        need = fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=Q.device) if need else None
+    ws, nbytes = _scratch(workspace)
+    _here(workspace)
+    rc = lib().fq_kv4_attention_chunk_ws(Q.data_ptr(), q_scale.data_ptr(), *geometry, block_table.data_ptr(), width, starts.data_ptr(),
+                                         seq_lens.data_ptr(), _ptr(first), _ptr(end), window, ctypes.c_float(float(cap)), _ptr(slopes),
+                                         ctypes.c_float(float(out_scale)), out.data_ptr(), T, B, Hq, Hkv, max_new, max_len, ws, nbytes, _stream())
+    if rc != 0:
+        raise FireqError(rc, where)
+    return out
+
+
+def fq_sample_workspace_bytes(B: int, V: int) -> int:
+    """Bytes of scratch that fq_sample needs for B rows of V logits; 0 for sizes that it refuses."""
+    return int(lib().fq_sample_workspace_bytes(int(B), int(V))) if _fits(int(B), int(V)) else 0
+
+
+def fq_sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+              top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+              workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(int32 [B] tokens, float32 [B] log-probabilities) drawn from logits [B,V] (bf16 or float32, rows may be strided) with one uniform number of
+    [0, 1) a row, u float32 [B].  temperature, top_p, min_p float32 [B] and top_k int32 [B] hold a value for each row (None: 1, and no filter; a
+    temperature of 0 takes the best token).  min-p and top-k cut first, top-p what they leave; the log-probability is that of softmax(logits /
+    temperature) before any cut.  A row that cannot be drawn from (NaN, +infinity, no finite logit) gives token -1 and NaN."""
+    r = (_marshal or marshal()).sample(logits, u, temperature, top_k, top_p, min_p, workspace)
+    if r is not None:
+        if type(r) is int:
+            raise FireqError(r, "fq_sample")
+        return r
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise TypeError("logits must be a GPU tensor")
+    if logits.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("logits must have dtype torch.bfloat16 or torch.float32, got %s" % logits.dtype)
+    if logits.dim() != 2:
+        raise FireqError(-2, "fq_sample")
+    B, V = logits.shape
+    if (V > 1 and logits.stride(1) != 1) or (B > 1 and logits.stride(0) < V):
+        raise ValueError("logits must have contiguous rows")
+    for name, t, dtype in (("u", u, torch.float32), ("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                           ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+        if (t is not None or name == "u") and _dev(t, dtype, name).numel() != B:
+            raise FireqError(-2, "fq_sample")
+    if not _fits(B, V):
+        raise FireqError(-2, "fq_sample")
+    _here(logits, u, temperature, top_k, top_p, min_p)
+    token = torch.empty((B,), dtype=torch.int32, device=logits.device)
+    logprob = torch.empty((B,), dtype=torch.float32, device=logits.device)
+    if workspace is None:
+        need = fq_sample_workspace_bytes(B, V)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=logits.device) if need else None
+    ws, nbytes = _scratch(workspace)
+    _here(workspace)
+    call = lib().fq_sample_bf16_ws if logits.dtype == torch.bfloat16 else lib().fq_sample_fp32_ws
+    rc = call(logits.data_ptr(), logits.stride(0) if B > 1 else V, u.data_ptr(), _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+              token.data_ptr(), logprob.data_ptr(), B, V, ws, nbytes, _stream())
+    if rc != 0:
+        raise FireqError(rc, "fq_sample")
+    return token, logprob

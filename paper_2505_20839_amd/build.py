@@ -53,8 +53,8 @@ def marshal_path() -> str:
     import torch
     include = os.path.join(os.path.dirname(os.path.dirname(CSRC)), "include")
     digest = hashlib.sha256()
-    for path in (os.path.join(CSRC, "fq_marshal.cpp"), os.path.join(include, "fireq.h"), os.path.join(include, "fireq_kv4_ws.h"),
-                 os.path.join(include, "fireq_wquant_ws.h"), os.path.join(include, "fireq_norm.h"), os.path.join(include, "fireq_paged.h")):
+    for path in [os.path.join(CSRC, "fq_marshal.cpp")] + [os.path.join(include, "fireq%s.h" % part) for part in (
+            "", "_kv4_ws", "_wquant_ws", "_norm", "_paged", "_norm_block", "_chunk", "_sample")]:
         with open(path, "rb") as f:
             digest.update(f.read())
     digest.update(repr((torch.__version__, sysconfig.get_config_var("EXT_SUFFIX"))).encode())

@@ -1,9 +1,12 @@
 // C entry points of the W4A8-FP library: argument validation, kernel choice, launch.
 // Declarations and the contract of every call are in include/fireq.h.
 #include "../../include/fireq.h"
+#include "../../include/fireq_chunk.h"
 #include "../../include/fireq_kv4_ws.h"
 #include "../../include/fireq_norm.h"
+#include "../../include/fireq_norm_block.h"
 #include "../../include/fireq_paged.h"
+#include "../../include/fireq_sample.h"
 #include "../../include/fireq_wquant_ws.h"
 #include "fq_common.h"
 #include "fq_kernels.h"
@@ -557,6 +560,41 @@ int check_norm(const uint16_t* X, const uint16_t* R, const uint16_t* w, float ep
     return FQ_OK;
 }
 
+// The GEMM's workspace, where a quantising norm is to prepare it: NULL in `planes` where there is nothing to prepare.
+int norm_workspace(int M, int K, void* workspace, size_t workspace_bytes, void*& planes) {
+    planes = nullptr;
+    if (!workspace || choose_kernel(M) != GemmKernel::Large) return FQ_OK;
+    if (!fq_quantize_can_write_zero_point(K)) return FQ_ERR_SHAPE;
+    if (workspace_bytes < fq_gemm_large_workspace_bytes(M, K)) return FQ_ERR_MEMORY;
+    if (!aligned16(workspace)) return FQ_ERR_ALIGN;
+    planes = workspace;
+    return FQ_OK;
+}
+
+// Both forms of the norm between two blocks (Y, or A and a_scale).
+int norm_block(const uint16_t* X, const uint16_t* post, const uint16_t* gate, const int32_t* gate_rows, int gates, float scale, const uint16_t* R,
+               const uint16_t* w, float eps, uint16_t* H, uint16_t* Y, uint8_t* A, float* a_scale, int M, int K, void* workspace, size_t workspace_bytes,
+               void* stream) {
+    const void* out = Y ? static_cast<const void*>(Y) : A;
+    int rc = check_norm(X, R, w, eps, H, out, Y ? 2 : 1, M, K);
+    if (rc != FQ_OK) return rc;
+    if (!(scale >= -3.402823466e38f && scale <= 3.402823466e38f)) return FQ_ERR_SHAPE;
+    if (gate && (gates < 1 || (!gate_rows && gates != 1 && gates != M))) return FQ_ERR_SHAPE;
+    if (M == 0) return FQ_OK;
+    if (!R || (!Y && !a_scale) || (gate_rows && !gate)) return FQ_ERR_NULL;
+    if (!aligned16(post) || !aligned16(gate)) return FQ_ERR_ALIGN;
+    void* planes;
+    rc = norm_workspace(M, K, workspace, workspace_bytes, planes);
+    if (rc != FQ_OK) return rc;
+    const size_t n = (size_t)M * K;
+    const bytes in[] = {{post, post ? (size_t)K * 2 : 0}, {gate, gate ? (size_t)gates * K * 2 : 0}, {gate_rows, gate_rows ? (size_t)M * 4 : 0},
+                        {X, n * 2}, {R, n * 2}, {w, (size_t)K * 2}, {H, n * 2}, {out, n * (Y ? 2 : 1)},
+                        {a_scale, a_scale ? (size_t)M * 4 : 0}, {planes, planes ? fq_gemm_large_workspace_bytes(M, K) : 0}};
+    if (meet(in[6], in, 3) || meet(in[7], in, 3) || meet(in[8], in, 8) || meet(in[9], in, 9)) return FQ_ERR_SHAPE;
+    fq_launch_rmsnorm_block(X, {post, gate, gate_rows, gate ? gates : 1, scale}, R, w, eps, H, Y, A, a_scale, M, K, planes, static_cast<hipStream_t>(stream));
+    return after_launch();
+}
+
 // A paged cache's geometry.
 int check_paged(const uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages, int page, int heads) {
     if (pages < 0 || page <= 0 || page % FQ_KV4_TILE_TOKENS != 0 || heads <= 0 || heads > 65535) return FQ_ERR_SHAPE;
@@ -607,6 +645,88 @@ int attend(const uint8_t* Q_fp8, const float* q_scale, const uint8_t* cache, int
     return after_launch();
 }
 
+// axis_of_pair NULL: one axis for all pairs.
+int append(const uint16_t* QKV_bf16, int64_t ld, const float* cos_sin, int max_positions, const int32_t* positions, int axes, const int8_t* axis_of_pair,
+           const int64_t* slots, int interleaved, uint8_t* Q_fp8, float* q_scale, uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages,
+           int page, int T, int Hq, int Hkv, void* stream) {
+    if (T < 0 || Hq <= 0 || Hq > 65535 || Hkv <= 0 || Hq % Hkv != 0 || max_positions < 0) return FQ_ERR_SHAPE;
+    const int rc = check_paged(cache, page_stride, head_stride, pages, page, Hkv);
+    if (rc != FQ_OK) return rc;
+    const int64_t heads = (int64_t)Hq + 2 * (int64_t)Hkv;
+    if (ld < heads * 128 || ld % 8 != 0 || (int64_t)T * heads > (int64_t)0x0FFFFFF0 || T >= 1 << 23) return FQ_ERR_SHAPE;
+    if (T == 0) return FQ_OK;
+    if (!QKV_bf16 || !positions || !slots || !Q_fp8 || !q_scale || (max_positions > 0 && !cos_sin)) return FQ_ERR_NULL;
+    if (!aligned16(QKV_bf16) || !aligned16(cos_sin) || !aligned16(Q_fp8)) return FQ_ERR_ALIGN;
+    const size_t rows = (size_t)T * Hq;
+    const bytes in[] = {{cos_sin, (size_t)max_positions * 512}, {positions, (size_t)T * 4 * axes}, {slots, (size_t)T * 8}, {Q_fp8, rows * 128}, {q_scale, rows * 4}};
+    const blocks all = paged_blocks(cache, page_stride, head_stride, pages, page, Hkv), tokens = {QKV_bf16, T, ld * 2, 1, 0, heads * 256};
+    if (meet(in[3], in, 3) || meet(in[4], in, 4) || overlap(Q_fp8, rows * 128, tokens) || overlap(q_scale, rows * 4, tokens) ||
+        overlap(QKV_bf16, ((size_t)(T - 1) * ld + heads * 128) * 2, all))
+        return FQ_ERR_SHAPE;
+    for (const bytes& x : in)
+        if (overlap(x.p, x.n, all)) return FQ_ERR_SHAPE;
+    const fq_paged_cache c = {cache, page_stride, head_stride, pages, page};
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (!axis_of_pair) {
+        fq_launch_kv4_append(QKV_bf16, ld, cos_sin, max_positions, positions, slots, interleaved != 0, Q_fp8, q_scale, c, T, Hq, Hkv, st);
+        return after_launch();
+    }
+    fq_pair_axes axis;
+    std::memcpy(axis.of, axis_of_pair, 64);
+    fq_launch_kv4_append_axes(QKV_bf16, ld, cos_sin, max_positions, positions, axis, slots, interleaved != 0, Q_fp8, q_scale, c, T, Hq, Hkv, st);
+    return after_launch();
+}
+
+// The sizes that the attention of new tokens takes.
+bool chunk_sizes(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
+    return T >= 0 && T < 1 << 23 && B >= 0 && B <= 65535 && Hq > 0 && Hq <= 65535 && Hkv > 0 && Hq % Hkv == 0 && (int64_t)T * Hq <= 1 << 25 &&
+           ((int64_t)T * (Hq / Hkv) / 16 + B) * Hkv <= 0x3FFFFFFF && max_new >= 0 && max_len >= 0 && max_len <= 1 << 30;
+}
+
+int attend_chunk(const fq_chunk_args& a, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!chunk_sizes(a.T, a.B, a.Hq, a.Hkv, a.max_new, a.max_len) || a.width < 0 || a.window < 0 || !(a.out_scale > 0.f) || !(a.out_scale <= 3.402823466e38f) ||
+        !(a.cap == 0.f || (a.cap >= 0x1p-60f && a.cap <= 3.402823466e38f)) || (a.cap > 0.f && !(a.out_scale / a.cap <= 3.402823466e38f)))
+        return FQ_ERR_SHAPE;
+    const fq_paged_cache& c = a.c;
+    const int rc = check_paged(c.base, c.page_stride, c.head_stride, c.pages, c.page, a.Hkv);
+    if (rc != FQ_OK) return rc;
+    if (a.T == 0 || a.B == 0) return FQ_OK;
+    if (!a.Q || !a.q_scale || !a.starts || !a.lens || !a.O || (a.width > 0 && !a.table)) return FQ_ERR_NULL;
+    if (!aligned16(a.Q) || !aligned16(a.O)) return FQ_ERR_ALIGN;
+    if (c.pages == 0 && a.width > 0 && a.max_len > 0) return FQ_ERR_SHAPE;   // no page to fall back on
+    const size_t need = fq_chunk_scratch_bytes(a.T, a.B, a.Hq, a.Hkv, a.max_new, a.max_len);
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need) return FQ_ERR_MEMORY;
+        if (!aligned16(workspace)) return FQ_ERR_ALIGN;
+    }
+    const size_t rows = (size_t)a.T * a.Hq;
+    const bytes in[] = {{a.Q, rows * 128}, {a.q_scale, rows * 4}, {a.table, (size_t)a.B * a.width * 4}, {a.starts, (size_t)a.B * 4 + 4}, {a.lens, (size_t)a.B * 4},
+                        {a.first, a.first ? (size_t)a.T * 4 : 0}, {a.end, a.end ? (size_t)a.T * 4 : 0}, {a.slopes, a.slopes ? (size_t)a.Hq * 4 : 0}, {workspace, need}};
+    const blocks all = paged_blocks(c.base, c.page_stride, c.head_stride, c.pages, c.page, a.Hkv);
+    if (meet({a.O, rows * 256}, in, 9) || overlap(a.O, rows * 256, all) || meet({workspace, need}, in, 8) || overlap(workspace, need, all)) return FQ_ERR_SHAPE;
+    fq_launch_chunk(a, workspace, static_cast<hipStream_t>(stream));
+    return after_launch();
+}
+
+int sample(const fq_sample_args& a, void* workspace, size_t workspace_bytes, void* stream) {
+    const size_t size = a.wide ? 4 : 2;
+    if (a.B < 0 || a.B > 65535 || a.V < 1 || a.V > 1 << 20 || a.ld < a.V || a.ld > (int64_t)1 << 40) return FQ_ERR_SHAPE;
+    if (a.B == 0) return FQ_OK;
+    if (!a.logits || !a.u || !a.token) return FQ_ERR_NULL;
+    if (reinterpret_cast<uintptr_t>(a.logits) % size != 0) return FQ_ERR_ALIGN;
+    const size_t need = fq_sample_scratch_bytes(a.B, a.V);
+    if (!workspace || workspace_bytes < need) return FQ_ERR_MEMORY;
+    if (!aligned16(workspace)) return FQ_ERR_ALIGN;
+    const size_t n = (size_t)a.B * 4;
+    const blocks rows = {a.logits, a.B, (int64_t)(a.ld * size), 1, 0, (int64_t)(a.V * size)};
+    const bytes all[] = {{a.u, n}, {a.temperature, a.temperature ? n : 0}, {a.top_k, a.top_k ? n : 0}, {a.top_p, a.top_p ? n : 0}, {a.min_p, a.min_p ? n : 0},
+                         {a.token, n}, {a.logprob, a.logprob ? n : 0}, {workspace, need}};
+    for (int i = 5; i < 8; ++i)
+        if (meet(all[i], all, i) || overlap(all[i].p, all[i].n, rows)) return FQ_ERR_SHAPE;
+    fq_launch_sample(a, workspace, static_cast<hipStream_t>(stream));
+    return after_launch();
+}
+
 }  // namespace
 
 extern "C" {
@@ -625,12 +745,8 @@ int fq_rmsnorm_quant_ws(const uint16_t* X_bf16, const uint16_t* R_bf16, const ui
     if (rc != FQ_OK || M == 0) return rc;
     if (!a_scale) return FQ_ERR_NULL;
     void* planes = nullptr;
-    if (workspace && choose_kernel(M) == GemmKernel::Large) {
-        if (!fq_quantize_can_write_zero_point(K)) return FQ_ERR_SHAPE;
-        if (workspace_bytes < fq_gemm_large_workspace_bytes(M, K)) return FQ_ERR_MEMORY;
-        if (!aligned16(workspace)) return FQ_ERR_ALIGN;
-        planes = workspace;
-    }
+    const int ws = norm_workspace(M, K, workspace, workspace_bytes, planes);
+    if (ws != FQ_OK) return ws;
     const size_t n = (size_t)M * K;
     const bytes in[] = {{X_bf16, n * 2}, {R_bf16, R_bf16 ? n * 2 : 0}, {w_bf16, (size_t)K * 2}, {H_bf16, H_bf16 ? n * 2 : 0}, {A_fp8, n},
                         {planes, planes ? fq_gemm_large_workspace_bytes(M, K) : 0}};
@@ -642,26 +758,19 @@ int fq_rmsnorm_quant_ws(const uint16_t* X_bf16, const uint16_t* R_bf16, const ui
 int fq_kv4_append(const uint16_t* QKV_bf16, int64_t ld, const float* cos_sin, int max_positions, const int32_t* positions,
                   const int64_t* slots, int interleaved, uint8_t* Q_fp8, float* q_scale, uint8_t* cache, int64_t page_stride,
                   int64_t head_stride, int pages, int page, int T, int Hq, int Hkv, void* stream) {
-    if (T < 0 || Hq <= 0 || Hq > 65535 || Hkv <= 0 || Hq % Hkv != 0 || max_positions < 0) return FQ_ERR_SHAPE;
-    const int rc = check_paged(cache, page_stride, head_stride, pages, page, Hkv);
-    if (rc != FQ_OK) return rc;
-    const int64_t heads = (int64_t)Hq + 2 * (int64_t)Hkv;
-    if (ld < heads * 128 || ld % 8 != 0 || (int64_t)T * heads > (int64_t)0x0FFFFFF0 || T >= 1 << 23) return FQ_ERR_SHAPE;
-    if (T == 0) return FQ_OK;
-    if (!QKV_bf16 || !positions || !slots || !Q_fp8 || !q_scale || (max_positions > 0 && !cos_sin)) return FQ_ERR_NULL;
-    if (!aligned16(QKV_bf16) || !aligned16(cos_sin) || !aligned16(Q_fp8)) return FQ_ERR_ALIGN;
-    const size_t rows = (size_t)T * Hq;
-    const bytes in[] = {{cos_sin, (size_t)max_positions * 512}, {positions, (size_t)T * 4}, {slots, (size_t)T * 8}, {Q_fp8, rows * 128}, {q_scale, rows * 4}};
-    const blocks all = paged_blocks(cache, page_stride, head_stride, pages, page, Hkv), tokens = {QKV_bf16, T, ld * 2, 1, 0, heads * 256};
-    if (meet(in[3], in, 3) || meet(in[4], in, 4) || overlap(Q_fp8, rows * 128, tokens) || overlap(q_scale, rows * 4, tokens) ||
-        overlap(QKV_bf16, ((size_t)(T - 1) * ld + heads * 128) * 2, all))
-        return FQ_ERR_SHAPE;
-    for (const bytes& x : in)
-        if (overlap(x.p, x.n, all)) return FQ_ERR_SHAPE;
-    const fq_paged_cache c = {cache, page_stride, head_stride, pages, page};
-    fq_launch_kv4_append(QKV_bf16, ld, cos_sin, max_positions, positions, slots, interleaved != 0, Q_fp8, q_scale, c, T, Hq, Hkv,
-                         static_cast<hipStream_t>(stream));
-    return after_launch();
+    return append(QKV_bf16, ld, cos_sin, max_positions, positions, 1, nullptr, slots, interleaved, Q_fp8, q_scale, cache, page_stride, head_stride, pages,
+                  page, T, Hq, Hkv, stream);
+}
+
+int fq_kv4_append_axes(const uint16_t* QKV_bf16, int64_t ld, const float* cos_sin, int max_positions, const int32_t* positions, int axes,
+                       const int8_t* axis_of_pair, const int64_t* slots, int interleaved, uint8_t* Q_fp8, float* q_scale, uint8_t* cache,
+                       int64_t page_stride, int64_t head_stride, int pages, int page, int T, int Hq, int Hkv, void* stream) {
+    if (axes < 1 || axes > 127) return FQ_ERR_SHAPE;
+    if (!axis_of_pair) return T == 0 ? FQ_OK : FQ_ERR_NULL;
+    for (int j = 0; j < 64; ++j)
+        if (axis_of_pair[j] < -1 || axis_of_pair[j] >= axes) return FQ_ERR_SHAPE;
+    return append(QKV_bf16, ld, cos_sin, max_positions, positions, axes, axis_of_pair, slots, interleaved, Q_fp8, q_scale, cache, page_stride,
+                  head_stride, pages, page, T, Hq, Hkv, stream);
 }
 
 int fq_kv4_read(const uint8_t* cache, int64_t page_stride, int64_t head_stride, int pages, int page, const int64_t* slots,
@@ -701,6 +810,49 @@ int fq_kv4_attention_prefix_ws(const uint8_t* Q_fp8, const float* q_scale, const
                                void* stream) {
     return attend(Q_fp8, q_scale, cache, page_stride, head_stride, pages, page, prefix_pages, prefix_len, block_table, table_width, seq_lens,
                   out_scale, O_bf16, B, Hq, Hkv, max_len, workspace, workspace_bytes, stream);
+}
+
+int fq_rmsnorm_block(const uint16_t* X_bf16, const uint16_t* post_bf16, const uint16_t* gate_bf16, const int32_t* gate_rows, int gates,
+                     float scale, const uint16_t* R_bf16, const uint16_t* w_bf16, float eps, uint16_t* H_bf16, uint16_t* Y_bf16, int M, int K,
+                     void* stream) {
+    if (M > 0 && !Y_bf16) return FQ_ERR_NULL;
+    return norm_block(X_bf16, post_bf16, gate_bf16, gate_rows, gates, scale, R_bf16, w_bf16, eps, H_bf16, Y_bf16, nullptr, nullptr, M, K, nullptr, 0,
+                      stream);
+}
+
+int fq_rmsnorm_block_quant_ws(const uint16_t* X_bf16, const uint16_t* post_bf16, const uint16_t* gate_bf16, const int32_t* gate_rows,
+                              int gates, float scale, const uint16_t* R_bf16, const uint16_t* w_bf16, float eps, uint16_t* H_bf16,
+                              uint8_t* A_fp8, float* a_scale, int M, int K, void* workspace, size_t workspace_bytes, void* stream) {
+    return norm_block(X_bf16, post_bf16, gate_bf16, gate_rows, gates, scale, R_bf16, w_bf16, eps, H_bf16, nullptr, A_fp8, a_scale, M, K, workspace,
+                      workspace_bytes, stream);
+}
+
+size_t fq_kv4_attention_chunk_workspace_bytes(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
+    if (T <= 0 || B <= 0 || !chunk_sizes(T, B, Hq, Hkv, max_new, max_len)) return 0;
+    return fq_chunk_scratch_bytes(T, B, Hq, Hkv, max_new, max_len);
+}
+
+int fq_kv4_attention_chunk_ws(const uint8_t* Q_fp8, const float* q_scale, const uint8_t* cache, int64_t page_stride, int64_t head_stride,
+                              int pages, int page, const int32_t* block_table, int table_width, const int32_t* starts,
+                              const int32_t* seq_lens, const int32_t* first, const int32_t* end, int window, float cap, const float* slopes,
+                              float out_scale, uint16_t* O_bf16, int T, int B, int Hq, int Hkv, int max_new, int max_len, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+    return attend_chunk({Q_fp8, q_scale, {const_cast<uint8_t*>(cache), page_stride, head_stride, pages, page}, block_table, starts, seq_lens, first, end,
+                         slopes, table_width, window, T, B, Hq, Hkv, max_new, max_len, out_scale, cap, O_bf16},
+                        workspace, workspace_bytes, stream);
+}
+
+size_t fq_sample_workspace_bytes(int B, int V) { return B > 0 && B <= 65535 && V > 0 && V <= 1 << 20 ? fq_sample_scratch_bytes(B, V) : 0; }
+
+int fq_sample_bf16_ws(const uint16_t* logits, int64_t ld, const float* u, const float* temperature, const int32_t* top_k,
+                      const float* top_p, const float* min_p, int32_t* token, float* logprob, int B, int V, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+    return sample({logits, false, ld, u, temperature, top_p, min_p, top_k, token, logprob, B, V}, workspace, workspace_bytes, stream);
+}
+
+int fq_sample_fp32_ws(const float* logits, int64_t ld, const float* u, const float* temperature, const int32_t* top_k, const float* top_p,
+                      const float* min_p, int32_t* token, float* logprob, int B, int V, void* workspace, size_t workspace_bytes, void* stream) {
+    return sample({logits, true, ld, u, temperature, top_p, min_p, top_k, token, logprob, B, V}, workspace, workspace_bytes, stream);
 }
 
 size_t fq_w4a8_gemm_static_max_workspace(void) { return FQ_STATIC_SCRATCH_BYTES; }

@@ -15,39 +15,9 @@
 //     sum p         one more such product, against ones: the sum of the same rounded numbers.
 // O stays in registers.  A query's maximum moves only when a score passes it by more than FQA_SLACK powers of two, which fp16 has room
 // for: the lanes of a query compare their own scores with it, and only then with each other.
-#include "fq_common.h"
-#include "fq_kernels.h"
+#include "fq_attend.h"
 
 namespace {
-
-typedef _Float16 fqa_v8h __attribute__((ext_vector_type(8)));
-typedef _Float16 fqa_v2h __attribute__((ext_vector_type(2)));
-
-#define FQA_LIFT 7.0f                                     // log2 of the factor on the probabilities: down to 2^-31 above fp16's smallest
-#define FQA_SLACK 6.0f                                    // ... and 2^(7 + 6) is the largest
-
-#define FQA_MFMA_QK(a, b, c) __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4((a), (b), (c), 0, 0, 0, 0, 0, 0)
-
-__device__ __forceinline__ float fqa_over_groups_max(float v) {   // over the four lanes of a query
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
-}
-// The lane's values for channel j of 16 (word j / 2 of each of two tiles) as eight fp16 numbers sigma * (code - 8): a word holds, for j
-// even and odd, nibbles 0 / 1 (tokens 0, 1 of four) and 2 / 3 (tokens 2, 3) of both halves.  `mask` and `base` are 0x03C003C0 and
-// 0x4C004C00 held in registers, for one and-or instead of an and and an or with a literal each.
-struct fqa_sigmas { fqa_v2h s[2], n[2]; };                // sigma and -24 sigma of tokens 0, 1 and 2, 3
-__device__ __forceinline__ fqa_v2h fqa_value_pair(unsigned w, unsigned mask, unsigned base, fqa_v2h s, fqa_v2h n) {
-    return __builtin_elementwise_fma(__builtin_bit_cast(fqa_v2h, (w & mask) | base), s, n);
-}
-template <int ODD>
-__device__ __forceinline__ fqa_v8h fqa_values(int w0, int w1, unsigned mask, unsigned base, const fqa_sigmas& a, const fqa_sigmas& b) {
-    const unsigned x = (unsigned)w0, y = (unsigned)w1;
-    const fqa_v2h r0 = fqa_value_pair(ODD ? x << 2 : x << 6, mask, base, a.s[0], a.n[0]), r1 = fqa_value_pair(ODD ? x >> 6 : x >> 2, mask, base, a.s[1], a.n[1]);
-    const fqa_v2h r2 = fqa_value_pair(ODD ? y << 2 : y << 6, mask, base, b.s[0], b.n[0]), r3 = fqa_value_pair(ODD ? y >> 6 : y >> 2, mask, base, b.s[1], b.n[1]);
-    return (fqa_v8h){r0[0], r0[1], r1[0], r1[1], r2[0], r2[1], r3[0], r3[1]};
-}
-
-struct fqa_tile { fq_v4i k, v; fq_v2i s; };
 
 // The tiles of a range one after the other: page numbers 64 at a time in a register, the tile within its page counted along.
 struct fqa_cursor {
@@ -96,35 +66,6 @@ struct fqa_cursor {
         }
     }
 };
-
-#define FQA_LOWEST (-3.0e38f)                             // below every score, and finite: times a scale of 0 it is 0
-
-// A query tile's state.  Scores are kept before the query's factor: s = sum q k * sigma_k, probability 2^(qs * (s - m)).
-template <int RT>
-struct fqa_state {
-    float m[RT], sub[RT];                                 // the reference score (within the slack of the largest so far), LIFT - qs * m
-    fq_v4f o[RT][8], l[RT];                               // O^T; sum p, the same in all four
-};
-
-template <int RT>
-struct fqa_queries {
-    fq_v8i q[RT];                                         // codes, as the B operand
-    fq_v4f zp[RT];                                        // -2^-6 sum of the codes
-    float qs[RT];                                         // factor of a score in log2, not negative
-};
-
-// One query (16 lanes of a query tile: 32 bytes each): a negative factor turns the codes' signs instead.
-template <int RT>
-__device__ __forceinline__ void fqa_take_query(fqa_queries<RT>& Q, int r, const uint8_t* codes, float scale, float out_scale, int g) {
-    const fq_v4i* p = reinterpret_cast<const fq_v4i*>(codes + 32 * g);
-    const fq_v4i a = p[0], b = p[1];
-    const int flip = scale < 0.f ? (int)0x80808080 : 0;
-    Q.q[r] = (fq_v8i){a[0] ^ flip, a[1] ^ flip, a[2] ^ flip, a[3] ^ flip, b[0] ^ flip, b[1] ^ flip, b[2] ^ flip, b[3] ^ flip};
-    Q.qs[r] = fabsf(scale) * out_scale * (512.0f * 1.44269504088896340736f);
-    constexpr int E = (int)FQ_ZP_BYTES;
-    const fq_v8i eights = {E, E, E, E, E, E, E, E};
-    Q.zp[r] = FQA_MFMA_QK(eights, Q.q[r], ((fq_v4f){0.f, 0.f, 0.f, 0.f}));
-}
 
 // NT (even) tiles from tile tb on.  TAIL: tokens from `len` on are masked.
 template <int RT, int NT, bool TAIL>
@@ -246,61 +187,9 @@ __device__ __forceinline__ void fqa_range(fqa_cursor& cur, int t0, int t1, int l
     }
 }
 
-// Parts of a row (query head of a sequence), one behind the other: 128 sums and, apart from them, (maximum, sum).
-struct fqa_parts {
-    float* o;                                             // [B * Hq][slots][128]
-    float* ml;                                            // [B * Hq][slots][2]
-    int slots;
-};
-
-// Parts first, first + STEP, .. of n of a row added to (m, l, o), four requested at a time (po: at the lane's four channels).
-template <int STEP>
-__device__ __forceinline__ void fqa_add_parts(const fq_v2f* ml, const fq_v4f* po, int first, int n, float& m, float& l, fq_v4f& o) {
-    for (int s0 = first; s0 < n; s0 += 4 * STEP) {
-        fq_v2f pm[4];
-        fq_v4f x[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int s = s0 + STEP * u < n ? s0 + STEP * u : s0;
-            pm[u] = ml[s];
-            x[u] = po[(size_t)s * 32];
-        }
-        float top = m;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (s0 + STEP * u >= n) pm[u][1] = 0.f;
-            if (pm[u][1] != 0.f) top = fmaxf(top, pm[u][0]);   // (an empty part has no sums)
-        }
-        const float f = __builtin_amdgcn_exp2f(m - top);
-        l *= f;
-        o *= f;
-        m = top;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (pm[u][1] == 0.f) continue;
-            const float fu = __builtin_amdgcn_exp2f(pm[u][0] - top);
-            l += pm[u][1] * fu;
-            o += x[u] * fu;
-        }
-    }
-}
-
-// o / l as four bf16 (a row without tokens: zeros).
-__device__ __forceinline__ uint2 fqa_output(fq_v4f o, float l) {
-    o *= l == 0.f ? 0.f : 1.0f / l;
-    uint2 out;
-    out.x = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[0], o[1]}, fq_v2bf));
-    out.y = __builtin_bit_cast(unsigned, __builtin_convertvector((fq_v2f){o[2], o[3]}, fq_v2bf));
-    return out;
-}
-
 // A workgroup's work: tiles c0 .. c1 of one key/value head for `rows` (up to 16 RT) query rows, numbered by row_of(0 .. rows - 1).  Its waves
 // share the tiles out and join their sums through LDS; the result is a part of each row, or (finish) its output, with the `earlier` parts that a
 // kernel before has left added.
-template <int RT, int WAVES>
-struct __attribute__((aligned(16))) fqa_shared {
-    float o[WAVES][16 * RT][132], m[WAVES][16 * RT], l[WAVES][16 * RT];
-};
 template <int RT, int WAVES, int NT, int AHEAD, class F>
 __device__ __forceinline__ void fqa_group(const fq_attend_args& a, const fqa_parts& parts, fqa_shared<RT, WAVES>& sh, int c0, int c1, int len,
                                           const int* pages_of, bool bad, int kv, int rows, F row_of, int slot, bool finish, int earlier) {
@@ -422,56 +311,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void fqa_prefix_kernel(fq_attend_arg
                                     [&](int i) { return (size_t)((first + i) / G) * a.Hq + kv * G + (first + i) % G; }, slot, false, 0);
 }
 
-// The parts' sums, each brought to the largest maximum.  32 lanes hold the 128 channels of a row; GROUPS of 32 lanes share its parts, four
-// requested at a time.  A wave per row for up to 8 parts (no LDS, no barrier; 96 sequences behind a prefix, 32 query heads, 6 parts, the whole
-// call 46.8 us, 50.1 with a workgroup each; 1 x 1000 tokens 6.9 and 7.3), a workgroup for more (12 parts 7.9 us, 8.3 with a wave; 32 parts
-// 12.4 and 14.0).
-template <int GROUPS>
-__global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t* __restrict__ O, int rows) {
-    constexpr int ROWS = 8 / GROUPS;                      // of a workgroup
-    __shared__ float wm[GROUPS], wl[GROUPS];
-    __shared__ fq_v4f wo[GROUPS][32];
-    const int c = threadIdx.x & 31, grp = (int)(threadIdx.x >> 5) % GROUPS, row = (int)blockIdx.x * ROWS + (int)(threadIdx.x >> 5) / GROUPS, n = parts.slots;
-    if (row >= rows) return;                              // (one row a workgroup where there is a barrier)
-    const fq_v2f* ml = reinterpret_cast<const fq_v2f*>(parts.ml) + (size_t)row * n;
-    const fq_v4f* po = reinterpret_cast<const fq_v4f*>(parts.o) + (size_t)row * n * 32 + c;
-    float m = FQA_LOWEST, l = 0.f;
-    fq_v4f o = {0.f, 0.f, 0.f, 0.f};
-    fqa_add_parts<GROUPS>(ml, po, grp, n, m, l, o);
-    if (GROUPS == 2) {                                    // the other half of the wave
-        const float top = fmaxf(m, __shfl_xor(m, 32, 64)), f = __builtin_amdgcn_exp2f(m - top);
-        l *= f;
-        l += __shfl_xor(l, 32, 64);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            o[i] *= f;
-            o[i] += __shfl_xor(o[i], 32, 64);
-        }
-        if (grp) return;
-    } else {
-        if (c == 0) {
-            wm[grp] = m;
-            wl[grp] = l;
-        }
-        wo[grp][c] = o;
-        __syncthreads();
-        if (grp) return;
-#pragma unroll
-        for (int i = 1; i < GROUPS; ++i) m = fmaxf(m, wm[i]);
-        l = 0.f;
-        o = (fq_v4f){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < GROUPS; ++i) {
-            const float f = __builtin_amdgcn_exp2f(wm[i] - m);
-            l += wl[i] * f;
-            o += wo[i][c] * f;
-        }
-    }
-    reinterpret_cast<uint2*>(O)[(size_t)row * 32 + c] = fqa_output(o, l);
-}
-
 constexpr int FQA_OWN_WAVES = 4, FQA_OWN_NT = 2, FQA_OWN_AHEAD = 1, FQA_PREFIX_RT = 2, FQA_PREFIX_WAVES = 4, FQA_PREFIX_NT = 2, FQA_PREFIX_AHEAD = 1;
-constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 24000, FQA_APART_FEW = 48000, FQA_JOIN_FEW = 8, FQA_FINISH = 16;
+constexpr int FQA_PREFIX_WANT = 2, FQA_PREFIX_MIN = 16, FQA_APART = 24000, FQA_APART_FEW = 48000, FQA_FINISH = 16;
 
 // own_chunk and own_slots: tiles of a part of a sequence, and parts of the longest; the same for the prefix, which is worked on for
 // row_groups groups of rows together, or (row_groups 0) for each sequence apart, like its own tokens.  finish: the kernel of a sequence's own
@@ -570,7 +411,6 @@ void fq_launch_attend(const fq_attend_args& a, void* scratch, hipStream_t stream
                        p.finish() ? p.prefix_slots : 0);
     if (!p.finish()) {
         const int rows = a.B * a.Hq;
-        if (slots <= FQA_JOIN_FEW) hipLaunchKernelGGL(fqa_join_kernel<2>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, parts, a.O, rows);
-        else hipLaunchKernelGGL(fqa_join_kernel<8>, dim3((unsigned)rows), dim3(256), 0, stream, parts, a.O, rows);
+        fqa_join(parts, a.O, rows, stream);
     }
 }

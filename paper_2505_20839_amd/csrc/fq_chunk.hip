@@ -1,0 +1,460 @@
+// Attention of new tokens, one or many of each sequence, over the paged INT4 cache (include/fireq_chunk.h): prompts, chunks of prompts and
+// single tokens, with a range of tokens for each row, a window, scores capped by a tanh and a bias by distance.
+//
+// Rows are (token, query head) pairs of a key/value head, a token's heads one behind the other; 16 RT of them are a wave's query tile, and
+// the products are those of fq_attend.hip (S^T = K Q^T in FP8, O^T = V^T P^T in fp16, sums in FP32).  What differs:
+//     ranges     a row's tokens are lo <= t < hi.  A wave takes the tiles that any of its rows has; where all of its rows have all of a step's
+//                tokens, no score is compared with a range.
+//     shape      x = cap tanh(out_scale q k / cap) - slope |pos - t|, in units of log2 e.  tanh(y) = y + y^3 P(y^2), five terms for |y| <= 5/8
+//                (relative error 2^-23), 1 - 2 / (1 + exp(2 y)) above.  A distance is counted from the row's nearest token: a constant less for
+//                all scores of a row, and exact in FP32 where it counts.
+//     broken     a value whose scale is NaN must not reach the rows that do not see its token (0 * NaN): its NaN moves to the key's scale,
+//                which makes the probabilities NaN of those rows only that see it; so does a tile of a page outside the cache.
+#include "fq_attend.h"
+
+namespace {
+
+// log2 e * cap * the coefficients of tanh(y) / y in y^2 (least squares in relative error on |y| <= 5/8)
+#define FQC_SMALL 0.625f
+struct fqc_shape {
+    float k[5];                                           // polynomial
+    float k1, k2;                                         // log2 e * cap and twice that
+};
+
+struct fqc_args {
+    const uint8_t* Q;
+    const float* q_scale;
+    fq_paged_cache c;
+    const int32_t *table, *starts, *lens, *first, *end;
+    const float* slopes;
+    int width, window, T, B, Hq, Hkv, max_len, slots;
+    float out_scale, inv_cap;                             // inv_cap: 1 / cap (0: uncapped)
+    fqc_shape shape;
+    uint16_t* O;
+};
+
+// The tiles of a range one after the other, as in fq_attend.hip; a tile of a page outside the cache has NaN scales.
+struct fqc_cursor {
+    const int* pages_of;
+    const uint8_t* head;
+    unsigned page_stride;                                 // in 16 bytes
+    int last, tile, page, within, tiles_per_page, first, pages;
+    int ids;                                              // lane l: page number first + l
+    __device__ __forceinline__ void fetch(int lane) {
+        const int last_page = last / tiles_per_page;
+        const int p = first + lane < last_page ? first + lane : last_page;
+        const int id = pages_of[p];
+        ids = (unsigned)id < (unsigned)pages ? id : -1;
+    }
+    __device__ __forceinline__ void start(int t0, int t1, int lane) {
+        tile = t0;
+        last = t1 - 1;
+        page = first = t0 / tiles_per_page;
+        within = t0 - page * tiles_per_page;
+        fetch(lane);
+    }
+    template <int NT>
+    __device__ __forceinline__ void next(fqa_tile (&t)[NT], int lane) {
+        if (page - first > 64 - NT) {
+            first = page;
+            fetch(lane);
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const int id = __builtin_amdgcn_readlane(ids, page - first), lost = id < 0 ? 0x7F7F7F7F : 0;
+            const uint8_t* p = head + (((unsigned long long)(unsigned)(id < 0 ? 0 : id) * page_stride) << 4) + (unsigned)(within * FQP_TILE);
+            t[i].k = *reinterpret_cast<const fq_v4i*>(p + 16 * lane);
+            t[i].v = *reinterpret_cast<const fq_v4i*>(p + 1024 + 16 * lane);
+            t[i].s = *reinterpret_cast<const fq_v2i*>(p + 2048 + 8 * (lane >> 4)) | lost;
+            const int on = tile < last ? 1 : 0;
+            tile += on;
+            within += on;
+            const int over = within == tiles_per_page ? 1 : 0;
+            page += over;
+            within = over ? 0 : within;
+        }
+    }
+};
+
+// A wave's rows: lane n (and n + 16, ..) has row 16 r + n of each query tile r.
+template <int RT>
+struct fqc_rows {
+    int lo[RT], hi[RT];                                   // its tokens
+    int pos[RT], near[RT];                                // its own place, and the distance of its nearest token
+    float slope[RT];                                      // -log2 e * slope
+};
+
+// A NaN in a value's scale moves to the key's (four of each: s[0] keys, s[1] values).
+__device__ __forceinline__ void fqc_move_nans(fq_v2i& s) {
+    const unsigned bad = (((unsigned)s[1] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u, bytes = (bad >> 7) * 0xFFu;
+    s[0] = (int)((unsigned)s[0] | (bytes & 0x7F7F7F7Fu));
+    s[1] = (int)((unsigned)s[1] & ~bytes);
+}
+
+// NT (even) tiles from tile tb on.  whole: every row has all of their tokens; otherwise the others' scores become -infinity, whose probability
+// is 0 beside any finite reference (a row's before its first token too, and its factor is not 0).
+template <int RT, int NT, bool CAP, bool BIAS>
+__device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], int tb, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows, const fqc_shape& shape,
+                                         fqa_state<RT>& st, bool whole, unsigned mask, unsigned base, int g) {
+    unsigned odd = 0u;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) odd |= ((unsigned)now[i].s[1] & 0x7F7F7F7Fu) + 0x01010101u;
+    if (__any((odd & 0x80808080u) != 0u))
+#pragma unroll
+        for (int i = 0; i < NT; ++i) fqc_move_nans(now[i].s);
+    fq_v8i k[NT];
+    float ks[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        k[i] = fq_unpack_chunk(now[i].k);
+        const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[0], false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[0], true);
+        ks[i][0] = s01[0]; ks[i][1] = s01[1]; ks[i][2] = s23[0]; ks[i][3] = s23[1];
+    }
+    fq_v4i pt[RT][NT / 2];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        // scores: before the row's factor f = qs, or, with a shape, whole
+        float s[NT][4], top = FQA_LOWEST;
+        const float f = CAP || BIAS ? 1.0f : Q.qs[r];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            const fq_v4f c = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[i][e] = CAP || BIAS ? c[e] * ks[i][e] * Q.qs[r] : c[e] * ks[i][e];
+        }
+        if (CAP) {
+            bool small = true;
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) small = small && fabsf(s[i][e]) <= FQC_SMALL;
+            const bool all = __all(small);
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float y = s[i][e], u = y * y;
+                    float z = y * fmaf(fmaf(fmaf(fmaf(shape.k[4], u, shape.k[3]), u, shape.k[2]), u, shape.k[1]), u, shape.k[0]);
+                    if (!all) {
+                        const float far = fmaf(-shape.k2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * 1.44269504088896340736f)) + 1.0f), shape.k1);
+                        z = fabsf(y) <= FQC_SMALL ? z : far;
+                    }
+                    s[i][e] = z;
+                }
+        }
+        if (BIAS) {
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int d = rows.pos[r] - ((tb + i) * 16 + 4 * g + e), away = (d < 0 ? -d : d) - rows.near[r];
+                    s[i][e] = fmaf(rows.slope[r], (float)away, s[i][e]);
+                }
+        }
+        if (!whole) {
+            const int at = tb * 16 + 4 * g - rows.lo[r], n = rows.hi[r] - rows.lo[r];
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[i][e] = (unsigned)(at + 16 * i + e) < (unsigned)n ? s[i][e] : -__builtin_inff();
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
+        if (__any((top - st.m[r]) * f > FQA_SLACK)) {
+            const float m = fmaxf(st.m[r], fqa_over_groups_max(top)), x = __builtin_amdgcn_exp2f((st.m[r] - m) * f);
+            st.m[r] = m;
+            st.sub[r] = fmaf(m, -f, FQA_LIFT);
+            st.l[r] *= x;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) st.o[r][j] *= x;
+        }
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                float p[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) p[u] = __builtin_amdgcn_exp2f(fmaf(s[i][e + u], f, st.sub[r]));
+                pt[r][i / 2][2 * (i & 1) + e / 2] = __builtin_bit_cast(int, __builtin_convertvector((fq_v2f){p[0], p[1]}, fqa_v2h));
+            }
+    }
+    constexpr int ONE = 0x3C003C00;
+    const fq_v4i ones = {ONE, ONE, ONE, ONE};
+#pragma unroll
+    for (int i = 0; i < NT / 2; ++i) {
+        fqa_sigmas sg[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int w = now[2 * i + u].s[1];
+            sg[u].s[0] = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, false), fqa_v2h);
+            sg[u].s[1] = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, true), fqa_v2h);
+            sg[u].n[0] = sg[u].s[0] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
+            sg[u].n[1] = sg[u].s[1] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+            st.l[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fqa_v8h, ones), __builtin_bit_cast(fqa_v8h, pt[r][i]), st.l[r], 0, 0, 0);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const fqa_v8h even = fqa_values<0>(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1]);
+            const fqa_v8h odds = fqa_values<1>(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                st.o[r][2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, __builtin_bit_cast(fqa_v8h, pt[r][i]), st.o[r][2 * w], 0, 0, 0);
+                st.o[r][2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odds, __builtin_bit_cast(fqa_v8h, pt[r][i]), st.o[r][2 * w + 1], 0, 0, 0);
+            }
+        }
+    }
+}
+
+// Tiles t0 .. t1 for a wave's rows; from token `whole0` to `whole1` all rows have all tokens.
+template <int RT, int NT, bool CAP, bool BIAS>
+__device__ __forceinline__ void fqc_range(fqc_cursor& cur, int t0, int t1, int whole0, int whole1, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows,
+                                          const fqc_shape& shape, fqa_state<RT>& st, int lane) {
+    const int g = lane >> 4;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        // below every score (sums of 128 products of FP8 numbers and codes, at most 10^9; with a shape, FP32's own range)
+        st.m[r] = CAP || BIAS ? FQA_LOWEST : -1.0e30f;
+        st.sub[r] = CAP || BIAS ? -FQA_LOWEST : fminf(1.0e30f * Q.qs[r], -FQA_LOWEST);
+        st.l[r] = (fq_v4f){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) st.o[r][j] = (fq_v4f){0.f, 0.f, 0.f, 0.f};
+    }
+    unsigned mask = 0x03C003C0u, base = 0x4C004C00u;
+    asm("" : "+s"(mask));
+    asm("" : "+v"(base));
+    auto step = [&](fqa_tile (&now)[NT], int tb) __attribute__((always_inline)) {
+        // (a step past t1 repeats the last tile behind its end: its tokens are masked there, for `whole1` is at most 16 t1)
+        fqc_step<RT, NT, CAP, BIAS>(now, tb, Q, rows, shape, st, tb * 16 >= whole0 && (tb + NT) * 16 <= whole1, mask, base, g);
+    };
+    fqa_tile a[NT], b[NT];
+    cur.next(a, lane);
+    for (int tb = t0; tb < t1; tb += 2 * NT) {
+        if (tb + NT < t1) cur.next(b, lane);
+        step(a, tb);
+        if (tb + NT >= t1) break;
+        if (tb + 2 * NT < t1) cur.next(a, lane);
+        step(b, tb + NT);
+    }
+    if (!(CAP || BIAS))
+#pragma unroll
+        for (int r = 0; r < RT; ++r) st.m[r] *= Q.qs[r];
+}
+
+__device__ __forceinline__ int fqc_row16_min(int v) {
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) {
+        const int o = __shfl_xor(v, d, 64);
+        v = o < v ? o : v;
+    }
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
+__device__ __forceinline__ int fqc_clamp(int v, int hi) { return v < 0 ? 0 : v > hi ? hi : v; }
+
+// Query tiles of `rows` rows: those of sequence b are numbered from starts[b] * G / rows + b on, which leaves each sequence room for what it can
+// need without anyone knowing their lengths.  The sequence of tile k (or -1), 64 candidates at a time.
+__device__ __forceinline__ int fqc_sequence_of(const fqc_args& a, int k, int G, int rows, int lane, int& tile0) {
+    int lo = 0, n = a.B;
+    while (true) {
+        const int stride = (n + 63) >> 6, i = lo + lane * stride;
+        const bool in = i < lo + n;
+        const int at = in ? (int)((long long)fqc_clamp(a.starts[i], a.T) * G / rows) + i : 0;
+        const unsigned long long below = __ballot(in && at <= k);
+        if (below == 0ull) return -1;
+        const int count = __popcll(below) - 1;
+        lo += count * stride;
+        tile0 = __builtin_amdgcn_readlane(at, count);
+        if (stride == 1) return lo;
+        n = n - count * stride < stride ? n - count * stride : stride;
+    }
+}
+
+// A workgroup: one query tile of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among KVW waves
+// (one: the wave writes its rows straight out; more: they meet in LDS).
+template <int RT, int KVW, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * KVW, KVW == 1 ? 1 : RT == 1 ? 4 : RT == 2 ? 2 : 1) void fqc_kernel(fqc_args a, fqa_parts parts) {
+    constexpr int ROWS = 16 * RT, NT = 2;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int G = a.Hq / a.Hkv, tiles = (int)((long long)a.T * G / ROWS) + a.B;
+    const int kv = (int)(blockIdx.x % a.Hkv), k = tiles - 1 - (int)(blockIdx.x / a.Hkv);   // (later rows of a prompt have more tokens: they begin)
+    int tile0 = 0;
+    const int b = fqc_sequence_of(a, k, G, ROWS, lane, tile0);
+    if (b < 0) return;
+    const int start = fqc_clamp(a.starts[b], a.T), stop = fqc_clamp(a.starts[b + 1], a.T), count = stop - start;
+    const int row0 = (k - tile0) * ROWS, left = count * G - row0;   // (T * G is bounded: 32 bits hold it)
+    if (count <= 0 || left <= 0) return;
+    const int nrows = left < ROWS ? left : ROWS;
+    const int raw = a.lens[b];
+    const long long room = (long long)a.width * a.c.page;
+    const int cap = a.max_len < room ? a.max_len : (int)room;
+    const bool too_long = raw > cap;
+    const int len = too_long ? cap : raw < 0 ? 0 : raw;
+    auto row_of = [&](int i) __attribute__((always_inline)) {       // row i of the tile: token, query head
+        const int x = row0 + i, t = x / G;
+        return (size_t)(start + t) * a.Hq + kv * G + (x - t * G);
+    };
+    fqc_rows<RT> rows;
+    unsigned none = 0u;                                   // rows without a token: they take any range, and are zeros in the end
+    int lo = 0x7FFFFFFF, hi = 0x7FFFFFFF, wlo = 0x7FFFFFFF, whi = 0x7FFFFFFF;   // the least lo and hi, and of minus them
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int i = 16 * r + n < nrows ? 16 * r + n : 0, x = row0 + i, t = x / G;
+        const int pos = raw - count + t;
+        int f = a.first ? a.first[start + t] : 0, e = a.end ? a.end[start + t] : pos + 1;
+        if (a.window > 0 && f < pos - a.window + 1) f = pos - a.window + 1;
+        f = f < 0 ? 0 : f;
+        e = e > len ? len : e;
+        const bool empty = f >= e;
+        none |= empty ? 1u << r : 0u;
+        rows.lo[r] = empty ? 0 : f;
+        rows.hi[r] = empty ? 0x7FFFFFFF : e;
+        if (BIAS) {
+            rows.pos[r] = pos;
+            rows.near[r] = empty ? 0 : pos < f ? f - pos : pos >= e ? pos - (e - 1) : 0;
+            rows.slope[r] = a.slopes[kv * G + (x - t * G)] * -1.44269504088896340736f;
+        }
+        if (!empty) {
+            lo = f < lo ? f : lo;
+            whi = -e < whi ? -e : whi;
+        }
+        wlo = -rows.lo[r] < wlo ? -rows.lo[r] : wlo;
+        hi = rows.hi[r] < hi ? rows.hi[r] : hi;
+    }
+    const int tok0 = fqc_row16_min(lo), last = fqc_row16_min(whi), tok1 = last == 0x7FFFFFFF ? 0 : -last;
+    const int whole0 = -fqc_row16_min(wlo), whole1 = fqc_row16_min(hi);
+    const int first_tile = tok1 > 0 ? tok0 >> 4 : 0, all = tok1 > 0 ? ((tok1 + 15) >> 4) - first_tile : 0;
+    // this workgroup's part, and the waves' shares: steps of NT tiles
+    const int part = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, c0 = first_tile + (int)blockIdx.y * part;
+    const int c1 = c0 + part < first_tile + all ? c0 + part : first_tile + all;
+    const int share = c1 > c0 ? ((c1 - c0 + NT - 1) / NT + KVW - 1) / KVW * NT : 0, t0 = c0 + wave * share, t1 = t0 + share < c1 ? t0 + share : c1;
+    fqa_state<RT> st;
+    const bool work = t0 < t1;
+    if (work) {
+        fqc_cursor cur;
+        cur.pages_of = a.table + (size_t)b * a.width;
+        cur.head = a.c.base + kv * a.c.head_stride;
+        cur.page_stride = (unsigned)(a.c.page_stride >> 4);
+        cur.tiles_per_page = a.c.page >> 4;
+        cur.pages = a.c.pages;
+        cur.start(t0, t1, lane);
+        fqa_queries<RT> Q;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const size_t row = row_of(16 * r + n < nrows ? 16 * r + n : 0);
+            fqa_take_query(Q, r, a.Q + row * 128, a.q_scale[row], a.out_scale, g);
+            if (!(CAP || BIAS)) Q.qs[r] = fmaxf(Q.qs[r], 1.0e-30f);
+            if (CAP) Q.qs[r] *= a.inv_cap * 0.693147180559945309417f;   // (a capped score's factor has no log2 e)
+        }
+        fqc_range<RT, NT, CAP, BIAS>(cur, t0, t1, whole0, whole1 < 16 * t1 ? whole1 : 16 * t1, Q, rows, a.shape, st, lane);
+    }
+    if constexpr (KVW == 1) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            if (16 * r + n >= nrows) continue;
+            const bool zero = !work || (none >> r & 1u) != 0u;
+            const float l = too_long ? __builtin_nanf("") : zero ? 0.f : st.l[r][0];
+            uint16_t* dst = a.O + row_of(16 * r + n) * 128 + 4 * g;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint2*>(dst + 16 * j) = fqa_output(zero ? (fq_v4f){0.f, 0.f, 0.f, 0.f} : st.o[r][j], l);
+        }
+    } else {
+        __shared__ fqa_shared<RT, KVW> sh;
+        if (work) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                if (g == 0) {
+                    sh.m[wave][16 * r + n] = st.m[r];
+                    sh.l[wave][16 * r + n] = too_long ? __builtin_nanf("") : (none >> r & 1u) != 0u ? 0.f : st.l[r][0];
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(&sh.o[wave][16 * r + n][16 * j + 4 * g]) = st.o[r][j];
+            }
+        } else if (lane < ROWS) {
+            sh.m[wave][lane] = FQA_LOWEST;
+            sh.l[wave][lane] = too_long ? __builtin_nanf("") : 0.f;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < nrows * 32; i += 64 * KVW) {  // four channels of a row
+            const int r = i >> 5, c = 4 * (i & 31);
+            float top = FQA_LOWEST, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < KVW; ++w)
+                if (sh.l[w][r] != 0.f) top = fmaxf(top, sh.m[w][r]);
+            fq_v4f o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < KVW; ++w) {
+                if (sh.l[w][r] == 0.f) continue;          // (a wave without tokens of this row; a NaN is kept)
+                const float f = __builtin_amdgcn_exp2f(sh.m[w][r] - top);
+                l += sh.l[w][r] * f;
+                o += *reinterpret_cast<const fq_v4f*>(&sh.o[w][r][c]) * f;
+            }
+            const size_t row = row_of(r);
+            if (a.slots == 1) {
+                *reinterpret_cast<uint2*>(a.O + row * 128 + c) = fqa_output(o, l);
+            } else {
+                const size_t at = row * parts.slots + blockIdx.y;
+                *reinterpret_cast<fq_v4f*>(parts.o + at * 128 + c) = o;
+                if (c == 0) {
+                    parts.ml[at * 2] = top;
+                    parts.ml[at * 2 + 1] = l;
+                }
+            }
+        }
+    }
+}
+
+// rt: query tiles of a wave; waves: of a workgroup, sharing out its tokens; slots: parts of a row's tokens.
+struct fqc_plan { int rt, waves, slots; };
+fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
+    const int G = Hq / Hkv, cus = fq_device_cus();
+    const long long most = (long long)(max_new < T ? max_new : T) * G;
+    fqc_plan p = {most <= 16 ? 1 : most <= 32 ? 2 : 4, 4, 1};
+    const long long tiles = ((long long)max_len + 15) / 16, groups = ((long long)T * G + 16 * p.rt - 1) / (16 * p.rt) > B ? ((long long)T * G + 16 * p.rt - 1) / (16 * p.rt) : B;
+    const long long units = groups * Hkv;
+    if (p.rt == 4 && units >= 4 * cus) {
+        p.waves = 1;
+        return p;
+    }
+    const long long want = units < cus ? cus / units : 1, room = tiles / 16;
+    long long slots = want < room ? want : room;
+    if (slots > 64) slots = 64;
+    p.slots = (int)(slots < 1 ? 1 : slots);
+    return p;
+}
+
+template <int RT, int KVW>
+void fqc_launch(const fqc_args& a, const fqa_parts& parts, hipStream_t stream) {
+    const dim3 grid((unsigned)(((long long)a.T * (a.Hq / a.Hkv) / (16 * RT) + a.B) * a.Hkv), (unsigned)a.slots), block(64 * KVW);
+    const bool cap = a.inv_cap != 0.f, bias = a.slopes != nullptr;
+    if (cap && bias) hipLaunchKernelGGL((fqc_kernel<RT, KVW, true, true>), grid, block, 0, stream, a, parts);
+    else if (cap) hipLaunchKernelGGL((fqc_kernel<RT, KVW, true, false>), grid, block, 0, stream, a, parts);
+    else if (bias) hipLaunchKernelGGL((fqc_kernel<RT, KVW, false, true>), grid, block, 0, stream, a, parts);
+    else hipLaunchKernelGGL((fqc_kernel<RT, KVW, false, false>), grid, block, 0, stream, a, parts);
+}
+
+}  // namespace
+
+size_t fq_chunk_scratch_bytes(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
+    const int slots = fqc_choose(T, B, Hq, Hkv, max_new, max_len).slots;
+    return slots > 1 ? (size_t)slots * T * Hq * 130 * sizeof(float) : 0;
+}
+
+void fq_launch_chunk(const fq_chunk_args& x, void* scratch, hipStream_t stream) {
+    const fqc_plan p = fqc_choose(x.T, x.B, x.Hq, x.Hkv, x.max_new, x.max_len);
+    fqc_args a = {x.Q, x.q_scale, x.c, x.table, x.starts, x.lens, x.first, x.end, x.slopes, x.width, x.window, x.T, x.B, x.Hq, x.Hkv, x.max_len, p.slots,
+                  x.out_scale, x.cap > 0.f ? 1.0f / x.cap : 0.f, {}, x.O};
+    const double c[5] = {0x1.fffffcp-1, -0x1.5551b8p-2, 0x1.107a08p-3, -0x1.a88656p-5, 0x1.ed307ap-7}, k1 = 1.44269504088896340736 * x.cap;
+    for (int i = 0; i < 5; ++i) a.shape.k[i] = (float)(k1 * c[i]);
+    a.shape.k1 = (float)k1;
+    a.shape.k2 = (float)(2.0 * k1);
+    const fqa_parts parts = {static_cast<float*>(scratch), static_cast<float*>(scratch) + (size_t)p.slots * x.T * x.Hq * 128, p.slots};
+    if (p.waves == 1) fqc_launch<4, 1>(a, parts, stream);
+    else if (p.rt == 4) fqc_launch<4, 4>(a, parts, stream);
+    else if (p.rt == 2) fqc_launch<2, 4>(a, parts, stream);
+    else fqc_launch<1, 4>(a, parts, stream);
+    if (p.slots > 1) fqa_join(parts, x.O, x.T * x.Hq, stream, x.starts, x.B, x.Hq);
+}

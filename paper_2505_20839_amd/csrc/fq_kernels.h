@@ -133,6 +133,16 @@ void fq_launch_rmsnorm(const uint16_t* X, const uint16_t* R, const uint16_t* W, 
 void fq_launch_rmsnorm_quant(const uint16_t* X, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint8_t* A, float* a_scale,
                              int M, int K, void* workspace, hipStream_t stream);
 
+// The same where the stream takes X by a norm of its own, a gate and a factor.  Y (bf16) or A and a_scale.
+struct fq_norm_branch {
+    const uint16_t *post, *gate;                          // weights [K] of the norm of X, gates [gates][K]; either may be NULL
+    const int32_t* rows;                                  // the gate of each row; NULL: the only one, or the row's own
+    int gates;
+    float scale;
+};
+void fq_launch_rmsnorm_block(const uint16_t* X, const fq_norm_branch& branch, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint16_t* Y,
+                             uint8_t* A, float* a_scale, int M, int K, void* workspace, hipStream_t stream);
+
 // Paged INT4 key/value cache (fq_paged.hip, fq_attend.hip; layout in include/fireq_paged.h).
 #define FQP_TILE 2080                                     // bytes of 16 tokens of a head
 struct fq_paged_cache {
@@ -143,6 +153,11 @@ struct fq_paged_cache {
 void fq_launch_kv4_append(const uint16_t* QKV, long long ld, const float* cos_sin, int max_positions, const int32_t* positions,
                           const int64_t* slots, bool interleaved, uint8_t* Q, float* q_scale, const fq_paged_cache& c, int T, int Hq,
                           int Hkv, hipStream_t stream);
+// positions [axes][T]; pair j of a head turns by positions[axis[j]], or not at all (axis[j] < 0).
+struct fq_pair_axes { signed char of[64]; };
+void fq_launch_kv4_append_axes(const uint16_t* QKV, long long ld, const float* cos_sin, int max_positions, const int32_t* positions,
+                               const fq_pair_axes& axis, const int64_t* slots, bool interleaved, uint8_t* Q, float* q_scale,
+                               const fq_paged_cache& c, int T, int Hq, int Hkv, hipStream_t stream);
 void fq_launch_kv4_read(const fq_paged_cache& c, const int64_t* slots, uint16_t* K, uint16_t* V, int n, int Hkv, hipStream_t stream);
 struct fq_attend_args {
     const uint8_t* Q;
@@ -156,3 +171,31 @@ struct fq_attend_args {
 };
 size_t fq_attend_scratch_bytes(int B, int Hq, int Hkv, int max_len, int prefix);
 void fq_launch_attend(const fq_attend_args& a, void* scratch, hipStream_t stream);
+
+// New tokens against their cached tokens (fq_chunk.hip; include/fireq_chunk.h).
+struct fq_chunk_args {
+    const uint8_t* Q;
+    const float* q_scale;
+    fq_paged_cache c;
+    const int32_t *table, *starts, *lens, *first, *end;   // first, end: may be NULL
+    const float* slopes;                                  // may be NULL
+    int width, window, T, B, Hq, Hkv, max_new, max_len;
+    float out_scale, cap;                                 // cap 0: uncapped
+    uint16_t* O;
+};
+size_t fq_chunk_scratch_bytes(int T, int B, int Hq, int Hkv, int max_new, int max_len);
+void fq_launch_chunk(const fq_chunk_args& a, void* scratch, hipStream_t stream);
+
+// A token for each row of logits (fq_sample.hip; include/fireq_sample.h).
+struct fq_sample_args {
+    const void* logits;                                   // bf16 or FP32 [B][ld]
+    bool wide;                                            // FP32
+    long long ld;
+    const float *u, *temperature, *top_p, *min_p;         // the last three may be NULL
+    const int32_t* top_k;                                 // may be NULL
+    int32_t* token;
+    float* logprob;                                       // may be NULL
+    int B, V;
+};
+size_t fq_sample_scratch_bytes(int B, int V);
+void fq_launch_sample(const fq_sample_args& a, void* scratch, hipStream_t stream);

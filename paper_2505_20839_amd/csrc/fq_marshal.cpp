@@ -16,9 +16,12 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/fireq.h"
+#include "../../include/fireq_chunk.h"
 #include "../../include/fireq_kv4_ws.h"
 #include "../../include/fireq_norm.h"
+#include "../../include/fireq_norm_block.h"
 #include "../../include/fireq_paged.h"
+#include "../../include/fireq_sample.h"
 #include "../../include/fireq_wquant_ws.h"
 
 namespace {
@@ -52,6 +55,14 @@ struct Api {
     decltype(&fq_kv4_attention_workspace_bytes) attention_workspace_bytes;
     decltype(&fq_kv4_attention_ws) attention_ws;
     decltype(&fq_kv4_attention_prefix_ws) attention_prefix_ws;
+    decltype(&fq_rmsnorm_block) rmsnorm_block;
+    decltype(&fq_rmsnorm_block_quant_ws) rmsnorm_block_quant_ws;
+    decltype(&fq_kv4_append_axes) kv4_append_axes;
+    decltype(&fq_kv4_attention_chunk_workspace_bytes) chunk_workspace_bytes;
+    decltype(&fq_kv4_attention_chunk_ws) attention_chunk_ws;
+    decltype(&fq_sample_workspace_bytes) sample_workspace_bytes;
+    decltype(&fq_sample_bf16_ws) sample_bf16_ws;
+    decltype(&fq_sample_fp32_ws) sample_fp32_ws;
 };
 Api api = {};
 bool bound = false;
@@ -565,6 +576,168 @@ PyObject* kv4_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// A tensor on the device whose stream the call takes, of a type and `n` numbers (below 0: any number); none where None is given.
+const at::Tensor& here(PyObject* o, at::ScalarType t, int64_t n) {
+    const at::Tensor& x = dev(o, t);
+    want(x.device().index() == c10::hip::current_device() && (n < 0 || x.numel() == n));
+    return x;
+}
+template <class T>
+const T* maybe(PyObject* o, at::ScalarType t, int64_t n) { return o == Py_None ? nullptr : (const T*)here(o, t, n).data_ptr(); }
+
+void scratch_here(PyObject* o) {
+    scratch_or_none(o);
+    if (o != Py_None) want(tensor(o).device().index() == c10::hip::current_device());
+}
+
+// rmsnorm_block(X, weight, eps, residual, post, gate, gate_rows, scale, out), rmsnorm_block_quant(.., workspace)
+template <bool QUANT>
+PyObject* rmsnorm_block(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n == (QUANT ? 10 : 9));
+        const at::Tensor& X = here(a[0], at::kBFloat16, -1);
+        want(X.dim() == 2 && X.size(0) > 0 && X.size(0) <= INT_LIMIT && X.size(1) > 0 && X.size(1) <= INT_LIMIT);
+        const int M = (int)X.size(0), K = (int)X.size(1);
+        const uint16_t* w = (const uint16_t*)here(a[1], at::kBFloat16, K).data_ptr();
+        const float eps = number(a[2]), scale = number(a[7]);
+        const at::Tensor& R = here(a[3], at::kBFloat16, -1);
+        want(R.sizes() == X.sizes());
+        const uint16_t *post = maybe<uint16_t>(a[4], at::kBFloat16, K), *gate = maybe<uint16_t>(a[5], at::kBFloat16, -1);
+        int gates = 1;
+        if (gate) {
+            const at::Tensor& g = tensor(a[5]);
+            want(g.dim() == 2 ? g.size(1) == K && g.size(0) <= INT_LIMIT : g.numel() == K);
+            gates = g.dim() == 2 ? (int)g.size(0) : 1;
+        }
+        want(gate || a[6] == Py_None);
+        const int32_t* rows = maybe<int32_t>(a[6], at::kInt, M);
+        if (a[8] != Py_None) here(a[8], at::kBFloat16, -1);
+        at::Tensor H = output(a[8], X.sizes(), X);
+        const uint16_t *x = (const uint16_t*)X.data_ptr(), *r = (const uint16_t*)R.data_ptr();
+        uint16_t* h = (uint16_t*)H.data_ptr();
+        void* st = stream();
+        if (!QUANT) {
+            at::Tensor Y = fresh({M, K}, at::kBFloat16, X);
+            uint16_t* y = (uint16_t*)Y.data_ptr();
+            const int rc = call([&] { return api.rmsnorm_block(x, post, gate, rows, gates, scale, r, w, eps, h, y, M, K, st); });
+            return wrap(rc, {Y, H});
+        }
+        at::Tensor A = fresh({M, K}, at::kByte, X), s = fresh({M}, at::kFloat, X);
+        PyObject* const o = a[QUANT ? 9 : 0];
+        scratch_here(o);
+        const Scratch ws(o, 0, X);
+        uint8_t* pa = (uint8_t*)A.data_ptr();
+        float* ps = (float*)s.data_ptr();
+        const int rc = call([&] { return api.rmsnorm_block_quant_ws(x, post, gate, rows, gates, scale, r, w, eps, h, pa, ps, M, K, ws.p, ws.bytes, st); });
+        return wrap(rc, {A, s, H});
+    });
+}
+
+// kv4_append_axes(QKV, cos_sin, positions, axis_of_pair, slots, cache, interleaved)
+PyObject* kv4_append_axes(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n == 7);
+        const at::Tensor &X = tensor(a[0]), &rot = here(a[1], at::kFloat, -1), &pos = here(a[2], at::kInt, -1), &slots = here(a[4], at::kLong, -1);
+        want(X.is_cuda() && X.device() == rot.device() && X.scalar_type() == at::kBFloat16 && X.dim() == 2 && X.stride(1) == 1);
+        int8_t axis[64];
+        const bool list = PyList_CheckExact(a[3]);
+        want((list || PyTuple_CheckExact(a[3])) && (list ? PyList_GET_SIZE(a[3]) : PyTuple_GET_SIZE(a[3])) == 64 && pos.dim() == 2 && pos.size(0) >= 1 &&
+             pos.size(0) <= 127);
+        for (int j = 0; j < 64; ++j) {
+            PyObject* const v = list ? PyList_GET_ITEM(a[3], j) : PyTuple_GET_ITEM(a[3], j);
+            want(PyLong_CheckExact(v));
+            const long x = PyLong_AsLong(v);              // (an overflow answers -1 and leaves an exception)
+            want(x >= -1 && x < pos.size(0) && !(x == -1 && PyErr_Occurred()));
+            axis[j] = (int8_t)x;
+        }
+        const Paged c(a[5]);
+        want(c.c.device() == rot.device());
+        const int interleaved = truth(a[6]) ? 1 : 0;
+        const int64_t T = X.size(0), width = X.size(1), Hq = width / 128 - 2 * (int64_t)c.heads, ld = T > 1 ? X.stride(0) : width;
+        want(T > 0 && T <= INT_LIMIT && width % 128 == 0 && Hq > 0 && Hq <= INT_LIMIT && ld >= width && pos.size(1) == T && slots.numel() == T &&
+             rot.dim() == 3 && rot.size(0) <= INT_LIMIT && rot.size(1) == 64 && rot.size(2) == 2);
+        at::Tensor Q = fresh({T, Hq, 128}, at::kByte, X), s = fresh({T, Hq}, at::kFloat, X);
+        const uint16_t* x = (const uint16_t*)X.data_ptr();
+        const float* cs = (const float*)rot.data_ptr();
+        const int32_t* pp = (const int32_t*)pos.data_ptr();
+        const int64_t* sl = (const int64_t*)slots.data_ptr();
+        uint8_t* q = (uint8_t*)Q.data_ptr();
+        float* qs = (float*)s.data_ptr();
+        const int positions = (int)rot.size(0), axes = (int)pos.size(0);
+        void* st = stream();
+        const int rc = call([&] {
+            return api.kv4_append_axes(x, ld, cs, positions, pp, axes, axis, sl, interleaved, q, qs, c.p(), c.page_stride, c.head_stride, c.pages, c.page,
+                                       (int)T, (int)Hq, c.heads, st);
+        });
+        return wrap(rc, {Q, s});
+    });
+}
+
+// kv4_attention_chunk(Q, q_scale, cache, block_table, starts, seq_lens, out_scale, max_new, max_len, first, end, window, cap, slopes, out, workspace)
+PyObject* kv4_attention_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n == 16);
+        const at::Tensor& Q = here(a[0], at::kByte, -1);
+        const Paged c(a[2]);
+        const at::Tensor& table = here(a[3], at::kInt, -1);
+        want(c.c.device() == Q.device() && Q.dim() == 3 && Q.size(2) == 128 && table.dim() == 2);
+        const int64_t T = Q.size(0), Hq = Q.size(1), B = table.size(0), width = table.size(1);
+        want(T > 0 && T <= INT_LIMIT && B > 0 && B < INT_LIMIT && Hq > 0 && Hq <= INT_LIMIT && Hq % c.heads == 0 && width <= INT_LIMIT);
+        const float* s = (const float*)here(a[1], at::kFloat, T * Hq).data_ptr();
+        const int32_t *starts = (const int32_t*)here(a[4], at::kInt, B + 1).data_ptr(), *lens = (const int32_t*)here(a[5], at::kInt, B).data_ptr();
+        const float out_scale = number(a[6]), cap = number(a[12]);
+        const int max_new = a[7] == Py_None ? (int)T : whole(a[7]), max_len = a[8] == Py_None ? (int)std::min<int64_t>(width * c.page, 1 << 30) : whole(a[8]);
+        const int window = whole(a[11]);
+        const int32_t *first = maybe<int32_t>(a[9], at::kInt, T), *end = maybe<int32_t>(a[10], at::kInt, T);
+        const float* slopes = maybe<float>(a[13], at::kFloat, Hq);
+        at::Tensor O;
+        if (a[14] == Py_None) {
+            O = fresh({T, Hq, 128}, at::kBFloat16, Q);
+        } else {
+            O = here(a[14], at::kBFloat16, -1);
+            want(O.sizes() == at::IntArrayRef({T, Hq, 128}) || O.sizes() == at::IntArrayRef({T, Hq * 128}));
+        }
+        scratch_here(a[15]);
+        const Scratch ws(a[15], a[15] == Py_None ? api.chunk_workspace_bytes((int)T, (int)B, (int)Hq, c.heads, max_new, max_len) : 0, Q);
+        const uint8_t* q = (const uint8_t*)Q.data_ptr();
+        const int32_t* tb = (const int32_t*)table.data_ptr();
+        uint16_t* o = (uint16_t*)O.data_ptr();
+        void* st = stream();
+        const int rc = call([&] {
+            return api.attention_chunk_ws(q, s, c.p(), c.page_stride, c.head_stride, c.pages, c.page, tb, (int)width, starts, lens, first, end, window, cap, slopes,
+                                          out_scale, o, (int)T, (int)B, (int)Hq, c.heads, max_new, max_len, ws.p, ws.bytes, st);
+        });
+        return wrap(rc, O);
+    });
+}
+
+// sample(logits, u, temperature, top_k, top_p, min_p, workspace)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&] {
+        want(n == 7);
+        const at::Tensor& X = tensor(a[0]);
+        want(X.is_cuda() && X.device().index() == c10::hip::current_device() && X.dim() == 2 && (X.scalar_type() == at::kBFloat16 || X.scalar_type() == at::kFloat));
+        const int64_t B = X.size(0), V = X.size(1), ld = B > 1 ? X.stride(0) : V;
+        want(B > 0 && B <= INT_LIMIT && V > 0 && V <= INT_LIMIT && (V == 1 || X.stride(1) == 1) && ld >= V);
+        const float *u = (const float*)here(a[1], at::kFloat, B).data_ptr(), *T = maybe<float>(a[2], at::kFloat, B), *p = maybe<float>(a[4], at::kFloat, B),
+                    *m = maybe<float>(a[5], at::kFloat, B);
+        const int32_t* k = maybe<int32_t>(a[3], at::kInt, B);
+        scratch_here(a[6]);
+        const Scratch ws(a[6], a[6] == Py_None ? api.sample_workspace_bytes((int)B, (int)V) : 0, X);
+        at::Tensor token = fresh({B}, at::kInt, X), logprob = fresh({B}, at::kFloat, X);
+        int32_t* pt = (int32_t*)token.data_ptr();
+        float* pl = (float*)logprob.data_ptr();
+        const void* x = X.data_ptr();
+        const bool wide = X.scalar_type() == at::kFloat;
+        void* st = stream();
+        const int rc = call([&] {
+            return wide ? api.sample_fp32_ws((const float*)x, ld, u, T, k, p, m, pt, pl, (int)B, (int)V, ws.p, ws.bytes, st)
+                        : api.sample_bf16_ws((const uint16_t*)x, ld, u, T, k, p, m, pt, pl, (int)B, (int)V, ws.p, ws.bytes, st);
+        });
+        return wrap(rc, {token, logprob});
+    });
+}
+
 // gemm_workspace_bytes(M, N, K)
 PyObject* gemm_workspace_bytes(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&] {
@@ -614,6 +787,11 @@ PyMethodDef methods[] = {
     FQ_METHOD("kv4_append", kv4_append),
     FQ_METHOD("kv4_read", kv4_read),
     FQ_METHOD("kv4_attention", kv4_attention),
+    FQ_METHOD("rmsnorm_block", rmsnorm_block<false>),
+    FQ_METHOD("rmsnorm_block_quant", rmsnorm_block<true>),
+    FQ_METHOD("kv4_append_axes", kv4_append_axes),
+    FQ_METHOD("kv4_attention_chunk", kv4_attention_chunk),
+    FQ_METHOD("sample", sample),
     FQ_METHOD("gemm_workspace_bytes", gemm_workspace_bytes),
     {nullptr, nullptr, 0, nullptr}};
 

@@ -3,6 +3,10 @@
 // in one pass over the row: with t = max |h w| the row's two statistics, sum h^2 and t, come out of one reduction, beta is
 // t * rstd / 448 and a code is E4M3(448 h w / t) -- rstd cancels, so no value waits for it, and adds no rounding.
 // Bound by HBM: 7 bytes per element with the residual, 3 without (bf16 output: 8 and 4).
+//
+// Between two blocks with a norm on both sides (include/fireq_norm_block.h) the stream takes x by its own norm, a gate and a factor first:
+//     h = bf16(r + scale * gate * (x * post / sqrt(mean x^2 + eps)))
+// The same bytes and one more reduction over the row, which is in registers by then.
 #include <type_traits>
 #include "fq_common.h"
 #include "fq_kernels.h"
@@ -60,15 +64,37 @@ __device__ __forceinline__ fq_v2i fqn_codes8(fq_v4i h, fq_v4i w, F quotient) {
     return o;
 }
 
+struct fqn_none {};
+
+// Eight numbers of the stream, each rounded once: r + scale * g * (x * f * p).
+__device__ __forceinline__ fq_v4i fqn_branch8(fq_v4i x, fq_v4i r, fq_v4i p, fq_v4i g, float f, float scale) {
+    fq_v4i h;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        h[j] = (int)fqn_pack_bf16(fmaf(scale, fq_bf16_lo(g[j]) * (fq_bf16_lo(x[j]) * f * fq_bf16_lo(p[j])), fq_bf16_lo(r[j])),
+                                  fmaf(scale, fq_bf16_hi(g[j]) * (fq_bf16_hi(x[j]) * f * fq_bf16_hi(p[j])), fq_bf16_hi(r[j])));
+    return h;
+}
+__device__ __forceinline__ float fqn_squares8(fq_v4i x, float ss) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        ss = fmaf(fq_bf16_lo(x[j]), fq_bf16_lo(x[j]), ss);
+        ss = fmaf(fq_bf16_hi(x[j]), fq_bf16_hi(x[j]), ss);
+    }
+    return ss;
+}
+
 // WPR waves per row with up to CH chunks (16 bytes, 8 numbers) of it per thread; workgroups of max(4, WPR) waves.  The row and
 // the weights stay in registers between the reduction and the conversion; rows that do not fit are read twice (REREAD).
 // X, R, H and Y may be one array (no __restrict__): a chunk is read and written by one thread only, and a thread requests all of
 // its chunks before it stores any.
-template <int WPR, int CH, bool RES, int OUT, bool REREAD>
+template <int WPR, int CH, bool RES, int OUT, bool REREAD, bool BRANCH>
 __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uint16_t* X, const uint16_t* R, const uint16_t* __restrict__ Wt,
                                                                       float eps, uint16_t* H, uint16_t* Y, uint8_t* __restrict__ A,
-                                                                      float* __restrict__ a_scale, int K, uint16_t* __restrict__ planes, int M) {
+                                                                      float* __restrict__ a_scale, int K, uint16_t* __restrict__ planes, int M,
+                                                                      std::conditional_t<BRANCH, fq_norm_branch, fqn_none> branch) {
     static_assert(!(OUT == FQN_CODES_ZP && REREAD), "the zero-point terms are summed from registers");
+    static_assert(RES || !BRANCH, "the branch is added to a residual");
     constexpr int WAVES = WPR > 4 ? WPR : 4, ROWS = WAVES / WPR, T = 64 * WPR;
     constexpr int MAXG = T * CH / 16 + 16;                // groups of a row, padded
     constexpr bool ZP = OUT == FQN_CODES_ZP;
@@ -90,7 +116,70 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
     float ss = 0.f;
     unsigned top = 0u;
     fq_v4i keep[CH], wt[CH];
-    if (!REREAD) {
+    constexpr int ONES = 0x3F803F80;                      // bf16 ones, where there is no weight or gate
+    // the block form: 1 / sqrt(mean x^2 + eps) of the row (1 without that norm); NaN for a row that has none, or no gate
+    auto branch_factor = [&](float xx, bool lost) __attribute__((always_inline)) {
+        float f = 1.0f;
+        if constexpr (BRANCH) {
+            __shared__ float red_x[WAVES];
+            if (branch.post) {
+                xx = fqn_wave_sum(xx);
+                if (WPR > 1) {
+                    if ((t & 63) == 0) red_x[(int)threadIdx.x >> 6] = xx;
+                    __syncthreads();
+                    xx = red_x[row * WPR];
+#pragma unroll
+                    for (int i = 1; i < WPR; ++i) xx += red_x[row * WPR + i];
+                }
+                f = xx < __builtin_inff() ? 1.0f / sqrtf(xx / (float)K + eps) : __builtin_nanf("");
+            }
+            if (lost) f = __builtin_nanf("");
+        }
+        return f;
+    };
+    const fq_v4i *post = nullptr, *gate = nullptr;
+    bool lost = false;
+    if constexpr (BRANCH) {
+        const int mm = on ? m : M - 1, g = branch.rows ? branch.rows[mm] : branch.gates == 1 ? 0 : mm;
+        lost = branch.gate && (unsigned)g >= (unsigned)branch.gates;
+        post = reinterpret_cast<const fq_v4i*>(branch.post);
+        if (branch.gate) gate = reinterpret_cast<const fq_v4i*>(branch.gate + (size_t)(lost ? 0 : g) * K);
+    }
+    if constexpr (BRANCH && !REREAD) {
+        fq_v4i add[CH], pw[CH], gt[CH];
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            const int c = t + i * T < nchunk ? t + i * T : nchunk - 1;
+            keep[i] = x[c];
+            add[i] = r[c];
+            wt[i] = w[c];
+            pw[i] = post ? post[c] : (fq_v4i){ONES, ONES, ONES, ONES};
+            gt[i] = gate ? gate[c] : (fq_v4i){ONES, ONES, ONES, ONES};
+        }
+        float xx = 0.f;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+            if (t + i * T < nchunk) xx = fqn_squares8(keep[i], xx);
+        const float f = branch_factor(xx, lost);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            keep[i] = fqn_branch8(keep[i], add[i], pw[i], gt[i], f, branch.scale);
+            if (t + i * T >= nchunk) keep[i] = (fq_v4i){0, 0, 0, 0};
+            fqn_take8(keep[i], wt[i], ss, top);
+        }
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+            if (on && t + i * T < nchunk) hs[t + i * T] = keep[i];
+    } else if constexpr (BRANCH) {
+        float xx = 0.f;
+        for (int c = t; c < nchunk; c += T) xx = fqn_squares8(x[c], xx);
+        const float f = branch_factor(xx, lost);
+        for (int c = t; c < nchunk; c += T) {
+            const fq_v4i ones = {ONES, ONES, ONES, ONES}, h = fqn_branch8(x[c], r[c], post ? post[c] : ones, gate ? gate[c] : ones, f, branch.scale);
+            if (on) hs[c] = h;
+            fqn_take8(h, w[c], ss, top);
+        }
+    } else if (!REREAD) {
         fq_v4i add[CH];
 #pragma unroll
         for (int i = 0; i < CH; ++i) {                    // all requested before the first is used; past the row's end its last chunk again
@@ -213,17 +302,18 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
 //     64 x 11008    <16, 2> 4.2; <8, 4> 4.4; <4, 8> 4.9                 2000 x 11008  <16, 2> 30.3; <8, 4> 29.6; <4, 8> 31.0
 //     1 x 16384     <16, 2> 3.9; <8, 4> 4.1; <4, 8> 4.6                 2048 x 16384  <16, 2> 44.9; <8, 4> 45.0; <4, 8> 45.8
 //     8192 x 2048   <1, 4> 21.1 and 8192 x 1024 11.8 (one wave a row); 300 x 2048 <4, 2> 3.5; <2, 4> 3.6; <1, 8> 4.5
-template <bool RES, int OUT>
+template <bool RES, int OUT, class BR>
 void fqn_launch(const uint16_t* X, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint16_t* Y, uint8_t* A, float* a_scale,
-                int M, int K, uint16_t* planes, hipStream_t stream) {
+                int M, int K, uint16_t* planes, const BR& branch, hipStream_t stream) {
+    constexpr bool BRANCH = std::is_same<BR, fq_norm_branch>::value;
 #define FQN_LAUNCH(WPR_, CH_, REREAD_) \
-    hipLaunchKernelGGL((fqn_kernel<WPR_, CH_, RES, OUT, REREAD_>), dim3((unsigned)((M + (WPR_ > 4 ? 1 : 4 / WPR_) - 1) / (WPR_ > 4 ? 1 : 4 / WPR_))), \
-                       dim3(WPR_ > 4 ? 64 * WPR_ : 256), 0, stream, X, R, W, eps, H, Y, A, a_scale, K, planes, M)
+    hipLaunchKernelGGL((fqn_kernel<WPR_, CH_, RES, OUT, REREAD_, BRANCH>), dim3((unsigned)((M + (WPR_ > 4 ? 1 : 4 / WPR_) - 1) / (WPR_ > 4 ? 1 : 4 / WPR_))), \
+                       dim3(WPR_ > 4 ? 64 * WPR_ : 256), 0, stream, X, R, W, eps, H, Y, A, a_scale, K, planes, M, branch)
     if (K > 16384) {
         if constexpr (OUT != FQN_CODES_ZP) {              // (no zero-point terms for rows this long)
             // (row, residual and weights of more than 32768 numbers do not fit the registers where bf16 leaves: 512 x 40960
             // 68.3 us held, 40.2 read twice; the codes' kernel 33.5 held, 36.0 read twice)
-            constexpr int HELD = RES && OUT == FQN_BF16 ? 32768 : 65536;
+            constexpr int HELD = BRANCH || (RES && OUT == FQN_BF16) ? 32768 : 65536;
             if (K > HELD) FQN_LAUNCH(16, 1, true);
             else if constexpr (HELD > 32768) {
                 if (K > 32768) FQN_LAUNCH(16, 8, false);
@@ -242,18 +332,26 @@ void fqn_launch(const uint16_t* X, const uint16_t* R, const uint16_t* W, float e
 
 void fq_launch_rmsnorm(const uint16_t* X, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint16_t* Y, int M, int K,
                        hipStream_t stream) {
-    if (R) fqn_launch<true, FQN_BF16>(X, R, W, eps, H, Y, nullptr, nullptr, M, K, nullptr, stream);
-    else fqn_launch<false, FQN_BF16>(X, nullptr, W, eps, nullptr, Y, nullptr, nullptr, M, K, nullptr, stream);
+    if (R) fqn_launch<true, FQN_BF16>(X, R, W, eps, H, Y, nullptr, nullptr, M, K, nullptr, fqn_none(), stream);
+    else fqn_launch<false, FQN_BF16>(X, nullptr, W, eps, nullptr, Y, nullptr, nullptr, M, K, nullptr, fqn_none(), stream);
 }
 
 void fq_launch_rmsnorm_quant(const uint16_t* X, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint8_t* A, float* a_scale,
                              int M, int K, void* workspace, hipStream_t stream) {
     uint16_t* planes = static_cast<uint16_t*>(workspace);
     if (planes) {
-        if (R) fqn_launch<true, FQN_CODES_ZP>(X, R, W, eps, H, nullptr, A, a_scale, M, K, planes, stream);
-        else fqn_launch<false, FQN_CODES_ZP>(X, nullptr, W, eps, nullptr, nullptr, A, a_scale, M, K, planes, stream);
+        if (R) fqn_launch<true, FQN_CODES_ZP>(X, R, W, eps, H, nullptr, A, a_scale, M, K, planes, fqn_none(), stream);
+        else fqn_launch<false, FQN_CODES_ZP>(X, nullptr, W, eps, nullptr, nullptr, A, a_scale, M, K, planes, fqn_none(), stream);
     } else {
-        if (R) fqn_launch<true, FQN_CODES>(X, R, W, eps, H, nullptr, A, a_scale, M, K, nullptr, stream);
-        else fqn_launch<false, FQN_CODES>(X, nullptr, W, eps, nullptr, nullptr, A, a_scale, M, K, nullptr, stream);
+        if (R) fqn_launch<true, FQN_CODES>(X, R, W, eps, H, nullptr, A, a_scale, M, K, nullptr, fqn_none(), stream);
+        else fqn_launch<false, FQN_CODES>(X, nullptr, W, eps, nullptr, nullptr, A, a_scale, M, K, nullptr, fqn_none(), stream);
     }
+}
+
+void fq_launch_rmsnorm_block(const uint16_t* X, const fq_norm_branch& branch, const uint16_t* R, const uint16_t* W, float eps, uint16_t* H, uint16_t* Y,
+                             uint8_t* A, float* a_scale, int M, int K, void* workspace, hipStream_t stream) {
+    uint16_t* planes = static_cast<uint16_t*>(workspace);
+    if (Y) fqn_launch<true, FQN_BF16>(X, R, W, eps, H, Y, nullptr, nullptr, M, K, nullptr, branch, stream);
+    else if (planes) fqn_launch<true, FQN_CODES_ZP>(X, R, W, eps, H, nullptr, A, a_scale, M, K, planes, branch, stream);
+    else fqn_launch<true, FQN_CODES>(X, R, W, eps, H, nullptr, A, a_scale, M, K, nullptr, branch, stream);
 }

@@ -3,6 +3,7 @@
 // The rotation of a pair, a c - b s and b c + a s, has bf16 a and b and FP32 c and s: the products are exact in FP64 and the
 // difference is rounded there once, then to FP32.  In FP32 the two products' own roundings would leave a code to the order of the
 // operations wherever a key lies next to the border between two codes.
+#include <type_traits>
 #include "fq_common.h"
 #include "fq_kernels.h"
 
@@ -152,8 +153,11 @@ __device__ __forceinline__ int fqp_row_of(int i, int rows) {
     return i < whole ? (i & ~127) + (i & 7) * 16 + ((i >> 3) & 15) : i;
 }
 
-template <bool INTERLEAVED>
-__global__ __launch_bounds__(512) void fqp_append_kernel(fqp_append_args a) {
+// AXES: each lane's four pairs take their cosines by positions of their own (four loads of 8 bytes instead of two of 16, one step
+// further behind the row's start); a position outside the table in any pair spoils the row.
+struct fqp_one_axis {};
+template <bool INTERLEAVED, bool AXES>
+__global__ __launch_bounds__(512) void fqp_append_kernel(fqp_append_args a, std::conditional_t<AXES, fq_pair_axes, fqp_one_axis> axes) {
     const int heads = a.Hq + 2 * a.Hkv, j = threadIdx.x & 15, token = fqp_row_of(blockIdx.x, a.T);
     const int groups = (int)(blockDim.x >> 4), h0 = (int)blockIdx.y * 2 * groups + (int)(threadIdx.x >> 4), h1 = h0 + groups;
     const uint16_t* src = a.QKV + (long long)token * a.ld;
@@ -165,15 +169,38 @@ __global__ __launch_bounds__(512) void fqp_append_kernel(fqp_append_args a) {
         w[u][0] = *reinterpret_cast<const fqp_v2u*>(src + hh * 128 + (mixed ? 8 * j : 4 * j));
         w[u][1] = *reinterpret_cast<const fqp_v2u*>(src + hh * 128 + (mixed ? 8 * j + 4 : 64 + 4 * j));
     }
-    const int pos = a.positions[token];
     const int64_t slot = a.slots[token];
-    const bool lost = slot >= (int64_t)a.c.pages * a.c.page, bad = pos < 0 || pos >= a.max_positions || lost, cached = slot >= 0 && !lost;
+    const bool lost = slot >= (int64_t)a.c.pages * a.c.page, cached = slot >= 0 && !lost;
     double cs[4] = {1., 1., 1., 1.}, sn[4] = {0., 0., 0., 0.};
-    if (!bad) {
-        const fq_v4f* t = reinterpret_cast<const fq_v4f*>(a.cos_sin + ((size_t)pos * 64 + 4 * j) * 2);
-        const fq_v4f t0 = t[0], t1 = t[1];
-        cs[0] = t0[0]; sn[0] = t0[1]; cs[1] = t0[2]; sn[1] = t0[3];
-        cs[2] = t1[0]; sn[2] = t1[1]; cs[3] = t1[2]; sn[3] = t1[3];
+    bool bad = lost;
+    if constexpr (AXES) {
+        unsigned out = 0u;
+        const int of = reinterpret_cast<const int*>(axes.of)[j];
+        int pos[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int axis = of << (24 - 8 * i) >> 24;
+            pos[i] = axis < 0 ? -1 : a.positions[(size_t)axis * a.T + token];
+            out |= axis >= 0 && (unsigned)pos[i] >= (unsigned)a.max_positions ? 1u : 0u;
+        }
+        bad |= fq_row16_max(out) != 0u;
+        if (!bad)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (pos[i] >= 0) {
+                    const fq_v2f t = reinterpret_cast<const fq_v2f*>(a.cos_sin)[(size_t)pos[i] * 64 + 4 * j + i];
+                    cs[i] = t[0];
+                    sn[i] = t[1];
+                }
+    } else {
+        const int pos = a.positions[token];
+        bad |= pos < 0 || pos >= a.max_positions;
+        if (!bad) {
+            const fq_v4f* t = reinterpret_cast<const fq_v4f*>(a.cos_sin + ((size_t)pos * 64 + 4 * j) * 2);
+            const fq_v4f t0 = t[0], t1 = t[1];
+            cs[0] = t0[0]; sn[0] = t0[1]; cs[1] = t0[2]; sn[1] = t0[3];
+            cs[2] = t1[0]; sn[2] = t1[1]; cs[3] = t1[2]; sn[3] = t1[3];
+        }
     }
     const fqp_place place = fqp_find(a.c, cached ? slot : 0);
 #pragma unroll
@@ -236,16 +263,27 @@ __global__ __launch_bounds__(256) void fqp_read_kernel(fq_paged_cache c, const i
     *reinterpret_cast<fq_v4i*>(V + (size_t)unit * 128 + 8 * j) = v;
 }
 
+template <class AX>
+void fqp_launch_append(const fqp_append_args& a, const AX& axes, bool interleaved, hipStream_t stream) {
+    constexpr bool AXES = std::is_same<AX, fq_pair_axes>::value;
+    const int heads = a.Hq + 2 * a.Hkv, pairs = (heads + 1) / 2, groups = pairs < 32 ? (pairs + 3) / 4 * 4 : 32;
+    const dim3 grid((unsigned)a.T, (unsigned)((pairs + groups - 1) / groups)), block((unsigned)(16 * groups));
+    if (interleaved) hipLaunchKernelGGL((fqp_append_kernel<true, AXES>), grid, block, 0, stream, a, axes);
+    else hipLaunchKernelGGL((fqp_append_kernel<false, AXES>), grid, block, 0, stream, a, axes);
+}
+
 }  // namespace
 
 void fq_launch_kv4_append(const uint16_t* QKV, long long ld, const float* cos_sin, int max_positions, const int32_t* positions,
                           const int64_t* slots, bool interleaved, uint8_t* Q, float* q_scale, const fq_paged_cache& c, int T, int Hq,
                           int Hkv, hipStream_t stream) {
-    const int heads = Hq + 2 * Hkv, pairs = (heads + 1) / 2, groups = pairs < 32 ? (pairs + 3) / 4 * 4 : 32;
-    const dim3 grid((unsigned)T, (unsigned)((pairs + groups - 1) / groups)), block((unsigned)(16 * groups));
-    const fqp_append_args a = {QKV, ld, cos_sin, positions, slots, Q, q_scale, c, max_positions, T, Hq, Hkv};
-    if (interleaved) hipLaunchKernelGGL((fqp_append_kernel<true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((fqp_append_kernel<false>), grid, block, 0, stream, a);
+    fqp_launch_append({QKV, ld, cos_sin, positions, slots, Q, q_scale, c, max_positions, T, Hq, Hkv}, fqp_one_axis(), interleaved, stream);
+}
+
+void fq_launch_kv4_append_axes(const uint16_t* QKV, long long ld, const float* cos_sin, int max_positions, const int32_t* positions,
+                               const fq_pair_axes& axis, const int64_t* slots, bool interleaved, uint8_t* Q, float* q_scale,
+                               const fq_paged_cache& c, int T, int Hq, int Hkv, hipStream_t stream) {
+    fqp_launch_append({QKV, ld, cos_sin, positions, slots, Q, q_scale, c, max_positions, T, Hq, Hkv}, axis, interleaved, stream);
 }
 
 void fq_launch_kv4_read(const fq_paged_cache& c, const int64_t* slots, uint16_t* K, uint16_t* V, int n, int Hkv, hipStream_t stream) {
