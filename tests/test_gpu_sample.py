@@ -1,0 +1,233 @@
+"""Sampling (fireq_sample.h) against its definition in 64 bits: ties, masks, borders of every filter, odd sizes and strides."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def fq():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: torch.cuda.is_available() is False")
+    from paper_2505_20839_amd import binding
+    return binding
+
+
+# An FP32 exponential of an argument of at most 26 log2 e (its rounding, 2^-24 of up to 38, and the hardware's 2^-22) is off by 2^-18 relative at most; a
+# sum of them by as much, and a border between two tokens, u times a sum or p times a sum, by twice that.  Dropped and rounded masses add 2^-36 a token.
+REL = 2.0 ** -17
+
+
+def check(x, token, logprob, u, T=1.0, k=0, p=1.0, m=0.0):
+    """x float64 [V]: the token lies within the rounding of the borders that the definition sets."""
+    V = len(x)
+    greedy = T == 0
+    if greedy:
+        T, k = 1.0, 1
+    top = x.max()
+    with np.errstate(invalid="ignore"):
+        e = np.where(x == -math.inf, 0.0, np.exp((x - top) / T))
+    slack = 2.0 ** -36 * V
+    assert 0 <= token < V and e[token] > 0
+    want = (x[token] - top) / T - math.log(e.sum())
+    assert abs(logprob - want) <= 2.0 ** -23 * abs(want) + 2 * REL, (logprob, want)
+    order = np.argsort(-x, kind="stable")
+    rank = np.empty(V, np.int64)
+    rank[order] = np.arange(V)
+    keep = np.ones(V, bool)
+    if m > 0:
+        keep &= x >= top + T * math.log(min(np.float32(m), 1.0))
+    if 0 < k < V:
+        keep &= rank < k
+    assert keep[token], (token, rank[token])
+    if greedy:
+        return
+    mass = np.where(keep, e, 0.0)
+    lo = hi = keep                                        # the least and the most that top-p may keep
+    if p < 1:
+        c = mass[order].cumsum()
+        before = c - mass[order]
+        lo, hi = np.zeros(V, bool), np.zeros(V, bool)
+        lo[order] = keep[order] & ((before < p * c[-1] * (1 - 4 * REL) - slack) | (np.arange(V) == 0))
+        hi[order] = keep[order] & ((before < p * c[-1] * (1 + 4 * REL) + slack) | (np.arange(V) == 0))
+    assert hi[token], (token, rank[token], int(lo.sum()), int(hi.sum()))
+    # The kept set is one between `lo` and `hi`; the masses of the tokens up to each one, and of all, lie between theirs
+    u = min(max(float(np.float32(u)), 0.0), 1 - 2.0 ** -24)
+    a, b = np.where(lo, e, 0.0).cumsum(), np.where(hi, e, 0.0).cumsum()
+    assert a[token] - (e[token] if lo[token] else 0.0) <= u * b[-1] * (1 + 4 * REL) + slack, "a later token"
+    assert b[token] >= u * a[-1] * (1 - 4 * REL) - slack, "an earlier token"
+
+
+def run(fq, x, u, T=None, k=None, p=None, m=None, **kw):
+    """x: a GPU tensor [B,V]; u and the parameters: lists."""
+    B = x.shape[0]
+    t = lambda v, d: None if v is None else torch.tensor(v, dtype=d, device="cuda")     # noqa: E731
+    token, logprob = fq.fq_sample(x, t(u, torch.float32), t(T, torch.float32), t(k, torch.int32), t(p, torch.float32), t(m, torch.float32), **kw)
+    token, logprob, y = token.cpu().numpy(), logprob.cpu().double().numpy(), x.double().cpu().numpy()
+    f = lambda v, b, d: d if v is None else float(np.float32(v[b]))                     # noqa: E731
+    for b in range(B):
+        check(y[b], int(token[b]), logprob[b], u[b], f(T, b, 1.0), 0 if k is None else k[b], f(p, b, 1.0), f(m, b, 0.0))
+    return token, logprob
+
+
+PARAMS = [dict(), dict(T=0.7), dict(T=0.0), dict(k=1), dict(k=50), dict(k=1000), dict(p=0.9), dict(p=1e-9), dict(p=0.0), dict(p=0.999), dict(m=0.05), dict(m=1.0),
+          dict(T=1.4, k=40, p=0.95, m=0.02), dict(T=0.3, k=3, p=0.5), dict(T=50.0, k=700, p=0.6), dict(k=10 ** 9, p=1.5, m=-1.0)]
+
+
+def lists(params, B):
+    return {n: None if not any(n in q for q in params) else [params[b % len(params)].get(n, {"T": 1.0, "k": 0, "p": 1.0, "m": 0.0}[n]) for b in range(B)]
+            for n in ("T", "k", "p", "m")}
+
+
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 255, 1000, 2049, 5001, 32000, 100003])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_sizes_and_filters(fq, V, dtype):
+    g = torch.Generator(device="cuda").manual_seed(V)
+    B = 2 * len(PARAMS)
+    x = (2.5 * torch.randn((B, V), generator=g, device="cuda")).to(dtype)
+    run(fq, x, np.random.default_rng(V).random(B).astype(np.float32).tolist(), **lists(PARAMS, B))
+
+
+@pytest.mark.parametrize("one", PARAMS, ids=str)
+def test_each_filter_alone(fq, one):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = (4.0 * torch.randn((9, 4097), generator=g, device="cuda")).bfloat16()
+    u = [0.0, 1e-7, 0.1, 0.37, 0.5, 0.75, 0.9, 0.999, 1 - 2.0 ** -24]
+    run(fq, x, u, **lists([one], 9))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [300, 20000, 1 << 20])
+def test_ties(fq, dtype, V):
+    """All alike, a few values, two values: filters end inside ties, which the lower index wins."""
+    x = torch.zeros((6, V), dtype=dtype, device="cuda")
+    x[1] = torch.arange(V, device="cuda") % 3 - 1.0
+    x[2, : V // 2] = -0.0
+    x[3] = (torch.arange(V, device="cuda") // 7 % 5).to(dtype)
+    x[4] = -1000.5
+    x[5, 1::2] = 3.0
+    u = [0.5, 0.99, 0.001, 0.3, 0.7, 1 - 2.0 ** -24]
+    k = V // 3 + 1
+    run(fq, x, u, k=[k] * 6)
+    run(fq, x, u, p=[0.4] * 6)
+    run(fq, x, u, k=[k] * 6, p=[0.8] * 6, T=[2.0] * 6)
+    # the kept run of equal logits is the first k by index
+    token, _ = run(fq, x[:1], [1 - 2.0 ** -24], k=[k])
+    assert token[0] == k - 1
+    token, _ = run(fq, x, u, T=[0.0] * 6)
+    assert token.tolist() == [0, 2, 0, 28 % V, 0, 1]
+
+
+def test_masked_logits(fq):
+    """-infinity and the type's lowest value, whole parts of a row among them."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for low in (-math.inf, -3.3895e38):
+        x = torch.full((4, 20000), low, device="cuda").bfloat16()
+        x[0, 17777] = -3.0                                # one token
+        x[1, 9000:9100] = torch.randn(100, generator=g, device="cuda").bfloat16()
+        x[2, ::3] = torch.randn(6667, generator=g, device="cuda").bfloat16()
+        x[3, 19999] = 2.0
+        x[3, 0] = 1.0
+        for params in (dict(), dict(k=[5] * 4), dict(p=[0.5] * 4), dict(m=[0.1] * 4), dict(T=[0.0] * 4)):
+            token, _ = run(fq, x, [0.6, 0.2, 0.9, 0.05], **params)
+            assert token[0] == 17777
+
+
+def test_rows_that_cannot_be_drawn_from(fq):
+    x = torch.randn((12, 5000), device="cuda").bfloat16()
+    x[0, 77], x[1, 4999], x[2] = math.nan, math.inf, -math.inf
+    T, p, m, u = [1.0] * 12, [0.9] * 12, [0.0] * 12, [0.5] * 12
+    T[3], T[4], T[5], p[6], m[7], u[8] = -1.0, math.nan, math.inf, math.nan, math.nan, math.nan
+    t = lambda v: torch.tensor(v, device="cuda")          # noqa: E731
+    token, logprob = fq.fq_sample(x, t(u), t(T), None, t(p), t(m))
+    assert token[:9].tolist() == [-1] * 9 and torch.isnan(logprob[:9]).all()
+    for b in range(9, 12):
+        check(x[b].double().cpu().numpy(), int(token[b]), float(logprob[b]), 0.5, p=float(np.float32(0.9)))
+
+
+@pytest.mark.parametrize("T", [1e-38, 1e-6, 0.01, 1e4, 3e38])
+def test_temperatures_at_the_ends(fq, T):
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x = 3.0 * torch.randn((3, 3001), generator=g, device="cuda")
+    best = x.argmax(-1).cpu()
+    for params in (dict(), dict(k=[100] * 3, p=[0.7] * 3)):
+        t = lambda v, d=torch.float32: torch.tensor(v, dtype=d, device="cuda")         # noqa: E731
+        token, logprob = fq.fq_sample(x, t([0.2, 0.5, 0.99]), t([T] * 3), *(t(params[n], d) if n in params else None for n, d in (("k", torch.int32), ("p", torch.float32))))
+        if T < 1e-5:
+            assert torch.equal(token.cpu().long(), best) and (logprob.abs() < 1e-3).all()
+        else:
+            for b in range(3):
+                check(x[b].double().cpu().numpy(), int(token[b]), float(logprob[b]), [0.2, 0.5, 0.99][b], float(np.float32(T)), params.get("k", [0])[0],
+                      float(np.float32(params.get("p", [1.0])[0])))
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e10, 1e37])
+def test_logits_of_every_size(fq, scale):
+    g = torch.Generator(device="cuda").manual_seed(11)
+    x = scale * torch.randn((2, 2000), generator=g, device="cuda")
+    for params in (dict(), dict(k=[10] * 2), dict(p=[0.5] * 2), dict(m=[0.3] * 2), dict(T=[0.0] * 2)):
+        run(fq, x, [0.3, 0.8], **params)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("offset", [0, 1, 3, 5])
+def test_strided_rows_at_any_alignment(fq, dtype, offset):
+    """A slice of wider rows, NaN on both sides of it, rows beginning anywhere within 16 bytes."""
+    V, ld = 4999, 5013
+    pool = torch.full((5, ld), math.nan, dtype=dtype, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(13)
+    x = pool[:, offset:offset + V]
+    x.copy_(2.0 * torch.randn((5, V), generator=g, device="cuda"))
+    run(fq, x, [0.0, 0.25, 0.5, 0.75, 0.9999], k=[0, 0, 40, 40, 40], p=[1.0, 0.8, 1.0, 0.9, 0.5])
+
+
+def test_numbers_outside_the_unit_interval(fq):
+    x = torch.zeros((4, 1000), device="cuda")
+    token, _ = fq.fq_sample(x, torch.tensor([-0.5, 1.0, 7.0, math.inf], device="cuda"), None, torch.full((4,), 10, dtype=torch.int32, device="cuda"))
+    assert token.tolist() == [0, 9, 9, 9]
+
+
+def test_frequencies(fq):
+    """Evenly spaced numbers draw every token as often as its probability says, within one."""
+    x = torch.log(torch.tensor([1.0, 2.0, 3.0, 4.0, 6.0], device="cuda"))[None].expand(1600, 5).contiguous()
+    u = (torch.arange(1600, device="cuda") + 0.5) / 1600
+    token, _ = fq.fq_sample(x, u)
+    assert (torch.bincount(token.cpu().long(), minlength=5) - torch.tensor([100, 200, 300, 400, 600])).abs().max() <= 1
+
+
+def test_captured_and_repeated(fq):
+    g = torch.Generator(device="cuda").manual_seed(17)
+    x = (2.5 * torch.randn((33, 50001), generator=g, device="cuda")).bfloat16()
+    u = torch.rand(33, generator=g, device="cuda")
+    T, p, k = torch.full((33,), 0.9, device="cuda"), torch.full((33,), 0.9, device="cuda"), torch.full((33,), 500, dtype=torch.int32, device="cuda")
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        want = fq.fq_sample(x, u, T, k, p)
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = fq.fq_sample(x, u, T, k, p)
+    for _ in range(4):
+        graph.replay()
+        other = fq.fq_sample(x[:3, :1000], u[:3])
+        torch.cuda.synchronize()
+        want = fq.fq_sample(x, u, T, k, p)
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]) and other[0].numel() == 3
+        x.mul_(0.9)
+        u.copy_(u.flip(0))
+
+
+def test_workspace_is_the_callers(fq):
+    x, u = torch.randn((3, 9000), device="cuda"), torch.rand(3, device="cuda")
+    need = fq.fq_sample_workspace_bytes(3, 9000)
+    pool = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+    k = torch.full((3,), 9, dtype=torch.int32, device="cuda")
+    got = fq.fq_sample(x, u, None, k, workspace=pool[16: 16 + need])
+    want = fq.fq_sample(x, u, None, k)
+    assert torch.equal(got[0], want[0]) and (pool[:16] == 0xFF).all() and (pool[16 + need:] == 0xFF).all()
+    with pytest.raises(fq.FireqError):
+        fq.fq_sample(x, u, workspace=pool[16: need])
