@@ -53,25 +53,36 @@ struct fqc_cursor {
         within = t0 - page * tiles_per_page;
         fetch(lane);
     }
+    // where the next NT tiles lie, and what their scales are or-ed with; behind the range its last tile again
     template <int NT>
-    __device__ __forceinline__ void next(fqa_tile (&t)[NT], int lane) {
+    __device__ __forceinline__ void places(const uint8_t* (&p)[NT], int (&lost)[NT], int lane) {
         if (page - first > 64 - NT) {
             first = page;
             fetch(lane);
         }
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            const int id = __builtin_amdgcn_readlane(ids, page - first), lost = id < 0 ? 0x7F7F7F7F : 0;
-            const uint8_t* p = head + (((unsigned long long)(unsigned)(id < 0 ? 0 : id) * page_stride) << 4) + (unsigned)(within * FQP_TILE);
-            t[i].k = *reinterpret_cast<const fq_v4i*>(p + 16 * lane);
-            t[i].v = *reinterpret_cast<const fq_v4i*>(p + 1024 + 16 * lane);
-            t[i].s = *reinterpret_cast<const fq_v2i*>(p + 2048 + 8 * (lane >> 4)) | lost;
+            const int id = __builtin_amdgcn_readlane(ids, page - first);
+            lost[i] = id < 0 ? 0x7F7F7F7F : 0;
+            p[i] = head + (((unsigned long long)(unsigned)(id < 0 ? 0 : id) * page_stride) << 4) + (unsigned)(within * FQP_TILE);
             const int on = tile < last ? 1 : 0;
             tile += on;
             within += on;
             const int over = within == tiles_per_page ? 1 : 0;
             page += over;
             within = over ? 0 : within;
+        }
+    }
+    template <int NT>
+    __device__ __forceinline__ void next(fqa_tile (&t)[NT], int lane) {
+        const uint8_t* p[NT];
+        int lost[NT];
+        places(p, lost, lane);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            t[i].k = *reinterpret_cast<const fq_v4i*>(p[i] + 16 * lane);
+            t[i].v = *reinterpret_cast<const fq_v4i*>(p[i] + 1024 + 16 * lane);
+            t[i].s = *reinterpret_cast<const fq_v2i*>(p[i] + 2048 + 8 * (lane >> 4)) | lost[i];
         }
     }
 };
@@ -91,8 +102,92 @@ __device__ __forceinline__ void fqc_move_nans(fq_v2i& s) {
     s[1] = (int)((unsigned)s[1] & ~bytes);
 }
 
-// NT (even) tiles from tile tb on.  whole: every row has all of their tokens; otherwise the others' scores become -infinity, whose probability
-// is 0 beside any finite reference (a row's before its first token too, and its factor is not 0).
+// Scores c of query tile r against NT tiles from tile tb on (times the keys' sigmas ks) -> probabilities, two tiles of them the B operand of a
+// product with values.  whole: every row has all of the tokens; otherwise the others' scores become -infinity, whose probability is 0 beside any
+// finite reference (a row's before its first token too, and its factor is not 0).
+template <int RT, int NT, bool CAP, bool BIAS>
+__device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[NT], const float (&ks)[NT][4], int r, int tb, const fqa_queries<RT>& Q,
+                                                  const fqc_rows<RT>& rows, const fqc_shape& shape, fqa_state<RT>& st, bool whole, int g,
+                                                  fq_v4i (&pt)[NT / 2]) {
+    // scores: before the row's factor f = qs, or, with a shape, whole
+    float s[NT][4], top = FQA_LOWEST;
+    const float f = CAP || BIAS ? 1.0f : Q.qs[r];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[i][e] = CAP || BIAS ? c[i][e] * ks[i][e] * Q.qs[r] : c[i][e] * ks[i][e];
+    if (CAP) {
+        bool small = true;
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) small = small && fabsf(s[i][e]) <= FQC_SMALL;
+        const bool all = __all(small);
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float y = s[i][e], u = y * y;
+                float z = y * fmaf(fmaf(fmaf(fmaf(shape.k[4], u, shape.k[3]), u, shape.k[2]), u, shape.k[1]), u, shape.k[0]);
+                if (!all) {
+                    const float far = fmaf(-shape.k2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * 1.44269504088896340736f)) + 1.0f), shape.k1);
+                    z = fabsf(y) <= FQC_SMALL ? z : far;
+                }
+                s[i][e] = z;
+            }
+    }
+    if (BIAS) {
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int d = rows.pos[r] - ((tb + i) * 16 + 4 * g + e), away = (d < 0 ? -d : d) - rows.near[r];
+                s[i][e] = fmaf(rows.slope[r], (float)away, s[i][e]);
+            }
+    }
+    if (!whole) {
+        asm volatile("");                                 // (a branch, not a selection in every step)
+        const int at = tb * 16 + 4 * g - rows.lo[r], n = rows.hi[r] - rows.lo[r];
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[i][e] = (unsigned)(at + 16 * i + e) < (unsigned)n ? s[i][e] : -__builtin_inff();
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
+    if (__any((top - st.m[r]) * f > FQA_SLACK)) {
+        const float m = fmaxf(st.m[r], fqa_over_groups_max(top)), x = __builtin_amdgcn_exp2f((st.m[r] - m) * f);
+        st.m[r] = m;
+        st.sub[r] = fmaf(m, -f, FQA_LIFT);
+        st.l[r] *= x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) st.o[r][j] *= x;
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; e += 2) {
+            float p[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) p[u] = __builtin_amdgcn_exp2f(fmaf(s[i][e + u], f, st.sub[r]));
+            pt[i / 2][2 * (i & 1) + e / 2] = __builtin_bit_cast(int, __builtin_convertvector((fq_v2f){p[0], p[1]}, fqa_v2h));
+        }
+}
+
+__device__ __forceinline__ fqa_sigmas fqc_value_sigmas(int w) {
+    fqa_sigmas s;
+    s.s[0] = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, false), fqa_v2h);
+    s.s[1] = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, true), fqa_v2h);
+    s.n[0] = s.s[0] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
+    s.n[1] = s.s[1] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
+    return s;
+}
+#define FQC_MFMA_PV(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fqa_v8h, (a)), __builtin_bit_cast(fqa_v8h, (b)), (c), 0, 0, 0)
+#define FQC_ONES ((fq_v4i){0x3C003C00, 0x3C003C00, 0x3C003C00, 0x3C003C00})
+
+// NT (even) tiles from tile tb on.
 template <int RT, int NT, bool CAP, bool BIAS>
 __device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], int tb, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows, const fqc_shape& shape,
                                          fqa_state<RT>& st, bool whole, unsigned mask, unsigned base, int g) {
@@ -113,107 +208,31 @@ __device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], int tb, const fqa_
     fq_v4i pt[RT][NT / 2];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        // scores: before the row's factor f = qs, or, with a shape, whole
-        float s[NT][4], top = FQA_LOWEST;
-        const float f = CAP || BIAS ? 1.0f : Q.qs[r];
+        fq_v4f c[NT];
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const fq_v4f c = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[i][e] = CAP || BIAS ? c[e] * ks[i][e] * Q.qs[r] : c[e] * ks[i][e];
-        }
-        if (CAP) {
-            bool small = true;
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) small = small && fabsf(s[i][e]) <= FQC_SMALL;
-            const bool all = __all(small);
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float y = s[i][e], u = y * y;
-                    float z = y * fmaf(fmaf(fmaf(fmaf(shape.k[4], u, shape.k[3]), u, shape.k[2]), u, shape.k[1]), u, shape.k[0]);
-                    if (!all) {
-                        const float far = fmaf(-shape.k2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * 1.44269504088896340736f)) + 1.0f), shape.k1);
-                        z = fabsf(y) <= FQC_SMALL ? z : far;
-                    }
-                    s[i][e] = z;
-                }
-        }
-        if (BIAS) {
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int d = rows.pos[r] - ((tb + i) * 16 + 4 * g + e), away = (d < 0 ? -d : d) - rows.near[r];
-                    s[i][e] = fmaf(rows.slope[r], (float)away, s[i][e]);
-                }
-        }
-        if (!whole) {
-            const int at = tb * 16 + 4 * g - rows.lo[r], n = rows.hi[r] - rows.lo[r];
-#pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[i][e] = (unsigned)(at + 16 * i + e) < (unsigned)n ? s[i][e] : -__builtin_inff();
-        }
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
-        if (__any((top - st.m[r]) * f > FQA_SLACK)) {
-            const float m = fmaxf(st.m[r], fqa_over_groups_max(top)), x = __builtin_amdgcn_exp2f((st.m[r] - m) * f);
-            st.m[r] = m;
-            st.sub[r] = fmaf(m, -f, FQA_LIFT);
-            st.l[r] *= x;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) st.o[r][j] *= x;
-        }
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                float p[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) p[u] = __builtin_amdgcn_exp2f(fmaf(s[i][e + u], f, st.sub[r]));
-                pt[r][i / 2][2 * (i & 1) + e / 2] = __builtin_bit_cast(int, __builtin_convertvector((fq_v2f){p[0], p[1]}, fqa_v2h));
-            }
+        for (int i = 0; i < NT; ++i) c[i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
+        fqc_probabilities<RT, NT, CAP, BIAS>(c, ks, r, tb, Q, rows, shape, st, whole, g, pt[r]);
     }
-    constexpr int ONE = 0x3C003C00;
-    const fq_v4i ones = {ONE, ONE, ONE, ONE};
 #pragma unroll
     for (int i = 0; i < NT / 2; ++i) {
-        fqa_sigmas sg[2];
+        const fqa_sigmas sg[2] = {fqc_value_sigmas(now[2 * i].s[1]), fqc_value_sigmas(now[2 * i + 1].s[1])};
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int w = now[2 * i + u].s[1];
-            sg[u].s[0] = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, false), fqa_v2h);
-            sg[u].s[1] = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, true), fqa_v2h);
-            sg[u].n[0] = sg[u].s[0] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
-            sg[u].n[1] = sg[u].s[1] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
-        }
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-            st.l[r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fqa_v8h, ones), __builtin_bit_cast(fqa_v8h, pt[r][i]), st.l[r], 0, 0, 0);
+        for (int r = 0; r < RT; ++r) st.l[r] = FQC_MFMA_PV(FQC_ONES, pt[r][i], st.l[r]);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             const fqa_v8h even = fqa_values<0>(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1]);
             const fqa_v8h odds = fqa_values<1>(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1]);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                st.o[r][2 * w] = __builtin_amdgcn_mfma_f32_16x16x32_f16(even, __builtin_bit_cast(fqa_v8h, pt[r][i]), st.o[r][2 * w], 0, 0, 0);
-                st.o[r][2 * w + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(odds, __builtin_bit_cast(fqa_v8h, pt[r][i]), st.o[r][2 * w + 1], 0, 0, 0);
+                st.o[r][2 * w] = FQC_MFMA_PV(even, pt[r][i], st.o[r][2 * w]);
+                st.o[r][2 * w + 1] = FQC_MFMA_PV(odds, pt[r][i], st.o[r][2 * w + 1]);
             }
         }
     }
 }
 
-// Tiles t0 .. t1 for a wave's rows; from token `whole0` to `whole1` all rows have all tokens.
-template <int RT, int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void fqc_range(fqc_cursor& cur, int t0, int t1, int whole0, int whole1, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows,
-                                          const fqc_shape& shape, fqa_state<RT>& st, int lane) {
-    const int g = lane >> 4;
+template <int RT, bool CAP, bool BIAS>
+__device__ __forceinline__ void fqc_begin(const fqa_queries<RT>& Q, fqa_state<RT>& st) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         // below every score (sums of 128 products of FP8 numbers and codes, at most 10^9; with a shape, FP32's own range)
@@ -223,6 +242,14 @@ __device__ __forceinline__ void fqc_range(fqc_cursor& cur, int t0, int t1, int w
 #pragma unroll
         for (int j = 0; j < 8; ++j) st.o[r][j] = (fq_v4f){0.f, 0.f, 0.f, 0.f};
     }
+}
+
+// Tiles t0 .. t1 for a wave's rows; from token `whole0` to `whole1` all rows have all tokens.
+template <int RT, int NT, bool CAP, bool BIAS>
+__device__ __forceinline__ void fqc_range(fqc_cursor& cur, int t0, int t1, int whole0, int whole1, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows,
+                                          const fqc_shape& shape, fqa_state<RT>& st, int lane) {
+    const int g = lane >> 4;
+    fqc_begin<RT, CAP, BIAS>(Q, st);
     unsigned mask = 0x03C003C0u, base = 0x4C004C00u;
     asm("" : "+s"(mask));
     asm("" : "+v"(base));
@@ -273,49 +300,61 @@ __device__ __forceinline__ int fqc_sequence_of(const fqc_args& a, int k, int G, 
     }
 }
 
-// A workgroup: one query tile of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among KVW waves
-// (one: the wave writes its rows straight out; more: they meet in LDS).
-template <int RT, int KVW, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * KVW, KVW == 1 ? 1 : RT == 1 ? 4 : RT == 2 ? 2 : 1) void fqc_kernel(fqc_args a, fqa_parts parts) {
-    constexpr int ROWS = 16 * RT, NT = 2;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
-    const int G = a.Hq / a.Hkv, tiles = (int)((long long)a.T * G / ROWS) + a.B;
-    const int kv = (int)(blockIdx.x % a.Hkv), k = tiles - 1 - (int)(blockIdx.x / a.Hkv);   // (later rows of a prompt have more tokens: they begin)
-    int tile0 = 0;
-    const int b = fqc_sequence_of(a, k, G, ROWS, lane, tile0);
-    if (b < 0) return;
-    const int start = fqc_clamp(a.starts[b], a.T), stop = fqc_clamp(a.starts[b + 1], a.T), count = stop - start;
-    const int row0 = (k - tile0) * ROWS, left = count * G - row0;   // (T * G is bounded: 32 bits hold it)
-    if (count <= 0 || left <= 0) return;
-    const int nrows = left < ROWS ? left : ROWS;
-    const int raw = a.lens[b];
-    const long long room = (long long)a.width * a.c.page;
-    const int cap = a.max_len < room ? a.max_len : (int)room;
-    const bool too_long = raw > cap;
-    const int len = too_long ? cap : raw < 0 ? 0 : raw;
-    auto row_of = [&](int i) __attribute__((always_inline)) {       // row i of the tile: token, query head
+// What a workgroup works on: rows row0 .. row0 + nrows - 1 of the (new token, query head) pairs of sequence b under key/value head kv.
+struct fqc_place {
+    int b, kv, G, start, count, row0, nrows, raw, len;
+    bool too_long;
+    template <int ROWS>
+    __device__ __forceinline__ bool find(const fqc_args& a, int lane) {
+        G = a.Hq / a.Hkv;
+        const int tiles = (int)((long long)a.T * G / ROWS) + a.B;
+        const int k = tiles - 1 - (int)(blockIdx.x / a.Hkv);   // (later rows of a prompt have more tokens: they begin)
+        kv = (int)(blockIdx.x % a.Hkv);
+        int tile0 = 0;
+        b = fqc_sequence_of(a, k, G, ROWS, lane, tile0);
+        if (b < 0) return false;
+        start = fqc_clamp(a.starts[b], a.T);
+        count = fqc_clamp(a.starts[b + 1], a.T) - start;
+        row0 = (k - tile0) * ROWS;                        // (T * G is bounded: 32 bits hold it)
+        if (count <= 0 || count * G <= row0) return false;
+        nrows = count * G - row0 < ROWS ? count * G - row0 : ROWS;
+        raw = a.lens[b];
+        const long long room = (long long)a.width * a.c.page;
+        const int cap = a.max_len < room ? a.max_len : (int)room;
+        too_long = raw > cap;
+        len = too_long ? cap : raw < 0 ? 0 : raw;
+        return true;
+    }
+    __device__ __forceinline__ size_t row(const fqc_args& a, int i) const {       // row i: token, query head
         const int x = row0 + i, t = x / G;
         return (size_t)(start + t) * a.Hq + kv * G + (x - t * G);
-    };
-    fqc_rows<RT> rows;
-    unsigned none = 0u;                                   // rows without a token: they take any range, and are zeros in the end
+    }
+};
+
+// The ranges of a wave's rows (first .. of the workgroup's), and what they have together: tokens tok0 .. tok1, all of them those from whole0 to whole1.
+// none: rows without a token, which take any range and are zeros in the end.
+struct fqc_span { int tok0, tok1, whole0, whole1; unsigned none; };
+template <int RT, bool BIAS>
+__device__ __forceinline__ fqc_span fqc_take_rows(const fqc_args& a, const fqc_place& at, int first_row, int n, fqc_rows<RT>& rows) {
+    fqc_span sp;
+    sp.none = 0u;
     int lo = 0x7FFFFFFF, hi = 0x7FFFFFFF, wlo = 0x7FFFFFFF, whi = 0x7FFFFFFF;   // the least lo and hi, and of minus them
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int i = 16 * r + n < nrows ? 16 * r + n : 0, x = row0 + i, t = x / G;
-        const int pos = raw - count + t;
-        int f = a.first ? a.first[start + t] : 0, e = a.end ? a.end[start + t] : pos + 1;
+        const int i = first_row + 16 * r + n < at.nrows ? first_row + 16 * r + n : 0, x = at.row0 + i, t = x / at.G;
+        const int pos = at.raw - at.count + t;
+        int f = a.first ? a.first[at.start + t] : 0, e = a.end ? a.end[at.start + t] : pos + 1;
         if (a.window > 0 && f < pos - a.window + 1) f = pos - a.window + 1;
         f = f < 0 ? 0 : f;
-        e = e > len ? len : e;
-        const bool empty = f >= e;
-        none |= empty ? 1u << r : 0u;
+        e = e > at.len ? at.len : e;
+        const bool empty = f >= e || first_row + 16 * r + n >= at.nrows;
+        sp.none |= empty ? 1u << r : 0u;
         rows.lo[r] = empty ? 0 : f;
         rows.hi[r] = empty ? 0x7FFFFFFF : e;
         if (BIAS) {
             rows.pos[r] = pos;
             rows.near[r] = empty ? 0 : pos < f ? f - pos : pos >= e ? pos - (e - 1) : 0;
-            rows.slope[r] = a.slopes[kv * G + (x - t * G)] * -1.44269504088896340736f;
+            rows.slope[r] = a.slopes[at.kv * at.G + (x - t * at.G)] * -1.44269504088896340736f;
         }
         if (!empty) {
             lo = f < lo ? f : lo;
@@ -324,8 +363,37 @@ __global__ __launch_bounds__(64 * KVW, KVW == 1 ? 1 : RT == 1 ? 4 : RT == 2 ? 2 
         wlo = -rows.lo[r] < wlo ? -rows.lo[r] : wlo;
         hi = rows.hi[r] < hi ? rows.hi[r] : hi;
     }
-    const int tok0 = fqc_row16_min(lo), last = fqc_row16_min(whi), tok1 = last == 0x7FFFFFFF ? 0 : -last;
-    const int whole0 = -fqc_row16_min(wlo), whole1 = fqc_row16_min(hi);
+    sp.tok0 = fqc_row16_min(lo);
+    const int last = fqc_row16_min(whi);
+    sp.tok1 = last == 0x7FFFFFFF ? 0 : -last;
+    sp.whole0 = -fqc_row16_min(wlo);
+    sp.whole1 = fqc_row16_min(hi);
+    return sp;
+}
+template <int RT, bool CAP, bool BIAS>
+__device__ __forceinline__ void fqc_take_queries(const fqc_args& a, const fqc_place& at, int first_row, int n, int g, fqa_queries<RT>& Q) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const size_t row = at.row(a, first_row + 16 * r + n < at.nrows ? first_row + 16 * r + n : 0);
+        fqa_take_query(Q, r, a.Q + row * 128, a.q_scale[row], a.out_scale, g);
+        if (!(CAP || BIAS)) Q.qs[r] = fmaxf(Q.qs[r], 1.0e-30f);
+        if (CAP) Q.qs[r] *= a.inv_cap * 0.693147180559945309417f;   // (a capped score's factor has no log2 e)
+    }
+}
+
+// Few rows: one query tile of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among the waves, which meet in LDS.
+template <int RT, int KVW, bool CAP, bool BIAS>
+__global__ __launch_bounds__(64 * KVW, RT == 1 ? 4 : RT == 2 ? 2 : 1) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
+    constexpr int ROWS = 16 * RT, NT = 2;
+    __shared__ fqa_shared<RT, KVW> sh;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    fqc_place at;
+    if (!at.find<ROWS>(a, lane)) return;
+    fqc_rows<RT> rows;
+    const fqc_span sp = fqc_take_rows<RT, BIAS>(a, at, 0, n, rows);
+    const int tok0 = sp.tok0, tok1 = sp.tok1, whole0 = sp.whole0, whole1 = sp.whole1, nrows = at.nrows;
+    const unsigned none = sp.none;
+    const bool too_long = at.too_long;
     const int first_tile = tok1 > 0 ? tok0 >> 4 : 0, all = tok1 > 0 ? ((tok1 + 15) >> 4) - first_tile : 0;
     // this workgroup's part, and the waves' shares: steps of NT tiles
     const int part = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, c0 = first_tile + (int)blockIdx.y * part;
@@ -335,105 +403,246 @@ __global__ __launch_bounds__(64 * KVW, KVW == 1 ? 1 : RT == 1 ? 4 : RT == 2 ? 2 
     const bool work = t0 < t1;
     if (work) {
         fqc_cursor cur;
-        cur.pages_of = a.table + (size_t)b * a.width;
-        cur.head = a.c.base + kv * a.c.head_stride;
+        cur.pages_of = a.table + (size_t)at.b * a.width;
+        cur.head = a.c.base + at.kv * a.c.head_stride;
         cur.page_stride = (unsigned)(a.c.page_stride >> 4);
         cur.tiles_per_page = a.c.page >> 4;
         cur.pages = a.c.pages;
         cur.start(t0, t1, lane);
         fqa_queries<RT> Q;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const size_t row = row_of(16 * r + n < nrows ? 16 * r + n : 0);
-            fqa_take_query(Q, r, a.Q + row * 128, a.q_scale[row], a.out_scale, g);
-            if (!(CAP || BIAS)) Q.qs[r] = fmaxf(Q.qs[r], 1.0e-30f);
-            if (CAP) Q.qs[r] *= a.inv_cap * 0.693147180559945309417f;   // (a capped score's factor has no log2 e)
-        }
+        fqc_take_queries<RT, CAP, BIAS>(a, at, 0, n, g, Q);
         fqc_range<RT, NT, CAP, BIAS>(cur, t0, t1, whole0, whole1 < 16 * t1 ? whole1 : 16 * t1, Q, rows, a.shape, st, lane);
     }
-    if constexpr (KVW == 1) {
+    if (work) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            if (16 * r + n >= nrows) continue;
-            const bool zero = !work || (none >> r & 1u) != 0u;
-            const float l = too_long ? __builtin_nanf("") : zero ? 0.f : st.l[r][0];
-            uint16_t* dst = a.O + row_of(16 * r + n) * 128 + 4 * g;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint2*>(dst + 16 * j) = fqa_output(zero ? (fq_v4f){0.f, 0.f, 0.f, 0.f} : st.o[r][j], l);
-        }
-    } else {
-        __shared__ fqa_shared<RT, KVW> sh;
-        if (work) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                if (g == 0) {
-                    sh.m[wave][16 * r + n] = st.m[r];
-                    sh.l[wave][16 * r + n] = too_long ? __builtin_nanf("") : (none >> r & 1u) != 0u ? 0.f : st.l[r][0];
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(&sh.o[wave][16 * r + n][16 * j + 4 * g]) = st.o[r][j];
+            if (g == 0) {
+                sh.m[wave][16 * r + n] = st.m[r];
+                sh.l[wave][16 * r + n] = too_long ? __builtin_nanf("") : (none >> r & 1u) != 0u ? 0.f : st.l[r][0];
             }
-        } else if (lane < ROWS) {
-            sh.m[wave][lane] = FQA_LOWEST;
-            sh.l[wave][lane] = too_long ? __builtin_nanf("") : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(&sh.o[wave][16 * r + n][16 * j + 4 * g]) = st.o[r][j];
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < nrows * 32; i += 64 * KVW) {  // four channels of a row
-            const int r = i >> 5, c = 4 * (i & 31);
-            float top = FQA_LOWEST, l = 0.f;
+    } else if (lane < ROWS) {
+        sh.m[wave][lane] = FQA_LOWEST;
+        sh.l[wave][lane] = too_long ? __builtin_nanf("") : 0.f;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < nrows * 32; i += 64 * KVW) {  // four channels of a row
+        const int r = i >> 5, c = 4 * (i & 31);
+        float top = FQA_LOWEST, l = 0.f;
 #pragma unroll
-            for (int w = 0; w < KVW; ++w)
-                if (sh.l[w][r] != 0.f) top = fmaxf(top, sh.m[w][r]);
-            fq_v4f o = {0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < KVW; ++w)
+            if (sh.l[w][r] != 0.f) top = fmaxf(top, sh.m[w][r]);
+        fq_v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < KVW; ++w) {
-                if (sh.l[w][r] == 0.f) continue;          // (a wave without tokens of this row; a NaN is kept)
-                const float f = __builtin_amdgcn_exp2f(sh.m[w][r] - top);
-                l += sh.l[w][r] * f;
-                o += *reinterpret_cast<const fq_v4f*>(&sh.o[w][r][c]) * f;
-            }
-            const size_t row = row_of(r);
-            if (a.slots == 1) {
-                *reinterpret_cast<uint2*>(a.O + row * 128 + c) = fqa_output(o, l);
-            } else {
-                const size_t at = row * parts.slots + blockIdx.y;
-                *reinterpret_cast<fq_v4f*>(parts.o + at * 128 + c) = o;
-                if (c == 0) {
-                    parts.ml[at * 2] = top;
-                    parts.ml[at * 2 + 1] = l;
-                }
+        for (int w = 0; w < KVW; ++w) {
+            if (sh.l[w][r] == 0.f) continue;          // (a wave without tokens of this row; a NaN is kept)
+            const float f = __builtin_amdgcn_exp2f(sh.m[w][r] - top);
+            l += sh.l[w][r] * f;
+            o += *reinterpret_cast<const fq_v4f*>(&sh.o[w][r][c]) * f;
+        }
+        const size_t row = at.row(a, r);
+        if (a.slots == 1) {
+            *reinterpret_cast<uint2*>(a.O + row * 128 + c) = fqa_output(o, l);
+        } else {
+            const size_t place = row * parts.slots + blockIdx.y;
+            *reinterpret_cast<fq_v4f*>(parts.o + place * 128 + c) = o;
+            if (c == 0) {
+                parts.ml[place * 2] = top;
+                parts.ml[place * 2 + 1] = l;
             }
         }
     }
 }
 
-// rt: query tiles of a wave; waves: of a workgroup, sharing out its tokens; slots: parts of a row's tokens.
-struct fqc_plan { int rt, waves, slots; };
+// Many rows: four waves with a query tile each (16 RT rows) walk the same tokens, 32 of a step.  Each wave unpacks a quarter of the step's codes into LDS,
+// where all read their operands; the next step's codes are unpacked while this one's products run, and those behind it are on their way.
+// Bound by vector instructions: per step and wave 30 to unpack its quarter, then 24 and 8 exponentials (16 cycles each) per 16 rows, beside 18 matrix
+// instructions of 16 to 32 cycles on the other pipe.
+struct fqc_stage {
+    fq_v4i k[2][2][64];                                   // keys' bytes: tile, low and high nibbles, lane
+    fq_v4i v[8][64];                                      // values in fp16: 16 channels, lane
+    float ks[2][16];                                      // keys' sigmas
+};
+struct fqc_fetched { fq_v4i k; int v[2]; fq_v2i s[2]; };  // a wave's quarter of two tiles
+
+template <int RT, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts parts) {
+    constexpr int ROWS = 64 * RT;
+    __shared__ fqc_stage stage[2];
+    __shared__ int span[4][2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    fqc_place at;
+    if (!at.find<ROWS>(a, lane)) return;
+    fqc_rows<RT> rows;
+    const int first_row = 16 * RT * wave;
+    const fqc_span sp = fqc_take_rows<RT, BIAS>(a, at, first_row, n, rows);
+    if (lane == 0) {
+        span[wave][0] = sp.tok1 > 0 ? sp.tok0 : 0x7FFFFFFF;
+        span[wave][1] = sp.tok1;
+    }
+    __syncthreads();
+    int tok0 = 0x7FFFFFFF, tok1 = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        tok0 = span[w][0] < tok0 ? span[w][0] : tok0;
+        tok1 = span[w][1] > tok1 ? span[w][1] : tok1;
+    }
+    tok0 = __builtin_amdgcn_readfirstlane(tok0);
+    tok1 = __builtin_amdgcn_readfirstlane(tok1);
+    const int first_tile = tok1 > 0 ? tok0 >> 4 : 0, all = tok1 > 0 ? ((tok1 + 15) >> 4) - first_tile : 0;
+    const int part = ((all + a.slots - 1) / a.slots + 1) & ~1, t0 = first_tile + (int)blockIdx.y * part;
+    const int t1 = t0 + part < first_tile + all ? t0 + part : first_tile + all;
+    const int whole0 = sp.whole0, whole1 = sp.whole1 < 16 * t1 ? sp.whole1 : 16 * t1;
+    fqa_state<RT> st;
+    fqa_queries<RT> Q;
+    fqc_take_queries<RT, CAP, BIAS>(a, at, first_row, n, g, Q);
+    fqc_begin<RT, CAP, BIAS>(Q, st);
+    unsigned mask = 0x03C003C0u, base = 0x4C004C00u;
+    asm("" : "+s"(mask));
+    asm("" : "+v"(base));
+    if (t0 < t1) {
+        fqc_cursor cur;
+        cur.pages_of = a.table + (size_t)at.b * a.width;
+        cur.head = a.c.base + at.kv * a.c.head_stride;
+        cur.page_stride = (unsigned)(a.c.page_stride >> 4);
+        cur.tiles_per_page = a.c.page >> 4;
+        cur.pages = a.c.pages;
+        cur.start(t0, t1, lane);
+        const int my_tile = wave & 1, half = wave >> 1;
+        auto fetch = [&](fqc_fetched& f) __attribute__((always_inline)) {
+            const uint8_t* p[2];
+            int lost[2];
+            cur.places(p, lost, lane);
+            f.k = *reinterpret_cast<const fq_v4i*>((my_tile ? p[1] : p[0]) + 16 * lane);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f.v[i] = *reinterpret_cast<const int*>(p[i] + 1024 + 16 * lane + 4 * wave);
+                f.s[i] = *reinterpret_cast<const fq_v2i*>(p[i] + 2048 + 8 * g) | lost[i];
+            }
+        };
+        auto unpack = [&](fqc_fetched& f, fqc_stage& to) __attribute__((always_inline)) {
+            unsigned odd = (((unsigned)f.s[0][1] & 0x7F7F7F7Fu) + 0x01010101u) | (((unsigned)f.s[1][1] & 0x7F7F7F7Fu) + 0x01010101u);
+            if (__any((odd & 0x80808080u) != 0u)) {
+                fqc_move_nans(f.s[0]);
+                fqc_move_nans(f.s[1]);
+            }
+            fq_v4i k;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = (int)((half ? (unsigned)f.k[i] >> 4 : (unsigned)f.k[i]) & 0x0F0F0F0Fu);
+            to.k[my_tile][half][lane] = k;
+            const fqa_sigmas s0 = fqc_value_sigmas(f.s[0][1]), s1 = fqc_value_sigmas(f.s[1][1]);
+            to.v[2 * wave][lane] = __builtin_bit_cast(fq_v4i, fqa_values<0>(f.v[0], f.v[1], mask, base, s0, s1));
+            to.v[2 * wave + 1][lane] = __builtin_bit_cast(fq_v4i, fqa_values<1>(f.v[0], f.v[1], mask, base, s0, s1));
+            if (wave < 2 && n == 0) {
+                const int w = wave ? f.s[1][0] : f.s[0][0];
+                const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                *reinterpret_cast<fq_v4f*>(&to.ks[wave][4 * g]) = (fq_v4f){s01[0], s01[1], s23[0], s23[1]};
+            }
+        };
+        auto products = [&](const fqc_stage& from, int tb) __attribute__((always_inline)) {
+            if (tb * 16 >= sp.tok1 || (tb + 2) * 16 <= sp.tok0) return;   // (none of this wave's rows has any of them)
+            const bool whole = tb * 16 >= whole0 && (tb + 2) * 16 <= whole1;
+            fq_v8i k[2];
+            float ks[2][4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const fq_v4i lo = from.k[i][0][lane], hi = from.k[i][1][lane];
+                k[i] = (fq_v8i){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                const fq_v4f s = *reinterpret_cast<const fq_v4f*>(&from.ks[i][4 * g]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ks[i][e] = s[e];
+            }
+            fq_v4i pt[RT][1];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                fq_v4f c[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) c[i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
+                fqc_probabilities<RT, 2, CAP, BIAS>(c, ks, r, tb, Q, rows, a.shape, st, whole, g, pt[r]);
+            }
+#pragma unroll
+            for (int r = 0; r < RT; ++r) st.l[r] = FQC_MFMA_PV(FQC_ONES, pt[r][0], st.l[r]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const fq_v4i v = from.v[j][lane];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) st.o[r][j] = FQC_MFMA_PV(v, pt[r][0], st.o[r][j]);
+            }
+        };
+        fqc_fetched f;
+        fetch(f);
+        unpack(f, stage[0]);
+        if (t0 + 2 < t1) fetch(f);
+        for (int tb = t0; tb < t1; tb += 4) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int now = tb + 2 * u;
+                if (now >= t1) break;
+                __syncthreads();                          // this step's operands are there, and the other stage is free
+                if (now + 2 < t1) unpack(f, stage[u ^ 1]);
+                if (now + 4 < t1) fetch(f);
+                products(stage[u], now);
+            }
+        }
+        if (!(CAP || BIAS))
+#pragma unroll
+            for (int r = 0; r < RT; ++r) st.m[r] *= Q.qs[r];
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int i = first_row + 16 * r + n;
+        if (i >= at.nrows) continue;
+        const size_t row = at.row(a, i);
+        const bool zero = t0 >= t1 || (sp.none >> r & 1u) != 0u;
+        const float l = at.too_long ? __builtin_nanf("") : zero ? 0.f : st.l[r][0];
+        if (a.slots == 1) {
+            uint16_t* dst = a.O + row * 128 + 4 * g;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint2*>(dst + 16 * j) = fqa_output(zero ? (fq_v4f){0.f, 0.f, 0.f, 0.f} : st.o[r][j], l);
+        } else {
+            const size_t place = row * parts.slots + blockIdx.y;
+            if (g == 0) {
+                parts.ml[place * 2] = st.m[r];
+                parts.ml[place * 2 + 1] = l;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(parts.o + place * 128 + 16 * j + 4 * g) = st.o[r][j];
+        }
+    }
+}
+
+#ifndef FQC_MANY_RT
+#define FQC_MANY_RT 2
+#endif
+// few: 16 * few rows of a query tile, whose tokens four waves share out (0: many rows); slots: parts of a row's tokens.
+struct fqc_plan { int few, slots; };
 fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
     const int G = Hq / Hkv, cus = fq_device_cus();
     const long long most = (long long)(max_new < T ? max_new : T) * G;
-    fqc_plan p = {most <= 16 ? 1 : most <= 32 ? 2 : 4, 4, 1};
-    const long long tiles = ((long long)max_len + 15) / 16, groups = ((long long)T * G + 16 * p.rt - 1) / (16 * p.rt) > B ? ((long long)T * G + 16 * p.rt - 1) / (16 * p.rt) : B;
-    const long long units = groups * Hkv;
-    if (p.rt == 4 && units >= 4 * cus) {
-        p.waves = 1;
-        return p;
-    }
-    const long long want = units < cus ? cus / units : 1, room = tiles / 16;
-    long long slots = want < room ? want : room;
-    if (slots > 64) slots = 64;
-    p.slots = (int)(slots < 1 ? 1 : slots);
+    fqc_plan p = {most <= 16 ? 1 : most <= 32 ? 2 : 0, 1};
+    const int rows = p.few ? 16 * p.few : 64 * FQC_MANY_RT;
+    const long long tiles = ((long long)max_len + 15) / 16, units = ((long long)T * G / rows + B) * Hkv, room = tiles / 16;
+    const long long want = (p.few ? cus : 2 * cus) / units, slots = want < room ? want : room;
+    p.slots = (int)(slots < 1 ? 1 : slots > 64 ? 64 : slots);
     return p;
 }
 
-template <int RT, int KVW>
+template <int FEW, bool CAP, bool BIAS>
 void fqc_launch(const fqc_args& a, const fqa_parts& parts, hipStream_t stream) {
-    const dim3 grid((unsigned)(((long long)a.T * (a.Hq / a.Hkv) / (16 * RT) + a.B) * a.Hkv), (unsigned)a.slots), block(64 * KVW);
+    constexpr int ROWS = FEW ? 16 * FEW : 64 * FQC_MANY_RT;
+    const dim3 grid((unsigned)(((long long)a.T * (a.Hq / a.Hkv) / ROWS + a.B) * a.Hkv), (unsigned)a.slots);
+    if constexpr (FEW != 0) hipLaunchKernelGGL((fqc_few_kernel<FEW, 4, CAP, BIAS>), grid, dim3(256), 0, stream, a, parts);
+    else hipLaunchKernelGGL((fqc_many_kernel<FQC_MANY_RT, CAP, BIAS>), grid, dim3(256), 0, stream, a, parts);
+}
+template <int FEW>
+void fqc_launch(const fqc_args& a, const fqa_parts& parts, hipStream_t stream) {
     const bool cap = a.inv_cap != 0.f, bias = a.slopes != nullptr;
-    if (cap && bias) hipLaunchKernelGGL((fqc_kernel<RT, KVW, true, true>), grid, block, 0, stream, a, parts);
-    else if (cap) hipLaunchKernelGGL((fqc_kernel<RT, KVW, true, false>), grid, block, 0, stream, a, parts);
-    else if (bias) hipLaunchKernelGGL((fqc_kernel<RT, KVW, false, true>), grid, block, 0, stream, a, parts);
-    else hipLaunchKernelGGL((fqc_kernel<RT, KVW, false, false>), grid, block, 0, stream, a, parts);
+    if (cap && bias) fqc_launch<FEW, true, true>(a, parts, stream);
+    else if (cap) fqc_launch<FEW, true, false>(a, parts, stream);
+    else if (bias) fqc_launch<FEW, false, true>(a, parts, stream);
+    else fqc_launch<FEW, false, false>(a, parts, stream);
 }
 
 }  // namespace
@@ -452,9 +661,8 @@ void fq_launch_chunk(const fq_chunk_args& x, void* scratch, hipStream_t stream) 
     a.shape.k1 = (float)k1;
     a.shape.k2 = (float)(2.0 * k1);
     const fqa_parts parts = {static_cast<float*>(scratch), static_cast<float*>(scratch) + (size_t)p.slots * x.T * x.Hq * 128, p.slots};
-    if (p.waves == 1) fqc_launch<4, 1>(a, parts, stream);
-    else if (p.rt == 4) fqc_launch<4, 4>(a, parts, stream);
-    else if (p.rt == 2) fqc_launch<2, 4>(a, parts, stream);
-    else fqc_launch<1, 4>(a, parts, stream);
+    if (p.few == 1) fqc_launch<1>(a, parts, stream);
+    else if (p.few == 2) fqc_launch<2>(a, parts, stream);
+    else fqc_launch<0>(a, parts, stream);
     if (p.slots > 1) fqa_join(parts, x.O, x.T * x.Hq, stream, x.starts, x.B, x.Hq);
 }
