@@ -102,78 +102,120 @@ __device__ __forceinline__ void fqc_move_nans(fq_v2i& s) {
     s[1] = (int)((unsigned)s[1] & ~bytes);
 }
 
-// Scores c of query tile r against NT tiles from tile tb on (times the keys' sigmas ks) -> probabilities, two tiles of them the B operand of a
+// Products c of RT query tiles and NT tiles from tile tb on, with the keys' sigmas ks -> probabilities, two tiles of them the B operand of a
 // product with values.  whole: every row has all of the tokens; otherwise the others' scores become -infinity, whose probability is 0 beside any
-// finite reference (a row's before its first token too, and its factor is not 0).
+// finite reference (a row's before its first token too, and its factor is not 0).  The query tiles go through each stage together: one branch for all,
+// and each one's chain of instructions beside the others'.
 template <int RT, int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[NT], const float (&ks)[NT][4], int r, int tb, const fqa_queries<RT>& Q,
+__device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], const float (&ks)[NT][4], int tb, const fqa_queries<RT>& Q,
                                                   const fqc_rows<RT>& rows, const fqc_shape& shape, fqa_state<RT>& st, bool whole, int g,
-                                                  fq_v4i (&pt)[NT / 2]) {
+                                                  fq_v4i (&pt)[RT][NT / 2]) {
+    constexpr bool SHAPED = CAP || BIAS;
     // scores: before the row's factor f = qs, or, with a shape, whole
-    float s[NT][4], top = FQA_LOWEST;
-    const float f = CAP || BIAS ? 1.0f : Q.qs[r];
+    float s[RT][NT][4];
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] = CAP || BIAS ? c[i][e] * ks[i][e] * Q.qs[r] : c[i][e] * ks[i][e];
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[r][i][e] = BIAS && !CAP ? c[r][i][e] * ks[i][e] * Q.qs[r] : c[r][i][e] * ks[i][e];
     if (CAP) {
-        bool small = true;
+        // y = t * qs; while every |y| is small, the polynomial alone
+        float most = 0.f;
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+        for (int r = 0; r < RT; ++r) {
+            float top = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) small = small && fabsf(s[i][e]) <= FQC_SMALL;
-        const bool all = __all(small);
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+                for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(s[r][i][e]));
+            most = fmaxf(most, top * Q.qs[r]);
+        }
+        auto small = [&](float u) __attribute__((always_inline)) {
+            return fmaf(fmaf(fmaf(fmaf(shape.k[4], u, shape.k[3]), u, shape.k[2]), u, shape.k[1]), u, shape.k[0]);
+        };
+        if (!__any(!(most <= FQC_SMALL))) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float y = s[i][e], u = y * y;
-                float z = y * fmaf(fmaf(fmaf(fmaf(shape.k[4], u, shape.k[3]), u, shape.k[2]), u, shape.k[1]), u, shape.k[0]);
-                if (!all) {
-                    const float far = fmaf(-shape.k2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * (2.0f * 1.44269504088896340736f)) + 1.0f), shape.k1);
-                    z = fabsf(y) <= FQC_SMALL ? z : far;
-                }
-                s[i][e] = z;
-            }
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = s[r][i][e] * Q.qs[r];
+                        s[r][i][e] = y * small(y * y);
+                    }
+        } else {
+            float two = 2.0f * 1.44269504088896340736f;
+            asm volatile("" : "+v"(two));                 // (a branch: nothing of this beside the other)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = s[r][i][e] * Q.qs[r], z = y * small(y * y);
+                        const float far = fmaf(-shape.k2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * two) + 1.0f), shape.k1);
+                        s[r][i][e] = fabsf(y) <= FQC_SMALL ? z : far;
+                    }
+        }
     }
     if (BIAS) {
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = rows.pos[r] - ((tb + i) * 16 + 4 * g + e), away = (d < 0 ? -d : d) - rows.near[r];
-                s[i][e] = fmaf(rows.slope[r], (float)away, s[i][e]);
-            }
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int d = rows.pos[r] - ((tb + i) * 16 + 4 * g + e), away = (d < 0 ? -d : d) - rows.near[r];
+                    s[r][i][e] = fmaf(rows.slope[r], (float)away, s[r][i][e]);
+                }
     }
     if (!whole) {
-        asm volatile("");                                 // (a branch, not a selection in every step)
-        const int at = tb * 16 + 4 * g - rows.lo[r], n = rows.hi[r] - rows.lo[r];
+        int here = tb * 16 + 4 * g;
+        asm volatile("" : "+v"(here));                    // (a branch, not selections in every step)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int at = here - rows.lo[r], n = rows.hi[r] - rows.lo[r];
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[r][i][e] = (unsigned)(at + 16 * i + e) < (unsigned)n ? s[r][i][e] : -__builtin_inff();
+        }
+    }
+    float top[RT];
+    bool past = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        top[r] = FQA_LOWEST;
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[i][e] = (unsigned)(at + 16 * i + e) < (unsigned)n ? s[i][e] : -__builtin_inff();
+            for (int e = 0; e < 4; ++e) top[r] = fmaxf(top[r], s[r][i][e]);
+        past = past || (SHAPED ? top[r] - st.m[r] : (top[r] - st.m[r]) * Q.qs[r]) > FQA_SLACK;
     }
+    if (__any(past))
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+        for (int r = 0; r < RT; ++r) {
+            const float f = SHAPED ? 1.0f : Q.qs[r], over = fqa_over_groups_max(top[r]);
+            // (a row that is not past its slack keeps its reference, whatever the others do)
+            const float m = (over - st.m[r]) * f > FQA_SLACK ? over : st.m[r], x = __builtin_amdgcn_exp2f((st.m[r] - m) * f);
+            st.m[r] = m;
+            st.sub[r] = fmaf(m, -f, FQA_LIFT);
+            st.l[r] *= x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, s[i][e]);
-    if (__any((top - st.m[r]) * f > FQA_SLACK)) {
-        const float m = fmaxf(st.m[r], fqa_over_groups_max(top)), x = __builtin_amdgcn_exp2f((st.m[r] - m) * f);
-        st.m[r] = m;
-        st.sub[r] = fmaf(m, -f, FQA_LIFT);
-        st.l[r] *= x;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) st.o[r][j] *= x;
-    }
-#pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; e += 2) {
-            float p[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) p[u] = __builtin_amdgcn_exp2f(fmaf(s[i][e + u], f, st.sub[r]));
-            pt[i / 2][2 * (i & 1) + e / 2] = __builtin_bit_cast(int, __builtin_convertvector((fq_v2f){p[0], p[1]}, fqa_v2h));
+            for (int j = 0; j < 8; ++j) st.o[r][j] *= x;
         }
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2) {
+                float p[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) p[u] = __builtin_amdgcn_exp2f(SHAPED ? s[r][i][e + u] + st.sub[r] : fmaf(s[r][i][e + u], Q.qs[r], st.sub[r]));
+                pt[r][i / 2][2 * (i & 1) + e / 2] = __builtin_bit_cast(int, __builtin_convertvector((fq_v2f){p[0], p[1]}, fqa_v2h));
+            }
 }
 
 __device__ __forceinline__ fqa_sigmas fqc_value_sigmas(int w) {
@@ -206,13 +248,12 @@ __device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], int tb, const fqa_
         ks[i][0] = s01[0]; ks[i][1] = s01[1]; ks[i][2] = s23[0]; ks[i][3] = s23[1];
     }
     fq_v4i pt[RT][NT / 2];
+    fq_v4f c[RT][NT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        fq_v4f c[NT];
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int i = 0; i < NT; ++i) c[i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
-        fqc_probabilities<RT, NT, CAP, BIAS>(c, ks, r, tb, Q, rows, shape, st, whole, g, pt[r]);
-    }
+        for (int i = 0; i < NT; ++i) c[r][i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
+    fqc_probabilities<RT, NT, CAP, BIAS>(c, ks, tb, Q, rows, shape, st, whole, g, pt);
 #pragma unroll
     for (int i = 0; i < NT / 2; ++i) {
         const fqa_sigmas sg[2] = {fqc_value_sigmas(now[2 * i].s[1]), fqc_value_sigmas(now[2 * i + 1].s[1])};
@@ -467,8 +508,11 @@ struct fqc_stage {
 };
 struct fqc_fetched { fq_v4i k; int v[2]; fq_v2i s[2]; };  // a wave's quarter of two tiles
 
+#ifndef FQC_MANY_WAVES
+#define FQC_MANY_WAVES 2
+#endif
 template <int RT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts parts) {
+__global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args a, fqa_parts parts) {
     constexpr int ROWS = 64 * RT;
     __shared__ fqc_stage stage[2];
     __shared__ int span[4][2];
@@ -555,13 +599,12 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
                 for (int e = 0; e < 4; ++e) ks[i][e] = s[e];
             }
             fq_v4i pt[RT][1];
+            fq_v4f c[RT][2];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                fq_v4f c[2];
+            for (int r = 0; r < RT; ++r)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) c[i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
-                fqc_probabilities<RT, 2, CAP, BIAS>(c, ks, r, tb, Q, rows, a.shape, st, whole, g, pt[r]);
-            }
+                for (int i = 0; i < 2; ++i) c[r][i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
+            fqc_probabilities<RT, 2, CAP, BIAS>(c, ks, tb, Q, rows, a.shape, st, whole, g, pt);
 #pragma unroll
             for (int r = 0; r < RT; ++r) st.l[r] = FQC_MFMA_PV(FQC_ONES, pt[r][0], st.l[r]);
 #pragma unroll
