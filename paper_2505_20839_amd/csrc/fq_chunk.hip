@@ -87,6 +87,57 @@ struct fqc_cursor {
     }
 };
 
+// The same for a longer walk: where 64 of them lie is worked out at a time, a tile a lane, from page numbers requested 64 tiles before;
+// a step reads two lanes and adds.  A tile of a page outside the cache has NaN scales.
+struct fqc_walk {
+    const int* pages_of;
+    const uint8_t* head;
+    unsigned page_stride;                                 // in 16 bytes
+    int last, tile, first, tiles_per_page, pages;
+    int id;                                               // lane l: the page of tile first + 64 + l
+    unsigned lo, hi;                                      // lane l: where tile first + l lies
+    unsigned long long lost;                              // bit l: its page is outside the cache
+    __device__ __forceinline__ int page_of(int lane) const {
+        const int t = first + lane < last ? first + lane : last;
+        return (int)((unsigned)t / (unsigned)tiles_per_page);
+    }
+    __device__ __forceinline__ void window(int lane) {    // the window whose pages are in `id`, from tile `first` on
+        const int t = first + lane < last ? first + lane : last, page = page_of(lane);
+        const bool ok = (unsigned)id < (unsigned)pages;
+        const unsigned long long at = ((unsigned long long)(ok ? (unsigned)id : 0u) * page_stride << 4) + (unsigned)((t - page * tiles_per_page) * FQP_TILE);
+        lo = (unsigned)at;
+        hi = (unsigned)(at >> 32);
+        lost = __ballot(!ok);
+        first += 64;
+        id = pages_of[page_of(lane)];
+        first -= 64;
+    }
+    __device__ __forceinline__ void start(int t0, int t1, int lane) {
+        tile = first = t0;
+        last = t1 - 1;
+        id = pages_of[page_of(lane)];
+        window(lane);
+    }
+    __device__ __forceinline__ void refill(int lane) {    // before every `places`
+        if (tile - first >= 64) {
+            first += 64;
+            window(lane);
+        }
+    }
+    // where the next NT tiles lie, and what their scales are or-ed with; behind the range its last tile again.  (64 is a multiple of NT, and every
+    // call of a range takes the same.)
+    template <int NT>
+    __device__ __forceinline__ void places(const uint8_t* (&p)[NT], int (&bad)[NT]) {
+        const int j = tile - first;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            p[i] = head + ((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)hi, j + i) << 32 | (unsigned)__builtin_amdgcn_readlane((int)lo, j + i));
+            bad[i] = lost >> (j + i) & 1ull ? 0x7F7F7F7F : 0;
+        }
+        tile += NT;
+    }
+};
+
 // A wave's rows: lane n (and n + 16, ..) has row 16 r + n of each query tile r.
 template <int RT>
 struct fqc_rows {
@@ -501,20 +552,25 @@ __global__ __launch_bounds__(64 * KVW, RT == 1 ? 4 : RT == 2 ? 2 : 1) void fqc_f
 // where all read their operands; the next step's codes are unpacked while this one's products run, and those behind it are on their way.
 // Bound by vector instructions: per step and wave 30 to unpack its quarter, then 24 and 8 exponentials (16 cycles each) per 16 rows, beside 18 matrix
 // instructions of 16 to 32 cycles on the other pipe.
+#ifndef FQC_MANY_NT
+#define FQC_MANY_NT 4
+#endif
+template <int NT>
 struct fqc_stage {
-    fq_v4i k[2][2][64];                                   // keys' bytes: tile, low and high nibbles, lane
-    fq_v4i v[8][64];                                      // values in fp16: 16 channels, lane
-    float ks[2][16];                                      // keys' sigmas
+    fq_v4i k[NT][2][64];                                  // keys' bytes: tile, low and high nibbles, lane
+    fq_v4i v[NT / 2][8][64];                              // values in fp16: two tiles, 16 channels, lane
+    float ks[NT][16];                                     // keys' sigmas
 };
-struct fqc_fetched { fq_v4i k; int v[2]; fq_v2i s[2]; };  // a wave's quarter of two tiles
+template <int NT>
+struct fqc_fetched { fq_v4i k; int v[NT]; fq_v2i s[NT]; };   // a wave's quarter of NT tiles (of keys half a tile, or one)
 
 #ifndef FQC_MANY_WAVES
 #define FQC_MANY_WAVES 2
 #endif
 template <int RT, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args a, fqa_parts parts) {
-    constexpr int ROWS = 64 * RT;
-    __shared__ fqc_stage stage[2];
+    constexpr int ROWS = 64 * RT, NT = FQC_MANY_NT;
+    __shared__ fqc_stage<NT> stage[2];
     __shared__ int span[4][2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     fqc_place at;
@@ -536,7 +592,7 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
     tok0 = __builtin_amdgcn_readfirstlane(tok0);
     tok1 = __builtin_amdgcn_readfirstlane(tok1);
     const int first_tile = tok1 > 0 ? tok0 >> 4 : 0, all = tok1 > 0 ? ((tok1 + 15) >> 4) - first_tile : 0;
-    const int part = ((all + a.slots - 1) / a.slots + 1) & ~1, t0 = first_tile + (int)blockIdx.y * part;
+    const int part = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, t0 = first_tile + (int)blockIdx.y * part;
     const int t1 = t0 + part < first_tile + all ? t0 + part : first_tile + all;
     const int whole0 = sp.whole0, whole1 = sp.whole1 < 16 * t1 ? sp.whole1 : 16 * t1;
     fqa_state<RT> st;
@@ -547,86 +603,104 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
     asm("" : "+s"(mask));
     asm("" : "+v"(base));
     if (t0 < t1) {
-        fqc_cursor cur;
+        fqc_walk cur;
         cur.pages_of = a.table + (size_t)at.b * a.width;
         cur.head = a.c.base + at.kv * a.c.head_stride;
         cur.page_stride = (unsigned)(a.c.page_stride >> 4);
         cur.tiles_per_page = a.c.page >> 4;
         cur.pages = a.c.pages;
         cur.start(t0, t1, lane);
-        const int my_tile = wave & 1, half = wave >> 1;
-        auto fetch = [&](fqc_fetched& f) __attribute__((always_inline)) {
-            const uint8_t* p[2];
-            int lost[2];
-            cur.places(p, lost, lane);
-            f.k = *reinterpret_cast<const fq_v4i*>((my_tile ? p[1] : p[0]) + 16 * lane);
+        // NT 4: a tile of keys a wave; NT 2: one kind of nibbles of a tile
+        const int my_tile = NT == 4 ? wave : wave & 1, half = wave >> 1;
+        auto fetch = [&](fqc_fetched<NT>& f) __attribute__((always_inline)) {
+            const uint8_t* p[NT];
+            int bad[NT];
+            cur.places(p, bad);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                f.v[i] = *reinterpret_cast<const int*>(p[i] + 1024 + 16 * lane + 4 * wave);
-                f.s[i] = *reinterpret_cast<const fq_v2i*>(p[i] + 2048 + 8 * g) | lost[i];
+            for (int i = 0; i < NT; ++i) {
+                if (i == my_tile) f.k = *reinterpret_cast<const fq_v4i*>(p[i] + 16u * (unsigned)lane);
+                f.v[i] = *reinterpret_cast<const int*>(p[i] + 1024 + (16u * (unsigned)lane + 4u * (unsigned)wave));
+                f.s[i] = *reinterpret_cast<const fq_v2i*>(p[i] + 2048 + 8u * (unsigned)g) | bad[i];
             }
         };
-        auto unpack = [&](fqc_fetched& f, fqc_stage& to) __attribute__((always_inline)) {
-            unsigned odd = (((unsigned)f.s[0][1] & 0x7F7F7F7Fu) + 0x01010101u) | (((unsigned)f.s[1][1] & 0x7F7F7F7Fu) + 0x01010101u);
-            if (__any((odd & 0x80808080u) != 0u)) {
-                fqc_move_nans(f.s[0]);
-                fqc_move_nans(f.s[1]);
-            }
-            fq_v4i k;
+        auto mend = [&](fqc_fetched<NT>& f) __attribute__((always_inline)) {
+            unsigned odd = 0u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) k[i] = (int)((half ? (unsigned)f.k[i] >> 4 : (unsigned)f.k[i]) & 0x0F0F0F0Fu);
-            to.k[my_tile][half][lane] = k;
-            const fqa_sigmas s0 = fqc_value_sigmas(f.s[0][1]), s1 = fqc_value_sigmas(f.s[1][1]);
-            to.v[2 * wave][lane] = __builtin_bit_cast(fq_v4i, fqa_values<0>(f.v[0], f.v[1], mask, base, s0, s1));
-            to.v[2 * wave + 1][lane] = __builtin_bit_cast(fq_v4i, fqa_values<1>(f.v[0], f.v[1], mask, base, s0, s1));
-            if (wave < 2 && n == 0) {
-                const int w = wave ? f.s[1][0] : f.s[0][0];
+            for (int i = 0; i < NT; ++i) odd |= ((unsigned)f.s[i][1] & 0x7F7F7F7Fu) + 0x01010101u;
+            if (__any((odd & 0x80808080u) != 0u))
+#pragma unroll
+                for (int i = 0; i < NT; ++i) fqc_move_nans(f.s[i]);
+        };
+        auto unpack = [&](const fqc_fetched<NT>& f, fqc_stage<NT>& to) __attribute__((always_inline)) {
+            if (NT == 4) {
+                const fq_v8i k = fq_unpack_chunk(f.k);
+                to.k[my_tile][0][lane] = (fq_v4i){k[0], k[1], k[2], k[3]};
+                to.k[my_tile][1][lane] = (fq_v4i){k[4], k[5], k[6], k[7]};
+            } else {
+                fq_v4i k;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) k[i] = (int)((half ? (unsigned)f.k[i] >> 4 : (unsigned)f.k[i]) & 0x0F0F0F0Fu);
+                to.k[my_tile][half][lane] = k;
+            }
+#pragma unroll
+            for (int i = 0; i < NT / 2; ++i) {
+                const fqa_sigmas s0 = fqc_value_sigmas(f.s[2 * i][1]), s1 = fqc_value_sigmas(f.s[2 * i + 1][1]);
+                to.v[i][2 * wave][lane] = __builtin_bit_cast(fq_v4i, fqa_values<0>(f.v[2 * i], f.v[2 * i + 1], mask, base, s0, s1));
+                to.v[i][2 * wave + 1][lane] = __builtin_bit_cast(fq_v4i, fqa_values<1>(f.v[2 * i], f.v[2 * i + 1], mask, base, s0, s1));
+            }
+            if (wave < NT && n == 0) {
+                int w = f.s[0][0];
+#pragma unroll
+                for (int i = 1; i < NT; ++i) w = wave == i ? f.s[i][0] : w;
                 const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
                 *reinterpret_cast<fq_v4f*>(&to.ks[wave][4 * g]) = (fq_v4f){s01[0], s01[1], s23[0], s23[1]};
             }
         };
-        auto products = [&](const fqc_stage& from, int tb) __attribute__((always_inline)) {
-            if (tb * 16 >= sp.tok1 || (tb + 2) * 16 <= sp.tok0) return;   // (none of this wave's rows has any of them)
-            const bool whole = tb * 16 >= whole0 && (tb + 2) * 16 <= whole1;
-            fq_v8i k[2];
-            float ks[2][4];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const fq_v4i lo = from.k[i][0][lane], hi = from.k[i][1][lane];
-                k[i] = (fq_v8i){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-                const fq_v4f s = *reinterpret_cast<const fq_v4f*>(&from.ks[i][4 * g]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) ks[i][e] = s[e];
-            }
-            fq_v4i pt[RT][1];
-            fq_v4f c[RT][2];
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) c[r][i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
-            fqc_probabilities<RT, 2, CAP, BIAS>(c, ks, tb, Q, rows, a.shape, st, whole, g, pt);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) st.l[r] = FQC_MFMA_PV(FQC_ONES, pt[r][0], st.l[r]);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const fq_v4i v = from.v[j][lane];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) st.o[r][j] = FQC_MFMA_PV(v, pt[r][0], st.o[r][j]);
-            }
-        };
-        fqc_fetched f;
+        fqc_fetched<NT> f;
         fetch(f);
+        mend(f);
         unpack(f, stage[0]);
-        if (t0 + 2 < t1) fetch(f);
-        for (int tb = t0; tb < t1; tb += 4) {
+        cur.refill(lane);
+        fetch(f);
+        for (int tb = t0; tb < t1; tb += 2 * NT) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int now = tb + 2 * u;
+                const int now = tb + NT * u;
                 if (now >= t1) break;
                 __syncthreads();                          // this step's operands are there, and the other stage is free
-                if (now + 2 < t1) unpack(f, stage[u ^ 1]);
-                if (now + 4 < t1) fetch(f);
-                products(stage[u], now);
+                cur.refill(lane);
+                mend(f);
+                // (behind the range the last tile again, into a stage that nobody reads)
+                const fqc_stage<NT>& from = stage[u];
+                fq_v4f c[RT][NT];
+                float ks[NT][4];
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    const fq_v4i lo = from.k[i][0][lane], hi = from.k[i][1][lane];
+                    const fq_v8i k = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) c[r][i] = FQA_MFMA_QK(k, Q.q[r], Q.zp[r]);
+                    const fq_v4f s = *reinterpret_cast<const fq_v4f*>(&from.ks[i][4 * g]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ks[i][e] = s[e];
+                }
+                unpack(f, stage[u ^ 1]);
+                fetch(f);
+                if (now * 16 >= sp.tok1 || (now + NT) * 16 <= sp.tok0) continue;   // (none of this wave's rows has any of the tokens)
+                const bool whole = now * 16 >= whole0 && (now + NT) * 16 <= whole1;
+                fq_v4i pt[RT][NT / 2];
+                fqc_probabilities<RT, NT, CAP, BIAS>(c, ks, now, Q, rows, a.shape, st, whole, g, pt);
+#pragma unroll
+                for (int i = 0; i < NT / 2; ++i) {
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) st.l[r] = FQC_MFMA_PV(FQC_ONES, pt[r][i], st.l[r]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const fq_v4i v = from.v[i][j][lane];
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) st.o[r][j] = FQC_MFMA_PV(v, pt[r][i], st.o[r][j]);
+                    }
+                }
             }
         }
         if (!(CAP || BIAS))
