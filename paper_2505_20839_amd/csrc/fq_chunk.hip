@@ -118,23 +118,20 @@ struct fqc_walk {
         id = pages_of[page_of(lane)];
         window(lane);
     }
-    __device__ __forceinline__ void refill(int lane) {    // before every `places`
+    // before every step's `places`; all steps take the same number of tiles, a divisor of 64
+    __device__ __forceinline__ void refill(int lane) {
         if (tile - first >= 64) {
             first += 64;
             window(lane);
         }
     }
-    // where the next NT tiles lie, and what their scales are or-ed with; behind the range its last tile again.  (64 is a multiple of NT, and every
-    // call of a range takes the same.)
-    template <int NT>
-    __device__ __forceinline__ void places(const uint8_t* (&p)[NT], int (&bad)[NT]) {
-        const int j = tile - first;
+    // where tiles i and i + 1 of the next ones lie; bits 0 and 1: their pages are outside.  Behind the range its last tile again.
+    __device__ __forceinline__ unsigned places(int i, const uint8_t* (&p)[2]) const {
+        const int j = tile - first + i;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            p[i] = head + ((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)hi, j + i) << 32 | (unsigned)__builtin_amdgcn_readlane((int)lo, j + i));
-            bad[i] = lost >> (j + i) & 1ull ? 0x7F7F7F7F : 0;
-        }
-        tile += NT;
+        for (int u = 0; u < 2; ++u)
+            p[u] = head + ((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)hi, j + u) << 32 | (unsigned)__builtin_amdgcn_readlane((int)lo, j + u));
+        return (unsigned)(lost >> j) & 3u;
     }
 };
 
@@ -269,13 +266,28 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
             }
 }
 
+// Values as fq_attend.hip has them, one shift less for each word: a code in bits 4 .. 7 of a half under the exponent of 1024 is the number 1024 + 16 c, and
+// one fused multiply-add with sigma / 16 and -72 sigma makes it sigma * (c - 8), exact (72 sigma has 8 bits and is at most 32256).
 __device__ __forceinline__ fqa_sigmas fqc_value_sigmas(int w) {
     fqa_sigmas s;
-    s.s[0] = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, false), fqa_v2h);
-    s.s[1] = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, true), fqa_v2h);
-    s.n[0] = s.s[0] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
-    s.n[1] = s.s[1] * (fqa_v2h){(_Float16)-24.f, (_Float16)-24.f};
+    const fqa_v2h a = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, false), fqa_v2h), b = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, true), fqa_v2h);
+    s.s[0] = a * (fqa_v2h){(_Float16)0.0625f, (_Float16)0.0625f};
+    s.s[1] = b * (fqa_v2h){(_Float16)0.0625f, (_Float16)0.0625f};
+    s.n[0] = a * (fqa_v2h){(_Float16)-72.f, (_Float16)-72.f};
+    s.n[1] = b * (fqa_v2h){(_Float16)-72.f, (_Float16)-72.f};
     return s;
+}
+#define FQC_VALUE_MASK 0x00F000F0u
+#define FQC_VALUE_BASE 0x64006400u
+// The lane's values for channels j and j + 1 of 16, j even: word w of each of two tiles (nibble 0: channel j of tokens 0, 1; 2: of tokens 2, 3; 1 and 3: j + 1).
+__device__ __forceinline__ void fqc_values(int w0, int w1, unsigned mask, unsigned base, const fqa_sigmas& a, const fqa_sigmas& b, fqa_v8h& even, fqa_v8h& odds) {
+    const unsigned x = (unsigned)w0, y = (unsigned)w1;
+    const fqa_v2h e0 = fqa_value_pair(x << 4, mask, base, a.s[0], a.n[0]), e1 = fqa_value_pair(x >> 4, mask, base, a.s[1], a.n[1]);
+    const fqa_v2h e2 = fqa_value_pair(y << 4, mask, base, b.s[0], b.n[0]), e3 = fqa_value_pair(y >> 4, mask, base, b.s[1], b.n[1]);
+    const fqa_v2h o0 = fqa_value_pair(x, mask, base, a.s[0], a.n[0]), o1 = fqa_value_pair(x >> 8, mask, base, a.s[1], a.n[1]);
+    const fqa_v2h o2 = fqa_value_pair(y, mask, base, b.s[0], b.n[0]), o3 = fqa_value_pair(y >> 8, mask, base, b.s[1], b.n[1]);
+    even = (fqa_v8h){e0[0], e0[1], e1[0], e1[1], e2[0], e2[1], e3[0], e3[1]};
+    odds = (fqa_v8h){o0[0], o0[1], o1[0], o1[1], o2[0], o2[1], o3[0], o3[1]};
 }
 #define FQC_MFMA_PV(a, b, c) __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(fqa_v8h, (a)), __builtin_bit_cast(fqa_v8h, (b)), (c), 0, 0, 0)
 #define FQC_ONES ((fq_v4i){0x3C003C00, 0x3C003C00, 0x3C003C00, 0x3C003C00})
@@ -312,8 +324,8 @@ __device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], int tb, const fqa_
         for (int r = 0; r < RT; ++r) st.l[r] = FQC_MFMA_PV(FQC_ONES, pt[r][i], st.l[r]);
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-            const fqa_v8h even = fqa_values<0>(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1]);
-            const fqa_v8h odds = fqa_values<1>(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1]);
+            fqa_v8h even, odds;
+            fqc_values(now[2 * i].v[w], now[2 * i + 1].v[w], mask, base, sg[0], sg[1], even, odds);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 st.o[r][2 * w] = FQC_MFMA_PV(even, pt[r][i], st.o[r][2 * w]);
@@ -342,7 +354,7 @@ __device__ __forceinline__ void fqc_range(fqc_cursor& cur, int t0, int t1, int w
                                           const fqc_shape& shape, fqa_state<RT>& st, int lane) {
     const int g = lane >> 4;
     fqc_begin<RT, CAP, BIAS>(Q, st);
-    unsigned mask = 0x03C003C0u, base = 0x4C004C00u;
+    unsigned mask = FQC_VALUE_MASK, base = FQC_VALUE_BASE;
     asm("" : "+s"(mask));
     asm("" : "+v"(base));
     auto step = [&](fqa_tile (&now)[NT], int tb) __attribute__((always_inline)) {
@@ -552,25 +564,20 @@ __global__ __launch_bounds__(64 * KVW, RT == 1 ? 4 : RT == 2 ? 2 : 1) void fqc_f
 // where all read their operands; the next step's codes are unpacked while this one's products run, and those behind it are on their way.
 // Bound by vector instructions: per step and wave 30 to unpack its quarter, then 24 and 8 exponentials (16 cycles each) per 16 rows, beside 18 matrix
 // instructions of 16 to 32 cycles on the other pipe.
-#ifndef FQC_MANY_NT
-#define FQC_MANY_NT 4
-#endif
-template <int NT>
 struct fqc_stage {
-    fq_v4i k[NT][2][64];                                  // keys' bytes: tile, low and high nibbles, lane
-    fq_v4i v[NT / 2][8][64];                              // values in fp16: two tiles, 16 channels, lane
-    float ks[NT][16];                                     // keys' sigmas
+    fq_v4i k[4][2][64];                                   // keys' bytes: tile, low and high nibbles, lane
+    fq_v4i v[2][8][64];                                   // values in fp16: two tiles, 16 channels, lane
+    float ks[4][16];                                      // keys' sigmas
 };
-template <int NT>
-struct fqc_fetched { fq_v4i k; int v[NT]; fq_v2i s[NT]; };   // a wave's quarter of NT tiles (of keys half a tile, or one)
+struct fqc_fetched { fq_v4i k; fq_v2i v[2], s[2]; unsigned bad; };   // a wave's quarter: keys of one tile, half the values of its pair
 
 #ifndef FQC_MANY_WAVES
 #define FQC_MANY_WAVES 2
 #endif
 template <int RT, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args a, fqa_parts parts) {
-    constexpr int ROWS = 64 * RT, NT = FQC_MANY_NT;
-    __shared__ fqc_stage<NT> stage[2];
+    constexpr int ROWS = 64 * RT, NT = 4;
+    __shared__ fqc_stage stage[2];
     __shared__ int span[4][2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     fqc_place at;
@@ -599,7 +606,7 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
     fqa_queries<RT> Q;
     fqc_take_queries<RT, CAP, BIAS>(a, at, first_row, n, g, Q);
     fqc_begin<RT, CAP, BIAS>(Q, st);
-    unsigned mask = 0x03C003C0u, base = 0x4C004C00u;
+    unsigned mask = FQC_VALUE_MASK, base = FQC_VALUE_BASE;
     asm("" : "+s"(mask));
     asm("" : "+v"(base));
     if (t0 < t1) {
@@ -610,53 +617,48 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
         cur.tiles_per_page = a.c.page >> 4;
         cur.pages = a.c.pages;
         cur.start(t0, t1, lane);
-        // NT 4: a tile of keys a wave; NT 2: one kind of nibbles of a tile
-        const int my_tile = NT == 4 ? wave : wave & 1, half = wave >> 1;
-        auto fetch = [&](fqc_fetched<NT>& f) __attribute__((always_inline)) {
-            const uint8_t* p[NT];
-            int bad[NT];
-            cur.places(p, bad);
+        const int pair = wave & 1, half = wave >> 1;       // tiles 2 pair and 2 pair + 1; words 2 half and 2 half + 1 of their values
+        auto fetch = [&](fqc_fetched& f) __attribute__((always_inline)) {
+            const uint8_t* p[2];
+            f.bad = cur.places(2 * pair, p);
+            cur.tile += NT;
+            __amdgpu_buffer_rsrc_t r[2];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                if (i == my_tile) f.k = *reinterpret_cast<const fq_v4i*>(p[i] + 16u * (unsigned)lane);
-                f.v[i] = *reinterpret_cast<const int*>(p[i] + 1024 + (16u * (unsigned)lane + 4u * (unsigned)wave));
-                f.s[i] = *reinterpret_cast<const fq_v2i*>(p[i] + 2048 + 8u * (unsigned)g) | bad[i];
+            for (int i = 0; i < 2; ++i) r[i] = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p[i]), 0, FQP_TILE, 0x00020000);
+            f.k = __builtin_bit_cast(fq_v4i, __builtin_amdgcn_raw_buffer_load_b128(half ? r[1] : r[0], 16 * lane, 0, 0));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f.v[i] = __builtin_bit_cast(fq_v2i, __builtin_amdgcn_raw_buffer_load_b64(r[i], 16 * lane, 1024 + 8 * half, 0));
+                f.s[i] = __builtin_bit_cast(fq_v2i, __builtin_amdgcn_raw_buffer_load_b64(r[i], 8 * g, 2048, 0));
             }
         };
-        auto mend = [&](fqc_fetched<NT>& f) __attribute__((always_inline)) {
-            unsigned odd = 0u;
+        auto mend = [&](fqc_fetched& f) __attribute__((always_inline)) {
+            const unsigned odd = (((unsigned)f.s[0][1] & 0x7F7F7F7Fu) + 0x01010101u) | (((unsigned)f.s[1][1] & 0x7F7F7F7Fu) + 0x01010101u);
+            if (f.bad != 0u || __any((odd & 0x80808080u) != 0u))
 #pragma unroll
-            for (int i = 0; i < NT; ++i) odd |= ((unsigned)f.s[i][1] & 0x7F7F7F7Fu) + 0x01010101u;
-            if (__any((odd & 0x80808080u) != 0u))
-#pragma unroll
-                for (int i = 0; i < NT; ++i) fqc_move_nans(f.s[i]);
+                for (int i = 0; i < 2; ++i) {
+                    f.s[i] |= f.bad >> i & 1u ? 0x7F7F7F7F : 0;
+                    fqc_move_nans(f.s[i]);
+                }
         };
-        auto unpack = [&](const fqc_fetched<NT>& f, fqc_stage<NT>& to) __attribute__((always_inline)) {
-            if (NT == 4) {
-                const fq_v8i k = fq_unpack_chunk(f.k);
-                to.k[my_tile][0][lane] = (fq_v4i){k[0], k[1], k[2], k[3]};
-                to.k[my_tile][1][lane] = (fq_v4i){k[4], k[5], k[6], k[7]};
-            } else {
-                fq_v4i k;
+        auto unpack = [&](const fqc_fetched& f, fqc_stage& to) __attribute__((always_inline)) {
+            const int tile = 2 * pair + half;
+            const fq_v8i k = fq_unpack_chunk(f.k);
+            to.k[tile][0][lane] = (fq_v4i){k[0], k[1], k[2], k[3]};
+            to.k[tile][1][lane] = (fq_v4i){k[4], k[5], k[6], k[7]};
+            const fqa_sigmas s0 = fqc_value_sigmas(f.s[0][1]), s1 = fqc_value_sigmas(f.s[1][1]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) k[i] = (int)((half ? (unsigned)f.k[i] >> 4 : (unsigned)f.k[i]) & 0x0F0F0F0Fu);
-                to.k[my_tile][half][lane] = k;
+            for (int i = 0; i < 2; ++i) {
+                fqa_v8h even, odds;
+                fqc_values(f.v[0][i], f.v[1][i], mask, base, s0, s1, even, odds);
+                to.v[pair][4 * half + 2 * i][lane] = __builtin_bit_cast(fq_v4i, even);
+                to.v[pair][4 * half + 2 * i + 1][lane] = __builtin_bit_cast(fq_v4i, odds);
             }
-#pragma unroll
-            for (int i = 0; i < NT / 2; ++i) {
-                const fqa_sigmas s0 = fqc_value_sigmas(f.s[2 * i][1]), s1 = fqc_value_sigmas(f.s[2 * i + 1][1]);
-                to.v[i][2 * wave][lane] = __builtin_bit_cast(fq_v4i, fqa_values<0>(f.v[2 * i], f.v[2 * i + 1], mask, base, s0, s1));
-                to.v[i][2 * wave + 1][lane] = __builtin_bit_cast(fq_v4i, fqa_values<1>(f.v[2 * i], f.v[2 * i + 1], mask, base, s0, s1));
-            }
-            if (wave < NT && n == 0) {
-                int w = f.s[0][0];
-#pragma unroll
-                for (int i = 1; i < NT; ++i) w = wave == i ? f.s[i][0] : w;
-                const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-                *reinterpret_cast<fq_v4f*>(&to.ks[wave][4 * g]) = (fq_v4f){s01[0], s01[1], s23[0], s23[1]};
-            }
+            const int w = half ? f.s[1][0] : f.s[0][0];
+            const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+            *reinterpret_cast<fq_v4f*>(&to.ks[tile][4 * g]) = (fq_v4f){s01[0], s01[1], s23[0], s23[1]};   // (by all lanes of a group, the same)
         };
-        fqc_fetched<NT> f;
+        fqc_fetched f;
         fetch(f);
         mend(f);
         unpack(f, stage[0]);
@@ -671,7 +673,7 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
                 cur.refill(lane);
                 mend(f);
                 // (behind the range the last tile again, into a stage that nobody reads)
-                const fqc_stage<NT>& from = stage[u];
+                const fqc_stage& from = stage[u];
                 fq_v4f c[RT][NT];
                 float ks[NT][4];
 #pragma unroll
