@@ -15,7 +15,7 @@
  *                      and O[i,h,:] = bf16( sum_t p_t v_t / sum_t p_t ), p_t = exp(x_t).  first and end hold a document's borders, a prefix that is
  *                      seen whole, or any range; a row with no token gets zeros.  A query row in no sequence (before starts[0], behind
  *                      starts[B]) is left as it was.  The products are those of fq_kv4_attention_ws with their error; tanh and the bias are FP32
- *                      (2^-20 of a score), a distance is counted from the row's nearest token on.
+ *                      (2^-19 of a score), a distance is counted from the row's nearest token on.
  *                      A key or value whose scale is NaN, or a page number outside the cache, gives NaN to the rows that attend to its tokens, and to no
  *                      other.  A sequence longer than max_len or than table_width * page gives NaN to its rows.
  *                      starts int32 [B + 1], not decreasing, 0 .. T (what lies outside is taken as the nearest of these, and rows of

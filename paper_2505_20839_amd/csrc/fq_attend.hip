@@ -323,37 +323,6 @@ struct fqa_plan {
     int slots() const { return prefix_slots + (finish() ? 0 : own_slots); }   // parts of a row that go through memory
 };
 
-// Tiles of a part, for `heads` (sequence, key/value head, 16 query rows) of up to `tiles` each; uneven: of several sequences, whose lengths
-// differ.  A wave of a part's four takes about 0.25 us a tile beyond 4; a second part costs the joining kernel, 2 us and more.  us, from a
-// graph, 32 query and 8 key/value heads unless said otherwise:
-//     one workgroup per compute unit           1 x 32001 tokens, parts of 64 (256 workgroups) 12.3; 32 (504) 13.4; 16 (1008) 15.0; 128 (128) 16.0
-//                                              1 x 8000, 16 (256) 8.5; 32 9.4; 64 10.9     16 x 4000, 128 (256) 17.1; 64 (512) 18.4; 32 18.5
-//     ... but at least 16 tiles                1 x 1000, 16 6.8; 64 8.2
-//     ... and up to 64 parts                   1 x 32001, 8 / 1 heads, 32 (63 parts) 9.3; 16 (126) 9.4
-//     one part of a short sequence             1 x 600, 7.0 -> 6.4;  with many heads 16 x 1000, 16 10.2; 64 9.5    30 x 700 of 32 heads 26.6 -> 20.5
-//     several sequences: parts of 128 tiles or a sixteenth, for the longest may be one of few as long, and would be left to its
-//     8 workgroups                             one of 32001 among 200: 8 142 (76 of 16, 42 of 8 sequences); 128 36 (34, 34) for 32 sequences
-//                                              0 .. 32001: 32 sequences 152 -> 114, 24 148 -> 82     0 .. 4000: 32 22.4 -> 22.3, 17 22.3 -> 16.5
-//     ... which costs even lengths that one    32 x 4000, 250 27.9; 128 30.8    32 x 32001, 2001 183; 128 201    16 x 32001, 1008 97; 128 104
-//     workgroup per head suited, and not else  24 x 32001, 2001 161; 128 153    17 x 32001, 2001 154; 128 111     8 x 32001, 512 53.6; 128 55.0
-//     more workgroups than compute units: short parts even out different lengths
-//                                              37 x 0 .. 6000, 64 31.1; 128 35.2           128 x 0 .. 1500 (1024 heads), 94 30.0; 48 30.4
-int fqa_part(long long heads, int tiles, long long cus, bool uneven) {
-    if (tiles <= 40 || (tiles <= 64 && 2 * heads >= cus)) return tiles;
-    const long long want = heads < cus ? cus / heads : 1;
-    long long chunk = (tiles + want - 1) / want;
-    if (chunk < (tiles + 63) / 64) chunk = (tiles + 63) / 64;
-    chunk = chunk < 16 ? 16 : (chunk + 15) / 16 * 16;
-    const long long few = heads < 2 * cus ? 64 : 128, longest = tiles / 16 > 128 ? tiles / 16 : 128;
-    if (heads * ((tiles + chunk - 1) / chunk) > cus) chunk = chunk > few ? few : chunk;
-    else if (uneven && chunk > longest) {
-        const long long n = (tiles + longest - 1) / longest;
-        chunk = ((tiles + n - 1) / n + 15) / 16 * 16;
-    }
-    if (chunk < tiles / 60000 + 1) chunk = (tiles / 60000 + 16) / 16 * 16;   // (a grid has 65535 in its second dimension; a step may not pass a part's end)
-    return (int)(chunk < tiles ? chunk : tiles);
-}
-
 fqa_plan fqa_choose(int B, int Hq, int Hkv, int max_len, int prefix) {
     fqa_plan p = {0, 0, 0, 0, 0};
     const int G = Hq / Hkv, row_tiles = (G + 15) / 16, cus = fq_device_cus();

@@ -5,8 +5,8 @@
 // the products are those of fq_attend.hip (S^T = K Q^T in FP8, O^T = V^T P^T in fp16, sums in FP32).  What differs:
 //     ranges     a row's tokens are lo <= t < hi.  A wave takes the tiles that any of its rows has; where all of its rows have all of a step's
 //                tokens, no score is compared with a range.
-//     shape      x = cap tanh(out_scale q k / cap) - slope |pos - t|, in units of log2 e.  tanh(y) = y + y^3 P(y^2), five terms for |y| <= 5/8
-//                (relative error 2^-23), 1 - 2 / (1 + exp(2 y)) above.  A distance is counted from the row's nearest token: a constant less for
+//     shape      x = cap tanh(out_scale q k / cap) - slope |pos - t|, in units of log2 e.  tanh(y) = y P(y^2) of three terms while every |y| is
+//                at most 5/16 (relative error 2^-19), of five up to 5/8 (2^-23), 1 - 2 / (1 + exp(2 y)) above.  A distance is counted from the row's nearest token: a constant less for
 //                all scores of a row, and exact in FP32 where it counts.
 //     broken     a value whose scale is NaN must not reach the rows that do not see its token (0 * NaN): its NaN moves to the key's scale,
 //                which makes the probabilities NaN of those rows only that see it; so does a tile of a page outside the cache.
@@ -14,10 +14,12 @@
 
 namespace {
 
-// log2 e * cap * the coefficients of tanh(y) / y in y^2 (least squares in relative error on |y| <= 5/8)
+// log2 e * cap * the coefficients of tanh(y) / y in y^2, least squares in relative error
 #define FQC_SMALL 0.625f
+#define FQC_TINY 0.3125f
 struct fqc_shape {
-    float k[5];                                           // polynomial
+    float t[3];                                           // |y| <= FQC_TINY: 2^-19
+    float k[5];                                           // |y| <= FQC_SMALL: 2^-23
     float k1, k2;                                         // log2 e * cap and twice that
 };
 
@@ -27,7 +29,7 @@ struct fqc_args {
     fq_paged_cache c;
     const int32_t *table, *starts, *lens, *first, *end;
     const float* slopes;
-    int width, window, T, B, Hq, Hkv, max_len, slots;
+    int width, window, T, B, Hq, Hkv, max_len, slots, chunk;   // parts of a row, and tiles of one at least
     float out_scale, inv_cap;                             // inv_cap: 1 / cap (0: uncapped)
     fqc_shape shape;
     uint16_t* O;
@@ -80,9 +82,10 @@ struct fqc_cursor {
         places(p, lost, lane);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-            t[i].k = *reinterpret_cast<const fq_v4i*>(p[i] + 16 * lane);
-            t[i].v = *reinterpret_cast<const fq_v4i*>(p[i] + 1024 + 16 * lane);
-            t[i].s = *reinterpret_cast<const fq_v2i*>(p[i] + 2048 + 8 * (lane >> 4)) | lost[i];
+            const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p[i]), 0, FQP_TILE, 0x00020000);
+            t[i].k = __builtin_bit_cast(fq_v4i, __builtin_amdgcn_raw_buffer_load_b128(r, 16 * lane, 0, 0));
+            t[i].v = __builtin_bit_cast(fq_v4i, __builtin_amdgcn_raw_buffer_load_b128(r, 16 * lane, 1024, 0));
+            t[i].s = __builtin_bit_cast(fq_v2i, __builtin_amdgcn_raw_buffer_load_b64(r, 8 * (lane >> 4), 2048, 0)) | lost[i];
         }
     }
 };
@@ -182,7 +185,18 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
         auto small = [&](float u) __attribute__((always_inline)) {
             return fmaf(fmaf(fmaf(fmaf(shape.k[4], u, shape.k[3]), u, shape.k[2]), u, shape.k[1]), u, shape.k[0]);
         };
-        if (!__any(!(most <= FQC_SMALL))) {
+        if (!__any(!(most <= FQC_TINY))) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = s[r][i][e] * Q.qs[r], u = y * y;
+                        s[r][i][e] = y * fmaf(fmaf(shape.t[2], u, shape.t[1]), u, shape.t[0]);
+                    }
+        } else if (!__any(!(most <= FQC_SMALL))) {
+            asm volatile("" : "+v"(most));                // (branches: nothing of one beside another)
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -194,7 +208,7 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
                     }
         } else {
             float two = 2.0f * 1.44269504088896340736f;
-            asm volatile("" : "+v"(two));                 // (a branch: nothing of this beside the other)
+            asm volatile("" : "+v"(two));
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
@@ -375,31 +389,32 @@ __device__ __forceinline__ void fqc_range(fqc_cursor& cur, int t0, int t1, int w
         for (int r = 0; r < RT; ++r) st.m[r] *= Q.qs[r];
 }
 
+// The least of 16 neighbouring lanes (the same in all four groups of a wave), for all.
 __device__ __forceinline__ int fqc_row16_min(int v) {
-#pragma unroll
-    for (int d = 1; d < 16; d *= 2) {
-        const int o = __shfl_xor(v, d, 64);
-        v = o < v ? o : v;
-    }
-    return __builtin_amdgcn_readfirstlane(v);
+    return __builtin_amdgcn_readfirstlane((int)(~fq_row16_max(~((unsigned)v ^ 0x80000000u)) ^ 0x80000000u));
 }
 
 __device__ __forceinline__ int fqc_clamp(int v, int hi) { return v < 0 ? 0 : v > hi ? hi : v; }
 
 // Query tiles of `rows` rows: those of sequence b are numbered from starts[b] * G / rows + b on, which leaves each sequence room for what it can
 // need without anyone knowing their lengths.  The sequence of tile k (or -1), 64 candidates at a time.
-__device__ __forceinline__ int fqc_sequence_of(const fqc_args& a, int k, int G, int rows, int lane, int& tile0) {
+__device__ __forceinline__ int fqc_sequence_of(const fqc_args& a, int k, int G, int rows, int lane, int& tile0, int& start, int& stop) {
     int lo = 0, n = a.B;
     while (true) {
         const int stride = (n + 63) >> 6, i = lo + lane * stride;
         const bool in = i < lo + n;
-        const int at = in ? (int)((long long)fqc_clamp(a.starts[i], a.T) * G / rows) + i : 0;
+        const int first = in ? fqc_clamp(a.starts[i], a.T) : 0;
+        const int at = in ? (int)((unsigned)(first * G) / (unsigned)rows) + i : 0;   // (T * G is below 2^25)
         const unsigned long long below = __ballot(in && at <= k);
         if (below == 0ull) return -1;
         const int count = __popcll(below) - 1;
         lo += count * stride;
         tile0 = __builtin_amdgcn_readlane(at, count);
-        if (stride == 1) return lo;
+        if (stride == 1) {
+            start = __builtin_amdgcn_readlane(first, count);
+            stop = count + 1 < n ? __builtin_amdgcn_readlane(first, count + 1) : fqc_clamp(a.starts[lo + 1], a.T);
+            return lo;
+        }
         n = n - count * stride < stride ? n - count * stride : stride;
     }
 }
@@ -411,14 +426,13 @@ struct fqc_place {
     template <int ROWS>
     __device__ __forceinline__ bool find(const fqc_args& a, int lane) {
         G = a.Hq / a.Hkv;
-        const int tiles = (int)((long long)a.T * G / ROWS) + a.B;
+        const int tiles = a.T * G / ROWS + a.B;
         const int k = tiles - 1 - (int)(blockIdx.x / a.Hkv);   // (later rows of a prompt have more tokens: they begin)
         kv = (int)(blockIdx.x % a.Hkv);
-        int tile0 = 0;
-        b = fqc_sequence_of(a, k, G, ROWS, lane, tile0);
+        int tile0 = 0, stop = 0;
+        b = fqc_sequence_of(a, k, G, ROWS, lane, tile0, start, stop);
         if (b < 0) return false;
-        start = fqc_clamp(a.starts[b], a.T);
-        count = fqc_clamp(a.starts[b + 1], a.T) - start;
+        count = stop - start;
         row0 = (k - tile0) * ROWS;                        // (T * G is bounded: 32 bits hold it)
         if (count <= 0 || count * G <= row0) return false;
         nrows = count * G - row0 < ROWS ? count * G - row0 : ROWS;
@@ -485,9 +499,12 @@ __device__ __forceinline__ void fqc_take_queries(const fqc_args& a, const fqc_pl
     }
 }
 
+#ifndef FQC_FEW_WAVES
+#define FQC_FEW_WAVES 3
+#endif
 // Few rows: one query tile of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among the waves, which meet in LDS.
 template <int RT, int KVW, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * KVW, RT == 1 ? 4 : RT == 2 ? 2 : 1) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
+__global__ __launch_bounds__(64 * KVW, RT == 1 ? FQC_FEW_WAVES : 2) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
     constexpr int ROWS = 16 * RT, NT = 2;
     __shared__ fqa_shared<RT, KVW> sh;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -500,7 +517,7 @@ __global__ __launch_bounds__(64 * KVW, RT == 1 ? 4 : RT == 2 ? 2 : 1) void fqc_f
     const bool too_long = at.too_long;
     const int first_tile = tok1 > 0 ? tok0 >> 4 : 0, all = tok1 > 0 ? ((tok1 + 15) >> 4) - first_tile : 0;
     // this workgroup's part, and the waves' shares: steps of NT tiles
-    const int part = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, c0 = first_tile + (int)blockIdx.y * part;
+    const int even = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, part = even > a.chunk ? even : a.chunk, c0 = first_tile + (int)blockIdx.y * part;
     const int c1 = c0 + part < first_tile + all ? c0 + part : first_tile + all;
     const int share = c1 > c0 ? ((c1 - c0 + NT - 1) / NT + KVW - 1) / KVW * NT : 0, t0 = c0 + wave * share, t1 = t0 + share < c1 ? t0 + share : c1;
     fqa_state<RT> st;
@@ -599,7 +616,7 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
     tok0 = __builtin_amdgcn_readfirstlane(tok0);
     tok1 = __builtin_amdgcn_readfirstlane(tok1);
     const int first_tile = tok1 > 0 ? tok0 >> 4 : 0, all = tok1 > 0 ? ((tok1 + 15) >> 4) - first_tile : 0;
-    const int part = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, t0 = first_tile + (int)blockIdx.y * part;
+    const int even = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, part = even > a.chunk ? even : a.chunk, t0 = first_tile + (int)blockIdx.y * part;
     const int t1 = t0 + part < first_tile + all ? t0 + part : first_tile + all;
     const int whole0 = sp.whole0, whole1 = sp.whole1 < 16 * t1 ? sp.whole1 : 16 * t1;
     fqa_state<RT> st;
@@ -735,16 +752,23 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
 #ifndef FQC_MANY_RT
 #define FQC_MANY_RT 2
 #endif
-// few: 16 * few rows of a query tile, whose tokens four waves share out (0: many rows); slots: parts of a row's tokens.
-struct fqc_plan { int few, slots; };
+// few: 16 * few rows of a query tile, whose tokens four waves share out (0: many rows); slots: parts of a row's tokens, chunk: tiles of one at least
+// (a multiple of 4; more where that many parts would not hold a row's tokens).
+struct fqc_plan { int few, slots, chunk; };
 fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
     const int G = Hq / Hkv, cus = fq_device_cus();
     const long long most = (long long)(max_new < T ? max_new : T) * G;
-    fqc_plan p = {most <= 16 ? 1 : most <= 32 ? 2 : 0, 1};
-    const int rows = p.few ? 16 * p.few : 64 * FQC_MANY_RT;
-    const long long tiles = ((long long)max_len + 15) / 16, units = ((long long)T * G / rows + B) * Hkv, room = tiles / 16;
-    const long long want = (p.few ? cus : 2 * cus) / units, slots = want < room ? want : room;
-    p.slots = (int)(slots < 1 ? 1 : slots > 64 ? 64 : slots);
+    fqc_plan p = {most <= 16 ? 1 : most <= 32 ? 2 : 0, 1, 4};
+    const int rows = p.few ? 16 * p.few : 64 * FQC_MANY_RT, tiles = max_len > 0 ? (int)(((long long)max_len + 15) / 16) : 1;
+    const long long units = ((long long)T * G / rows + (p.few ? 0 : B)) * Hkv;
+    if (p.few) {
+        const int chunk = fqa_part(((long long)T * G + rows - 1) / rows > B ? ((long long)T * G + rows - 1) / rows * Hkv : (long long)B * Hkv, tiles, cus, B > 1);
+        p.chunk = (chunk + 3) / 4 * 4;
+        p.slots = (tiles + p.chunk - 1) / p.chunk;
+    } else {
+        const long long want = 2 * cus / units, room = tiles / 16, slots = want < room ? want : room;
+        p.slots = (int)(slots < 1 ? 1 : slots > 64 ? 64 : slots);
+    }
     return p;
 }
 
@@ -773,10 +797,12 @@ size_t fq_chunk_scratch_bytes(int T, int B, int Hq, int Hkv, int max_new, int ma
 
 void fq_launch_chunk(const fq_chunk_args& x, void* scratch, hipStream_t stream) {
     const fqc_plan p = fqc_choose(x.T, x.B, x.Hq, x.Hkv, x.max_new, x.max_len);
-    fqc_args a = {x.Q, x.q_scale, x.c, x.table, x.starts, x.lens, x.first, x.end, x.slopes, x.width, x.window, x.T, x.B, x.Hq, x.Hkv, x.max_len, p.slots,
+    fqc_args a = {x.Q, x.q_scale, x.c, x.table, x.starts, x.lens, x.first, x.end, x.slopes, x.width, x.window, x.T, x.B, x.Hq, x.Hkv, x.max_len, p.slots, p.chunk,
                   x.out_scale, x.cap > 0.f ? 1.0f / x.cap : 0.f, {}, x.O};
     const double c[5] = {0x1.fffffcp-1, -0x1.5551b8p-2, 0x1.107a08p-3, -0x1.a88656p-5, 0x1.ed307ap-7}, k1 = 1.44269504088896340736 * x.cap;
+    const double t[3] = {0x1.ffffcep-1, -0x1.550db4p-2, 0x1.0193e6p-3};
     for (int i = 0; i < 5; ++i) a.shape.k[i] = (float)(k1 * c[i]);
+    for (int i = 0; i < 3; ++i) a.shape.t[i] = (float)(k1 * t[i]);
     a.shape.k1 = (float)k1;
     a.shape.k2 = (float)(2.0 * k1);
     const fqa_parts parts = {static_cast<float*>(scratch), static_cast<float*>(scratch) + (size_t)p.slots * x.T * x.Hq * 128, p.slots};
