@@ -15,7 +15,7 @@ namespace {
 
 typedef unsigned long long fqs_u64;
 
-constexpr int FQS_BINS = 512, FQS_LIST = 4096, FQS_T1 = 256, FQS_T2 = 1024, FQS_MOST_PARTS = 256;
+constexpr int FQS_BINS = 512, FQS_LIST = 4096, FQS_T1 = 256, FQS_T2 = 512, FQS_MOST_PARTS = 256;
 constexpr float FQS_UNIT = 0x1p36f;                       // masses in 2^-36 of the largest
 constexpr float FQS_SPAN = 26.0f;                         // nats that the bins cover: e^-26 is below 2^-37
 constexpr fqs_u64 FQS_MASS = (1ull << 50) - 1;            // a part's bin: number of tokens << 50 | mass (8192 * 2^36 at most)
@@ -218,17 +218,17 @@ __device__ __forceinline__ fqs_u64 fqs_scan(fqs_u64 v, fqs_u64* scratch, fqs_u64
 }
 
 struct fqs_shared {
-    fqs_u64 scan[FQS_T2 / 64];
+    fqs_u64 scan[FQS_T2 / 64], reach[FQS_T2 / 64];
     fqs_u64 part_mass[FQS_MOST_PARTS];                    // kept mass of each part
     float top[FQS_MOST_PARTS];
     float factor[FQS_MOST_PARTS];                         // of a part's masses
     int shift[FQS_MOST_PARTS];                            // of its bins
-    unsigned count[FQS_BINS];
-    fqs_u64 mass[FQS_BINS];                               // inclusive sums after the scan
-    fqs_u64 digit[256];
+    fqs_u64 mass[FQS_BINS];                               // inclusive sums
+    fqs_u64 digit[2][256];
     fqs_u64 list[FQS_LIST];                               // comps of one bin
-    fqs_u64 least, found_before;
-    int n, found;
+    int some[FQS_MOST_PARTS];                             // parts that have tokens in it
+    fqs_u64 found_before, found_own;
+    int n, parts, found;
 };
 
 template <bool WIDE>
@@ -266,26 +266,38 @@ struct fqs_finder {
         const unsigned k = (unsigned)(comp >> 20), o = WIDE ? k : k << 16;
         return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : WIDE ? ~o : ~o & 0xFFFF0000u);
     }
-    // the tokens of a bin into the list; only those parts are read that have some
+    // a part's numbers in the row's bin i (0 before its first)
+    __device__ __forceinline__ fqs_u64 bin_of(int p, int i) {
+        const int q = i - sh.shift[p];
+        const fqs_u64 v = w.bins[((size_t)b * w.plan.parts + p) * FQS_BINS + (q < 0 ? 0 : q)];
+        return q < 0 ? 0ull : v;
+    }
+    // the tokens of a bin into the list; only those parts are read that have some, four chunks of a thread at a time
     __device__ __forceinline__ void gather(int bin) {
         __syncthreads();
-        if (t == 0) sh.n = 0;
+        if (t == 0) sh.n = sh.parts = 0;
         __syncthreads();
-        const int chunks = (a.V + skew + 7) / 8;
-        for (int p = 0; p < w.plan.parts; ++p) {
-            const int q = bin - sh.shift[p];
-            if (q < 0 || q >= FQS_BINS) continue;
-            if (w.bins[((size_t)b * w.plan.parts + p) * FQS_BINS + q] == 0) continue;   // (the same for all threads)
-            for (int c = p * w.plan.per + t; c < (p + 1) * w.plan.per && c < chunks; c += FQS_T2) {
-                float x[8];
-                fqs_load<WIDE>(a, b, skew, c, x);
+        if (t < w.plan.parts && bin_of(t, bin) != 0) sh.some[atomicAdd(&sh.parts, 1)] = t;
+        __syncthreads();
+        const int chunks = (a.V + skew + 7) / 8, all = sh.parts * w.plan.per;
+        for (int i0 = t; i0 < all; i0 += 4 * FQS_T2) {
+            float x[4][8];
+            int c[4];
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (x[e] > -__builtin_inff() && in_bin(x[e], bin)) {
-                        const int at = atomicAdd(&sh.n, 1);
-                        if (at < FQS_LIST) sh.list[at] = fqs_comp<WIDE>(x[e], 8 * c - skew + e);
-                    }
+            for (int u = 0; u < 4; ++u) {
+                const int i = i0 + u * FQS_T2, p = i < all ? i / w.plan.per : 0;
+                c[u] = i < all ? sh.some[p] * w.plan.per + (i - p * w.plan.per) : chunks;
+                if (c[u] < chunks) fqs_load<WIDE>(a, b, skew, c[u], x[u]);
             }
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (c[u] < chunks)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (x[u][e] > -__builtin_inff() && in_bin(x[u][e], bin)) {
+                            const int at = atomicAdd(&sh.n, 1);
+                            if (at < FQS_LIST) sh.list[at] = fqs_comp<WIDE>(x[u][e], 8 * c[u] - skew + e);
+                        }
         }
         __syncthreads();
     }
@@ -297,10 +309,12 @@ struct fqs_finder {
             each_logit([&](float x, int i) __attribute__((always_inline)) { if (in_bin(x, bin)) f(fqs_comp<WIDE>(x, i)); });
     }
     __device__ __forceinline__ fqs_u64 mass_of(fqs_u64 comp) { return fqs_mass(value_of(comp), top, r.c); }
-    // The least comp of the bin's best tokens: of the first `want`, or (BY_MASS) of the first whose mass reaches `want`.
+    // The least comp of the bin's best tokens: of the first `want`, or (BY_MASS) of the first whose mass reaches `want`.  Eight bits at a time from the
+    // highest in which the bin's comps differ: sums for each digit, then the first wave finds the digit in which the run ends, while the others clear
+    // the sums of the next eight.
     template <bool BY_MASS>
     __device__ __forceinline__ fqs_u64 select(int bin, fqs_u64 want) {
-        // bits above the highest in which the bin's comps differ are the same for all
+        const int lane = t & 63, wave = t >> 6;
         fqs_u64 lo = ~0ull, hi = 0ull;
         each_in_bin(bin, [&](fqs_u64 c) __attribute__((always_inline)) { lo = c < lo ? c : lo; hi = c > hi ? c : hi; });
 #pragma unroll
@@ -310,32 +324,62 @@ struct fqs_finder {
             hi = h > hi ? h : hi;
         }
         __syncthreads();
-        if ((t & 63) == 0) { sh.digit[t >> 6] = lo; sh.digit[32 + (t >> 6)] = hi; }
+        if (lane == 0) { sh.scan[wave] = lo; sh.reach[wave] = hi; }
+        for (int i = t; i < 256; i += FQS_T2) sh.digit[0][i] = 0;
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < FQS_T2 / 64; ++i) {
-            lo = sh.digit[i] < lo ? sh.digit[i] : lo;
-            hi = sh.digit[32 + i] > hi ? sh.digit[32 + i] : hi;
+            lo = sh.scan[i] < lo ? sh.scan[i] : lo;
+            hi = sh.reach[i] > hi ? sh.reach[i] : hi;
         }
         if (lo >= hi) return lo;                          // one token
         int above = 64 - __builtin_clzll(lo ^ hi);        // bits below are still open
-        fqs_u64 prefix = above >= 64 ? 0 : hi >> above << above;
-        while (above > 0) {
+        fqs_u64 prefix = hi >> above << above;            // (comps have 52 bits)
+        const bool listed = sh.n <= FQS_LIST;             // (their number then fits beside their mass)
+        for (int buf = 0; above > 0; buf ^= 1) {
             const int width = above < 8 ? above : 8, shift = above - width;
-            __syncthreads();
-            if (t < 256) sh.digit[t] = 0;
-            __syncthreads();
             each_in_bin(bin, [&](fqs_u64 c) __attribute__((always_inline)) {
-                if ((c ^ prefix) >> above == 0) atomicAdd(&sh.digit[255 - (int)(c >> shift & ((1u << width) - 1u))], BY_MASS ? mass_of(c) : 1ull);
+                if ((c ^ prefix) >> above == 0) atomicAdd(&sh.digit[buf][255 - (int)(c >> shift & ((1u << width) - 1u))], BY_MASS ? (listed ? 1ull << 50 : 0ull) + mass_of(c) : 1ull);
             });
             __syncthreads();
-            const fqs_u64 own = t < 256 ? sh.digit[t] : 0;
-            fqs_u64 all;
-            const fqs_u64 cum = fqs_scan(own, sh.scan, all);
-            first_reaching(own, cum, 256, want);
-            if (sh.found >= 256) return prefix;           // (all of them do not reach it: rounding)
+            if (wave == 0) {
+                fqs_u64 v[4], own = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] = sh.digit[buf][4 * lane + i];
+                    own += BY_MASS && listed ? v[i] & FQS_MASS : v[i];
+                }
+                fqs_u64 cum = own;
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const fqs_u64 o = __shfl_up(cum, d, 64);
+                    if (lane >= d) cum += o;
+                }
+                const unsigned long long reached = __ballot(cum >= want);
+                if (reached == 0ull) {
+                    if (lane == 0) sh.found = 256;
+                } else if (lane == __ffsll((long long)reached) - 1) {
+                    fqs_u64 before = cum - own;
+                    int i = 0;
+                    for (; i < 3; ++i) {
+                        const fqs_u64 x = BY_MASS && listed ? v[i] & FQS_MASS : v[i];
+                        if (before + x >= want) break;
+                        before += x;
+                    }
+                    sh.found = 4 * lane + i;
+                    sh.found_before = before;
+                    sh.found_own = i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : v[3];
+                }
+            } else {
+                for (int i = t - 64; i < 256; i += FQS_T2 - 64) sh.digit[buf ^ 1][i] = 0;
+            }
+            __syncthreads();
+            const int found = sh.found;
+            if (found >= 256) return prefix;              // (all of them do not reach it: rounding)
             want -= sh.found_before;
-            prefix |= (fqs_u64)(255 - sh.found) << shift;
+            prefix |= (fqs_u64)(255 - found) << shift;
+            // one token, or as many as are wanted: whatever its lower bits
+            if (BY_MASS ? listed && sh.found_own >> 50 == 1ull : sh.found_own == want) return prefix;
             above = shift;
         }
         return prefix;
@@ -364,10 +408,11 @@ __global__ __launch_bounds__(FQS_T2) void fqs_row_kernel(fq_sample_args a, fqs_w
         top = x;
     }
     top = fqs_wave_max(top);
-    if ((t & 63) == 0) sh.digit[t >> 6] = __float_as_uint(top);
+    if ((t & 63) == 0) sh.scan[t >> 6] = __float_as_uint(top);
     bad = __syncthreads_or(bad);
 #pragma unroll
-    for (int i = 0; i < FQS_T2 / 64; ++i) top = fmaxf(top, __uint_as_float((unsigned)sh.digit[i]));
+    for (int i = 0; i < FQS_T2 / 64; ++i) top = fmaxf(top, __uint_as_float((unsigned)sh.scan[i]));
+    __syncthreads();
     if (bad || !(top > -__builtin_inff())) {
         if (t == 0) {
             a.token[b] = -1;
@@ -393,20 +438,20 @@ __global__ __launch_bounds__(FQS_T2) void fqs_row_kernel(fq_sample_args a, fqs_w
     if (r.filtered) {
         unsigned count = 0;
         fqs_u64 mass = 0;
-        if (t < FQS_BINS)
-            for (int p = 0; p < parts; ++p) {
-                const int q = t - sh.shift[p];
-                if (q < 0) continue;
-                const fqs_u64 v = w.bins[((size_t)b * parts + p) * FQS_BINS + q];
-                count += (unsigned)(v >> 50);
-                mass += (fqs_u64)rint((double)(v & FQS_MASS) * (double)sh.factor[p]);
+        static_assert(FQS_BINS == FQS_T2, "a bin a thread");
+        for (int p0 = 0; p0 < parts; p0 += 8) {           // (eight requested at a time)
+            fqs_u64 v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = p0 + u < parts ? find.bin_of(p0 + u, t) : 0ull;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                count += (unsigned)(v[u] >> 50);
+                mass += (fqs_u64)rint((double)(v[u] & FQS_MASS) * (double)sh.factor[p0 + u < parts ? p0 + u : 0]);
             }
+        }
         fqs_u64 all;
         const fqs_u64 counts = fqs_scan(count, sh.scan, all), masses = fqs_scan(mass, sh.scan, all);
-        if (t < FQS_BINS) {
-            sh.count[t] = (unsigned)counts;
-            sh.mass[t] = masses;
-        }
+        sh.mass[t] = masses;
         int bin = FQS_BINS;                               // the bin in which the kept run ends (FQS_BINS: behind all)
         fqs_u64 run = all;                                // its mass
         // min-p: from a value on
@@ -461,13 +506,13 @@ __global__ __launch_bounds__(FQS_T2) void fqs_row_kernel(fq_sample_args a, fqs_w
         }
         // kept mass of each part: its bins before that one, and the kept of that one
         __syncthreads();
-        const int lane = t & 63, end = bin;
+        const int lane = t & 63;
         for (int p = t >> 6; p < parts; p += FQS_T2 / 64) {
-            fqs_u64 m = 0;
-            for (int i = lane; i < end; i += 64) {
-                const int q = i - sh.shift[p];
-                if (q >= 0) m += (fqs_u64)rint((double)(w.bins[((size_t)b * parts + p) * FQS_BINS + q] & FQS_MASS) * (double)sh.factor[p]);
-            }
+            fqs_u64 v[FQS_BINS / 64], m = 0;
+#pragma unroll
+            for (int i = 0; i < FQS_BINS / 64; ++i) v[i] = lane + 64 * i < bin ? find.bin_of(p, lane + 64 * i) : 0ull;
+#pragma unroll
+            for (int i = 0; i < FQS_BINS / 64; ++i) m += (fqs_u64)rint((double)(v[i] & FQS_MASS) * (double)sh.factor[p]);
             m = fqs_wave_sum(m);
             if (lane == 0) sh.part_mass[p] = m;
         }
@@ -487,14 +532,22 @@ __global__ __launch_bounds__(FQS_T2) void fqs_row_kernel(fq_sample_args a, fqs_w
     const double left = (double)(target - sh.found_before);   // in the row's unit
     const double scale = 1.0 / (double)sh.factor[part];
     const float part_top = sh.top[part];
-    float x[8];
+    constexpr int MINE = 4 * FQS_T1 / FQS_T2;             // chunks of a thread, one behind the other
+    static_assert(MINE * FQS_T2 == 4 * FQS_T1, "a part's chunks");
+    float x[MINE][8];
     fqs_u64 m = 0;
-    const int c = part * w.plan.per + t;                  // (a part has at most as many chunks as there are threads)
-    const bool on = t < w.plan.per;
-    if (on) fqs_load<WIDE>(a, b, skew, c, x);
+    const int c0 = part * w.plan.per + MINE * t;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (on && x[e] > -__builtin_inff() && fqs_comp<WIDE>(x[e], 8 * c - skew + e) >= least) m += fqs_mass(x[e], part_top, r.c);
+    for (int u = 0; u < MINE; ++u) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[u][e] = -__builtin_inff();
+        if (MINE * t + u < w.plan.per) fqs_load<WIDE>(a, b, skew, c0 + u, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < MINE; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (x[u][e] > -__builtin_inff() && fqs_comp<WIDE>(x[u][e], 8 * (c0 + u) - skew + e) >= least) m += fqs_mass(x[u][e], part_top, r.c);
     fqs_u64 in_part, run = fqs_scan(m, sh.scan, in_part) - m;
     // (the part's own sum and the bins' may differ by rounding: the last token with a mass then)
     double want = left * scale;
@@ -503,14 +556,17 @@ __global__ __launch_bounds__(FQS_T2) void fqs_row_kernel(fq_sample_args a, fqs_w
         int token = -1;
         float value = 0.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (token >= 0 || !(x[e] > -__builtin_inff()) || fqs_comp<WIDE>(x[e], 8 * c - skew + e) < least) continue;
-            run += fqs_mass(x[e], part_top, r.c);
-            if ((double)run > want) {
-                token = 8 * c - skew + e;
-                value = x[e];
+        for (int u = 0; u < MINE; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = 8 * (c0 + u) - skew + e;
+                if (token >= 0 || !(x[u][e] > -__builtin_inff()) || fqs_comp<WIDE>(x[u][e], i) < least) continue;
+                run += fqs_mass(x[u][e], part_top, r.c);
+                if ((double)run > want) {
+                    token = i;
+                    value = x[u][e];
+                }
             }
-        }
         a.token[b] = token;
         if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)total * 0x1p-36));
     }
