@@ -1,13 +1,14 @@
 // A token for each row of logits (include/fireq_sample.h).
 //
 // min-p, top-k and top-p all keep a first run of the tokens in one order (larger logit first, lower index first among equals), so
-// what is kept is comp >= tau for one number: comp = (ordered bits of the logit, inverted index).  Two kernels find it without sorting:
-//     parts   a row is cut into parts of up to 8192 logits.  Each finds its largest logit, takes e = exp((x - largest) / T) as a whole number of
-//             2^-36 (sums of whole numbers do not depend on their order; a token below 2^-37 of its part's best has no mass) and, where the row is
-//             filtered at all, counts numbers and masses in FQS_BINS equal steps of x / T.  The steps lie on one grid for all parts.
-//     row     one workgroup per row adds the parts' bins and finds the bin in which the kept run ends.  Only that bin's tokens are looked at
-//             one by one: a radix selection by number or by mass over comp, in LDS (or over the row again, where they are too many).  The token: the
-//             part, and in it the index, at which the kept mass in index order passes u times its sum.
+// what is kept is comp >= least for one number: comp = (ordered bits of the logit, inverted index).  Three kernels find it without sorting:
+//     parts    a row is cut into parts of up to 8192 logits.  Each finds its largest logit, takes e = exp((x - largest) / T) as a whole number of
+//              2^-36 (sums of whole numbers do not depend on their order; a token below 2^-37 of its part's best has no mass) and, where the row is
+//              filtered at all, counts numbers and masses in FQS_BINS equal steps of x / T.  The steps lie on one grid for all parts.
+//     borders  a workgroup per row adds the parts' bins and finds the bin in which min-p or top-k end, and those in which top-p may.
+//     draw     the parts again: the tokens of those bins into a list.  The row's last workgroup selects among them, by number and then by mass, eight
+//              bits of comp at a time (over the row again, where they are too many for its LDS), and finds the part, and in it the index, at which the
+//              kept mass in index order passes u times its sum.
 #include "fq_common.h"
 #include "fq_kernels.h"
 
@@ -15,7 +16,7 @@ namespace {
 
 typedef unsigned long long fqs_u64;
 
-constexpr int FQS_BINS = 512, FQS_LIST = 4096, FQS_T1 = 256, FQS_T2 = 512, FQS_MOST_PARTS = 256;
+constexpr int FQS_BINS = 512, FQS_LIST = 6144, FQS_T1 = 256, FQS_MOST_PARTS = 256;
 constexpr float FQS_UNIT = 0x1p36f;                       // masses in 2^-36 of the largest
 constexpr float FQS_SPAN = 26.0f;                         // nats that the bins cover: e^-26 is below 2^-37
 constexpr fqs_u64 FQS_MASS = (1ull << 50) - 1;            // a part's bin: number of tokens << 50 | mass (8192 * 2^36 at most)
@@ -29,10 +30,21 @@ __host__ __device__ inline fqs_plan fqs_choose(int B, int V) {
     return {per, (chunks + per - 1) / per};
 }
 
+// What `borders` finds of a row, and what its workgroups in `draw` count.
+struct fqs_border {
+    float top, line;                                      // largest logit, the grid line below it (NaN: nothing can be drawn)
+    fqs_u64 total, run, before, least;                    // masses: of all tokens; of the bins kept whole; of those before `low`.  min-p's comp
+    fqs_u64 rank_left;                                    // top-k: tokens to keep of bin `end` (0: all)
+    int end, low, high;                                   // bins: where min-p or top-k end, and from which to which top-p may (FQS_BINS: nowhere)
+    int listed, arrived;                                  // in `draw`: tokens in the list, workgroups that are through
+};
 struct fqs_work {
     float* top;                                           // [B][parts] largest logit of a part; NaN: one that is NaN or +infinity
     fqs_u64* total;                                       // [B][parts] mass of all its tokens
+    fqs_u64* sure;                                        // [B][parts] and of those in bins before the list's, in the row's unit
     fqs_u64* bins;                                        // [B][parts][FQS_BINS]
+    fqs_u64* list;                                        // [B][FQS_LIST] comps
+    fqs_border* border;                                   // [B]
     fqs_plan plan;
 };
 
@@ -196,7 +208,8 @@ __global__ __launch_bounds__(FQS_T1) void fqs_parts_kernel(fq_sample_args a, fqs
         for (int i = t; i < FQS_BINS; i += FQS_T1) w.bins[at * FQS_BINS + i] = bins[i];
 }
 
-// Inclusive sums over the workgroup's threads, in their order; `all`: the sum.  (scratch: one number a wave)
+// Inclusive sums over a workgroup of THREADS threads, in their order; `all`: the sum.  (scratch: one number a wave)
+template <int THREADS>
 __device__ __forceinline__ fqs_u64 fqs_scan(fqs_u64 v, fqs_u64* scratch, fqs_u64& all) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
@@ -210,113 +223,181 @@ __device__ __forceinline__ fqs_u64 fqs_scan(fqs_u64 v, fqs_u64* scratch, fqs_u64
     fqs_u64 before = 0;
     all = 0;
 #pragma unroll
-    for (int i = 0; i < FQS_T2 / 64; ++i) {
+    for (int i = 0; i < THREADS / 64; ++i) {
         if (i < wave) before += scratch[i];
         all += scratch[i];
     }
     return v + before;
 }
 
+__device__ __forceinline__ fqs_u64 fqs_scaled(fqs_u64 mass, float factor) { return (fqs_u64)rint((double)mass * (double)factor); }
+// A part's masses in the row's unit, and its bins' distance from the row's.
+__device__ __forceinline__ float fqs_factor(float part_top, float top, float c) { return part_top > -__builtin_inff() ? __builtin_amdgcn_exp2f((part_top - top) * c) : 0.0f; }
+__device__ __forceinline__ int fqs_shift(float part_top, float line, float steps) {
+    const float d = part_top > -__builtin_inff() ? line - fqs_line(part_top, steps) : (float)FQS_BINS;
+    return d < (float)FQS_BINS ? (int)d : FQS_BINS;
+}
+
+// A bin a thread.
+__global__ __launch_bounds__(FQS_BINS) void fqs_borders_kernel(fq_sample_args a, fqs_work w) {
+    constexpr int WAVES = FQS_BINS / 64;
+    __shared__ fqs_u64 scan[WAVES];
+    __shared__ float tops[WAVES], factor[FQS_MOST_PARTS];
+    __shared__ int shift[FQS_MOST_PARTS];
+    __shared__ fqs_u64 ends[3][2], at_end[2];             // of three borders: bin, what lies before it; masses before and up to `end`
+    const int b = blockIdx.x, t = threadIdx.x, parts = w.plan.parts;
+    const fqs_row r = fqs_parameters(a, b);
+    fqs_border* const out = w.border + b;
+    float top = -__builtin_inff(), mine = top;
+    fqs_u64 part_total = 0;
+    int bad = r.bad ? 1 : 0;
+    if (t < parts) {
+        mine = w.top[(size_t)b * parts + t];
+        part_total = w.total[(size_t)b * parts + t];
+        bad |= mine != mine ? 1 : 0;
+    }
+    top = fqs_wave_max(mine);
+    if ((t & 63) == 0) tops[t >> 6] = top;
+    bad = __syncthreads_or(bad);
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) top = fmaxf(top, tops[i]);
+    if (bad || !(top > -__builtin_inff())) {
+        if (t == 0) {
+            out->top = out->line = __builtin_nanf("");
+            out->listed = out->arrived = 0;
+        }
+        return;
+    }
+    const float line = fqs_line(top, r.steps);
+    if (t < parts) {
+        factor[t] = fqs_factor(mine, top, r.c);
+        shift[t] = fqs_shift(mine, line, r.steps);
+        part_total = fqs_scaled(part_total, factor[t]);
+    }
+    fqs_u64 total;
+    fqs_scan<FQS_BINS>(part_total, scan, total);          // (its barriers also publish factors and shifts)
+    fqs_border o = {top, line, total, total, 0, 0, 0, FQS_BINS, FQS_BINS, FQS_BINS, 0, 0};
+    if (r.filtered) {
+        unsigned count = 0;
+        fqs_u64 mass = 0;
+        for (int p0 = 0; p0 < parts; p0 += 16) {          // (sixteen requested at a time)
+            fqs_u64 v[16];
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                const int p = p0 + u < parts ? p0 + u : 0, q = t - shift[p];
+                v[u] = w.bins[((size_t)b * parts + p) * FQS_BINS + (q < 0 ? 0 : q)];
+                v[u] = q < 0 || p0 + u >= parts ? 0ull : v[u];
+            }
+#pragma unroll
+            for (int u = 0; u < 16; ++u) {
+                count += (unsigned)(v[u] >> 50);
+                mass += fqs_scaled(v[u] & FQS_MASS, factor[p0 + u < parts ? p0 + u : 0]);
+            }
+        }
+        fqs_u64 all, tokens;
+        const fqs_u64 counts = fqs_scan<FQS_BINS>(count, scan, tokens), masses = fqs_scan<FQS_BINS>(mass, scan, all);
+        // where min-p ends: at a value
+        int end = FQS_BINS;
+        if (r.low > 0.0f) {
+            const double from = (double)top + r.T * log((double)r.low);
+            float x = (float)from;
+            if ((double)x < from) x = x < 0.0f ? __uint_as_float(__float_as_uint(x) - 1u) : x == 0.0f ? 0x1p-149f : __uint_as_float(__float_as_uint(x) + 1u);
+            const unsigned bits = __float_as_uint(x + 0.0f), k = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
+            o.least = (a.wide ? (fqs_u64)k : ((fqs_u64)k + 0xFFFF) >> 16) << 20;
+            const float d = line - fqs_line(x, r.steps);
+            end = d < (float)FQS_BINS ? (int)d : FQS_BINS;
+        }
+        // ... and top-k: the first border of the two
+        if (t < 3) { ends[t][0] = FQS_BINS; ends[t][1] = all; }
+        __syncthreads();
+        const fqs_u64 k = (fqs_u64)r.k;
+        if (k > 0 && counts >= k && counts - count < k && t <= end) {
+            ends[0][0] = t;
+            ends[0][1] = counts - count;
+        }
+        __syncthreads();
+        if (ends[0][0] < FQS_BINS) {
+            end = (int)ends[0][0];
+            o.rank_left = k - ends[0][1];
+        }
+        if (t == end) { at_end[0] = masses - mass; at_end[1] = masses; }
+        __syncthreads();
+        // what is kept of that bin lies between nothing and all, and so lie top-p's borders
+        const fqs_u64 least_run = end < FQS_BINS ? at_end[0] : all, most_run = end < FQS_BINS ? at_end[1] : all;
+        o.end = end;
+        o.run = least_run;
+        if (r.p < 1.0f) {
+            const float p = fmaxf(r.p, 0.0f);
+            const fqs_u64 lo = (fqs_u64)ceil((double)least_run * (double)p), hi = (fqs_u64)ceil((double)most_run * (double)p);
+            const fqs_u64 first = lo < 1 ? 1 : lo, last = hi < 1 ? 1 : hi;
+            if (masses >= first && masses - mass < first) { ends[1][0] = t; ends[1][1] = masses - mass; }
+            if (masses >= last && masses - mass < last) ends[2][0] = t;
+            __syncthreads();
+            o.low = (int)ends[1][0];
+            o.high = (int)ends[2][0];
+            o.before = ends[1][1];
+            if (o.high > end) o.high = end;
+            if (o.low > o.high) o.low = o.high;           // (where only the end's bin is left)
+        }
+    }
+    if (t == 0) *out = o;
+}
+
 struct fqs_shared {
-    fqs_u64 scan[FQS_T2 / 64], reach[FQS_T2 / 64];
+    fqs_u64 scan[FQS_T1 / 64], reach[FQS_T1 / 64];
     fqs_u64 part_mass[FQS_MOST_PARTS];                    // kept mass of each part
-    float top[FQS_MOST_PARTS];
-    float factor[FQS_MOST_PARTS];                         // of a part's masses
-    int shift[FQS_MOST_PARTS];                            // of its bins
-    fqs_u64 mass[FQS_BINS];                               // inclusive sums
     fqs_u64 digit[2][256];
-    fqs_u64 list[FQS_LIST];                               // comps of one bin
-    int some[FQS_MOST_PARTS];                             // parts that have tokens in it
+    fqs_u64 list[FQS_LIST];                               // comps
     fqs_u64 found_before, found_own;
-    int n, parts, found;
+    int found, last;
 };
 
+// The row's last workgroup over the listed tokens.
 template <bool WIDE>
 struct fqs_finder {
     const fq_sample_args& a;
-    const fqs_work& w;
     const fqs_row& r;
     fqs_shared& sh;
-    int b, skew, t;
+    int b, skew, t, n;                                    // n: tokens listed (or more than the list holds)
     float top, line;
 
-    // the first index whose value in `cum` (inclusive, of n) reaches `want`, in sh.found (n: none), and what lies before it
-    __device__ __forceinline__ void first_reaching(fqs_u64 own, fqs_u64 cum, int n, fqs_u64 want) {
-        __syncthreads();
-        if (t == 0) { sh.found = n; sh.found_before = 0; }
-        __syncthreads();
-        if (t < n && cum >= want && cum - own < want) {
-            sh.found = t;
-            sh.found_before = cum - own;
-        }
-        __syncthreads();
+    __device__ __forceinline__ int bin(float x) const {   // (-infinity lies in none)
+        const float d = line - fqs_line(x, r.steps);
+        return d < (float)FQS_BINS ? (int)d : FQS_BINS;
     }
-    template <class F>
-    __device__ __forceinline__ void each_logit(F f) {     // of the whole row
-        for (int c = t; c < (a.V + skew + 7) / 8; c += FQS_T2) {
-            float x[8];
-            fqs_load<WIDE>(a, b, skew, c, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (x[e] > -__builtin_inff()) f(x[e], 8 * c - skew + e);
-        }
-    }
-    __device__ __forceinline__ bool in_bin(float x, int bin) { return line - fqs_line(x, r.steps) == (float)bin; }
-    __device__ __forceinline__ float value_of(fqs_u64 comp) {
+    __device__ __forceinline__ float value_of(fqs_u64 comp) const {
         const unsigned k = (unsigned)(comp >> 20), o = WIDE ? k : k << 16;
         return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : WIDE ? ~o : ~o & 0xFFFF0000u);
     }
-    // a part's numbers in the row's bin i (0 before its first)
-    __device__ __forceinline__ fqs_u64 bin_of(int p, int i) {
-        const int q = i - sh.shift[p];
-        const fqs_u64 v = w.bins[((size_t)b * w.plan.parts + p) * FQS_BINS + (q < 0 ? 0 : q)];
-        return q < 0 ? 0ull : v;
-    }
-    // the tokens of a bin into the list; only those parts are read that have some, four chunks of a thread at a time
-    __device__ __forceinline__ void gather(int bin) {
-        __syncthreads();
-        if (t == 0) sh.n = sh.parts = 0;
-        __syncthreads();
-        if (t < w.plan.parts && bin_of(t, bin) != 0) sh.some[atomicAdd(&sh.parts, 1)] = t;
-        __syncthreads();
-        const int chunks = (a.V + skew + 7) / 8, all = sh.parts * w.plan.per;
-        for (int i0 = t; i0 < all; i0 += 4 * FQS_T2) {
-            float x[4][8];
-            int c[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int i = i0 + u * FQS_T2, p = i < all ? i / w.plan.per : 0;
-                c[u] = i < all ? sh.some[p] * w.plan.per + (i - p * w.plan.per) : chunks;
-                if (c[u] < chunks) fqs_load<WIDE>(a, b, skew, c[u], x[u]);
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-                if (c[u] < chunks)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (x[u][e] > -__builtin_inff() && in_bin(x[u][e], bin)) {
-                            const int at = atomicAdd(&sh.n, 1);
-                            if (at < FQS_LIST) sh.list[at] = fqs_comp<WIDE>(x[u][e], 8 * c[u] - skew + e);
-                        }
-        }
-        __syncthreads();
-    }
+    __device__ __forceinline__ fqs_u64 mass_of(fqs_u64 comp) const { return fqs_mass(value_of(comp), top, r.c); }
+    // the tokens of bins lo .. hi
     template <class F>
-    __device__ __forceinline__ void each_in_bin(int bin, F f) {
-        if (sh.n <= FQS_LIST)
-            for (int i = t; i < sh.n; i += FQS_T2) f(sh.list[i]);
-        else
-            each_logit([&](float x, int i) __attribute__((always_inline)) { if (in_bin(x, bin)) f(fqs_comp<WIDE>(x, i)); });
+    __device__ __forceinline__ void each(int lo, int hi, F f) const {
+        if (n <= FQS_LIST) {
+            for (int i = t; i < n; i += FQS_T1) {
+                const int q = bin(value_of(sh.list[i]));
+                if (q >= lo && q <= hi) f(sh.list[i]);
+            }
+            return;
+        }
+        for (int c = t; c < (a.V + skew + 7) / 8; c += FQS_T1) {
+            float x[8];
+            fqs_load<WIDE>(a, b, skew, c, x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int q = bin(x[e]);
+                if (q < FQS_BINS && q >= lo && q <= hi) f(fqs_comp<WIDE>(x[e], 8 * c - skew + e));
+            }
+        }
     }
-    __device__ __forceinline__ fqs_u64 mass_of(fqs_u64 comp) { return fqs_mass(value_of(comp), top, r.c); }
-    // The least comp of the bin's best tokens: of the first `want`, or (BY_MASS) of the first whose mass reaches `want`.  Eight bits at a time from the
-    // highest in which the bin's comps differ: sums for each digit, then the first wave finds the digit in which the run ends, while the others clear
-    // the sums of the next eight.
+    // The least comp of the best tokens of bins lo .. hi: of the first `want`, or (BY_MASS) of the first whose mass reaches `want`.  Eight bits at a
+    // time from the highest in which their comps differ: sums for each digit, then the first wave finds the digit in which the run ends, while the
+    // others clear the sums of the next eight.
     template <bool BY_MASS>
-    __device__ __forceinline__ fqs_u64 select(int bin, fqs_u64 want) {
+    __device__ __forceinline__ fqs_u64 select(int lo_bin, int hi_bin, fqs_u64 want) {
         const int lane = t & 63, wave = t >> 6;
         fqs_u64 lo = ~0ull, hi = 0ull;
-        each_in_bin(bin, [&](fqs_u64 c) __attribute__((always_inline)) { lo = c < lo ? c : lo; hi = c > hi ? c : hi; });
+        each(lo_bin, hi_bin, [&](fqs_u64 c) __attribute__((always_inline)) { lo = c < lo ? c : lo; hi = c > hi ? c : hi; });
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const fqs_u64 l = __shfl_xor(lo, d, 64), h = __shfl_xor(hi, d, 64);
@@ -325,20 +406,20 @@ struct fqs_finder {
         }
         __syncthreads();
         if (lane == 0) { sh.scan[wave] = lo; sh.reach[wave] = hi; }
-        for (int i = t; i < 256; i += FQS_T2) sh.digit[0][i] = 0;
+        sh.digit[0][t] = 0;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < FQS_T2 / 64; ++i) {
+        for (int i = 0; i < FQS_T1 / 64; ++i) {
             lo = sh.scan[i] < lo ? sh.scan[i] : lo;
             hi = sh.reach[i] > hi ? sh.reach[i] : hi;
         }
-        if (lo >= hi) return lo;                          // one token
+        if (lo >= hi) return lo == hi ? lo : 0;           // one token, or none
         int above = 64 - __builtin_clzll(lo ^ hi);        // bits below are still open
         fqs_u64 prefix = hi >> above << above;            // (comps have 52 bits)
-        const bool listed = sh.n <= FQS_LIST;             // (their number then fits beside their mass)
+        const bool listed = n <= FQS_LIST;                // (their number then fits beside their mass)
         for (int buf = 0; above > 0; buf ^= 1) {
             const int width = above < 8 ? above : 8, shift = above - width;
-            each_in_bin(bin, [&](fqs_u64 c) __attribute__((always_inline)) {
+            each(lo_bin, hi_bin, [&](fqs_u64 c) __attribute__((always_inline)) {
                 if ((c ^ prefix) >> above == 0) atomicAdd(&sh.digit[buf][255 - (int)(c >> shift & ((1u << width) - 1u))], BY_MASS ? (listed ? 1ull << 50 : 0ull) + mass_of(c) : 1ull);
             });
             __syncthreads();
@@ -371,7 +452,7 @@ struct fqs_finder {
                     sh.found_own = i == 0 ? v[0] : i == 1 ? v[1] : i == 2 ? v[2] : v[3];
                 }
             } else {
-                for (int i = t - 64; i < 256; i += FQS_T2 - 64) sh.digit[buf ^ 1][i] = 0;
+                for (int i = t - 64; i < 256; i += FQS_T1 - 64) sh.digit[buf ^ 1][i] = 0;
             }
             __syncthreads();
             const int found = sh.found;
@@ -384,191 +465,179 @@ struct fqs_finder {
         }
         return prefix;
     }
-    // mass of the bin's tokens from `least` on
-    __device__ __forceinline__ fqs_u64 kept_in_bin(int bin, fqs_u64 least) {
+    // mass of the tokens of a bin from `least` on
+    __device__ __forceinline__ fqs_u64 kept_in(int at, fqs_u64 least) {
         fqs_u64 m = 0, all;
-        each_in_bin(bin, [&](fqs_u64 c) __attribute__((always_inline)) { if (c >= least) m += mass_of(c); });
-        fqs_scan(m, sh.scan, all);
+        each(at, at, [&](fqs_u64 c) __attribute__((always_inline)) { if (c >= least) m += mass_of(c); });
+        fqs_scan<FQS_T1>(m, sh.scan, all);
         return all;
     }
 };
 
+// At device scope: past the caches of an XCD.
+__device__ __forceinline__ void fqs_store(fqs_u64* p, fqs_u64 v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ fqs_u64 fqs_fetch(const fqs_u64* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
 template <bool WIDE>
-__global__ __launch_bounds__(FQS_T2) void fqs_row_kernel(fq_sample_args a, fqs_work w) {
+__global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_work w) {
     __shared__ fqs_shared sh;
-    const int b = blockIdx.x, t = threadIdx.x, parts = w.plan.parts;
-    const fqs_row r = fqs_parameters(a, b);
-    // largest logit, then each part's factor and shift
-    float top = -__builtin_inff();
-    int bad = r.bad ? 1 : 0;
-    if (t < parts) {
-        const float x = w.top[(size_t)b * parts + t];
-        sh.top[t] = x;
-        bad |= x != x ? 1 : 0;
-        top = x;
-    }
-    top = fqs_wave_max(top);
-    if ((t & 63) == 0) sh.scan[t >> 6] = __float_as_uint(top);
-    bad = __syncthreads_or(bad);
-#pragma unroll
-    for (int i = 0; i < FQS_T2 / 64; ++i) top = fmaxf(top, __uint_as_float((unsigned)sh.scan[i]));
-    __syncthreads();
-    if (bad || !(top > -__builtin_inff())) {
-        if (t == 0) {
+    const int own_part = blockIdx.x, b = blockIdx.y, t = threadIdx.x, lane = t & 63, parts = w.plan.parts, per = w.plan.per;
+    fqs_border* const border = w.border + b;
+    const float top = border->top, line = border->line;
+    if (!(top > -__builtin_inff())) {                     // (NaN)
+        if (own_part == 0 && t == 0) {
             a.token[b] = -1;
             if (a.logprob) a.logprob[b] = __builtin_nanf("");
         }
         return;
     }
-    const float line = fqs_line(top, r.steps);
-    fqs_u64 part_total = 0;
-    if (t < parts) {
-        const float x = sh.top[t], f = x > -__builtin_inff() ? __builtin_amdgcn_exp2f((x - top) * r.c) : 0.0f;
-        const float d = x > -__builtin_inff() ? line - fqs_line(x, r.steps) : (float)FQS_BINS;
-        sh.factor[t] = f;
-        sh.shift[t] = d < (float)FQS_BINS ? (int)d : FQS_BINS;
-        part_total = (fqs_u64)rint((double)w.total[(size_t)b * parts + t] * (double)f);
-    }
-    fqs_u64 total;
-    fqs_scan(part_total, sh.scan, total);                 // (its barriers also publish factors and shifts)
-    const int skew = fqs_skew<WIDE>(a, b);
-    fqs_finder<WIDE> find = {a, w, r, sh, b, skew, t, top, line};
-    fqs_u64 least = 0, kept;                              // kept tokens: comp >= least
-    if (t < parts) sh.part_mass[t] = part_total;
-    if (r.filtered) {
-        unsigned count = 0;
-        fqs_u64 mass = 0;
-        static_assert(FQS_BINS == FQS_T2, "a bin a thread");
-        for (int p0 = 0; p0 < parts; p0 += 8) {           // (eight requested at a time)
-            fqs_u64 v[8];
+    const fqs_row r = fqs_parameters(a, b);
+    const int skew = fqs_skew<WIDE>(a, b), end = border->end, low = border->low, high = border->high;
+    const bool by_mass = low < FQS_BINS, listing = by_mass || end < FQS_BINS;
+    const int first = by_mass ? low : end;                // bins before it are kept whole
+    if (!listing && own_part != 0) return;                // every token is kept: one workgroup draws
+    if (listing) {
+        const int chunks = (a.V + skew + 7) / 8, mine = per / FQS_T1;
+        const float part_top = w.top[(size_t)b * parts + own_part];
+        fqs_u64 bins[FQS_BINS / FQS_T1];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = p0 + u < parts ? find.bin_of(p0 + u, t) : 0ull;
+        for (int i = 0; i < FQS_BINS / FQS_T1; ++i) bins[i] = w.bins[((size_t)b * parts + own_part) * FQS_BINS + t + i * FQS_T1];
+        float x[4][8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                count += (unsigned)(v[u] >> 50);
-                mass += (fqs_u64)rint((double)(v[u] & FQS_MASS) * (double)sh.factor[p0 + u < parts ? p0 + u : 0]);
+        for (int u = 0; u < 4; ++u) {
+            const int c = own_part * per + u * FQS_T1 + t;
+            if (u < mine && c < chunks) fqs_load<WIDE>(a, b, skew, c, x[u]);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[u][e] = -__builtin_inff();
+        }
+        // the listed tokens: those of bin `end`, and of low .. high
+        const float at0 = line - (float)low, at1 = line - (float)high, at2 = line - (float)end;
+        unsigned hits = 0u;                               // bit 8 u + e
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float y = fqs_line(x[u][e], r.steps);
+                hits |= (by_mass && y <= at0 && y >= at1) || (end < FQS_BINS && y == at2) ? 1u << (8 * u + e) : 0u;
             }
+        const int count = __popc(hits);
+        int before = count;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(before, d, 64);
+            if (lane >= d) before += o;
         }
-        fqs_u64 all;
-        const fqs_u64 counts = fqs_scan(count, sh.scan, all), masses = fqs_scan(mass, sh.scan, all);
-        sh.mass[t] = masses;
-        int bin = FQS_BINS;                               // the bin in which the kept run ends (FQS_BINS: behind all)
-        fqs_u64 run = all;                                // its mass
-        // min-p: from a value on
-        if (r.low > 0.0f) {
-            const double from = (double)top + r.T * log((double)r.low);
-            float x = (float)from;
-            if ((double)x < from) x = x < 0.0f ? __uint_as_float(__float_as_uint(x) - 1u) : x == 0.0f ? 0x1p-149f : __uint_as_float(__float_as_uint(x) + 1u);
-            const unsigned bits = __float_as_uint(x + 0.0f), o = bits & 0x80000000u ? ~bits : bits | 0x80000000u;
-            least = (WIDE ? (fqs_u64)o : ((fqs_u64)o + 0xFFFF) >> 16) << 20;
-            const float d = line - fqs_line(x, r.steps);
-            bin = d < (float)FQS_BINS ? (int)d : FQS_BINS;
+        int at = 0;
+        if (lane == 63 && before > 0) at = atomicAdd(&border->listed, before);
+        at = __shfl(at, 63, 64) + before - count;
+        while (hits != 0u) {
+            const int bit = __ffs((int)hits) - 1;
+            hits &= hits - 1u;
+            float v = x[0][0];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v = bit == 8 * u + e ? x[u][e] : v;
+            const int c = own_part * per + (bit >> 3) * FQS_T1 + t;
+            if (at < FQS_LIST) fqs_store(w.list + (size_t)b * FQS_LIST + at, fqs_comp<WIDE>(v, 8 * c - skew + (bit & 7)));
+            ++at;
         }
-        bool ranked = false;
-        fqs_u64 rank_left = 0;
-        if (r.k > 0) {
-            find.first_reaching(count, counts, FQS_BINS, (fqs_u64)r.k);
-            if (sh.found <= bin && sh.found < FQS_BINS) {
-                bin = sh.found;
-                ranked = true;
-                rank_left = (fqs_u64)r.k - sh.found_before;
-            }
-        }
-        if (bin < FQS_BINS) {
-            find.gather(bin);
-            if (ranked && sh.n > 0) {
-                const fqs_u64 x = find.template select<false>(bin, rank_left);
-                least = x > least ? x : least;
-            }
-            run = (bin > 0 ? sh.mass[bin - 1] : 0) + find.kept_in_bin(bin, least);
-        }
-        if (r.p < 1.0f) {
-            fqs_u64 want = (fqs_u64)ceil((double)run * (double)r.p);
-            want = want < 1 ? 1 : want;
-            if (r.p <= 0.0f) want = 1;
-            const fqs_u64 before_bin = bin < FQS_BINS ? (bin > 0 ? sh.mass[bin - 1] : 0) : all;
-            if (bin < FQS_BINS && want > before_bin) {
-                if (sh.n > 0) {
-                    const fqs_u64 x = find.template select<true>(bin, want - before_bin);
-                    least = x > least ? x : least;
-                }
-            } else {
-                find.first_reaching(mass, masses, FQS_BINS, want);
-                const int at = sh.found;
-                const fqs_u64 left = want - sh.found_before;
-                if (at < FQS_BINS) {
-                    bin = at;
-                    find.gather(bin);
-                    const fqs_u64 x = find.template select<true>(bin, left);
-                    least = x > least ? x : least;
-                }
-            }
-        }
-        // kept mass of each part: its bins before that one, and the kept of that one
+        fqs_u64 sure = 0, all;
+        const int shift = fqs_shift(part_top, line, r.steps);
+        const float f = fqs_factor(part_top, top, r.c);
+#pragma unroll
+        for (int i = 0; i < FQS_BINS / FQS_T1; ++i)
+            if (t + i * FQS_T1 + shift < first) sure += fqs_scaled(bins[i] & FQS_MASS, f);
+        fqs_scan<FQS_T1>(sure, sh.scan, all);
+        if (t == 0) fqs_store(w.sure + (size_t)b * parts + own_part, all);
+        // The row's last workgroup goes on.  What it reads of the others was stored and is read at device scope, and every store has been acknowledged there
+        // before its workgroup counts itself in (a fence would write back the whole L2 for each).
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        const int lane = t & 63;
-        for (int p = t >> 6; p < parts; p += FQS_T2 / 64) {
-            fqs_u64 v[FQS_BINS / 64], m = 0;
-#pragma unroll
-            for (int i = 0; i < FQS_BINS / 64; ++i) v[i] = lane + 64 * i < bin ? find.bin_of(p, lane + 64 * i) : 0ull;
-#pragma unroll
-            for (int i = 0; i < FQS_BINS / 64; ++i) m += (fqs_u64)rint((double)(v[i] & FQS_MASS) * (double)sh.factor[p]);
-            m = fqs_wave_sum(m);
-            if (lane == 0) sh.part_mass[p] = m;
-        }
+        if (t == 0) sh.last = __hip_atomic_fetch_add(&border->arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1 ? 1 : 0;
         __syncthreads();
-        if (bin < FQS_BINS)
-            find.each_in_bin(bin, [&](fqs_u64 c) __attribute__((always_inline)) {
-                if (c >= least) atomicAdd(&sh.part_mass[((int)(0xFFFFF - (c & 0xFFFFF)) + skew) / 8 / w.plan.per], find.mass_of(c));
-            });
+        if (!sh.last) return;
     }
+    fqs_finder<WIDE> find = {a, r, sh, b, skew, t, 0, top, line};
+    fqs_u64 least = border->least, kept;                  // kept tokens: comp >= least
+    if (listing) {
+        find.n = __hip_atomic_load(&border->listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (find.n <= FQS_LIST)
+            for (int i = t; i < find.n; i += FQS_T1) sh.list[i] = fqs_fetch(w.list + (size_t)b * FQS_LIST + i);
+    }
+    if (t < parts) sh.part_mass[t] = listing ? fqs_fetch(w.sure + (size_t)b * parts + t) : fqs_scaled(w.total[(size_t)b * parts + t], fqs_factor(w.top[(size_t)b * parts + t], top, r.c));
     __syncthreads();
+    fqs_u64 run = border->run;
+    if (end < FQS_BINS) {
+        const fqs_u64 left = border->rank_left;
+        if (left > 0) {
+            const fqs_u64 x = find.template select<false>(end, end, left);
+            least = x > least ? x : least;
+        }
+        if (by_mass) run += find.kept_in(end, least);
+    }
+    if (by_mass) {
+        fqs_u64 want = (fqs_u64)ceil((double)run * (double)fmaxf(r.p, 0.0f));
+        want = want < 1 ? 1 : want;
+        const fqs_u64 before = border->before, x = find.template select<true>(low, high, want > before ? want - before : 1);
+        least = x > least ? x : least;
+    }
+    if (listing) {
+        find.each(first, by_mass ? high : end, [&](fqs_u64 c) __attribute__((always_inline)) {
+            if (c >= least) atomicAdd(&sh.part_mass[((int)(0xFFFFF - (c & 0xFFFFF)) + skew) / 8 / per], find.mass_of(c));
+        });
+        __syncthreads();
+    }
     // the part, then the token, at which the mass in index order passes u times the whole
-    const fqs_u64 own = t < parts ? sh.part_mass[t] : 0, cum = fqs_scan(own, sh.scan, kept);
+    const fqs_u64 own = t < parts ? sh.part_mass[t] : 0, cum = fqs_scan<FQS_T1>(own, sh.scan, kept);
     const float u = fminf(fmaxf(a.u[b], 0.0f), 0x1.fffffep-1f);
     const fqs_u64 target = (fqs_u64)((double)u * (double)kept);
-    find.first_reaching(own, cum, parts, target + 1);
-    const int part = sh.found < parts ? sh.found : parts - 1;
-    const double left = (double)(target - sh.found_before);   // in the row's unit
-    const double scale = 1.0 / (double)sh.factor[part];
-    const float part_top = sh.top[part];
-    constexpr int MINE = 4 * FQS_T1 / FQS_T2;             // chunks of a thread, one behind the other
-    static_assert(MINE * FQS_T2 == 4 * FQS_T1, "a part's chunks");
-    float x[MINE][8];
-    fqs_u64 m = 0;
-    const int c0 = part * w.plan.per + MINE * t;
-#pragma unroll
-    for (int u = 0; u < MINE; ++u) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[u][e] = -__builtin_inff();
-        if (MINE * t + u < w.plan.per) fqs_load<WIDE>(a, b, skew, c0 + u, x[u]);
+    if (cum > target && cum - own <= target) {            // (one thread's: u * kept is below kept)
+        sh.found = t;
+        sh.found_before = cum - own;
     }
+    __syncthreads();
+    const int part = sh.found;
+    const float part_top = w.top[(size_t)b * parts + part];
+    float x[4][8];
+    fqs_u64 m = 0;
+    const int c0 = part * per + 4 * t;                    // four chunks of a thread, one behind the other
 #pragma unroll
-    for (int u = 0; u < MINE; ++u)
+    for (int i = 0; i < 4; ++i) {
+        if (4 * t + i < per) fqs_load<WIDE>(a, b, skew, c0 + i, x[i]);
+        else
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (x[u][e] > -__builtin_inff() && fqs_comp<WIDE>(x[u][e], 8 * (c0 + u) - skew + e) >= least) m += fqs_mass(x[u][e], part_top, r.c);
-    fqs_u64 in_part, run = fqs_scan(m, sh.scan, in_part) - m;
+            for (int e = 0; e < 8; ++e) x[i][e] = -__builtin_inff();
+    }
+    auto mass = [&](int i, int e) __attribute__((always_inline)) {
+        const float v = x[i][e];
+        return v > -__builtin_inff() && fqs_comp<WIDE>(v, 8 * (c0 + i) - skew + e) >= least ? fqs_mass(v, part_top, r.c) : 0ull;
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m += mass(i, e);
+    fqs_u64 in_part, at = fqs_scan<FQS_T1>(m, sh.scan, in_part) - m;
     // (the part's own sum and the bins' may differ by rounding: the last token with a mass then)
-    double want = left * scale;
+    double want = (double)(target - sh.found_before) / (double)fqs_factor(part_top, top, r.c);
     if (!(want < (double)in_part)) want = in_part > 0 ? (double)(in_part - 1) : 0.0;
-    if ((double)run <= want && want < (double)(run + m)) {
+    if ((double)at <= want && want < (double)(at + m)) {
         int token = -1;
         float value = 0.f;
 #pragma unroll
-        for (int u = 0; u < MINE; ++u)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int i = 8 * (c0 + u) - skew + e;
-                if (token >= 0 || !(x[u][e] > -__builtin_inff()) || fqs_comp<WIDE>(x[u][e], i) < least) continue;
-                run += fqs_mass(x[u][e], part_top, r.c);
-                if ((double)run > want) {
-                    token = i;
-                    value = x[u][e];
+                if (token >= 0) continue;
+                at += mass(i, e);
+                if ((double)at > want) {
+                    token = 8 * (c0 + i) - skew + e;
+                    value = x[i][e];
                 }
             }
         a.token[b] = token;
-        if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)total * 0x1p-36));
+        if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)border->total * 0x1p-36));
     }
 }
 
@@ -576,7 +645,7 @@ __global__ __launch_bounds__(FQS_T2) void fqs_row_kernel(fq_sample_args a, fqs_w
 
 size_t fq_sample_scratch_bytes(int B, int V) {
     const size_t rows = (size_t)B * fqs_choose(B, V).parts;
-    return rows * (8 * FQS_BINS + 8) + (rows * 4 + 15) / 16 * 16;
+    return rows * (8 * FQS_BINS + 16) + (size_t)B * (8 * FQS_LIST + sizeof(fqs_border)) + (rows * 4 + 15) / 16 * 16;
 }
 
 void fq_launch_sample(const fq_sample_args& a, void* scratch, hipStream_t stream) {
@@ -585,13 +654,14 @@ void fq_launch_sample(const fq_sample_args& a, void* scratch, hipStream_t stream
     const size_t rows = (size_t)a.B * w.plan.parts;
     w.bins = static_cast<fqs_u64*>(scratch);
     w.total = w.bins + rows * FQS_BINS;
-    w.top = reinterpret_cast<float*>(w.total + rows);
+    w.sure = w.total + rows;
+    w.list = w.sure + rows;
+    w.border = reinterpret_cast<fqs_border*>(w.list + (size_t)a.B * FQS_LIST);
+    w.top = reinterpret_cast<float*>(w.border + a.B);
     const dim3 grid((unsigned)w.plan.parts, (unsigned)a.B);
-    if (a.wide) {
-        hipLaunchKernelGGL(fqs_parts_kernel<true>, grid, dim3(FQS_T1), 0, stream, a, w);
-        hipLaunchKernelGGL(fqs_row_kernel<true>, dim3((unsigned)a.B), dim3(FQS_T2), 0, stream, a, w);
-    } else {
-        hipLaunchKernelGGL(fqs_parts_kernel<false>, grid, dim3(FQS_T1), 0, stream, a, w);
-        hipLaunchKernelGGL(fqs_row_kernel<false>, dim3((unsigned)a.B), dim3(FQS_T2), 0, stream, a, w);
-    }
+    if (a.wide) hipLaunchKernelGGL(fqs_parts_kernel<true>, grid, dim3(FQS_T1), 0, stream, a, w);
+    else hipLaunchKernelGGL(fqs_parts_kernel<false>, grid, dim3(FQS_T1), 0, stream, a, w);
+    hipLaunchKernelGGL(fqs_borders_kernel, dim3((unsigned)a.B), dim3(FQS_BINS), 0, stream, a, w);
+    if (a.wide) hipLaunchKernelGGL(fqs_draw_kernel<true>, grid, dim3(FQS_T1), 0, stream, a, w);
+    else hipLaunchKernelGGL(fqs_draw_kernel<false>, grid, dim3(FQS_T1), 0, stream, a, w);
 }
