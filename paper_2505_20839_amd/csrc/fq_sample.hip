@@ -3,7 +3,7 @@
 // min-p, top-k and top-p all keep a first run of the tokens in one order (larger logit first, lower index first among equals), so
 // what is kept is comp >= least for one number: comp = (ordered bits of the logit, inverted index).  Three kernels find it without sorting:
 //     parts    a row is cut into parts of up to 8192 logits.  Each finds its largest logit, takes e = exp((x - largest) / T) as a whole number of
-//              2^-36 (sums of whole numbers do not depend on their order; a token below 2^-37 of its part's best has no mass) and, where the row is
+//              2^-32 (sums of whole numbers do not depend on their order; a token below 2^-33 of its part's best has no mass) and, where the row is
 //              filtered at all, counts numbers and masses in FQS_BINS equal steps of x / T.  The steps lie on one grid for all parts.
 //     borders  a workgroup per row adds the parts' bins and finds the bin in which min-p or top-k end, and those in which top-p may.
 //     draw     the parts again: the tokens of those bins into a list.  The row's last workgroup selects among them, by number and then by mass, eight
@@ -16,10 +16,10 @@ namespace {
 
 typedef unsigned long long fqs_u64;
 
-constexpr int FQS_BINS = 512, FQS_LIST = 6144, FQS_T1 = 256, FQS_MOST_PARTS = 256;
-constexpr float FQS_UNIT = 0x1p36f;                       // masses in 2^-36 of the largest
-constexpr float FQS_SPAN = 26.0f;                         // nats that the bins cover: e^-26 is below 2^-37
-constexpr fqs_u64 FQS_MASS = (1ull << 50) - 1;            // a part's bin: number of tokens << 50 | mass (8192 * 2^36 at most)
+constexpr int FQS_BINS = 512, FQS_LIST = 4096, FQS_T1 = 256, FQS_MOST_PARTS = 256;
+constexpr float FQS_UNIT = 0x1p32f;                       // masses in 2^-32 of the largest
+constexpr float FQS_SPAN = 23.0f;                         // nats that the bins cover: e^-23 is below 2^-33
+constexpr fqs_u64 FQS_MASS = (1ull << 50) - 1;            // a part's bin: number of tokens << 50 | mass (8192 * 2^32 at most)
 
 struct fqs_plan { int per, parts; };                      // chunks of 8 logits of a part; parts of a row
 __host__ __device__ inline fqs_plan fqs_choose(int B, int V) {
@@ -76,7 +76,7 @@ __device__ __forceinline__ fqs_row fqs_parameters(const fq_sample_args& a, int b
 // The grid line below x; x in bins from a line `top` (not below x's): top - line, dropped from FQS_BINS on.
 __device__ __forceinline__ float fqs_line(float x, float steps) { return floorf(fminf(x * steps, 0x1p100f)); }
 __device__ __forceinline__ fqs_u64 fqs_mass(float x, float top, float c) {
-    return (fqs_u64)(unsigned long long)rintf(__builtin_amdgcn_exp2f((x - top) * c) * FQS_UNIT);
+    return (unsigned)rintf(__builtin_amdgcn_exp2f((x - top) * c) * FQS_UNIT);   // (the conversion ends at 2^32 - 1)
 }
 
 // Bits that order as the numbers do (-0 as 0), 16 of bf16 and 32 of FP32, above the inverted index.
@@ -610,9 +610,13 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[i][e] = -__builtin_inff();
     }
+    // comp >= least as a value and the last index that is kept of it (a bound below -infinity's keeps all; -infinity itself has no mass)
+    const bool all_kept = least <= fqs_comp<WIDE>(-__builtin_inff(), 0);
+    const float bound = all_kept ? -__builtin_inff() : find.value_of(least);
+    const int last_index = 0xFFFFF - (int)(least & 0xFFFFF);
     auto mass = [&](int i, int e) __attribute__((always_inline)) {
         const float v = x[i][e];
-        return v > -__builtin_inff() && fqs_comp<WIDE>(v, 8 * (c0 + i) - skew + e) >= least ? fqs_mass(v, part_top, r.c) : 0ull;
+        return v > bound || (v == bound && 8 * (c0 + i) - skew + e <= last_index) ? (unsigned)fqs_mass(v, part_top, r.c) : 0u;
     };
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -637,7 +641,7 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
                 }
             }
         a.token[b] = token;
-        if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)border->total * 0x1p-36));
+        if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)border->total * 0x1p-32));
     }
 }
 

@@ -17,7 +17,7 @@ def fq():
 
 
 # An FP32 exponential of an argument of at most 26 log2 e (its rounding, 2^-24 of up to 38, and the hardware's 2^-22) is off by 2^-18 relative at most; a
-# sum of them by as much, and a border between two tokens, u times a sum or p times a sum, by twice that.  Dropped and rounded masses add 2^-36 a token.
+# sum of them by as much, and a border between two tokens, u times a sum or p times a sum, by twice that.  Masses are whole numbers of 2^-32 of their part's best: 2^-33 a token.
 REL = 2.0 ** -17
 
 
@@ -30,7 +30,7 @@ def check(x, token, logprob, u, T=1.0, k=0, p=1.0, m=0.0):
     top = x.max()
     with np.errstate(invalid="ignore"):
         e = np.where(x == -math.inf, 0.0, np.exp((x - top) / T))
-    slack = 2.0 ** -36 * V
+    slack = 2.0 ** -33 * V
     assert 0 <= token < V and e[token] > 0
     want = (x[token] - top) / T - math.log(e.sum())
     assert abs(logprob - want) <= 2.0 ** -23 * abs(want) + 2 * REL, (logprob, want)
