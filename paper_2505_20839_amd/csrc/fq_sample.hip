@@ -396,6 +396,30 @@ struct fqs_finder {
     template <bool BY_MASS>
     __device__ __forceinline__ fqs_u64 select(int lo_bin, int hi_bin, fqs_u64 want) {
         const int lane = t & 63, wave = t >> 6;
+        if (n <= 64) {                                    // each lane of a wave against every token
+            __syncthreads();
+            if (wave == 0) {
+                const fqs_u64 own = lane < n ? sh.list[lane] : 0ull;
+                const int q = lane < n ? bin(value_of(own)) : FQS_BINS;
+                const bool in = q >= lo_bin && q <= hi_bin && q < FQS_BINS;
+                const unsigned weight = in ? (BY_MASS ? (unsigned)mass_of(own) : 1u) : 0u;
+                fqs_u64 before = 0, least = in ? own : ~0ull;
+                for (int i = 0; i < n; ++i) {
+                    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)own, i), hi = (unsigned)__builtin_amdgcn_readlane((int)(own >> 32), i);
+                    const unsigned m = (unsigned)__builtin_amdgcn_readlane((int)weight, i);
+                    before += ((fqs_u64)hi << 32 | lo) > own ? m : 0u;
+                }
+                least = in && before < want ? least : ~0ull;   // the worst of those that are kept
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const fqs_u64 l = __shfl_xor(least, d, 64);
+                    least = l < least ? l : least;
+                }
+                if (lane == 0) sh.found_before = least == ~0ull ? 0ull : least;
+            }
+            __syncthreads();
+            return sh.found_before;
+        }
         fqs_u64 lo = ~0ull, hi = 0ull;
         each(lo_bin, hi_bin, [&](fqs_u64 c) __attribute__((always_inline)) { lo = c < lo ? c : lo; hi = c > hi ? c : hi; });
 #pragma unroll
@@ -482,6 +506,19 @@ template <bool WIDE>
 __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_work w) {
     __shared__ fqs_shared sh;
     const int own_part = blockIdx.x, b = blockIdx.y, t = threadIdx.x, lane = t & 63, parts = w.plan.parts, per = w.plan.per;
+    const int skew = fqs_skew<WIDE>(a, b), chunks = (a.V + skew + 7) / 8, mine = per / FQS_T1;
+    float x[4][8];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {                         // (requested before it is known that they are looked at)
+        const int c = own_part * per + u * FQS_T1 + t;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[u][e] = -__builtin_inff();
+        if (u < mine && c < chunks) fqs_load<WIDE>(a, b, skew, c, x[u]);
+    }
+    const float part_top = w.top[(size_t)b * parts + own_part];
+    fqs_u64 bins[FQS_BINS / FQS_T1];
+#pragma unroll
+    for (int i = 0; i < FQS_BINS / FQS_T1; ++i) bins[i] = w.bins[((size_t)b * parts + own_part) * FQS_BINS + t + i * FQS_T1];
     fqs_border* const border = w.border + b;
     const float top = border->top, line = border->line;
     if (!(top > -__builtin_inff())) {                     // (NaN)
@@ -492,25 +529,11 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
         return;
     }
     const fqs_row r = fqs_parameters(a, b);
-    const int skew = fqs_skew<WIDE>(a, b), end = border->end, low = border->low, high = border->high;
+    const int end = border->end, low = border->low, high = border->high;
     const bool by_mass = low < FQS_BINS, listing = by_mass || end < FQS_BINS;
     const int first = by_mass ? low : end;                // bins before it are kept whole
     if (!listing && own_part != 0) return;                // every token is kept: one workgroup draws
     if (listing) {
-        const int chunks = (a.V + skew + 7) / 8, mine = per / FQS_T1;
-        const float part_top = w.top[(size_t)b * parts + own_part];
-        fqs_u64 bins[FQS_BINS / FQS_T1];
-#pragma unroll
-        for (int i = 0; i < FQS_BINS / FQS_T1; ++i) bins[i] = w.bins[((size_t)b * parts + own_part) * FQS_BINS + t + i * FQS_T1];
-        float x[4][8];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int c = own_part * per + u * FQS_T1 + t;
-            if (u < mine && c < chunks) fqs_load<WIDE>(a, b, skew, c, x[u]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[u][e] = -__builtin_inff();
-        }
         // the listed tokens: those of bin `end`, and of low .. high
         const float at0 = line - (float)low, at1 = line - (float)high, at2 = line - (float)end;
         unsigned hits = 0u;                               // bit 8 u + e
@@ -599,24 +622,24 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
     }
     __syncthreads();
     const int part = sh.found;
-    const float part_top = w.top[(size_t)b * parts + part];
-    float x[4][8];
+    const float best = w.top[(size_t)b * parts + part];
+    float y[4][8];
     fqs_u64 m = 0;
     const int c0 = part * per + 4 * t;                    // four chunks of a thread, one behind the other
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (4 * t + i < per) fqs_load<WIDE>(a, b, skew, c0 + i, x[i]);
+        if (4 * t + i < per) fqs_load<WIDE>(a, b, skew, c0 + i, y[i]);
         else
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[i][e] = -__builtin_inff();
+            for (int e = 0; e < 8; ++e) y[i][e] = -__builtin_inff();
     }
     // comp >= least as a value and the last index that is kept of it (a bound below -infinity's keeps all; -infinity itself has no mass)
     const bool all_kept = least <= fqs_comp<WIDE>(-__builtin_inff(), 0);
     const float bound = all_kept ? -__builtin_inff() : find.value_of(least);
     const int last_index = 0xFFFFF - (int)(least & 0xFFFFF);
     auto mass = [&](int i, int e) __attribute__((always_inline)) {
-        const float v = x[i][e];
-        return v > bound || (v == bound && 8 * (c0 + i) - skew + e <= last_index) ? (unsigned)fqs_mass(v, part_top, r.c) : 0u;
+        const float v = y[i][e];
+        return v > bound || (v == bound && 8 * (c0 + i) - skew + e <= last_index) ? (unsigned)fqs_mass(v, best, r.c) : 0u;
     };
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -624,7 +647,7 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
         for (int e = 0; e < 8; ++e) m += mass(i, e);
     fqs_u64 in_part, at = fqs_scan<FQS_T1>(m, sh.scan, in_part) - m;
     // (the part's own sum and the bins' may differ by rounding: the last token with a mass then)
-    double want = (double)(target - sh.found_before) / (double)fqs_factor(part_top, top, r.c);
+    double want = (double)(target - sh.found_before) / (double)fqs_factor(best, top, r.c);
     if (!(want < (double)in_part)) want = in_part > 0 ? (double)(in_part - 1) : 0.0;
     if ((double)at <= want && want < (double)(at + m)) {
         int token = -1;
@@ -637,7 +660,7 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
                 at += mass(i, e);
                 if ((double)at > want) {
                     token = 8 * (c0 + i) - skew + e;
-                    value = x[i][e];
+                    value = y[i][e];
                 }
             }
         a.token[b] = token;
