@@ -23,6 +23,8 @@ struct fqc_shape {
     float k1, k2;                                         // log2 e * cap and twice that
 };
 
+constexpr int FQC_MANY_ROWS = 128;                       // of a workgroup with many rows
+
 struct fqc_args {
     const uint8_t* Q;
     const float* q_scale;
@@ -55,9 +57,9 @@ struct fqc_cursor {
         within = t0 - page * tiles_per_page;
         fetch(lane);
     }
-    // where the next NT tiles lie, and what their scales are or-ed with; behind the range its last tile again
+    // where the next NT tiles lie; bit i of `lost`: tile i's page is outside.  Behind the range its last tile again.
     template <int NT>
-    __device__ __forceinline__ void places(const uint8_t* (&p)[NT], int (&lost)[NT], int lane) {
+    __device__ __forceinline__ void places(const uint8_t* (&p)[NT], unsigned& lost, int lane) {
         if (page - first > 64 - NT) {
             first = page;
             fetch(lane);
@@ -65,7 +67,7 @@ struct fqc_cursor {
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             const int id = __builtin_amdgcn_readlane(ids, page - first);
-            lost[i] = id < 0 ? 0x7F7F7F7F : 0;
+            lost |= id < 0 ? 1u << i : 0u;
             p[i] = head + (((unsigned long long)(unsigned)(id < 0 ? 0 : id) * page_stride) << 4) + (unsigned)(within * FQP_TILE);
             const int on = tile < last ? 1 : 0;
             tile += on;
@@ -75,18 +77,20 @@ struct fqc_cursor {
             within = over ? 0 : within;
         }
     }
+    // the bytes of the next NT tiles; bit i of the answer: tile i's page is outside (its scales are made NaN when they have arrived)
     template <int NT>
-    __device__ __forceinline__ void next(fqa_tile (&t)[NT], int lane) {
+    __device__ __forceinline__ unsigned next(fqa_tile (&t)[NT], int lane) {
         const uint8_t* p[NT];
-        int lost[NT];
+        unsigned lost = 0u;
         places(p, lost, lane);
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
             const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p[i]), 0, FQP_TILE, 0x00020000);
             t[i].k = __builtin_bit_cast(fq_v4i, __builtin_amdgcn_raw_buffer_load_b128(r, 16 * lane, 0, 0));
             t[i].v = __builtin_bit_cast(fq_v4i, __builtin_amdgcn_raw_buffer_load_b128(r, 16 * lane, 1024, 0));
-            t[i].s = __builtin_bit_cast(fq_v2i, __builtin_amdgcn_raw_buffer_load_b64(r, 8 * (lane >> 4), 2048, 0)) | lost[i];
+            t[i].s = __builtin_bit_cast(fq_v2i, __builtin_amdgcn_raw_buffer_load_b64(r, 8 * (lane >> 4), 2048, 0));
         }
+        return lost;
     }
 };
 
@@ -153,14 +157,14 @@ __device__ __forceinline__ void fqc_move_nans(fq_v2i& s) {
     s[1] = (int)((unsigned)s[1] & ~bytes);
 }
 
-// Products c of RT query tiles and NT tiles from tile tb on, with the keys' sigmas ks -> probabilities, two tiles of them the B operand of a
-// product with values.  whole: every row has all of the tokens; otherwise the others' scores become -infinity, whose probability is 0 beside any
+// Products c of a lane's RT rows and NT times 4 tokens (`first` + i * STEP + e), with the keys' sigmas ks -> probabilities, eight of them a lane's part of
+// the B operand of a product with values.  STEP 16: a row's tokens are shared out among four lanes, 16 apart, STEP 8: two, 32 apart; rescale(r, x) multiplies its sums.  whole: every row has all of the tokens; otherwise the others' scores become -infinity, whose probability is 0 beside any
 // finite reference (a row's before its first token too, and its factor is not 0).  The query tiles go through each stage together: one branch for all,
 // and each one's chain of instructions beside the others'.
-template <int RT, int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], const float (&ks)[NT][4], int tb, const fqa_queries<RT>& Q,
-                                                  const fqc_rows<RT>& rows, const fqc_shape& shape, fqa_state<RT>& st, bool whole, int g,
-                                                  fq_v4i (&pt)[RT][NT / 2]) {
+template <int RT, int NT, int STEP, bool CAP, bool BIAS, class F>
+__device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], const float (&ks)[NT][4], int first, const float (&qs)[RT],
+                                                  const fqc_rows<RT>& rows, const fqc_shape& shape, float (&m)[RT], float (&sub)[RT], bool whole,
+                                                  fq_v4i (&pt)[RT][NT / 2], F rescale) {
     constexpr bool SHAPED = CAP || BIAS;
     // scores: before the row's factor f = qs, or, with a shape, whole
     float s[RT][NT][4];
@@ -169,7 +173,7 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
 #pragma unroll
         for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[r][i][e] = BIAS && !CAP ? c[r][i][e] * ks[i][e] * Q.qs[r] : c[r][i][e] * ks[i][e];
+            for (int e = 0; e < 4; ++e) s[r][i][e] = BIAS && !CAP ? c[r][i][e] * ks[i][e] * qs[r] : c[r][i][e] * ks[i][e];
     if (CAP) {
         // y = t * qs; while every |y| is small, the polynomial alone
         float most = 0.f;
@@ -180,7 +184,7 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
             for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(s[r][i][e]));
-            most = fmaxf(most, top * Q.qs[r]);
+            most = fmaxf(most, top * qs[r]);
         }
         auto small = [&](float u) __attribute__((always_inline)) {
             return fmaf(fmaf(fmaf(fmaf(shape.k[4], u, shape.k[3]), u, shape.k[2]), u, shape.k[1]), u, shape.k[0]);
@@ -192,7 +196,7 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
                 for (int i = 0; i < NT; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float y = s[r][i][e] * Q.qs[r], u = y * y;
+                        const float y = s[r][i][e] * qs[r], u = y * y;
                         s[r][i][e] = y * fmaf(fmaf(shape.t[2], u, shape.t[1]), u, shape.t[0]);
                     }
         } else if (!__any(!(most <= FQC_SMALL))) {
@@ -203,7 +207,7 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
                 for (int i = 0; i < NT; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float y = s[r][i][e] * Q.qs[r];
+                        const float y = s[r][i][e] * qs[r];
                         s[r][i][e] = y * small(y * y);
                     }
         } else {
@@ -215,7 +219,7 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
                 for (int i = 0; i < NT; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float y = s[r][i][e] * Q.qs[r], z = y * small(y * y);
+                        const float y = s[r][i][e] * qs[r], z = y * small(y * y);
                         const float far = fmaf(-shape.k2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(y * two) + 1.0f), shape.k1);
                         s[r][i][e] = fabsf(y) <= FQC_SMALL ? z : far;
                     }
@@ -228,12 +232,12 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
             for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int d = rows.pos[r] - ((tb + i) * 16 + 4 * g + e), away = (d < 0 ? -d : d) - rows.near[r];
+                    const int d = rows.pos[r] - (first + i * STEP + e), away = (d < 0 ? -d : d) - rows.near[r];
                     s[r][i][e] = fmaf(rows.slope[r], (float)away, s[r][i][e]);
                 }
     }
     if (!whole) {
-        int here = tb * 16 + 4 * g;
+        int here = first;
         asm volatile("" : "+v"(here));                    // (a branch, not selections in every step)
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -241,7 +245,7 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[r][i][e] = (unsigned)(at + 16 * i + e) < (unsigned)n ? s[r][i][e] : -__builtin_inff();
+                for (int e = 0; e < 4; ++e) s[r][i][e] = (unsigned)(at + STEP * i + e) < (unsigned)n ? s[r][i][e] : -__builtin_inff();
         }
     }
     float top[RT];
@@ -253,19 +257,17 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
         for (int i = 0; i < NT; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) top[r] = fmaxf(top[r], s[r][i][e]);
-        past = past || (SHAPED ? top[r] - st.m[r] : (top[r] - st.m[r]) * Q.qs[r]) > FQA_SLACK;
+        past = past || (SHAPED ? top[r] - m[r] : (top[r] - m[r]) * qs[r]) > FQA_SLACK;
     }
     if (__any(past))
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            const float f = SHAPED ? 1.0f : Q.qs[r], over = fqa_over_groups_max(top[r]);
+            const float f = SHAPED ? 1.0f : qs[r], half = fmaxf(top[r], __shfl_xor(top[r], 32, 64)), over = STEP == 16 ? fmaxf(half, __shfl_xor(half, 16, 64)) : half;
             // (a row that is not past its slack keeps its reference, whatever the others do)
-            const float m = (over - st.m[r]) * f > FQA_SLACK ? over : st.m[r], x = __builtin_amdgcn_exp2f((st.m[r] - m) * f);
-            st.m[r] = m;
-            st.sub[r] = fmaf(m, -f, FQA_LIFT);
-            st.l[r] *= x;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) st.o[r][j] *= x;
+            const float best = (over - m[r]) * f > FQA_SLACK ? over : m[r], x = __builtin_amdgcn_exp2f((m[r] - best) * f);
+            m[r] = best;
+            sub[r] = fmaf(best, -f, FQA_LIFT);
+            rescale(r, x);
         }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -275,7 +277,7 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
             for (int e = 0; e < 4; e += 2) {
                 float p[2];
 #pragma unroll
-                for (int u = 0; u < 2; ++u) p[u] = __builtin_amdgcn_exp2f(SHAPED ? s[r][i][e + u] + st.sub[r] : fmaf(s[r][i][e + u], Q.qs[r], st.sub[r]));
+                for (int u = 0; u < 2; ++u) p[u] = __builtin_amdgcn_exp2f(SHAPED ? s[r][i][e + u] + sub[r] : fmaf(s[r][i][e + u], qs[r], sub[r]));
                 pt[r][i / 2][2 * (i & 1) + e / 2] = __builtin_bit_cast(int, __builtin_convertvector((fq_v2f){p[0], p[1]}, fqa_v2h));
             }
 }
@@ -293,6 +295,12 @@ __device__ __forceinline__ fqa_sigmas fqc_value_sigmas(int w) {
 }
 #define FQC_VALUE_MASK 0x00F000F0u
 #define FQC_VALUE_BASE 0x64006400u
+// Four tokens' values of a word: nibbles 0 and 2 (tokens 0, 1 and 2, 3 of one channel), 1 and 3 (of the channel 16 on).
+__device__ __forceinline__ void fqc_values4(int w, unsigned mask, unsigned base, const fqa_sigmas& a, fq_v2i& even, fq_v2i& odds) {
+    const unsigned x = (unsigned)w;
+    even = (fq_v2i){__builtin_bit_cast(int, fqa_value_pair(x << 4, mask, base, a.s[0], a.n[0])), __builtin_bit_cast(int, fqa_value_pair(x >> 4, mask, base, a.s[1], a.n[1]))};
+    odds = (fq_v2i){__builtin_bit_cast(int, fqa_value_pair(x, mask, base, a.s[0], a.n[0])), __builtin_bit_cast(int, fqa_value_pair(x >> 8, mask, base, a.s[1], a.n[1]))};
+}
 // The lane's values for channels j and j + 1 of 16, j even: word w of each of two tiles (nibble 0: channel j of tokens 0, 1; 2: of tokens 2, 3; 1 and 3: j + 1).
 __device__ __forceinline__ void fqc_values(int w0, int w1, unsigned mask, unsigned base, const fqa_sigmas& a, const fqa_sigmas& b, fqa_v8h& even, fqa_v8h& odds) {
     const unsigned x = (unsigned)w0, y = (unsigned)w1;
@@ -308,14 +316,17 @@ __device__ __forceinline__ void fqc_values(int w0, int w1, unsigned mask, unsign
 
 // NT (even) tiles from tile tb on.
 template <int RT, int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], int tb, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows, const fqc_shape& shape,
+__device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], unsigned lost, int tb, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows, const fqc_shape& shape,
                                          fqa_state<RT>& st, bool whole, unsigned mask, unsigned base, int g) {
     unsigned odd = 0u;
 #pragma unroll
     for (int i = 0; i < NT; ++i) odd |= ((unsigned)now[i].s[1] & 0x7F7F7F7Fu) + 0x01010101u;
-    if (__any((odd & 0x80808080u) != 0u))
+    if (lost != 0u || __any((odd & 0x80808080u) != 0u))
 #pragma unroll
-        for (int i = 0; i < NT; ++i) fqc_move_nans(now[i].s);
+        for (int i = 0; i < NT; ++i) {
+            now[i].s |= lost >> i & 1u ? 0x7F7F7F7F : 0;
+            fqc_move_nans(now[i].s);
+        }
     fq_v8i k[NT];
     float ks[NT][4];
 #pragma unroll
@@ -330,7 +341,11 @@ __device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], int tb, const fqa_
     for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int i = 0; i < NT; ++i) c[r][i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
-    fqc_probabilities<RT, NT, CAP, BIAS>(c, ks, tb, Q, rows, shape, st, whole, g, pt);
+    fqc_probabilities<RT, NT, 16, CAP, BIAS>(c, ks, 16 * tb + 4 * g, Q.qs, rows, shape, st.m, st.sub, whole, pt, [&](int r, float x) __attribute__((always_inline)) {
+        st.l[r] *= x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) st.o[r][j] *= x;
+    });
 #pragma unroll
     for (int i = 0; i < NT / 2; ++i) {
         const fqa_sigmas sg[2] = {fqc_value_sigmas(now[2 * i].s[1]), fqc_value_sigmas(now[2 * i + 1].s[1])};
@@ -362,60 +377,58 @@ __device__ __forceinline__ void fqc_begin(const fqa_queries<RT>& Q, fqa_state<RT
     }
 }
 
-// Tiles t0 .. t1 for a wave's rows; from token `whole0` to `whole1` all rows have all tokens.
+// Tiles t0 .. t1 for a wave's rows, the first ones' bytes in `a`; from token `whole0` to `whole1` all rows have all tokens.
 template <int RT, int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void fqc_range(fqc_cursor& cur, int t0, int t1, int whole0, int whole1, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows,
+__device__ __forceinline__ void fqc_range(fqc_cursor& cur, fqa_tile (&a)[NT], unsigned lost_a, int t0, int t1, int whole0, int whole1, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows,
                                           const fqc_shape& shape, fqa_state<RT>& st, int lane) {
     const int g = lane >> 4;
     fqc_begin<RT, CAP, BIAS>(Q, st);
     unsigned mask = FQC_VALUE_MASK, base = FQC_VALUE_BASE;
     asm("" : "+s"(mask));
     asm("" : "+v"(base));
-    auto step = [&](fqa_tile (&now)[NT], int tb) __attribute__((always_inline)) {
+    auto step = [&](fqa_tile (&now)[NT], unsigned lost, int tb) __attribute__((always_inline)) {
         // (a step past t1 repeats the last tile behind its end: its tokens are masked there, for `whole1` is at most 16 t1)
-        fqc_step<RT, NT, CAP, BIAS>(now, tb, Q, rows, shape, st, tb * 16 >= whole0 && (tb + NT) * 16 <= whole1, mask, base, g);
+        fqc_step<RT, NT, CAP, BIAS>(now, lost, tb, Q, rows, shape, st, tb * 16 >= whole0 && (tb + NT) * 16 <= whole1, mask, base, g);
     };
-    fqa_tile a[NT], b[NT];
-    cur.next(a, lane);
+    fqa_tile b[NT];
+    unsigned lost_b = 0u;
     for (int tb = t0; tb < t1; tb += 2 * NT) {
-        if (tb + NT < t1) cur.next(b, lane);
-        step(a, tb);
+        if (tb + NT < t1) lost_b = cur.next(b, lane);
+        step(a, lost_a, tb);
         if (tb + NT >= t1) break;
-        if (tb + 2 * NT < t1) cur.next(a, lane);
-        step(b, tb + NT);
+        if (tb + 2 * NT < t1) lost_a = cur.next(a, lane);
+        step(b, lost_b, tb + NT);
     }
     if (!(CAP || BIAS))
 #pragma unroll
         for (int r = 0; r < RT; ++r) st.m[r] *= Q.qs[r];
 }
 
-// The least of 16 neighbouring lanes (the same in all four groups of a wave), for all.
-__device__ __forceinline__ int fqc_row16_min(int v) {
-    return __builtin_amdgcn_readfirstlane((int)(~fq_row16_max(~((unsigned)v ^ 0x80000000u)) ^ 0x80000000u));
-}
+// The least of a wave's lanes, for all.
+__device__ __forceinline__ int fqc_wave_min(int v) { return (int)(~fq_wave_max(~((unsigned)v ^ 0x80000000u)) ^ 0x80000000u); }
 
 __device__ __forceinline__ int fqc_clamp(int v, int hi) { return v < 0 ? 0 : v > hi ? hi : v; }
 
 // Query tiles of `rows` rows: those of sequence b are numbered from starts[b] * G / rows + b on, which leaves each sequence room for what it can
-// need without anyone knowing their lengths.  The sequence of tile k (or -1), 64 candidates at a time.
-__device__ __forceinline__ int fqc_sequence_of(const fqc_args& a, int k, int G, int rows, int lane, int& tile0, int& start, int& stop) {
+// need without anyone knowing their lengths.  The sequence of tile k (or -1), 64 candidates at a time; its first tile, rows and length.
+struct fqc_sequence { int b, tile0, start, stop, len; };
+__device__ __forceinline__ fqc_sequence fqc_sequence_of(const fqc_args& a, int k, int G, int rows, int lane) {
     int lo = 0, n = a.B;
     while (true) {
         const int stride = (n + 63) >> 6, i = lo + lane * stride;
         const bool in = i < lo + n;
-        const int first = in ? fqc_clamp(a.starts[i], a.T) : 0;
-        const int at = in ? (int)((unsigned)(first * G) / (unsigned)rows) + i : 0;   // (T * G is below 2^25)
+        const int raw = in ? a.starts[i] : 0, len = in && stride == 1 ? a.lens[i] : 0, behind = stride == 1 ? a.starts[lo + n] : 0;
+        const int first = fqc_clamp(raw, a.T);
+        const int at = in ? (int)((unsigned)(first * G) / (unsigned)rows) + i : 0;   // (T * G is below 2^25, rows a power of two)
         const unsigned long long below = __ballot(in && at <= k);
-        if (below == 0ull) return -1;
+        if (below == 0ull) return {-1, 0, 0, 0, 0};
         const int count = __popcll(below) - 1;
         lo += count * stride;
-        tile0 = __builtin_amdgcn_readlane(at, count);
-        if (stride == 1) {
-            start = __builtin_amdgcn_readlane(first, count);
-            stop = count + 1 < n ? __builtin_amdgcn_readlane(first, count + 1) : fqc_clamp(a.starts[lo + 1], a.T);
-            return lo;
-        }
         n = n - count * stride < stride ? n - count * stride : stride;
+        if (stride > 1) continue;
+        const int next = __builtin_amdgcn_readlane(first, count < 63 ? count + 1 : 63);
+        return {lo, __builtin_amdgcn_readlane(at, count), __builtin_amdgcn_readlane(first, count), count < 63 && count + 1 < __popcll(__ballot(in)) ? next : fqc_clamp(behind, a.T),
+                __builtin_amdgcn_readlane(len, count)};
     }
 }
 
@@ -429,23 +442,25 @@ struct fqc_place {
         const int tiles = a.T * G / ROWS + a.B;
         const int k = tiles - 1 - (int)(blockIdx.x / a.Hkv);   // (later rows of a prompt have more tokens: they begin)
         kv = (int)(blockIdx.x % a.Hkv);
-        int tile0 = 0, stop = 0;
-        b = fqc_sequence_of(a, k, G, ROWS, lane, tile0, start, stop);
+        const fqc_sequence q = fqc_sequence_of(a, k, G, ROWS, lane);
+        b = q.b;
         if (b < 0) return false;
-        count = stop - start;
-        row0 = (k - tile0) * ROWS;                        // (T * G is bounded: 32 bits hold it)
+        start = q.start;
+        count = q.stop - q.start;
+        row0 = (k - q.tile0) * ROWS;                        // (T * G is bounded: 32 bits hold it)
         if (count <= 0 || count * G <= row0) return false;
         nrows = count * G - row0 < ROWS ? count * G - row0 : ROWS;
-        raw = a.lens[b];
+        raw = q.len;
         const long long room = (long long)a.width * a.c.page;
         const int cap = a.max_len < room ? a.max_len : (int)room;
         too_long = raw > cap;
         len = too_long ? cap : raw < 0 ? 0 : raw;
         return true;
     }
-    __device__ __forceinline__ size_t row(const fqc_args& a, int i) const {       // row i: token, query head
-        const int x = row0 + i, t = x / G;
-        return (size_t)(start + t) * a.Hq + kv * G + (x - t * G);
+    __device__ __forceinline__ int token(int i) const { return count == 1 ? 0 : (int)((unsigned)(row0 + i) / (unsigned)G); }   // of row i, among the new ones
+    __device__ __forceinline__ size_t row(const fqc_args& a, int i) const {
+        const int t = token(i);
+        return (size_t)(start + t) * a.Hq + kv * G + (row0 + i - t * G);
     }
 };
 
@@ -459,33 +474,42 @@ __device__ __forceinline__ fqc_span fqc_take_rows(const fqc_args& a, const fqc_p
     int lo = 0x7FFFFFFF, hi = 0x7FFFFFFF, wlo = 0x7FFFFFFF, whi = 0x7FFFFFFF;   // the least lo and hi, and of minus them
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int i = first_row + 16 * r + n < at.nrows ? first_row + 16 * r + n : 0, x = at.row0 + i, t = x / at.G;
+        const int i = first_row + 16 * r + n < at.nrows ? first_row + 16 * r + n : 0, t = at.token(i);
         const int pos = at.raw - at.count + t;
         int f = a.first ? a.first[at.start + t] : 0, e = a.end ? a.end[at.start + t] : pos + 1;
         if (a.window > 0 && f < pos - a.window + 1) f = pos - a.window + 1;
         f = f < 0 ? 0 : f;
         e = e > at.len ? at.len : e;
-        const bool empty = f >= e || first_row + 16 * r + n >= at.nrows;
+        const bool none = f >= e, empty = none || first_row + 16 * r + n >= at.nrows;
         sp.none |= empty ? 1u << r : 0u;
-        rows.lo[r] = empty ? 0 : f;
-        rows.hi[r] = empty ? 0x7FFFFFFF : e;
+        rows.lo[r] = none ? 0 : f;
+        rows.hi[r] = none ? 0x7FFFFFFF : e;
         if (BIAS) {
             rows.pos[r] = pos;
-            rows.near[r] = empty ? 0 : pos < f ? f - pos : pos >= e ? pos - (e - 1) : 0;
-            rows.slope[r] = a.slopes[at.kv * at.G + (x - t * at.G)] * -1.44269504088896340736f;
+            rows.near[r] = none ? 0 : pos < f ? f - pos : pos >= e ? pos - (e - 1) : 0;
+            rows.slope[r] = a.slopes[at.kv * at.G + (at.row0 + i - t * at.G)] * -1.44269504088896340736f;
         }
-        if (!empty) {
+        if (!none) {
             lo = f < lo ? f : lo;
             whi = -e < whi ? -e : whi;
         }
         wlo = -rows.lo[r] < wlo ? -rows.lo[r] : wlo;
         hi = rows.hi[r] < hi ? rows.hi[r] : hi;
     }
-    sp.tok0 = fqc_row16_min(lo);
-    const int last = fqc_row16_min(whi);
+    if (at.count == 1) {                                  // one token: one range
+        lo = __builtin_amdgcn_readfirstlane(lo);
+        whi = __builtin_amdgcn_readfirstlane(whi);
+        sp.tok0 = lo;
+        sp.tok1 = whi == 0x7FFFFFFF ? 0 : -whi;
+        sp.whole0 = -__builtin_amdgcn_readfirstlane(wlo);
+        sp.whole1 = __builtin_amdgcn_readfirstlane(hi);
+        return sp;
+    }
+    sp.tok0 = fqc_wave_min(lo);
+    const int last = fqc_wave_min(whi);
     sp.tok1 = last == 0x7FFFFFFF ? 0 : -last;
-    sp.whole0 = -fqc_row16_min(wlo);
-    sp.whole1 = fqc_row16_min(hi);
+    sp.whole0 = -fqc_wave_min(wlo);
+    sp.whole1 = fqc_wave_min(hi);
     return sp;
 }
 template <int RT, bool CAP, bool BIAS>
@@ -510,6 +534,14 @@ __global__ __launch_bounds__(64 * KVW, RT == 1 ? FQC_FEW_WAVES : 2) void fqc_few
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     fqc_place at;
     if (!at.find<ROWS>(a, lane)) return;
+    if (a.slots > 1 && (long long)blockIdx.y * a.chunk * 16 >= at.len) {   // behind the sequence's end, wherever its rows' tokens begin
+        if ((int)threadIdx.x < at.nrows) {
+            float* ml = parts.ml + (at.row(a, threadIdx.x) * parts.slots + blockIdx.y) * 2;
+            ml[0] = FQA_LOWEST;
+            ml[1] = at.too_long ? __builtin_nanf("") : 0.f;
+        }
+        return;
+    }
     fqc_rows<RT> rows;
     const fqc_span sp = fqc_take_rows<RT, BIAS>(a, at, 0, n, rows);
     const int tok0 = sp.tok0, tok1 = sp.tok1, whole0 = sp.whole0, whole1 = sp.whole1, nrows = at.nrows;
@@ -531,8 +563,10 @@ __global__ __launch_bounds__(64 * KVW, RT == 1 ? FQC_FEW_WAVES : 2) void fqc_few
         cur.pages = a.c.pages;
         cur.start(t0, t1, lane);
         fqa_queries<RT> Q;
+        fqa_tile ahead[NT];
+        const unsigned lost = cur.next(ahead, lane);      // (on their way while the queries are taken)
         fqc_take_queries<RT, CAP, BIAS>(a, at, 0, n, g, Q);
-        fqc_range<RT, NT, CAP, BIAS>(cur, t0, t1, whole0, whole1 < 16 * t1 ? whole1 : 16 * t1, Q, rows, a.shape, st, lane);
+        fqc_range<RT, NT, CAP, BIAS>(cur, ahead, lost, t0, t1, whole0, whole1 < 16 * t1 ? whole1 : 16 * t1, Q, rows, a.shape, st, lane);
     }
     if (work) {
 #pragma unroll
@@ -577,31 +611,32 @@ __global__ __launch_bounds__(64 * KVW, RT == 1 ? FQC_FEW_WAVES : 2) void fqc_few
     }
 }
 
-// Many rows: four waves with a query tile each (16 RT rows) walk the same tokens, 32 of a step.  Each wave unpacks a quarter of the step's codes into LDS,
-// where all read their operands; the next step's codes are unpacked while this one's products run, and those behind it are on their way.
-// Bound by vector instructions: per step and wave 30 to unpack its quarter, then 24 and 8 exponentials (16 cycles each) per 16 rows, beside 18 matrix
-// instructions of 16 to 32 cycles on the other pipe.
+// Many rows: four waves with 32 rows each walk the same tokens, 64 of a step.  Each wave unpacks a quarter of the step's codes into LDS, where all read
+// their operands; the next step's codes are unpacked beside this one's score products, and those behind it are on their way.  The products are
+// v_mfma_f32_32x32x64_f8f6f4 and v_mfma_f32_32x32x16_f16, transposed as in fq_attend.hip: A = 32 tokens (two tiles), B = 32 rows; a lane then has, of one row
+// (lane % 32), the tokens 8 k + 4 h + e (h = lane / 32), and a tile's eight are its part of the B operand of a product with 32 channels, values in the same
+// order.  (A vector instruction costs half as much beside a product of 32 x 32 as beside one of 16 x 16, measured with two waves a SIMD.)  sum p: of the
+// rounded numbers, two to an instruction.
 struct fqc_stage {
-    fq_v4i k[4][2][64];                                   // keys' bytes: tile, low and high nibbles, lane
-    fq_v4i v[2][8][64];                                   // values in fp16: two tiles, 16 channels, lane
+    fq_v4i k[2][2][2][64];                                // keys' bytes: pair of tiles, 64 dimensions, low and high nibbles, lane
+    fq_v4i v[4][4][64];                                   // values in fp16: tile, 32 channels, lane
     float ks[4][16];                                      // keys' sigmas
 };
 struct fqc_fetched { fq_v4i k; fq_v2i v[2], s[2]; unsigned bad; };   // a wave's quarter: keys of one tile, half the values of its pair
+#define FQC_MFMA32_QK(a, b, c) __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4((a), (b), (c), 0, 0, 0, 0, 0, 0)
+#define FQC_MFMA32_PV(a, b, c) __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(fqa_v8h, (a)), __builtin_bit_cast(fqa_v8h, (b)), (c), 0, 0, 0)
 
-#ifndef FQC_MANY_WAVES
-#define FQC_MANY_WAVES 2
-#endif
-template <int RT, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args a, fqa_parts parts) {
-    constexpr int ROWS = 64 * RT, NT = 4;
+template <bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts parts) {
+    constexpr int NT = 4;
     __shared__ fqc_stage stage[2];
     __shared__ int span[4][2];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
     fqc_place at;
-    if (!at.find<ROWS>(a, lane)) return;
-    fqc_rows<RT> rows;
-    const int first_row = 16 * RT * wave;
-    const fqc_span sp = fqc_take_rows<RT, BIAS>(a, at, first_row, n, rows);
+    if (!at.find<FQC_MANY_ROWS>(a, lane)) return;
+    fqc_rows<1> rows;
+    const int first_row = 32 * wave;
+    const fqc_span sp = fqc_take_rows<1, BIAS>(a, at, first_row, n, rows);
     if (lane == 0) {
         span[wave][0] = sp.tok1 > 0 ? sp.tok0 : 0x7FFFFFFF;
         span[wave][1] = sp.tok1;
@@ -619,10 +654,31 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
     const int even = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, part = even > a.chunk ? even : a.chunk, t0 = first_tile + (int)blockIdx.y * part;
     const int t1 = t0 + part < first_tile + all ? t0 + part : first_tile + all;
     const int whole0 = sp.whole0, whole1 = sp.whole1 < 16 * t1 ? sp.whole1 : 16 * t1;
-    fqa_state<RT> st;
-    fqa_queries<RT> Q;
-    fqc_take_queries<RT, CAP, BIAS>(a, at, first_row, n, g, Q);
-    fqc_begin<RT, CAP, BIAS>(Q, st);
+    // this lane's row: its codes (dimensions 64 u + 32 h ..), their zero point, its factor
+    const int own_row = first_row + n;
+    const size_t row = at.row(a, own_row < at.nrows ? own_row : 0);
+    const float scale = a.q_scale[row];
+    fq_v8i q[2];
+    float qs[1];
+    fq_v16f zp = {};
+    {
+        const int flip = scale < 0.f ? (int)0x80808080 : 0;
+        constexpr int E = (int)FQ_ZP_BYTES;
+        const fq_v8i eights = {E, E, E, E, E, E, E, E};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const fq_v4i* p = reinterpret_cast<const fq_v4i*>(a.Q + row * 128 + 64 * u + 32 * h);
+            const fq_v4i x = p[0] ^ flip, y = p[1] ^ flip;
+            q[u] = (fq_v8i){x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            zp = FQC_MFMA32_QK(eights, q[u], zp);
+        }
+        qs[0] = fabsf(scale) * a.out_scale * (512.0f * 1.44269504088896340736f);
+        if (!(CAP || BIAS)) qs[0] = fmaxf(qs[0], 1.0e-30f);
+        if (CAP) qs[0] *= a.inv_cap * 0.693147180559945309417f;   // (a capped score's factor has no log2 e)
+    }
+    // (what the reference and its term begin with: fqc_begin)
+    float m[1] = {CAP || BIAS ? FQA_LOWEST : -1.0e30f}, sub[1] = {CAP || BIAS ? -FQA_LOWEST : fminf(1.0e30f * qs[0], -FQA_LOWEST)}, l = 0.f;
+    fq_v16f o[4] = {};
     unsigned mask = FQC_VALUE_MASK, base = FQC_VALUE_BASE;
     asm("" : "+s"(mask));
     asm("" : "+v"(base));
@@ -635,6 +691,7 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
         cur.pages = a.c.pages;
         cur.start(t0, t1, lane);
         const int pair = wave & 1, half = wave >> 1;       // tiles 2 pair and 2 pair + 1; words 2 half and 2 half + 1 of their values
+        const int t = lane & 15, g = lane >> 4;            // where a lane's bytes of a tile belong: token (channel) t, dimensions (tokens) of quarter g
         auto fetch = [&](fqc_fetched& f) __attribute__((always_inline)) {
             const uint8_t* p[2];
             f.bad = cur.places(2 * pair, p);
@@ -659,18 +716,21 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
                 }
         };
         auto unpack = [&](const fqc_fetched& f, fqc_stage& to) __attribute__((always_inline)) {
-            const int tile = 2 * pair + half;
+            const int tile = 2 * pair + half, place = 32 * (g & 1) + 16 * half + t;
             const fq_v8i k = fq_unpack_chunk(f.k);
-            to.k[tile][0][lane] = (fq_v4i){k[0], k[1], k[2], k[3]};
-            to.k[tile][1][lane] = (fq_v4i){k[4], k[5], k[6], k[7]};
-            const fqa_sigmas s0 = fqc_value_sigmas(f.s[0][1]), s1 = fqc_value_sigmas(f.s[1][1]);
+            to.k[pair][g >> 1][0][place] = (fq_v4i){k[0], k[1], k[2], k[3]};
+            to.k[pair][g >> 1][1][place] = (fq_v4i){k[4], k[5], k[6], k[7]};
+            const fqa_sigmas s[2] = {fqc_value_sigmas(f.s[0][1]), fqc_value_sigmas(f.s[1][1])};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                fqa_v8h even, odds;
-                fqc_values(f.v[0][i], f.v[1][i], mask, base, s0, s1, even, odds);
-                to.v[pair][4 * half + 2 * i][lane] = __builtin_bit_cast(fq_v4i, even);
-                to.v[pair][4 * half + 2 * i + 1][lane] = __builtin_bit_cast(fq_v4i, odds);
-            }
+            for (int i = 0; i < 2; ++i)                   // (tile of the pair)
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    fq_v2i even, odds;
+                    fqc_values4(f.v[i][w], mask, base, s[i], even, odds);
+                    fq_v2i* dst = reinterpret_cast<fq_v2i*>(&to.v[2 * pair + i][2 * half + w][32 * (g & 1) + t]) + (g >> 1);
+                    dst[0] = even;
+                    dst[32] = odds;                       // 16 lanes on
+                }
             const int w = half ? f.s[1][0] : f.s[0][0];
             const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
             *reinterpret_cast<fq_v4f*>(&to.ks[tile][4 * g]) = (fq_v4f){s01[0], s01[1], s23[0], s23[1]};   // (by all lanes of a group, the same)
@@ -691,67 +751,76 @@ __global__ __launch_bounds__(256, FQC_MANY_WAVES) void fqc_many_kernel(fqc_args 
                 mend(f);
                 // (behind the range the last tile again, into a stage that nobody reads)
                 const fqc_stage& from = stage[u];
-                fq_v4f c[RT][NT];
-                float ks[NT][4];
+                fq_v4f c[1][2 * NT];
+                float ks[2 * NT][4];
 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    const fq_v4i lo = from.k[i][0][lane], hi = from.k[i][1][lane];
-                    const fq_v8i k = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+                for (int i = 0; i < 2; ++i) {
+                    fq_v16f x = zp;
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) c[r][i] = FQA_MFMA_QK(k, Q.q[r], Q.zp[r]);
-                    const fq_v4f s = *reinterpret_cast<const fq_v4f*>(&from.ks[i][4 * g]);
+                    for (int d = 0; d < 2; ++d) {
+                        const fq_v4i lo = from.k[i][d][0][lane], hi = from.k[i][d][1][lane];
+                        x = FQC_MFMA32_QK(((fq_v8i){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}), q[d], x);
+                    }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) ks[i][e] = s[e];
+                    for (int k = 0; k < 4; ++k) c[0][4 * i + k] = (fq_v4f){x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+                }
+#pragma unroll
+                for (int k = 0; k < 2 * NT; ++k) {
+                    const fq_v4f s = *reinterpret_cast<const fq_v4f*>(&from.ks[k >> 1][8 * (k & 1) + 4 * h]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) ks[k][e] = s[e];
                 }
                 unpack(f, stage[u ^ 1]);
                 fetch(f);
                 if (now * 16 >= sp.tok1 || (now + NT) * 16 <= sp.tok0) continue;   // (none of this wave's rows has any of the tokens)
                 const bool whole = now * 16 >= whole0 && (now + NT) * 16 <= whole1;
-                fq_v4i pt[RT][NT / 2];
-                fqc_probabilities<RT, NT, CAP, BIAS>(c, ks, now, Q, rows, a.shape, st, whole, g, pt);
+                fq_v4i pt[1][NT];
+                fqc_probabilities<1, 2 * NT, 8, CAP, BIAS>(c, ks, 16 * now + 4 * h, qs, rows, a.shape, m, sub, whole, pt, [&](int, float x) __attribute__((always_inline)) {
+                    l *= x;
 #pragma unroll
-                for (int i = 0; i < NT / 2; ++i) {
+                    for (int j = 0; j < 4; ++j) o[j] *= x;
+                });
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) st.l[r] = FQC_MFMA_PV(FQC_ONES, pt[r][i], st.l[r]);
+                for (int i = 0; i < NT; ++i) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const fq_v4i v = from.v[i][j][lane];
-#pragma unroll
-                        for (int r = 0; r < RT; ++r) st.o[r][j] = FQC_MFMA_PV(v, pt[r][i], st.o[r][j]);
+                    for (int e = 0; e < 4; ++e) {
+                        const int two = pt[0][i][e];      // (a bit cast of the element itself takes the first one's bits)
+                        l = __builtin_amdgcn_fdot2(__builtin_bit_cast(fqa_v2h, two), (fqa_v2h){(_Float16)1.f, (_Float16)1.f}, l, false);
                     }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[j] = FQC_MFMA32_PV(from.v[i][j][lane], pt[0][i], o[j]);
                 }
             }
         }
-        if (!(CAP || BIAS))
-#pragma unroll
-            for (int r = 0; r < RT; ++r) st.m[r] *= Q.qs[r];
+        if (!(CAP || BIAS)) m[0] *= qs[0];
     }
+    l += __shfl_xor(l, 32, 64);
+    if (own_row >= at.nrows) return;
+    const bool zero = t0 >= t1 || sp.none != 0u;
+    l = at.too_long ? __builtin_nanf("") : zero ? 0.f : l;
+    if (a.slots == 1) {
+        uint16_t* dst = a.O + row * 128 + 4 * h;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int i = first_row + 16 * r + n;
-        if (i >= at.nrows) continue;
-        const size_t row = at.row(a, i);
-        const bool zero = t0 >= t1 || (sp.none >> r & 1u) != 0u;
-        const float l = at.too_long ? __builtin_nanf("") : zero ? 0.f : st.l[r][0];
-        if (a.slots == 1) {
-            uint16_t* dst = a.O + row * 128 + 4 * g;
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) *reinterpret_cast<uint2*>(dst + 16 * j) = fqa_output(zero ? (fq_v4f){0.f, 0.f, 0.f, 0.f} : st.o[r][j], l);
-        } else {
-            const size_t place = row * parts.slots + blockIdx.y;
-            if (g == 0) {
-                parts.ml[place * 2] = st.m[r];
-                parts.ml[place * 2 + 1] = l;
+            for (int k = 0; k < 4; ++k) {
+                const fq_v4f x = {o[j][4 * k], o[j][4 * k + 1], o[j][4 * k + 2], o[j][4 * k + 3]};
+                *reinterpret_cast<uint2*>(dst + 32 * j + 8 * k) = fqa_output(zero ? (fq_v4f){0.f, 0.f, 0.f, 0.f} : x, l);
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(parts.o + place * 128 + 16 * j + 4 * g) = st.o[r][j];
+    } else {
+        const size_t place = row * parts.slots + blockIdx.y;
+        if (h == 0) {
+            parts.ml[place * 2] = m[0];
+            parts.ml[place * 2 + 1] = l;
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<fq_v4f*>(parts.o + place * 128 + 32 * j + 8 * k + 4 * h) = (fq_v4f){o[j][4 * k], o[j][4 * k + 1], o[j][4 * k + 2], o[j][4 * k + 3]};
     }
 }
 
-#ifndef FQC_MANY_RT
-#define FQC_MANY_RT 2
-#endif
 // few: 16 * few rows of a query tile, whose tokens four waves share out (0: many rows); slots: parts of a row's tokens, chunk: tiles of one at least
 // (a multiple of 4; more where that many parts would not hold a row's tokens).
 struct fqc_plan { int few, slots, chunk; };
@@ -759,7 +828,7 @@ fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
     const int G = Hq / Hkv, cus = fq_device_cus();
     const long long most = (long long)(max_new < T ? max_new : T) * G;
     fqc_plan p = {most <= 16 ? 1 : most <= 32 ? 2 : 0, 1, 4};
-    const int rows = p.few ? 16 * p.few : 64 * FQC_MANY_RT, tiles = max_len > 0 ? (int)(((long long)max_len + 15) / 16) : 1;
+    const int rows = p.few ? 16 * p.few : FQC_MANY_ROWS, tiles = max_len > 0 ? (int)(((long long)max_len + 15) / 16) : 1;
     const long long units = ((long long)T * G / rows + (p.few ? 0 : B)) * Hkv;
     if (p.few) {
         const int chunk = fqa_part(((long long)T * G + rows - 1) / rows > B ? ((long long)T * G + rows - 1) / rows * Hkv : (long long)B * Hkv, tiles, cus, B > 1);
@@ -774,10 +843,10 @@ fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
 
 template <int FEW, bool CAP, bool BIAS>
 void fqc_launch(const fqc_args& a, const fqa_parts& parts, hipStream_t stream) {
-    constexpr int ROWS = FEW ? 16 * FEW : 64 * FQC_MANY_RT;
+    constexpr int ROWS = FEW ? 16 * FEW : FQC_MANY_ROWS;
     const dim3 grid((unsigned)(((long long)a.T * (a.Hq / a.Hkv) / ROWS + a.B) * a.Hkv), (unsigned)a.slots);
     if constexpr (FEW != 0) hipLaunchKernelGGL((fqc_few_kernel<FEW, 4, CAP, BIAS>), grid, dim3(256), 0, stream, a, parts);
-    else hipLaunchKernelGGL((fqc_many_kernel<FQC_MANY_RT, CAP, BIAS>), grid, dim3(256), 0, stream, a, parts);
+    else hipLaunchKernelGGL((fqc_many_kernel<CAP, BIAS>), grid, dim3(256), 0, stream, a, parts);
 }
 template <int FEW>
 void fqc_launch(const fqc_args& a, const fqa_parts& parts, hipStream_t stream) {
