@@ -672,7 +672,11 @@ int append(const uint16_t* QKV_bf16, int64_t ld, const float* cos_sin, int max_p
         return after_launch();
     }
     fq_pair_axes axis;
-    std::memcpy(axis.of, axis_of_pair, 64);
+    std::memcpy(axis.four, axis_of_pair, 64);
+    axis.axes = axes;
+    axis.used = 0;
+    for (int j = 0; j < 64; ++j)
+        if (axis_of_pair[j] >= 0 && axis_of_pair[j] < 32) axis.used |= 1u << axis_of_pair[j];
     fq_launch_kv4_append_axes(QKV_bf16, ld, cos_sin, max_positions, positions, axis, slots, interleaved != 0, Q_fp8, q_scale, c, T, Hq, Hkv, st);
     return after_launch();
 }

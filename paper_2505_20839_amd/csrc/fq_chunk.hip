@@ -436,11 +436,10 @@ __device__ __forceinline__ fqc_sequence fqc_sequence_of(const fqc_args& a, int k
 struct fqc_place {
     int b, kv, G, start, count, row0, nrows, raw, len;
     bool too_long;
+    // k: the workgroup's query tile, of ROWS rows
     template <int ROWS>
-    __device__ __forceinline__ bool find(const fqc_args& a, int lane) {
+    __device__ __forceinline__ bool find(const fqc_args& a, int k, int lane) {
         G = a.Hq / a.Hkv;
-        const int tiles = a.T * G / ROWS + a.B;
-        const int k = tiles - 1 - (int)(blockIdx.x / a.Hkv);   // (later rows of a prompt have more tokens: they begin)
         kv = (int)(blockIdx.x % a.Hkv);
         const fqc_sequence q = fqc_sequence_of(a, k, G, ROWS, lane);
         b = q.b;
@@ -533,7 +532,7 @@ __global__ __launch_bounds__(64 * KVW, RT == 1 ? FQC_FEW_WAVES : 2) void fqc_few
     __shared__ fqa_shared<RT, KVW> sh;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     fqc_place at;
-    if (!at.find<ROWS>(a, lane)) return;
+    if (!at.find<ROWS>(a, (int)(blockIdx.x / a.Hkv), lane)) return;
     if (a.slots > 1 && (long long)blockIdx.y * a.chunk * 16 >= at.len) {   // behind the sequence's end, wherever its rows' tokens begin
         if ((int)threadIdx.x < at.nrows) {
             float* ml = parts.ml + (at.row(a, threadIdx.x) * parts.slots + blockIdx.y) * 2;
@@ -633,7 +632,8 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
     __shared__ int span[4][2];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
     fqc_place at;
-    if (!at.find<FQC_MANY_ROWS>(a, lane)) return;
+    // (later rows of a prompt have more tokens: they begin)
+    if (!at.find<FQC_MANY_ROWS>(a, a.T * (a.Hq / a.Hkv) / FQC_MANY_ROWS + a.B - 1 - (int)(blockIdx.x / a.Hkv), lane)) return;
     fqc_rows<1> rows;
     const int first_row = 32 * wave;
     const fqc_span sp = fqc_take_rows<1, BIAS>(a, at, first_row, n, rows);

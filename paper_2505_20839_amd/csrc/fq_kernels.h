@@ -153,8 +153,8 @@ struct fq_paged_cache {
 void fq_launch_kv4_append(const uint16_t* QKV, long long ld, const float* cos_sin, int max_positions, const int32_t* positions,
                           const int64_t* slots, bool interleaved, uint8_t* Q, float* q_scale, const fq_paged_cache& c, int T, int Hq,
                           int Hkv, hipStream_t stream);
-// positions [axes][T]; pair j of a head turns by positions[axis[j]], or not at all (axis[j] < 0).
-struct fq_pair_axes { signed char of[64]; };
+// positions [axes][T]; pair j of a head turns by positions[axis], axis byte j % 4 of four[j / 4], or not at all (axis < 0).
+struct fq_pair_axes { int four[16]; int axes; unsigned used; };   // used: bit i, some pair turns by axis i (of the first 32)
 void fq_launch_kv4_append_axes(const uint16_t* QKV, long long ld, const float* cos_sin, int max_positions, const int32_t* positions,
                                const fq_pair_axes& axis, const int64_t* slots, bool interleaved, uint8_t* Q, float* q_scale,
                                const fq_paged_cache& c, int T, int Hq, int Hkv, hipStream_t stream);

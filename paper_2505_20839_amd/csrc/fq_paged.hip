@@ -153,8 +153,7 @@ __device__ __forceinline__ int fqp_row_of(int i, int rows) {
     return i < whole ? (i & ~127) + (i & 7) * 16 + ((i >> 3) & 15) : i;
 }
 
-// AXES: each lane's four pairs take their cosines by positions of their own (four loads of 8 bytes instead of two of 16, one step
-// further behind the row's start); a position outside the table in any pair spoils the row.
+// AXES: each pair takes its cosine by a position of its own; a position outside the table in any pair spoils the row.
 struct fqp_one_axis {};
 template <bool INTERLEAVED, bool AXES>
 __global__ __launch_bounds__(512) void fqp_append_kernel(fqp_append_args a, std::conditional_t<AXES, fq_pair_axes, fqp_one_axis> axes) {
@@ -174,24 +173,36 @@ __global__ __launch_bounds__(512) void fqp_append_kernel(fqp_append_args a, std:
     double cs[4] = {1., 1., 1., 1.}, sn[4] = {0., 0., 0., 0.};
     bool bad = lost;
     if constexpr (AXES) {
-        unsigned out = 0u;
-        const int of = reinterpret_cast<const int*>(axes.of)[j];
-        int pos[4];
+        // lane l of a wave fetches pair l's cosine and sine, one load for a wave, and they change lanes through LDS
+        __shared__ __attribute__((aligned(16))) fq_v2f turns[8][64];
+        const int l = threadIdx.x & 63;
+        int of = axes.four[0];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int axis = of << (24 - 8 * i) >> 24;
-            pos[i] = axis < 0 ? -1 : a.positions[(size_t)axis * a.T + token];
-            out |= axis >= 0 && (unsigned)pos[i] >= (unsigned)a.max_positions ? 1u : 0u;
+        for (int i = 1; i < 16; ++i) of = l >> 2 == i ? axes.four[i] : of;
+        const int axis = (int)((unsigned)of << (24 - 8 * (l & 3))) >> 24;
+        int pos = -1;
+        if (axes.axes <= 4) {                             // the token's positions are the same for all lanes: scalar loads, and a selection
+            int at[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                at[i] = a.positions[(size_t)(i < axes.axes ? i : 0) * a.T + token];
+                bad |= (axes.used >> i & 1u) != 0u && (unsigned)at[i] >= (unsigned)a.max_positions;
+            }
+            pos = axis < 0 ? -1 : axis == 0 ? at[0] : axis == 1 ? at[1] : axis == 2 ? at[2] : at[3];
+        } else {
+            if (axis >= 0) pos = a.positions[(size_t)axis * a.T + token];
+            bad |= __any(axis >= 0 && (unsigned)pos >= (unsigned)a.max_positions) != 0;
         }
-        bad |= fq_row16_max(out) != 0u;
-        if (!bad)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (pos[i] >= 0) {
-                    const fq_v2f t = reinterpret_cast<const fq_v2f*>(a.cos_sin)[(size_t)pos[i] * 64 + 4 * j + i];
-                    cs[i] = t[0];
-                    sn[i] = t[1];
-                }
+        fq_v2f turn = {1.0f, 0.0f};
+        if (!bad && axis >= 0) turn = reinterpret_cast<const fq_v2f*>(a.cos_sin)[(size_t)pos * 64 + l];
+        turns[threadIdx.x >> 6][l] = turn;
+        // (a wave's own LDS accesses stay in order, which the fence holds the compiler to)
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const fq_v4f* t = reinterpret_cast<const fq_v4f*>(&turns[threadIdx.x >> 6][4 * j]);
+        const fq_v4f t0 = t[0], t1 = t[1];
+        cs[0] = t0[0]; sn[0] = t0[1]; cs[1] = t0[2]; sn[1] = t0[3];
+        cs[2] = t1[0]; sn[2] = t1[1]; cs[3] = t1[2]; sn[3] = t1[3];
     } else {
         const int pos = a.positions[token];
         bad |= pos < 0 || pos >= a.max_positions;
