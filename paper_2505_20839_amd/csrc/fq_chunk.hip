@@ -447,7 +447,7 @@ struct fqc_place {
         start = q.start;
         count = q.stop - q.start;
         row0 = (k - q.tile0) * ROWS;                        // (T * G is bounded: 32 bits hold it)
-        if (count <= 0 || count * G <= row0) return false;
+        if (count <= 0 || count * G <= row0 || row0 < 0) return false;   // (row0 < 0: starts that decrease)
         nrows = count * G - row0 < ROWS ? count * G - row0 : ROWS;
         raw = q.len;
         const long long room = (long long)a.width * a.c.page;
@@ -486,7 +486,8 @@ __device__ __forceinline__ fqc_span fqc_take_rows(const fqc_args& a, const fqc_p
         if (BIAS) {
             rows.pos[r] = pos;
             rows.near[r] = none ? 0 : pos < f ? f - pos : pos >= e ? pos - (e - 1) : 0;
-            rows.slope[r] = a.slopes[at.kv * at.G + (at.row0 + i - t * at.G)] * -1.44269504088896340736f;
+            const float slope = a.slopes[at.kv * at.G + (at.row0 + i - t * at.G)] * -1.44269504088896340736f;
+            rows.slope[r] = slope < -0x1p127f ? -0x1p127f : slope;   // (finite: the nearest token's distance is 0; a NaN stays)
         }
         if (!none) {
             lo = f < lo ? f : lo;
@@ -517,7 +518,7 @@ __device__ __forceinline__ void fqc_take_queries(const fqc_args& a, const fqc_pl
     for (int r = 0; r < RT; ++r) {
         const size_t row = at.row(a, first_row + 16 * r + n < at.nrows ? first_row + 16 * r + n : 0);
         fqa_take_query(Q, r, a.Q + row * 128, a.q_scale[row], a.out_scale, g);
-        if (!(CAP || BIAS)) Q.qs[r] = fmaxf(Q.qs[r], 1.0e-30f);
+        if (!(CAP || BIAS)) Q.qs[r] = Q.qs[r] < 1.0e-30f ? 1.0e-30f : Q.qs[r];   // (a NaN stays)
         if (CAP) Q.qs[r] *= a.inv_cap * 0.693147180559945309417f;   // (a capped score's factor has no log2 e)
     }
 }
@@ -673,7 +674,7 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
             zp = FQC_MFMA32_QK(eights, q[u], zp);
         }
         qs[0] = fabsf(scale) * a.out_scale * (512.0f * 1.44269504088896340736f);
-        if (!(CAP || BIAS)) qs[0] = fmaxf(qs[0], 1.0e-30f);
+        if (!(CAP || BIAS)) qs[0] = qs[0] < 1.0e-30f ? 1.0e-30f : qs[0];   // (a NaN stays)
         if (CAP) qs[0] *= a.inv_cap * 0.693147180559945309417f;   // (a capped score's factor has no log2 e)
     }
     // (what the reference and its term begin with: fqc_begin)

@@ -268,3 +268,46 @@ def test_workspace_is_the_callers(fq):
     assert (pool[:16] == 0xFF).all() and (pool[16 + need:] == 0xFF).all()
     with pytest.raises(fq.FireqError):
         fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, max_new=1, max_len=3000, workspace=pool[16: need])
+
+
+@pytest.mark.parametrize("seqs, Hq, Hkv", [([(1, 30), (1, 1)], 4, 2), ([(1, 700)], 4, 2), ([(9, 40), (2, 90)], 4, 2), ([(80, 90), (3, 70)], 4, 2), ([(40, 900)], 8, 1)])
+@pytest.mark.parametrize("kw", [{}, {"cap": 5.0}, {"slopes": True}, {"cap": 5.0, "slopes": True}, {"window": 9}])
+@pytest.mark.parametrize("code", [False, True])
+def test_a_query_that_is_not_a_number(fq, seqs, Hq, Hkv, kw, code):
+    """A NaN scale, or a NaN among the codes: NaN to that row's head, and to nothing else."""
+    b = Batch(seqs, Hq, Hkv, 16, 43)
+    row = b.T // 2
+    if code:
+        b.q[row, 1, 77] = 0x7F
+    else:
+        b.qs[row, 1] = np.nan
+    if kw.get("slopes"):
+        kw = dict(kw, slopes=torch.full((Hq,), 0.1, device="cuda"))
+    out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, **kw).view(b.T, Hq, 128)
+    assert torch.isnan(out[row, 1]).all()
+    out[row, 1] = 0
+    assert not torch.isnan(out).any()
+
+
+@pytest.mark.parametrize("seqs", [[(1, 200)], [(20, 100)], [(70, 150)]])
+@pytest.mark.parametrize("forward", [False, True])
+def test_slopes_of_any_size(fq, seqs, forward):
+    """Up to the largest finite number, with which the nearest tokens alone count."""
+    b = Batch(seqs, 4, 2, 16, 47)
+    slopes = np.array([0.0, 1e-30, 1e10, 3.4e38], np.float32)
+    end = np.full(b.T, 120 if forward else 90, np.int32)  # (rows whose nearest token lies before them, at them, or behind)
+    first = np.full(b.T, 35, np.int32)
+    out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, first=torch.as_tensor(first).cuda(), end=torch.as_tensor(end).cuda(), slopes=torch.as_tensor(slopes).cuda())
+    b.check(out, first=first, end=end, slopes=slopes)
+
+
+@pytest.mark.parametrize("starts", [[0, 900, 1000, 0, 0], [0, 1000, 1000, 0, 3], [900, 0, 1000, 10, 1000], [0, 500, 400, 1000, 2], [1000, 900, 0, 1000, 0]])
+@pytest.mark.parametrize("max_new", [1, 16, 1000])
+def test_starts_that_decrease_far(fq, starts, max_new):
+    b = Batch([(1000, 40)] + [(0, 40)] * 3, 4, 2, 16, 53)
+    args = list(b.gpu())
+    args[4] = torch.tensor(starts, dtype=torch.int32, device="cuda")
+    pool = torch.full((3 * b.T, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    fq.fq_kv4_attention_chunk(*args, SCALE, max_new=max_new, out=pool[b.T: 2 * b.T])
+    torch.cuda.synchronize()
+    assert (pool[: b.T] == 7.0).all() and (pool[2 * b.T:] == 7.0).all()
