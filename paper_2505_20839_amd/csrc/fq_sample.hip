@@ -73,8 +73,11 @@ __device__ __forceinline__ fqs_row fqs_parameters(const fq_sample_args& a, int b
     r.filtered = r.k > 0 || r.p < 1.0f || r.low > 0.0f;
     return r;
 }
-// The grid line below x; x in bins from a line `top` (not below x's): top - line, dropped from FQS_BINS on.
-__device__ __forceinline__ float fqs_line(float x, float steps) { return floorf(fminf(x * steps, 0x1p100f)); }
+// The grid line below x, -infinity for -infinity alone; x in bins from a line `top` (not below x's): top - line, dropped from FQS_BINS on.
+__device__ __forceinline__ float fqs_line(float x, float steps) {
+    const float y = floorf(__builtin_amdgcn_fmed3f(x * steps, -0x1p100f, 0x1p100f));
+    return x > -__builtin_inff() ? y : x;
+}
 __device__ __forceinline__ fqs_u64 fqs_mass(float x, float top, float c) {
     return (unsigned)rintf(__builtin_amdgcn_exp2f((x - top) * c) * FQS_UNIT);   // (the conversion ends at 2^32 - 1)
 }

@@ -231,3 +231,23 @@ def test_workspace_is_the_callers(fq):
     assert torch.equal(got[0], want[0]) and (pool[:16] == 0xFF).all() and (pool[16 + need:] == 0xFF).all()
     with pytest.raises(fq.FireqError):
         fq.fq_sample(x, u, workspace=pool[16: need])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [5, 999, 20011])
+@pytest.mark.parametrize("hidden", [-math.inf, "lowest"])
+def test_rows_at_the_ends_of_the_type(fq, dtype, V, hidden):
+    """Logits whose steps leave FP32: rows of the lowest numbers alone, some of them -infinity, and rows of the largest."""
+    info = torch.finfo(dtype)
+    low, high = info.min, info.max
+    hidden = low if hidden == "lowest" else hidden
+    rows = []
+    for a in (low, high, low / 2, high / 2):
+        x = torch.full((V,), hidden, dtype=dtype)
+        x[V // 2:] = a
+        x[V - 1] = a * (1 - info.eps)
+        rows.append(x)
+    x = torch.stack(rows).cuda()
+    for p in (dict(T=0.0), dict(k=1), dict(k=2), dict(k=3, T=1e-3), dict(p=0.4), dict(m=0.5), dict(T=1e-30, k=2), dict(T=1e30, p=0.5), {}):
+        for u in (0.0, 0.3, 0.99999):
+            run(fq, x, [u] * 4, **{n: [v] * 4 for n, v in p.items()})
