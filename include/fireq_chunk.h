@@ -19,12 +19,12 @@
  *                      A key or value whose scale is NaN, or a page number outside the cache, gives NaN to the rows that attend to its tokens, and to no
  *                      other.  A sequence longer than max_len or than table_width * page gives NaN to its rows.
  *                      starts int32 [B + 1], not decreasing, 0 .. T (what lies outside is taken as the nearest of these, and rows of
- *                      sequences that overlap are unspecified); first, end int32 [T]; slopes FP32 [Hq], finite.
+ *                      sequences that overlap are unspecified); first, end int32 [T]; slopes FP32 [Hq], finite (a negative one times any distance, too).
  *                      max_new and max_len are upper bounds of a sequence's rows and of seq_lens that the caller knows; both decide how the work is
  *                      split, and max_new may be wrong at the cost of time alone.
  * Scratch: fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len) bytes (often 0), 16-byte aligned, under the rules of fireq_paged.h.
  *
- * window >= 0; cap >= 0 and finite, 0 or at least 2^-60; out_scale / cap finite; T < 2^23, T * Hq <= 2^23 * 4, B <= 65535, T * (Hq + 2 Hkv) below 2^28 - 16 (append); the other sizes, strides and alignments,
+ * window >= 0; cap >= 0 and finite, 0 or at least 2^-60; out_scale / cap finite; T < 2^23, T * Hq <= 2^25, B <= 65535, T * Hq / 16 + B * Hkv below 2^24, T * (Hq + 2 Hkv) below 2^28 - 16 (append); the other sizes, strides and alignments,
  * outputs that overlap nothing, and status codes as in fireq_paged.h.  T = 0 or B = 0 is a successful no-op.
  */
 #ifndef FIREQ_CHUNK_H

@@ -9,13 +9,13 @@
  * token[b] is the first token, by index, at which the kept mass up to it passes u times the whole kept mass (u is taken as one of [0, 1 - 2^-24]), and
  * logprob[b] = log softmax(x / T)[token], over all V.  T = 0 takes the best token, and its log-probability at T = 1.
  *
- * -infinity is a token of no mass.  Exponentials are FP32 and sums of whole numbers of 2^-32 of the largest of a part of the row: a token below 2^-33 of
+ * -infinity is a token of no mass.  Exponentials are FP32 and sums those of whole numbers of 2^-32 of the largest of the row or of a part of it (the log-probability's may be FP32's): a token below 2^-33 of
  * the row's best may be taken as one of no mass.  Results do not depend on the order in which anything runs.
  * A row with a NaN or +infinity, with no token above -infinity, with T negative or not finite, or with u, p or m NaN, gives token -1 and
  * logprob NaN.
  *
  * fq_sample_bf16_ws, fq_sample_fp32_ws   logits in bf16, in FP32; aligned to their size, ld >= V; logprob may be NULL.
- * Scratch: fq_sample_workspace_bytes(B, V) bytes, 16-byte aligned; it may be reused or freed once the work enqueued by the call has finished, and
+ * Scratch: fq_sample_workspace_bytes(B, V) bytes (0 up to V = 32761), 16-byte aligned; it may be reused or freed once the work enqueued by the call has finished, and
  * calls that overlap in time need scratch of their own.
  * 1 <= V <= 2^20, B <= 65535; outputs and scratch overlap neither each other nor an input (FQ_ERR_SHAPE).  Conventions and status codes are those of
  * fireq.h; B = 0 is a successful no-op.

@@ -684,7 +684,7 @@ int append(const uint16_t* QKV_bf16, int64_t ld, const float* cos_sin, int max_p
 // The sizes that the attention of new tokens takes.
 bool chunk_sizes(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
     return T >= 0 && T < 1 << 23 && B >= 0 && B <= 65535 && Hq > 0 && Hq <= 65535 && Hkv > 0 && Hq % Hkv == 0 && (int64_t)T * Hq <= 1 << 25 &&
-           ((int64_t)T * (Hq / Hkv) / 16 + B) * Hkv <= 0x3FFFFFFF && max_new >= 0 && max_len >= 0 && max_len <= 1 << 30;
+           ((int64_t)T * (Hq / Hkv) / 16 + B) * Hkv < 1 << 24 && max_new >= 0 && max_len >= 0 && max_len <= 1 << 30;
 }
 
 int attend_chunk(const fq_chunk_args& a, void* workspace, size_t workspace_bytes, void* stream) {
@@ -719,8 +719,10 @@ int sample(const fq_sample_args& a, void* workspace, size_t workspace_bytes, voi
     if (!a.logits || !a.u || !a.token) return FQ_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(a.logits) % size != 0) return FQ_ERR_ALIGN;
     const size_t need = fq_sample_scratch_bytes(a.B, a.V);
-    if (!workspace || workspace_bytes < need) return FQ_ERR_MEMORY;
-    if (!aligned16(workspace)) return FQ_ERR_ALIGN;
+    if (need > 0) {
+        if (!workspace || workspace_bytes < need) return FQ_ERR_MEMORY;
+        if (!aligned16(workspace)) return FQ_ERR_ALIGN;
+    }
     const size_t n = (size_t)a.B * 4;
     const blocks rows = {a.logits, a.B, (int64_t)(a.ld * size), 1, 0, (int64_t)(a.V * size)};
     const bytes all[] = {{a.u, n}, {a.temperature, a.temperature ? n : 0}, {a.top_k, a.top_k ? n : 0}, {a.top_p, a.top_p ? n : 0}, {a.min_p, a.min_p ? n : 0},

@@ -65,6 +65,8 @@ def run(fq, x, u, T=None, k=None, p=None, m=None, **kw):
     """x: a GPU tensor [B,V]; u and the parameters: lists."""
     B = x.shape[0]
     t = lambda v, d: None if v is None else torch.tensor(v, dtype=d, device="cuda")     # noqa: E731
+    poison = torch.full((B,), -7, dtype=torch.int32, device="cuda"), torch.full((B,), math.nan, device="cuda")
+    del poison                                            # (the memory that the outputs are likely to get)
     token, logprob = fq.fq_sample(x, t(u, torch.float32), t(T, torch.float32), t(k, torch.int32), t(p, torch.float32), t(m, torch.float32), **kw)
     token, logprob, y = token.cpu().numpy(), logprob.cpu().double().numpy(), x.double().cpu().numpy()
     f = lambda v, b, d: d if v is None else float(np.float32(v[b]))                     # noqa: E731
@@ -82,7 +84,7 @@ def lists(params, B):
             for n in ("T", "k", "p", "m")}
 
 
-@pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 255, 1000, 2049, 5001, 32000, 100003])
+@pytest.mark.parametrize("V", [1, 2, 7, 8, 9, 255, 1000, 2049, 5001, 8185, 8186, 32000, 32761, 32762, 100003])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_sizes_and_filters(fq, V, dtype):
     g = torch.Generator(device="cuda").manual_seed(V)
@@ -100,7 +102,7 @@ def test_each_filter_alone(fq, one):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("V", [300, 20000, 1 << 20])
+@pytest.mark.parametrize("V", [300, 20000, 50000, 1 << 20])
 def test_ties(fq, dtype, V):
     """All alike, a few values, two values: filters end inside ties, which the lower index wins."""
     x = torch.zeros((6, V), dtype=dtype, device="cuda")
@@ -222,8 +224,8 @@ def test_captured_and_repeated(fq):
 
 
 def test_workspace_is_the_callers(fq):
-    x, u = torch.randn((3, 9000), device="cuda"), torch.rand(3, device="cuda")
-    need = fq.fq_sample_workspace_bytes(3, 9000)
+    x, u = torch.randn((3, 40000), device="cuda"), torch.rand(3, device="cuda")
+    need = fq.fq_sample_workspace_bytes(3, 40000)
     pool = torch.full((need + 64,), 0xFF, dtype=torch.uint8, device="cuda")
     k = torch.full((3,), 9, dtype=torch.int32, device="cuda")
     got = fq.fq_sample(x, u, None, k, workspace=pool[16: 16 + need])
@@ -234,7 +236,7 @@ def test_workspace_is_the_callers(fq):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("V", [5, 999, 20011])
+@pytest.mark.parametrize("V", [5, 999, 20011, 40011])
 @pytest.mark.parametrize("hidden", [-math.inf, "lowest"])
 def test_rows_at_the_ends_of_the_type(fq, dtype, V, hidden):
     """Logits whose steps leave FP32: rows of the lowest numbers alone, some of them -infinity, and rows of the largest."""
@@ -251,3 +253,31 @@ def test_rows_at_the_ends_of_the_type(fq, dtype, V, hidden):
     for p in (dict(T=0.0), dict(k=1), dict(k=2), dict(k=3, T=1e-3), dict(p=0.4), dict(m=0.5), dict(T=1e-30, k=2), dict(T=1e30, p=0.5), {}):
         for u in (0.0, 0.3, 0.99999):
             run(fq, x, [u] * 4, **{n: [v] * 4 for n, v in p.items()})
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [1000, 30000])
+def test_lists_of_every_length(fq, dtype, V):
+    """top-k from one token to all: lists of tokens compared with each other, selected from, and too long; ties at the border; min-p and top-p within."""
+    g = torch.Generator(device="cuda").manual_seed(V)
+    ks = [1, 2, 3, 31, 63, 64, 65, 100, 127, 128, 129, 200, 255, 256, 257, 400, 499, 500, 501, 900, V - 1]
+    x = 2.5 * torch.randn((len(ks), V), generator=g, device="cuda")
+    for y in (x.to(dtype), x.round().to(dtype)):
+        for p in (dict(), dict(p=0.95), dict(p=0.3, m=0.01), dict(T=0.5, p=0.8), dict(T=4.0)):
+            for u in (0.01, 0.6, 0.9999):
+                run(fq, y, [u] * len(ks), k=ks, **{n: [v] * len(ks) for n, v in p.items()})
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [3000, 40000])
+@pytest.mark.parametrize("shift", [0.0, -40.0, 40.0, -1e30, 1e30])
+def test_the_border_of_min_p_at_numbers_of_both_signs(fq, dtype, V, shift):
+    """A few values about the border, some on it: none is dropped, none kept beside what the definition says."""
+    steps = torch.arange(V, device="cuda") % 11 * 0.25
+    x = (shift - steps).to(dtype)[None].expand(12, V).contiguous()
+    u = np.linspace(0.0, 0.9999, 12).tolist()
+    for m in (math.exp(-0.5), math.exp(-0.75) * 1.0001, math.exp(-1.0) * 0.9999, 0.3, 1.0, 1e-3):
+        for T in (1.0, 0.25 / 0.6):
+            run(fq, x, u, m=[m] * 12, T=[T] * 12)
+            run(fq, x, u, m=[m] * 12, T=[T] * 12, p=[0.7] * 12)
+            run(fq, x, u, m=[m] * 12, T=[T] * 12, k=[V // 4] * 12)

@@ -87,7 +87,7 @@ def test_chunk_calls(fq, new, B):  # noqa: F811
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_sample_calls(fq, dtype):  # noqa: F811
-    B, V = 5, 3001
+    B, V = 5, 33001
     x = _b(B, V).to(dtype)
     u, T, p = torch.rand(B, device="cuda"), torch.full((B,), 0.7, device="cuda"), torch.full((B,), 0.9, device="cuda")
     k = torch.full((B,), 20, dtype=torch.int32, device="cuda")

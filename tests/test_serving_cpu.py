@@ -117,13 +117,13 @@ def test_chunk_workspace():
 
 
 @pytest.mark.parametrize("change, status", [
-    (dict(B=0, x=0, u=0, token=0), OK), (dict(B=-1), SHAPE), (dict(B=65536), SHAPE), (dict(V=0), SHAPE), (dict(V=(1 << 20) + 1, ld=1 << 21), SHAPE), (dict(ld=999), SHAPE),
+    (dict(B=0, x=0, u=0, token=0), OK), (dict(B=-1), SHAPE), (dict(B=65536), SHAPE), (dict(V=0), SHAPE), (dict(V=(1 << 20) + 1, ld=1 << 21), SHAPE), (dict(ld=39999), SHAPE),
     (dict(ld=(1 << 40) + 1), SHAPE), (dict(x=0), NULL), (dict(u=0), NULL), (dict(token=0), NULL), (dict(x=P + 1), ALIGN), (dict(ws=0), MEMORY), (dict(n=100), MEMORY),
     (dict(ws=0x900008), ALIGN), (dict(token=P + 64), SHAPE), (dict(logprob=P + 64), SHAPE), (dict(token=0x100000), SHAPE), (dict(token=0x110000), SHAPE),
     (dict(logprob=0x120000), SHAPE), (dict(logprob=0x150000), SHAPE), (dict(ws=P), SHAPE), (dict(ws=0x150000), SHAPE), (dict(ws=0x140000), SHAPE)])
 @pytest.mark.parametrize("wide", [False, True])
 def test_sample_refusals(change, status, wide):
-    a = dict(x=P, ld=1000, u=0x100000, T=0x110000, k=0x120000, p=0x130000, m=0x140000, token=0x150000, logprob=0x160000, B=3, V=1000, ws=0x900000, n=1 << 24)
+    a = dict(x=P, ld=40000, u=0x100000, T=0x110000, k=0x120000, p=0x130000, m=0x140000, token=0x150000, logprob=0x160000, B=3, V=40000, ws=0x900000, n=1 << 24)
     a.update(change)
     call = binding.lib().fq_sample_fp32_ws if wide else binding.lib().fq_sample_bf16_ws
     assert call(a["x"], a["ld"], a["u"], a["T"], a["k"], a["p"], a["m"], a["token"], a["logprob"], a["B"], a["V"], a["ws"], a["n"], 0) == status
@@ -131,7 +131,7 @@ def test_sample_refusals(change, status, wide):
 
 def test_sample_workspace_sizes():
     need = binding.fq_sample_workspace_bytes
-    assert need(1, 1) > 0 and need(64, 131072) > need(1, 131072) > need(1, 32000) and need(65535, 1 << 20) > 0
+    assert need(1, 1) == need(64, 32761) == 0 and need(64, 131072) > need(1, 131072) > need(1, 32762) > 0 and need(65535, 1 << 20) > 0
     for bad in ((0, 5), (-1, 5), (5, 0), (65536, 5), (1, (1 << 20) + 1), (1, 1 << 40)):
         assert need(*bad) == 0
 
