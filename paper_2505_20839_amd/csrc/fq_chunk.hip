@@ -523,12 +523,9 @@ __device__ __forceinline__ void fqc_take_queries(const fqc_args& a, const fqc_pl
     }
 }
 
-#ifndef FQC_FEW_WAVES
-#define FQC_FEW_WAVES 3
-#endif
 // Few rows: one query tile of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among the waves, which meet in LDS.
 template <int RT, int KVW, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * KVW, RT == 1 ? FQC_FEW_WAVES : 2) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
+__global__ __launch_bounds__(64 * KVW, RT == 1 ? 3 : 2) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
     constexpr int ROWS = 16 * RT, NT = 2;
     __shared__ fqa_shared<RT, KVW> sh;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -659,26 +656,10 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
     const int own_row = first_row + n;
     const size_t row = at.row(a, own_row < at.nrows ? own_row : 0);
     const float scale = a.q_scale[row];
-    fq_v8i q[2];
-    float qs[1];
-    fq_v16f zp = {};
-    {
-        const int flip = scale < 0.f ? (int)0x80808080 : 0;
-        constexpr int E = (int)FQ_ZP_BYTES;
-        const fq_v8i eights = {E, E, E, E, E, E, E, E};
+    fq_v4i codes[4];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const fq_v4i* p = reinterpret_cast<const fq_v4i*>(a.Q + row * 128 + 64 * u + 32 * h);
-            const fq_v4i x = p[0] ^ flip, y = p[1] ^ flip;
-            q[u] = (fq_v8i){x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-            zp = FQC_MFMA32_QK(eights, q[u], zp);
-        }
-        qs[0] = fabsf(scale) * a.out_scale * (512.0f * 1.44269504088896340736f);
-        if (!(CAP || BIAS)) qs[0] = qs[0] < 1.0e-30f ? 1.0e-30f : qs[0];   // (a NaN stays)
-        if (CAP) qs[0] *= a.inv_cap * 0.693147180559945309417f;   // (a capped score's factor has no log2 e)
-    }
-    // (what the reference and its term begin with: fqc_begin)
-    float m[1] = {CAP || BIAS ? FQA_LOWEST : -1.0e30f}, sub[1] = {CAP || BIAS ? -FQA_LOWEST : fminf(1.0e30f * qs[0], -FQA_LOWEST)}, l = 0.f;
+    for (int u = 0; u < 4; ++u) codes[u] = reinterpret_cast<const fq_v4i*>(a.Q + row * 128 + 64 * (u >> 1) + 32 * h)[u & 1];
+    float m[1] = {FQA_LOWEST}, l = 0.f;
     fq_v16f o[4] = {};
     unsigned mask = FQC_VALUE_MASK, base = FQC_VALUE_BASE;
     asm("" : "+s"(mask));
@@ -738,6 +719,26 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
         };
         fqc_fetched f;
         fetch(f);
+        // (on its way while the queries are taken)
+        fq_v8i q[2];
+        float qs[1] = {fabsf(scale) * a.out_scale * (512.0f * 1.44269504088896340736f)};
+        fq_v16f zp = {};
+        {
+            const int flip = scale < 0.f ? (int)0x80808080 : 0;
+            constexpr int E = (int)FQ_ZP_BYTES;
+            const fq_v8i eights = {E, E, E, E, E, E, E, E};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const fq_v4i x = codes[2 * u] ^ flip, y = codes[2 * u + 1] ^ flip;
+                q[u] = (fq_v8i){x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                zp = FQC_MFMA32_QK(eights, q[u], zp);
+            }
+            if (!(CAP || BIAS)) qs[0] = qs[0] < 1.0e-30f ? 1.0e-30f : qs[0];   // (a NaN stays)
+            if (CAP) qs[0] *= a.inv_cap * 0.693147180559945309417f;   // (a capped score's factor has no log2 e)
+        }
+        // (what the reference and its term begin with: fqc_begin)
+        m[0] = CAP || BIAS ? FQA_LOWEST : -1.0e30f;
+        float sub[1] = {CAP || BIAS ? -FQA_LOWEST : fminf(1.0e30f * qs[0], -FQA_LOWEST)};
         mend(f);
         unpack(f, stage[0]);
         cur.refill(lane);
