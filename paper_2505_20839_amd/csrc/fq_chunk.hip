@@ -525,7 +525,7 @@ __device__ __forceinline__ void fqc_take_queries(const fqc_args& a, const fqc_pl
 
 // Few rows: one query tile of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among the waves, which meet in LDS.
 template <int RT, int KVW, bool CAP, bool BIAS>
-__global__ __launch_bounds__(64 * KVW, RT == 1 ? 3 : 2) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
+__global__ __launch_bounds__(64 * KVW, 2) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
     constexpr int ROWS = 16 * RT, NT = 2;
     __shared__ fqa_shared<RT, KVW> sh;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -824,22 +824,37 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
 }
 
 // few: 16 * few rows of a query tile, whose tokens four waves share out (0: many rows); slots: parts of a row's tokens, chunk: tiles of one at least
-// (a multiple of 4; more where that many parts would not hold a row's tokens).
+// (a multiple of 4; more where that many parts would not hold a row's tokens).  `tokens` bounds those of a row.
+//     few      up to 32 rows of a head.  16 x 4000 tokens under 32 heads, 8 of keys: 4 new tokens each 29 us (47 by the kernel of many rows), 8 each 37 (49);
+//              for 16 rows the wider tile takes 34.  With 64 rows they meet: 54 and 62, one sequence of 30000 35 and 30.
+//     parts    of many rows: one workgroup a compute unit, or two where that pays.  A step of 64 tokens takes about 1.8 us with one, 2.6 with two, so that half a
+//              microsecond a step is saved (nothing with a cap or a bias, whose vector instructions fill the time); a part adds 1040 bytes a row to
+//              what is joined, at 6 TB/s.  512 tokens at 4096: 4 parts 52 us, 2 parts 71; 33 at 30000: 32 parts 45, 16 52; 200 behind a window of 4096, capped:
+//              4 parts 41, 9 parts 45; 1000 behind a window of 1024: 1 part 32, 2 parts 41.
 struct fqc_plan { int few, slots, chunk; };
-fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
+fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int tokens, bool shaped) {
     const int G = Hq / Hkv, cus = fq_device_cus();
     const long long most = (long long)(max_new < T ? max_new : T) * G;
     fqc_plan p = {most <= 16 ? 1 : most <= 32 ? 2 : 0, 1, 4};
-    const int rows = p.few ? 16 * p.few : FQC_MANY_ROWS, tiles = max_len > 0 ? (int)(((long long)max_len + 15) / 16) : 1;
-    const long long units = ((long long)T * G / rows + (p.few ? 0 : B)) * Hkv;
+    const int rows = p.few ? 16 * p.few : FQC_MANY_ROWS, tiles = tokens > 0 ? (int)(((long long)tokens + 15) / 16) : 1;
+    const long long query_tiles = ((long long)T * G + rows - 1) / rows, units = (query_tiles > B ? query_tiles : B) * Hkv;
     if (p.few) {
-        const int chunk = fqa_part(((long long)T * G + rows - 1) / rows > B ? ((long long)T * G + rows - 1) / rows * Hkv : (long long)B * Hkv, tiles, cus, B > 1);
-        p.chunk = (chunk + 3) / 4 * 4;
+        p.chunk = (fqa_part(units, tiles, cus, B > 1) + 3) / 4 * 4;
         p.slots = (tiles + p.chunk - 1) / p.chunk;
     } else {
-        const long long want = 2 * cus / units, room = tiles / 16, slots = want < room ? want : room;
+        const long long one = cus / units > 1 ? cus / units : 1, room = tiles / 8;
+        const double part = (double)T * Hq * 1040 / 6.0e6, saved = shaped ? 0.0 : 0.5 * (tiles / 4) / one, joined = one > 1 ? one * part : 2.5 + 2 * part;   // us
+        const long long want = saved > joined ? 2 * cus / units : one, slots = want < room ? want : room;
         p.slots = (int)(slots < 1 ? 1 : slots > 64 ? 64 : slots);
     }
+    return p;
+}
+// For a call: a window may leave a row fewer tokens than max_len.  Never more parts than the scratch is for.
+fqc_plan fqc_choose(const fq_chunk_args& x) {
+    const fqc_plan most = fqc_choose(x.T, x.B, x.Hq, x.Hkv, x.max_new, x.max_len, false);
+    const long long span = (long long)x.window + (most.few ? 16 * most.few : FQC_MANY_ROWS) / (x.Hq / x.Hkv) + 15;   // (of a query tile, from a tile's beginning)
+    fqc_plan p = fqc_choose(x.T, x.B, x.Hq, x.Hkv, x.max_new, x.window > 0 && !x.end && span < x.max_len ? (int)span : x.max_len, x.cap > 0.f || x.slopes);
+    p.slots = p.slots < most.slots ? p.slots : most.slots;
     return p;
 }
 
@@ -862,12 +877,12 @@ void fqc_launch(const fqc_args& a, const fqa_parts& parts, hipStream_t stream) {
 }  // namespace
 
 size_t fq_chunk_scratch_bytes(int T, int B, int Hq, int Hkv, int max_new, int max_len) {
-    const int slots = fqc_choose(T, B, Hq, Hkv, max_new, max_len).slots;
+    const int slots = fqc_choose(T, B, Hq, Hkv, max_new, max_len, false).slots;
     return slots > 1 ? (size_t)slots * T * Hq * 130 * sizeof(float) : 0;
 }
 
 void fq_launch_chunk(const fq_chunk_args& x, void* scratch, hipStream_t stream) {
-    const fqc_plan p = fqc_choose(x.T, x.B, x.Hq, x.Hkv, x.max_new, x.max_len);
+    const fqc_plan p = fqc_choose(x);
     fqc_args a = {x.Q, x.q_scale, x.c, x.table, x.starts, x.lens, x.first, x.end, x.slopes, x.width, x.window, x.T, x.B, x.Hq, x.Hkv, x.max_len, p.slots, p.chunk,
                   x.out_scale, x.cap > 0.f ? 1.0f / x.cap : 0.f, {}, x.O};
     const double c[5] = {0x1.fffffcp-1, -0x1.5551b8p-2, 0x1.107a08p-3, -0x1.a88656p-5, 0x1.ed307ap-7}, k1 = 1.44269504088896340736 * x.cap;

@@ -311,3 +311,17 @@ def test_starts_that_decrease_far(fq, starts, max_new):
     fq.fq_kv4_attention_chunk(*args, SCALE, max_new=max_new, out=pool[b.T: 2 * b.T])
     torch.cuda.synchronize()
     assert (pool[: b.T] == 7.0).all() and (pool[2 * b.T:] == 7.0).all()
+
+
+@pytest.mark.parametrize("seqs, Hq, Hkv", [([(1, 2100)], 4, 2), ([(1, 1500), (1, 90), (1, 2000)], 2, 1), ([(6, 1700)], 4, 1), ([(70, 1900)], 2, 1), ([(45, 1500), (60, 700)], 4, 1)])
+@pytest.mark.parametrize("window", [1, 15, 16, 17, 129, 600])
+def test_windows_in_parts(fq, seqs, Hq, Hkv, window):
+    """Windows far shorter than the sequences, whose tokens are cut into parts by the window's length; a bound that is far off; an end of their own."""
+    b = Batch(seqs, Hq, Hkv, 32, 59 + window)
+    rows = [i for i in range(b.T) if i % 13 in (0, 5) or i == b.T - 1]
+    for max_len in (None, 4096):
+        kw = {} if max_len is None else {"max_len": max_len}
+        b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, window=window, **kw), window=window, rows=rows)
+    end = np.concatenate([np.full(k, n) for k, n in seqs]).astype(np.int32)
+    out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, window=window, end=torch.as_tensor(end).cuda(), max_new=1, cap=3.0)
+    b.check(out, window=window, end=end, cap=3.0, rows=rows)
