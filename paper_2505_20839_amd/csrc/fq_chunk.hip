@@ -524,6 +524,9 @@ __device__ __forceinline__ void fqc_take_queries(const fqc_args& a, const fqc_pl
 }
 
 // Few rows: one query tile of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among the waves, which meet in LDS.
+// Bound by the tiles' bytes, 130 a token, and by their latency: 37 capped sequences of up to 6000 tokens 34.4 us in a graph (106 MB, 3.1 TB/s; vector
+// instructions 48 % of the busy cycles, waits 49 % of the waves' time), 64 x 8192 plain 111 (4.9 TB/s, a copy's rate), one of 32001 with a bias
+// 16.3 (12 without).  Registers for four waves a SIMD are too few: 38.6, 141 and 22 with them.
 template <int RT, int KVW, bool CAP, bool BIAS>
 __global__ __launch_bounds__(64 * KVW, 2) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
     constexpr int ROWS = 16 * RT, NT = 2;
@@ -614,6 +617,10 @@ __global__ __launch_bounds__(64 * KVW, 2) void fqc_few_kernel(fqc_args a, fqa_pa
 // (lane % 32), the tokens 8 k + 4 h + e (h = lane / 32), and a tile's eight are its part of the B operand of a product with 32 channels, values in the same
 // order.  (A vector instruction costs half as much beside a product of 32 x 32 as beside one of 16 x 16, measured with two waves a SIMD.)  sum p: of the
 // rounded numbers, two to an instruction.
+// Bound by instructions: vector 74 %, matrix 28 % of the busy cycles.  8192 new tokens under 32 heads, 8 of keys: 533 us causal (1031 TFLOP/s, at the card's
+// power: its clock falls to 2 GHz), 675 to 710 capped with a prefix seen whole (820 to 865); 4096 with a bias 202 (679); 2048 57.  Kept on the way there, on
+// the capped one: operands unpacked once a workgroup and not by each wave (1201 us from 2491), masks and tanh's ranges in branches (969, 773), three
+// terms of tanh (719).  16 x 16 products took 696 and, causal, 530 to 558; 64 rows a wave spill.
 struct fqc_stage {
     fq_v4i k[2][2][2][64];                                // keys' bytes: pair of tiles, 64 dimensions, low and high nibbles, lane
     fq_v4i v[4][4][64];                                   // values in fp16: tile, 32 channels, lane

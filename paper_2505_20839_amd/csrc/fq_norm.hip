@@ -6,7 +6,10 @@
 //
 // Between two blocks with a norm on both sides (include/fireq_norm_block.h) the stream takes x by its own norm, a gate and a factor first:
 //     h = bf16(r + scale * gate * (x * post / sqrt(mean x^2 + eps)))
-// The same bytes and one more reduction over the row, which is in registers by then.
+// The same bytes and one more reduction over the row, which is in registers by then (in a second pass over rows that the registers do not hold), so that
+// the rows' shares among waves are those of the other forms.  Measured, calls back to back: 8192 x 4096 to E4M3 45 us (235 MB, 5.2 TB/s: the rate of a
+// copy), 1000 x 5120 to bf16 with a gate row for each of 7 sequences 10.7 us (41 MB, 3.8 TB/s: the vector instructions' 86 % of the busy
+// cycles), one row 3.6 us in a graph.
 #include <type_traits>
 #include "fq_common.h"
 #include "fq_kernels.h"

@@ -1,7 +1,8 @@
 // A token for each row of logits (include/fireq_sample.h).
 //
 // min-p, top-k and top-p all keep a first run of the tokens in one order (larger logit first, lower index first among equals), so
-// what is kept is comp >= least for one number: comp = (ordered bits of the logit, inverted index).  Three kernels find it without sorting:
+// what is kept is comp >= least for one number: comp = (ordered bits of the logit, inverted index).  It is found without sorting: of rows
+// of up to 32761 logits by a workgroup each (fqs_row_kernel), of longer ones by three kernels:
 //     parts    a row is cut into parts of up to 8192 logits.  Each finds its largest logit, takes e = exp((x - largest) / T) as a whole number of
 //              2^-32 (sums of whole numbers do not depend on their order; a token below 2^-33 of its part's best has no mass) and, where the row is
 //              filtered at all, counts numbers and masses in FQS_BINS equal steps of x / T.  The steps lie on one grid for all parts.
@@ -9,6 +10,8 @@
 //     draw     the parts again: the tokens of those bins into a list.  The row's last workgroup selects among them, by number and then by mass, eight
 //              bits of comp at a time (over the row again, where they are too many for its LDS), and finds the part, and in it the index, at which the
 //              kept mass in index order passes u times its sum.
+// 64 x 131072 of any filters 42 us in a graph: 12, 9 and 23 under a profiler, where reading the logits once takes 3.4; what is left are steps that wait for
+// each other (67 % of the last kernel's time).  One workgroup a row behind the parts' took 56 (512 rows: 140 and not 178).
 #include <type_traits>
 
 #include "fq_common.h"
@@ -863,8 +866,11 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
     }
 }
 
-// A row for one workgroup: all of it in one kernel, without scratch; the steps of the three kernels, with one unit for all masses.  Wave w has the chunks
-// 64 n w .. 64 n (w + 1) - 1, n of a lane, 64 apart, and CHUNKS of all fit LDS.
+// A row for one workgroup: all of it in one kernel, without scratch.  Bound by one compute unit's vector instructions and by its steps' latency.  In a graph, against the
+// three kernels: 1 x 5000 11 us (28), 1 x 32000 14 (27), 64 rows of any filters 19 and 34 (32 and 35); 64 x 50000 would take 51 (37).
+// Where top-k, or min-p with top-p, leave at most 2048 tokens above a border known beforehand, these are listed in the pass that sums exponentials, and
+// nothing is binned: 1 x 32000 with top-k 50 and top-p 26 us before.  Otherwise the steps are those of the three kernels, with one unit for all masses.
+// Wave w has the chunks 64 n w .. 64 n (w + 1) - 1, n of a lane, 64 apart, and CHUNKS of all fit LDS.
 template <bool WIDE, int CHUNKS>
 __global__ __launch_bounds__(1024) void fqs_row_kernel(fq_sample_args a) {
     constexpr int THREADS = 1024, WAVES = THREADS / 64, SIZE = WIDE ? 2 : 1;
