@@ -327,20 +327,18 @@ __device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], unsigned lost, int
             now[i].s |= lost >> i & 1u ? 0x7F7F7F7F : 0;
             fqc_move_nans(now[i].s);
         }
-    fq_v8i k[NT];
     float ks[NT][4];
+    fq_v4f c[RT][NT];
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        k[i] = fq_unpack_chunk(now[i].k);
+        const fq_v8i k = fq_unpack_chunk(now[i].k);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) c[r][i] = FQA_MFMA_QK(k, Q.q[r], Q.zp[r]);
+        if (RT == 1) __builtin_amdgcn_sched_barrier(0);   // (both tiles' operands at once are registers: 2 % of a large batch)
         const fq_v2f s01 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[0], false), s23 = __builtin_amdgcn_cvt_pk_f32_fp8(now[i].s[0], true);
         ks[i][0] = s01[0]; ks[i][1] = s01[1]; ks[i][2] = s23[0]; ks[i][3] = s23[1];
     }
     fq_v4i pt[RT][NT / 2];
-    fq_v4f c[RT][NT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int i = 0; i < NT; ++i) c[r][i] = FQA_MFMA_QK(k[i], Q.q[r], Q.zp[r]);
     fqc_probabilities<RT, NT, 16, CAP, BIAS>(c, ks, 16 * tb + 4 * g, Q.qs, rows, shape, st.m, st.sub, whole, pt, [&](int r, float x) __attribute__((always_inline)) {
         st.l[r] *= x;
 #pragma unroll
@@ -436,24 +434,27 @@ __device__ __forceinline__ fqc_sequence fqc_sequence_of(const fqc_args& a, int k
 struct fqc_place {
     int b, kv, G, start, count, row0, nrows, raw, len;
     bool too_long;
-    // k: the workgroup's query tile, of ROWS rows
-    template <int ROWS>
-    __device__ __forceinline__ bool find(const fqc_args& a, int k, int lane) {
+    __device__ __forceinline__ void take(const fqc_args& a, int sequence, int first, int stop, int length) {
+        b = sequence;
         G = a.Hq / a.Hkv;
         kv = (int)(blockIdx.x % a.Hkv);
-        const fqc_sequence q = fqc_sequence_of(a, k, G, ROWS, lane);
-        b = q.b;
-        if (b < 0) return false;
-        start = q.start;
-        count = q.stop - q.start;
-        row0 = (k - q.tile0) * ROWS;                        // (T * G is bounded: 32 bits hold it)
-        if (count <= 0 || count * G <= row0 || row0 < 0) return false;   // (row0 < 0: starts that decrease)
-        nrows = count * G - row0 < ROWS ? count * G - row0 : ROWS;
-        raw = q.len;
+        start = first;
+        count = stop - first;
+        raw = length;
         const long long room = (long long)a.width * a.c.page;
         const int cap = a.max_len < room ? a.max_len : (int)room;
         too_long = raw > cap;
         len = too_long ? cap : raw < 0 ? 0 : raw;
+    }
+    // k: the workgroup's query tile, of ROWS rows
+    template <int ROWS>
+    __device__ __forceinline__ bool find(const fqc_args& a, int k, int lane) {
+        const fqc_sequence q = fqc_sequence_of(a, k, a.Hq / a.Hkv, ROWS, lane);
+        if (q.b < 0) return false;
+        take(a, q.b, q.start, q.stop, q.len);
+        row0 = (k - q.tile0) * ROWS;                        // (T * G is bounded: 32 bits hold it)
+        if (count <= 0 || count * G <= row0 || row0 < 0) return false;   // (row0 < 0: starts that decrease)
+        nrows = count * G - row0 < ROWS ? count * G - row0 : ROWS;
         return true;
     }
     __device__ __forceinline__ int token(int i) const { return count == 1 ? 0 : (int)((unsigned)(row0 + i) / (unsigned)G); }   // of row i, among the new ones
@@ -523,91 +524,102 @@ __device__ __forceinline__ void fqc_take_queries(const fqc_args& a, const fqc_pl
     }
 }
 
-// Few rows: one query tile of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among the waves, which meet in LDS.
-// Bound by the tiles' bytes, 130 a token, and by their latency: 37 capped sequences of up to 6000 tokens 34.4 us in a graph (106 MB, 3.1 TB/s; vector
-// instructions 48 % of the busy cycles, waits 49 % of the waves' time), 64 x 8192 plain 111 (4.9 TB/s, a copy's rate), one of 32001 with a bias
-// 16.3 (12 without).  Registers for four waves a SIMD are too few: 38.6, 141 and 22 with them.
+// Few rows: a sequence's rows of one key/value head, and part blockIdx.y of the tokens that its rows have, shared out among the waves, which meet in LDS.
+// Bound by the tiles' bytes, 130 a token, and by their latency: 37 capped sequences of up to 6000 tokens 33 us in a graph (106 MB, 3.2 TB/s; vector
+// instructions 48 % of the busy cycles, waits 49 % of the waves' time), 30 without a cap, 64 x 8192 plain 109 to 111 (4.9 TB/s, a copy's rate), one of
+// 32001 with a bias 16 (14 without).  Registers for four waves a SIMD are too few: 38, 30, 128 and 20 with them.  A sequence with more rows than max_new
+// promised is worked on in turns.
 template <int RT, int KVW, bool CAP, bool BIAS>
 __global__ __launch_bounds__(64 * KVW, 2) void fqc_few_kernel(fqc_args a, fqa_parts parts) {
     constexpr int ROWS = 16 * RT, NT = 2;
     __shared__ fqa_shared<RT, KVW> sh;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int b = (int)(blockIdx.x / a.Hkv);
     fqc_place at;
-    if (!at.find<ROWS>(a, (int)(blockIdx.x / a.Hkv), lane)) return;
+    at.take(a, b, fqc_clamp(a.starts[b], a.T), fqc_clamp(a.starts[b + 1], a.T), a.lens[b]);
+    const int all_rows = at.count > 0 ? at.count * at.G : 0;
+    at.row0 = 0;
     if (a.slots > 1 && (long long)blockIdx.y * a.chunk * 16 >= at.len) {   // behind the sequence's end, wherever its rows' tokens begin
-        if ((int)threadIdx.x < at.nrows) {
-            float* ml = parts.ml + (at.row(a, threadIdx.x) * parts.slots + blockIdx.y) * 2;
+        for (int i = threadIdx.x; i < all_rows; i += 64 * KVW) {
+            float* ml = parts.ml + (at.row(a, i) * parts.slots + blockIdx.y) * 2;
             ml[0] = FQA_LOWEST;
             ml[1] = at.too_long ? __builtin_nanf("") : 0.f;
         }
         return;
     }
-    fqc_rows<RT> rows;
-    const fqc_span sp = fqc_take_rows<RT, BIAS>(a, at, 0, n, rows);
-    const int tok0 = sp.tok0, tok1 = sp.tok1, whole0 = sp.whole0, whole1 = sp.whole1, nrows = at.nrows;
-    const unsigned none = sp.none;
-    const bool too_long = at.too_long;
-    const int first_tile = tok1 > 0 ? tok0 >> 4 : 0, all = tok1 > 0 ? ((tok1 + 15) >> 4) - first_tile : 0;
-    // this workgroup's part, and the waves' shares: steps of NT tiles
-    const int even = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, part = even > a.chunk ? even : a.chunk, c0 = first_tile + (int)blockIdx.y * part;
-    const int c1 = c0 + part < first_tile + all ? c0 + part : first_tile + all;
-    const int share = c1 > c0 ? ((c1 - c0 + NT - 1) / NT + KVW - 1) / KVW * NT : 0, t0 = c0 + wave * share, t1 = t0 + share < c1 ? t0 + share : c1;
-    fqa_state<RT> st;
-    const bool work = t0 < t1;
-    if (work) {
-        fqc_cursor cur;
-        cur.pages_of = a.table + (size_t)at.b * a.width;
-        cur.head = a.c.base + at.kv * a.c.head_stride;
-        cur.page_stride = (unsigned)(a.c.page_stride >> 4);
-        cur.tiles_per_page = a.c.page >> 4;
-        cur.pages = a.c.pages;
-        cur.start(t0, t1, lane);
-        fqa_queries<RT> Q;
-        fqa_tile ahead[NT];
-        const unsigned lost = cur.next(ahead, lane);      // (on their way while the queries are taken)
-        fqc_take_queries<RT, CAP, BIAS>(a, at, 0, n, g, Q);
-        fqc_range<RT, NT, CAP, BIAS>(cur, ahead, lost, t0, t1, whole0, whole1 < 16 * t1 ? whole1 : 16 * t1, Q, rows, a.shape, st, lane);
-    }
-    if (work) {
+    for (; at.row0 < all_rows; at.row0 += ROWS) {
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));                    // (nothing of a turn is kept in registers for the next)
+        const int n = lane & 15, g = lane >> 4;
+        at.nrows = all_rows - at.row0 < ROWS ? all_rows - at.row0 : ROWS;
+        fqc_rows<RT> rows;
+        const fqc_span sp = fqc_take_rows<RT, BIAS>(a, at, 0, n, rows);
+        const int tok0 = sp.tok0, tok1 = sp.tok1, whole0 = sp.whole0, whole1 = sp.whole1, nrows = at.nrows;
+        const unsigned none = sp.none;
+        const bool too_long = at.too_long;
+        const int first_tile = tok1 > 0 ? tok0 >> 4 : 0, all = tok1 > 0 ? ((tok1 + 15) >> 4) - first_tile : 0;
+        // this workgroup's part, and the waves' shares: steps of NT tiles
+        const int even = ((all + a.slots - 1) / a.slots + NT - 1) / NT * NT, part = even > a.chunk ? even : a.chunk, c0 = first_tile + (int)blockIdx.y * part;
+        const int c1 = c0 + part < first_tile + all ? c0 + part : first_tile + all;
+        const int share = c1 > c0 ? ((c1 - c0 + NT - 1) / NT + KVW - 1) / KVW * NT : 0, t0 = c0 + wave * share, t1 = t0 + share < c1 ? t0 + share : c1;
+        fqa_state<RT> st;
+        const bool work = t0 < t1;
+        if (work) {
+            fqc_cursor cur;
+            cur.pages_of = a.table + (size_t)at.b * a.width;
+            cur.head = a.c.base + at.kv * a.c.head_stride;
+            cur.page_stride = (unsigned)(a.c.page_stride >> 4);
+            cur.tiles_per_page = a.c.page >> 4;
+            cur.pages = a.c.pages;
+            cur.start(t0, t1, lane);
+            fqa_queries<RT> Q;
+            fqa_tile ahead[NT];
+            const unsigned lost = cur.next(ahead, lane);      // (on their way while the queries are taken)
+            fqc_take_queries<RT, CAP, BIAS>(a, at, 0, n, g, Q);
+            fqc_range<RT, NT, CAP, BIAS>(cur, ahead, lost, t0, t1, whole0, whole1 < 16 * t1 ? whole1 : 16 * t1, Q, rows, a.shape, st, lane);
+        }
+        if (work) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (g == 0) {
-                sh.m[wave][16 * r + n] = st.m[r];
-                sh.l[wave][16 * r + n] = too_long ? __builtin_nanf("") : (none >> r & 1u) != 0u ? 0.f : st.l[r][0];
+            for (int r = 0; r < RT; ++r) {
+                if (g == 0) {
+                    sh.m[wave][16 * r + n] = st.m[r];
+                    sh.l[wave][16 * r + n] = too_long ? __builtin_nanf("") : (none >> r & 1u) != 0u ? 0.f : st.l[r][0];
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(&sh.o[wave][16 * r + n][16 * j + 4 * g]) = st.o[r][j];
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) *reinterpret_cast<fq_v4f*>(&sh.o[wave][16 * r + n][16 * j + 4 * g]) = st.o[r][j];
+        } else if (lane < ROWS) {
+            sh.m[wave][lane] = FQA_LOWEST;
+            sh.l[wave][lane] = too_long ? __builtin_nanf("") : 0.f;
         }
-    } else if (lane < ROWS) {
-        sh.m[wave][lane] = FQA_LOWEST;
-        sh.l[wave][lane] = too_long ? __builtin_nanf("") : 0.f;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < nrows * 32; i += 64 * KVW) {  // four channels of a row
-        const int r = i >> 5, c = 4 * (i & 31);
-        float top = FQA_LOWEST, l = 0.f;
+        __syncthreads();
+        for (int i = 64 * wave + lane; i < nrows * 32; i += 64 * KVW) {  // four channels of a row
+            const int r = i >> 5, c = 4 * (i & 31);
+            float top = FQA_LOWEST, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < KVW; ++w)
-            if (sh.l[w][r] != 0.f) top = fmaxf(top, sh.m[w][r]);
-        fq_v4f o = {0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < KVW; ++w)
+                if (sh.l[w][r] != 0.f) top = fmaxf(top, sh.m[w][r]);
+            fq_v4f o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int w = 0; w < KVW; ++w) {
-            if (sh.l[w][r] == 0.f) continue;          // (a wave without tokens of this row; a NaN is kept)
-            const float f = __builtin_amdgcn_exp2f(sh.m[w][r] - top);
-            l += sh.l[w][r] * f;
-            o += *reinterpret_cast<const fq_v4f*>(&sh.o[w][r][c]) * f;
-        }
-        const size_t row = at.row(a, r);
-        if (a.slots == 1) {
-            *reinterpret_cast<uint2*>(a.O + row * 128 + c) = fqa_output(o, l);
-        } else {
-            const size_t place = row * parts.slots + blockIdx.y;
-            *reinterpret_cast<fq_v4f*>(parts.o + place * 128 + c) = o;
-            if (c == 0) {
-                parts.ml[place * 2] = top;
-                parts.ml[place * 2 + 1] = l;
+            for (int w = 0; w < KVW; ++w) {
+                if (sh.l[w][r] == 0.f) continue;          // (a wave without tokens of this row; a NaN is kept)
+                const float f = __builtin_amdgcn_exp2f(sh.m[w][r] - top);
+                l += sh.l[w][r] * f;
+                o += *reinterpret_cast<const fq_v4f*>(&sh.o[w][r][c]) * f;
+            }
+            const size_t row = at.row(a, r);
+            if (a.slots == 1) {
+                *reinterpret_cast<uint2*>(a.O + row * 128 + c) = fqa_output(o, l);
+            } else {
+                const size_t place = row * parts.slots + blockIdx.y;
+                *reinterpret_cast<fq_v4f*>(parts.o + place * 128 + c) = o;
+                if (c == 0) {
+                    parts.ml[place * 2] = top;
+                    parts.ml[place * 2 + 1] = l;
+                }
             }
         }
+        if (at.row0 + ROWS < all_rows) __syncthreads();       // (max_new was too small: the next rows in the same LDS)
     }
 }
 
@@ -832,8 +844,8 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
 
 // few: 16 * few rows of a query tile, whose tokens four waves share out (0: many rows); slots: parts of a row's tokens, chunk: tiles of one at least
 // (a multiple of 4; more where that many parts would not hold a row's tokens).  `tokens` bounds those of a row.
-//     few      up to 32 rows of a head.  16 x 4000 tokens under 32 heads, 8 of keys: 4 new tokens each 29 us (47 by the kernel of many rows), 8 each 37 (49);
-//              for 16 rows the wider tile takes 34.  With 64 rows they meet: 54 and 62, one sequence of 30000 35 and 30.
+//     few      up to 32 rows of a head.  16 x 4000 tokens under 32 heads, 8 of keys: 4 new tokens each 24 us (40 by the kernel of many rows), 8 each 31 (41);
+//              for 16 rows the wider tile takes 28.  With 64 rows they meet: 54 and 61, two such sequences 23 and 20, one of 30000 35 and 30.
 //     parts    of many rows: one workgroup a compute unit, or two where that pays.  A step of 64 tokens takes about 1.8 us with one, 2.6 with two, so that half a
 //              microsecond a step is saved (nothing with a cap or a bias, whose vector instructions fill the time); a part adds 1040 bytes a row to
 //              what is joined, at 6 TB/s.  512 tokens at 4096: 4 parts 52 us, 2 parts 71; 33 at 30000: 32 parts 45, 16 52; 200 behind a window of 4096, capped:
@@ -844,7 +856,7 @@ fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int tokens, bool
     const long long most = (long long)(max_new < T ? max_new : T) * G;
     fqc_plan p = {most <= 16 ? 1 : most <= 32 ? 2 : 0, 1, 4};
     const int rows = p.few ? 16 * p.few : FQC_MANY_ROWS, tiles = tokens > 0 ? (int)(((long long)tokens + 15) / 16) : 1;
-    const long long query_tiles = ((long long)T * G + rows - 1) / rows, units = (query_tiles > B ? query_tiles : B) * Hkv;
+    const long long query_tiles = ((long long)T * G + rows - 1) / rows, units = (p.few || query_tiles < B ? B : query_tiles) * Hkv;
     if (p.few) {
         p.chunk = (fqa_part(units, tiles, cus, B > 1) + 3) / 4 * 4;
         p.slots = (tiles + p.chunk - 1) / p.chunk;
@@ -867,8 +879,8 @@ fqc_plan fqc_choose(const fq_chunk_args& x) {
 
 template <int FEW, bool CAP, bool BIAS>
 void fqc_launch(const fqc_args& a, const fqa_parts& parts, hipStream_t stream) {
-    constexpr int ROWS = FEW ? 16 * FEW : FQC_MANY_ROWS;
-    const dim3 grid((unsigned)(((long long)a.T * (a.Hq / a.Hkv) / ROWS + a.B) * a.Hkv), (unsigned)a.slots);
+    const long long query_tiles = FEW != 0 ? a.B : (long long)a.T * (a.Hq / a.Hkv) / FQC_MANY_ROWS + a.B;
+    const dim3 grid((unsigned)(query_tiles * a.Hkv), (unsigned)a.slots);
     if constexpr (FEW != 0) hipLaunchKernelGGL((fqc_few_kernel<FEW, 4, CAP, BIAS>), grid, dim3(256), 0, stream, a, parts);
     else hipLaunchKernelGGL((fqc_many_kernel<CAP, BIAS>), grid, dim3(256), 0, stream, a, parts);
 }
