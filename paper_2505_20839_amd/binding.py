@@ -1052,7 +1052,8 @@ def fq_kv4_attention_chunk(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch.
     scores cap * tanh(s / cap) (0: s) - slopes[h] * |pos - t| (float32 [Hq]).  Rows without a token are zeros; rows of no sequence are left as
     `out` had them.
 
-    `max_new`, `max_len`: upper bounds of a sequence's rows and of seq_lens that the host knows, by default T and what the table has room for;
+    `max_new`, `max_len`: upper bounds of a sequence's rows and of seq_lens that the host knows, by default T (1 where there are no more rows than
+    sequences: single tokens) and what the table has room for; both decide how the work is split, and a wrong max_new costs time alone;
     `workspace` of fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len) bytes is allocated here when not given."""
     where = "fq_kv4_attention_chunk"
     r = (_marshal or marshal()).kv4_attention_chunk(Q, q_scale, cache, block_table, starts, seq_lens, out_scale, max_new, max_len, first, end, window, cap,
@@ -1076,7 +1077,7 @@ def fq_kv4_attention_chunk(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch.
     for name, t, n, dtype in (("first", first, T, torch.int32), ("end", end, T, torch.int32), ("slopes", slopes, Hq, torch.float32)):
         if t is not None and _dev(t, dtype, name).numel() != n:
             raise FireqError(-2, where)
-    max_new = T if max_new is None else int(max_new)
+    max_new = (1 if T <= B else T) if max_new is None else int(max_new)
     max_len = min(width * geometry[4], 1 << 30) if max_len is None else int(max_len)
     window = int(window)
     if not _fits(T, Hq, B, width, max_new, window) or max_len < 0 or max_len > 1 << 30:

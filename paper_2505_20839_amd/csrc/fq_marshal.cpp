@@ -686,7 +686,7 @@ PyObject* kv4_attention_chunk(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const float* s = (const float*)here(a[1], at::kFloat, T * Hq).data_ptr();
         const int32_t *starts = (const int32_t*)here(a[4], at::kInt, B + 1).data_ptr(), *lens = (const int32_t*)here(a[5], at::kInt, B).data_ptr();
         const float out_scale = number(a[6]), cap = number(a[12]);
-        const int max_new = a[7] == Py_None ? (int)T : whole(a[7]), max_len = a[8] == Py_None ? (int)std::min<int64_t>(width * c.page, 1 << 30) : whole(a[8]);
+        const int max_new = a[7] == Py_None ? (T <= B ? 1 : (int)T) : whole(a[7]), max_len = a[8] == Py_None ? (int)std::min<int64_t>(width * c.page, 1 << 30) : whole(a[8]);
         const int window = whole(a[11]);
         const int32_t *first = maybe<int32_t>(a[9], at::kInt, T), *end = maybe<int32_t>(a[10], at::kInt, T);
         const float* slopes = maybe<float>(a[13], at::kFloat, Hq);

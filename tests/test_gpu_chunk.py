@@ -325,3 +325,11 @@ def test_windows_in_parts(fq, seqs, Hq, Hkv, window):
     end = np.concatenate([np.full(k, n) for k, n in seqs]).astype(np.int32)
     out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, window=window, end=torch.as_tensor(end).cuda(), max_new=1, cap=3.0)
     b.check(out, window=window, end=end, cap=3.0, rows=rows)
+
+
+@pytest.mark.parametrize("seqs", [[(5, 40), (0, 30), (0, 20), (0, 0), (0, 1)], [(0, 9), (33, 60)] + [(0, 5)] * 31, [(1, 40)] * 3])
+def test_rows_that_no_bound_is_given_for(fq, seqs):
+    """No more rows than sequences are taken for single tokens, whosever they are."""
+    b = Batch(seqs, 8, 2, 16, 61)
+    b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE))
+    b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, max_len=2000, window=11), window=11)
