@@ -10,6 +10,8 @@
 //                all scores of a row, and exact in FP32 where it counts.
 //     broken     a value whose scale is NaN must not reach the rows that do not see its token (0 * NaN): its NaN moves to the key's scale,
 //                which makes the probabilities NaN of those rows only that see it; so does a tile of a page outside the cache.
+#include <type_traits>
+
 #include "fq_attend.h"
 
 namespace {
@@ -760,58 +762,71 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
         float sub[1] = {CAP || BIAS ? -FQA_LOWEST : fminf(1.0e30f * qs[0], -FQA_LOWEST)};
         mend(f);
         unpack(f, stage[0]);
-        cur.refill(lane);
-        fetch(f);
-        for (int tb = t0; tb < t1; tb += 2 * NT) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int now = tb + NT * u;
-                if (now >= t1) break;
-                __syncthreads();                          // this step's operands are there, and the other stage is free
+        if (t0 + NT < t1) {
+            cur.refill(lane);
+            fetch(f);
+        }
+        // a step whose operands stage u holds; MORE: the next one's are unpacked beside its score products, and those behind are requested
+        auto step = [&](auto more, int u, int now) __attribute__((always_inline)) {
+            constexpr bool MORE = decltype(more)::value;
+            __syncthreads();                              // this step's operands are there, and the other stage is free
+            if (MORE) {
                 cur.refill(lane);
                 mend(f);
-                // (behind the range the last tile again, into a stage that nobody reads)
-                const fqc_stage& from = stage[u];
-                fq_v4f c[1][2 * NT];
-                float ks[2 * NT][4];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    fq_v16f x = zp;
-#pragma unroll
-                    for (int d = 0; d < 2; ++d) {
-                        const fq_v4i lo = from.k[i][d][0][lane], hi = from.k[i][d][1][lane];
-                        x = FQC_MFMA32_QK(((fq_v8i){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}), q[d], x);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) c[0][4 * i + k] = (fq_v4f){x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
-                }
-#pragma unroll
-                for (int k = 0; k < 2 * NT; ++k) {
-                    const fq_v4f s = *reinterpret_cast<const fq_v4f*>(&from.ks[k >> 1][8 * (k & 1) + 4 * h]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) ks[k][e] = s[e];
-                }
-                unpack(f, stage[u ^ 1]);
-                fetch(f);
-                if (now * 16 >= sp.tok1 || (now + NT) * 16 <= sp.tok0) continue;   // (none of this wave's rows has any of the tokens)
-                const bool whole = now * 16 >= whole0 && (now + NT) * 16 <= whole1;
-                fq_v4i pt[1][NT];
-                fqc_probabilities<1, 2 * NT, 8, CAP, BIAS>(c, ks, 16 * now + 4 * h, qs, rows, a.shape, m, sub, whole, pt, [&](int, float x) __attribute__((always_inline)) {
-                    l *= x;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] *= x;
-                });
-#pragma unroll
-                for (int i = 0; i < NT; ++i) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int two = pt[0][i][e];      // (a bit cast of the element itself takes the first one's bits)
-                        l = __builtin_amdgcn_fdot2(__builtin_bit_cast(fqa_v2h, two), (fqa_v2h){(_Float16)1.f, (_Float16)1.f}, l, false);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[j] = FQC_MFMA32_PV(from.v[i][j][lane], pt[0][i], o[j]);
-                }
             }
+            const fqc_stage& from = stage[u];
+            fq_v4f c[1][2 * NT];
+            float ks[2 * NT][4];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                fq_v16f x = zp;
+#pragma unroll
+                for (int d = 0; d < 2; ++d) {
+                    const fq_v4i lo = from.k[i][d][0][lane], hi = from.k[i][d][1][lane];
+                    x = FQC_MFMA32_QK(((fq_v8i){lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]}), q[d], x);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) c[0][4 * i + k] = (fq_v4f){x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]};
+            }
+#pragma unroll
+            for (int k = 0; k < 2 * NT; ++k) {
+                const fq_v4f s = *reinterpret_cast<const fq_v4f*>(&from.ks[k >> 1][8 * (k & 1) + 4 * h]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ks[k][e] = s[e];
+            }
+            if (MORE) {
+                unpack(f, stage[u ^ 1]);
+                fetch(f);                                 // (behind the range the last tile again)
+            }
+            if (now * 16 >= sp.tok1 || (now + NT) * 16 <= sp.tok0) return;   // (none of this wave's rows has any of the tokens)
+            const bool whole = now * 16 >= whole0 && (now + NT) * 16 <= whole1;
+            fq_v4i pt[1][NT];
+            fqc_probabilities<1, 2 * NT, 8, CAP, BIAS>(c, ks, 16 * now + 4 * h, qs, rows, a.shape, m, sub, whole, pt, [&](int, float x) __attribute__((always_inline)) {
+                l *= x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] *= x;
+            });
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int two = pt[0][i][e];          // (a bit cast of the element itself takes the first one's bits)
+                    l = __builtin_amdgcn_fdot2(__builtin_bit_cast(fqa_v2h, two), (fqa_v2h){(_Float16)1.f, (_Float16)1.f}, l, false);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] = FQC_MFMA32_PV(from.v[i][j][lane], pt[0][i], o[j]);
+            }
+        };
+        int now = t0;
+        for (; now + 2 * NT < t1; now += 2 * NT) {
+            step(std::true_type(), 0, now);
+            step(std::true_type(), 1, now + NT);
+        }
+        if (now + NT < t1) {
+            step(std::true_type(), 0, now);
+            step(std::false_type(), 1, now + NT);
+        } else {
+            step(std::false_type(), 0, now);
         }
         if (!(CAP || BIAS)) m[0] *= qs[0];
     }
