@@ -631,8 +631,9 @@ __global__ __launch_bounds__(64 * KVW, 2) void fqc_few_kernel(fqc_args a, fqa_pa
 // (lane % 32), the tokens 8 k + 4 h + e (h = lane / 32), and a tile's eight are its part of the B operand of a product with 32 channels, values in the same
 // order.  (A vector instruction costs half as much beside a product of 32 x 32 as beside one of 16 x 16, measured with two waves a SIMD.)  sum p: of the
 // rounded numbers, two to an instruction.
-// Bound by instructions: vector 74 %, matrix 28 % of the busy cycles.  8192 new tokens under 32 heads, 8 of keys: 533 us causal (1031 TFLOP/s, at the card's
-// power: its clock falls to 2 GHz), 675 to 710 capped with a prefix seen whole (820 to 865); 4096 with a bias 202 (679); 2048 57.  Kept on the way there, on
+// Bound by instructions: vector 76 %, matrix 28 % of the busy cycles.  8192 new tokens under 32 heads, 8 of keys: 515 to 528 us causal (1041 to 1067 TFLOP/s, at
+// the card's power: its clock falls to 2 GHz), 665 to 715 capped with a prefix seen whole (820 to 880); 4096 with a bias 204 (673); 2048 52 to 54; a
+// tile's own cost shows in 5000 tokens behind a window of one, 22 (60 MB).  Kept on the way there, on
 // the capped one: operands unpacked once a workgroup and not by each wave (1201 us from 2491), masks and tanh's ranges in branches (969, 773), three
 // terms of tanh (719).  16 x 16 products took 696 and, causal, 530 to 558; 64 rows a wave spill.
 struct fqc_stage {
