@@ -6,10 +6,10 @@
 //
 // Between two blocks with a norm on both sides (include/fireq_norm_block.h) the stream takes x by its own norm, a gate and a factor first:
 //     h = bf16(r + scale * gate * (x * post / sqrt(mean x^2 + eps)))
-// The same bytes and one more reduction over the row, which is in registers by then (in a second pass over rows that the registers do not hold), so that
-// the rows' shares among waves are those of the other forms.  Measured, calls back to back: 8192 x 4096 to E4M3 45 us (235 MB, 5.2 TB/s: the rate of a
-// copy), 1000 x 5120 to bf16 with a gate row for each of 7 sequences 10.7 us (41 MB, 3.8 TB/s: the vector instructions' 86 % of the busy
-// cycles), one row 3.6 us in a graph.
+// The same bytes and one more reduction over the row, which is in registers by then (in a second pass over rows that the registers do not hold).  The
+// norm's sums are added in the order of the other forms, so that it is that of the stream, bit for bit.  Measured, calls back to back: 8192 x 4096 to E4M3 45 us (235 MB,
+// 5.2 TB/s: the rate of a copy), 1000 x 5120 to bf16 with a gate row for each of 7 sequences 9.8 us (41 MB, 4.2 TB/s, vector instructions
+// nearly as busy), one row 3.6 us in a graph.
 #include <type_traits>
 #include "fq_common.h"
 #include "fq_kernels.h"
@@ -101,7 +101,9 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
     constexpr int WAVES = WPR > 4 ? WPR : 4, ROWS = WAVES / WPR, T = 64 * WPR;
     constexpr int MAXG = T * CH / 16 + 16;                // groups of a row, padded
     constexpr bool ZP = OUT == FQN_CODES_ZP;
-    __shared__ float red_sum[WAVES];
+    // the sums are those of twice the waves with two chunks a thread, bit for bit: a thread has chunks 0 and 2 of one of them, 1 and 3 of another
+    constexpr bool HALVES = BRANCH && !REREAD && (WPR == 4 || WPR == 8) && (CH == 3 || CH == 4);
+    __shared__ float red_sum[HALVES ? 2 * WAVES : WAVES];
     __shared__ unsigned red_top[WAVES];
     __shared__ __attribute__((aligned(16))) uint16_t zrow[ZP ? ROWS : 1][2][ZP ? MAXG : 8];   // [row][plane][group]
     const int row = (int)threadIdx.x / T, t = (int)threadIdx.x % T, m = (int)blockIdx.x * ROWS + row;
@@ -116,7 +118,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
     const fq_v4i *x = reinterpret_cast<const fq_v4i*>(X + at), *r = reinterpret_cast<const fq_v4i*>(R + (RES ? at : 0));
     const fq_v4i* w = reinterpret_cast<const fq_v4i*>(Wt);
     fq_v4i* hs = reinterpret_cast<fq_v4i*>(H + (RES ? at : 0));
-    float ss = 0.f;
+    float ss = 0.f, other = 0.f;
     unsigned top = 0u;
     fq_v4i keep[CH], wt[CH];
     constexpr int ONES = 0x3F803F80;                      // bf16 ones, where there is no weight or gate
@@ -168,7 +170,7 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
         for (int i = 0; i < CH; ++i) {
             keep[i] = fqn_branch8(keep[i], add[i], pw[i], gt[i], f, branch.scale);
             if (t + i * T >= nchunk) keep[i] = (fq_v4i){0, 0, 0, 0};
-            fqn_take8(keep[i], wt[i], ss, top);
+            fqn_take8(keep[i], wt[i], HALVES && i % 2 == 1 ? other : ss, top);
         }
 #pragma unroll
         for (int i = 0; i < CH; ++i)
@@ -214,7 +216,12 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
     top = fq_wave_max(top);
     if (WPR > 1) {                                        // (a workgroup is one row, or four waves of one row)
         const int wave = (int)threadIdx.x >> 6, first = row * WPR;
-        if ((t & 63) == 0) { red_sum[wave] = ss; red_top[wave] = top; }
+        if (HALVES) other = fqn_wave_sum(other);
+        if ((t & 63) == 0) {
+            red_sum[wave] = ss;
+            if (HALVES) red_sum[WAVES + wave] = other;
+            red_top[wave] = top;
+        }
         __syncthreads();
         ss = red_sum[first];
         top = red_top[first];
@@ -223,6 +230,9 @@ __global__ __launch_bounds__(WPR > 4 ? 64 * WPR : 256) void fqn_kernel(const uin
             ss += red_sum[first + i];
             top = red_top[first + i] > top ? red_top[first + i] : top;
         }
+        if (HALVES)
+#pragma unroll
+            for (int i = 0; i < WPR; ++i) ss += red_sum[WAVES + i];
     }
     const float rstd = 1.0f / sqrtf(ss / (float)K + eps), tf = __uint_as_float(top), ymax = tf * rstd;
     const bool bad = !(ss < __builtin_inff()) || top >= 0x7F800000u || (OUT != FQN_BF16 && !(ymax < __builtin_inff()));
@@ -324,8 +334,18 @@ void fqn_launch(const uint16_t* X, const uint16_t* R, const uint16_t* W, float e
             }
             else FQN_LAUNCH(16, 4, false);
         }
+    } else if (BRANCH && K > 8192) {
+        // (fewer waves of a row, and of the two sums that the branch needs: us, the choice here first, then the plain forms': 1000 x 5120 <4, 3> 10.1,
+        // <8, 2> 11.5; 8192 x 5120 to E4M3 55, 65; 4096 x 10240 <8, 3> 72, <16, 2> 103; 1000 x 16384 <8, 4> 23, 31; up to 8192 numbers <8, 2> is as fast
+        // as <4, 4>: 1000 x 8192 13.6, 13.3; 16 x 8192 4.1, 4.3)
+        if constexpr (BRANCH) {
+            if (K > 12288) FQN_LAUNCH(8, 4, false);
+            else FQN_LAUNCH(8, 3, false);
+        }
     } else if (K > 8192) FQN_LAUNCH(16, 2, false);
-    else if (K > 4096) FQN_LAUNCH(8, 2, false);
+    else if (BRANCH && K > 4096 && K <= 6144) {
+        if constexpr (BRANCH) FQN_LAUNCH(4, 3, false);
+    } else if (K > 4096) FQN_LAUNCH(8, 2, false);
     else if (K > 2048 || M <= 1536) FQN_LAUNCH(4, 2, false);
     else FQN_LAUNCH(1, 4, false);
 #undef FQN_LAUNCH

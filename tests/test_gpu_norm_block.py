@@ -37,7 +37,7 @@ def stream(x, r, post, gate, scale):
     return h, 2.0 ** -8 * h.abs() + 2.0 ** -19 * (b.abs() + r.double().abs()) + 1e-38
 
 
-CASES = [(1, 8), (1, 4096), (3, 128), (37, 2048), (2000, 1024), (5, 4104), (300, 5120), (9, 8192), (64, 11008), (3, 16384), (4, 20000), (2, 32768), (3, 40000)]
+CASES = [(1, 8), (1, 4096), (3, 128), (37, 2048), (2000, 1024), (5, 4104), (300, 5120), (7, 6144), (3, 6152), (9, 8192), (2, 8200), (64, 11008), (5, 12288), (3, 12296), (3, 16384), (4, 20000), (2, 32768), (3, 40000)]
 
 
 @pytest.mark.parametrize("M, K", CASES)
