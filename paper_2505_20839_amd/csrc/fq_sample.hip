@@ -798,14 +798,7 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
     if (listing) {
         find.n = __hip_atomic_load(&border->listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if (find.n <= FQS_LIST)
-            for (int i0 = t; i0 < find.n; i0 += 8 * FQS_T1) {   // (eight requested at a time)
-                fqs_u64 v[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = i0 + u * FQS_T1 < find.n ? fqs_fetch(w.list + (size_t)b * FQS_LIST + i0 + u * FQS_T1) : 0ull;
-#pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    if (i0 + u * FQS_T1 < find.n) sh.list[i0 + u * FQS_T1] = v[u];
-            }
+            for (int i = t; i < find.n; i += FQS_T1) sh.list[i] = fqs_fetch(w.list + (size_t)b * FQS_LIST + i);
     }
     if (t == 0) sh.found = 0;
     if (t < parts) part_mass[t] = listing ? fqs_fetch(w.sure + (size_t)b * parts + t) : fqs_scaled(w.total[(size_t)b * parts + t], fqs_factor(w.top[(size_t)b * parts + t], top, r.c));
