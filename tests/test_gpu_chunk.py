@@ -333,3 +333,34 @@ def test_rows_that_no_bound_is_given_for(fq, seqs):
     b = Batch(seqs, 8, 2, 16, 61)
     b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE))
     b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, max_len=2000, window=11), window=11)
+
+
+@pytest.mark.parametrize("seqs", [[(1, 50), (3, 40)], [(60, 90), (9, 33)]])
+def test_pages_past_four_gigabytes(fq, seqs):
+    """The same tokens in near pages and behind 4 GiB of cache: the same output."""
+    b = Batch(seqs, 4, 2, 16, 67)
+    q, qs, cache, table, starts, lens = b.gpu()
+    pages = (1 << 32) // cache[0].numel() + cache.shape[0] + 3
+    far = torch.empty((pages,) + tuple(cache.shape[1:]), dtype=torch.uint8, device="cuda")
+    far[-cache.shape[0]:].copy_(cache)
+    near = fq.fq_kv4_attention_chunk(q, qs, cache, table, starts, lens, SCALE)
+    out = fq.fq_kv4_attention_chunk(q, qs, far, (table + (pages - cache.shape[0])).to(torch.int32), starts, lens, SCALE)
+    assert torch.equal(out.view(torch.int16), near.view(torch.int16))
+
+
+def test_two_calls_at_once(fq):
+    """On two streams, each with scratch of its own: what each gives alone."""
+    a, b = Batch([(1, 1500), (1, 900)], 8, 2, 32, 71), Batch([(80, 700)], 8, 2, 32, 73)
+    args = [a.gpu(), b.gpu()]
+    want = [fq.fq_kv4_attention_chunk(*x, SCALE) for x in args]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = [None, None]
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                for _ in range(4):
+                    got[i] = fq.fq_kv4_attention_chunk(*args[i], SCALE)
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x.view(torch.int16), y.view(torch.int16))

@@ -281,3 +281,31 @@ def test_the_border_of_min_p_at_numbers_of_both_signs(fq, dtype, V, shift):
             run(fq, x, u, m=[m] * 12, T=[T] * 12)
             run(fq, x, u, m=[m] * 12, T=[T] * 12, p=[0.7] * 12)
             run(fq, x, u, m=[m] * 12, T=[T] * 12, k=[V // 4] * 12)
+
+
+def test_rows_past_four_gigabytes(fq):
+    ld, V = 1200 * 1000 * 1000, 40001
+    pool = torch.empty(2 * ld + V + 8, dtype=torch.bfloat16, device="cuda")
+    for n in (4001, V):
+        x = pool.as_strided((3, n), (ld, 1), 3)
+        x.copy_(2.0 * torch.randn((3, n), device="cuda"))
+        run(fq, x, [0.1, 0.5, 0.9], k=[0, 30, 0], p=[1.0, 0.9, 0.8])
+
+
+def test_two_calls_at_once(fq):
+    """On two streams, each with scratch of its own: what each gives alone."""
+    g = torch.Generator(device="cuda").manual_seed(19)
+    xs = [(2.5 * torch.randn((9, V), generator=g, device="cuda")).bfloat16() for V in (70001, 60000)]
+    u, k, p = torch.rand(9, generator=g, device="cuda"), torch.full((9,), 700, dtype=torch.int32, device="cuda"), torch.full((9,), 0.9, device="cuda")
+    want = [fq.fq_sample(x, u, None, k, p) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        got = [None, None]
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                for _ in range(4):
+                    got[i] = fq.fq_sample(xs[i], u, None, k, p)
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
