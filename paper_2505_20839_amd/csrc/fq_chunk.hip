@@ -896,7 +896,8 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
 //     few      up to 32 rows of a head.  16 x 4000 tokens under 32 heads, 8 of keys: 4 new tokens each 24 us (40 by the kernel of many rows), 8 each 31 (41);
 //              for 16 rows the wider tile takes 28.  With 64 rows they meet: 54 and 61, two such sequences 23 and 20, one of 30000 35 and 30.
 //     parts    of many rows: one workgroup a compute unit, or two where that pays.  A step of 64 tokens takes about 1.8 us with one, 2.6 with two, so that half a
-//              microsecond a step is saved (nothing with a cap or a bias, whose vector instructions fill the time); a part adds 1040 bytes a row to
+//              microsecond a step is saved (nothing with a cap or a bias, whose vector instructions fill the time, unless there are several sequences, which
+//              differ: capped, 3 x up to 137 tokens at up to 5888 35 us with two, 46 with one; 7 x 92 at 1392 33, 41); a part adds 1040 bytes a row to
 //              what is joined, at 6 TB/s.  512 tokens at 4096: 4 parts 52 us, 2 parts 71; 33 at 30000: 32 parts 45, 16 52; 200 behind a window of 4096, capped:
 //              4 parts 41, 9 parts 45; 1000 behind a window of 1024: 1 part 32, 2 parts 41.
 struct fqc_plan { int few, slots, chunk; };
@@ -911,7 +912,7 @@ fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int tokens, bool
         p.slots = (tiles + p.chunk - 1) / p.chunk;
     } else {
         const long long one = cus / units > 1 ? cus / units : 1, room = tiles / 8;
-        const double part = (double)T * Hq * 1040 / 6.0e6, saved = shaped ? 0.0 : 0.5 * (tiles / 4) / one, joined = one > 1 ? one * part : 2.5 + 2 * part;   // us
+        const double part = (double)T * Hq * 1040 / 6.0e6, saved = shaped && B == 1 ? 0.0 : 0.5 * (tiles / 4) / one, joined = one > 1 ? one * part : 2.5 + 2 * part;   // us
         const long long want = saved > joined ? 2 * cus / units : one, slots = want < room ? want : room;
         p.slots = (int)(slots < 1 ? 1 : slots > 64 ? 64 : slots);
     }
