@@ -111,3 +111,20 @@ def test_captured(fq):
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
         assert torch.equal(fq.fq_kv4_read(cache, slots)[0], fq.fq_kv4_read(other, slots)[0])
         pos.add_(17)
+
+
+@pytest.mark.parametrize("axis", [0, 2])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_all_pairs_by_one_axis(fq, axis, interleaved):
+    """The one-axis append's queries and cache, whatever the other axes' positions are."""
+    T, Hq, Hkv = 41, 6, 2
+    g = torch.Generator(device="cuda").manual_seed(axis)
+    x = torch.randn((T, (Hq + 2 * Hkv) * 128), generator=g, device="cuda").bfloat16()
+    rot = torch.rand((50, 64, 2), generator=g, device="cuda")
+    pos = torch.full((3, T), 1 << 30, device="cuda", dtype=torch.int32)
+    pos[axis] = torch.randint(0, 50, (T,), generator=g, device="cuda", dtype=torch.int32)
+    slots = torch.randperm(64, generator=g, device="cuda")[:T]
+    a, b = fq.fq_kv4_cache(4, Hkv, 16), fq.fq_kv4_cache(4, Hkv, 16)
+    got = fq.fq_kv4_append_axes(x, rot, pos, [axis] * 64, slots, a, interleaved)
+    want = fq.fq_kv4_append(x, rot, pos[axis].contiguous(), slots, b, interleaved)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]) and torch.equal(a, b)
