@@ -776,7 +776,7 @@ def _block_arguments(where, X, weight, residual, post, gate, gate_rows, scale, o
             raise FireqError(-1, where)
     else:
         gate = _dev(gate, torch.bfloat16, "gate")
-        if gate.numel() != K and (gate.dim() != 2 or gate.shape[1] != K):
+        if gate.shape[1] != K if gate.dim() == 2 else gate.numel() != K:
             raise FireqError(-2, where)
         gates = gate.shape[0] if gate.dim() == 2 else 1
         if not _fits(gates):

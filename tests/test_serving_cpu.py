@@ -168,3 +168,21 @@ def test_reference_ranges_and_scores():
     K[2, 0] = 1e6                                         # capped at 3: e^3 against 1
     o, _ = cu.attention(q, 1.0, (K, V, K, np.zeros((n, 1)), np.ones((n, 1))), 3, 0, 4, 1.0, 3.0, 0.0)
     assert np.allclose(o[:4], np.array([1, 1, np.exp(3), 1]) / (3 + np.exp(3)))
+
+
+def test_gates_of_another_shape(monkeypatch):
+    """K numbers in two dimensions are gates of fewer numbers each, of which rows would be read behind the tensor."""
+    monkeypatch.setattr(binding, "_dev", lambda t, dtype, name: t)
+    monkeypatch.setattr(binding, "_here", lambda *tensors: None)
+    b = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16)     # noqa: E731
+    K = 16
+    rows = torch.zeros(2, dtype=torch.int32)
+    for gate, gate_rows in ((b(2, K // 2), None), (b(2, K // 2), rows), (b(K, 1), rows), (b(K, 1), None), (b(1, 1, K, 1), None), (b(2, K + 1), None), (b(2 * K), None),
+                            (b(2, 2, K), rows)):
+        if gate.numel() == K and gate.dim() != 2:
+            assert binding._block_arguments("x", b(2, K), b(K), b(2, K), None, gate, gate_rows, 1.0, None)[2][4] == 1
+            continue
+        with pytest.raises(binding.FireqError):
+            binding._block_arguments("x", b(2, K), b(K), b(2, K), None, gate, gate_rows, 1.0, None)
+    for gate, gate_rows, gates in ((b(K), None, 1), (b(1, K), None, 1), (b(2, K), None, 2), (b(5, K), rows, 5)):
+        assert binding._block_arguments("x", b(2, K), b(K), b(2, K), None, gate, gate_rows, 1.0, None)[2][4] == gates
