@@ -779,7 +779,7 @@ def _block_arguments(where, X, weight, residual, post, gate, gate_rows, scale, o
         if gate.shape[1] != K if gate.dim() == 2 else gate.numel() != K:
             raise FireqError(-2, where)
         gates = gate.shape[0] if gate.dim() == 2 else 1
-        if not _fits(gates):
+        if gates < 1 or not _fits(gates):
             raise FireqError(-2, where)
         if gate_rows is not None:
             gate_rows = _dev(gate_rows, torch.int32, "gate_rows")

@@ -604,9 +604,9 @@ PyObject* rmsnorm_block(PyObject*, PyObject* const* a, Py_ssize_t n) {
         want(R.sizes() == X.sizes());
         const uint16_t *post = maybe<uint16_t>(a[4], at::kBFloat16, K), *gate = maybe<uint16_t>(a[5], at::kBFloat16, -1);
         int gates = 1;
-        if (gate) {
+        if (a[5] != Py_None) {                                // (the data of an empty tensor are NULL)
             const at::Tensor& g = tensor(a[5]);
-            want(g.dim() == 2 ? g.size(1) == K && g.size(0) <= INT_LIMIT : g.numel() == K);
+            want(g.dim() == 2 ? g.size(1) == K && g.size(0) >= 1 && g.size(0) <= INT_LIMIT : g.numel() == K);
             gates = g.dim() == 2 ? (int)g.size(0) : 1;
         }
         want(gate || a[6] == Py_None);

@@ -20,3 +20,12 @@ def test_gates_of_another_shape(fq, name):  # noqa: F811
     want = getattr(fq, name)(x, w, EPS, r, gate=gate)
     for got in (getattr(fq, name)(x, w, EPS, r, gate=gate.reshape(K)), getattr(fq, name)(x, w, EPS, r, gate=gate.reshape(1, 1, K))):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("name", ["fq_rmsnorm_block", "fq_rmsnorm_block_quant"])
+def test_a_gate_of_no_rows(fq, name):  # noqa: F811
+    x, r, w, _, gate = make(3, 512, 5, 3)
+    rows = torch.zeros(3, dtype=torch.int32, device="cuda")
+    for kw in ({}, {"gate_rows": rows}):
+        with pytest.raises(fq.FireqError):
+            getattr(fq, name)(x, w, EPS, r, gate=gate[:0], **kw)

@@ -177,12 +177,18 @@ def test_gates_of_another_shape(monkeypatch):
     b = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16)     # noqa: E731
     K = 16
     rows = torch.zeros(2, dtype=torch.int32)
-    for gate, gate_rows in ((b(2, K // 2), None), (b(2, K // 2), rows), (b(K, 1), rows), (b(K, 1), None), (b(1, 1, K, 1), None), (b(2, K + 1), None), (b(2 * K), None),
-                            (b(2, 2, K), rows)):
-        if gate.numel() == K and gate.dim() != 2:
-            assert binding._block_arguments("x", b(2, K), b(K), b(2, K), None, gate, gate_rows, 1.0, None)[2][4] == 1
-            continue
+    for gate, gate_rows in ((b(2, K // 2), None), (b(2, K // 2), rows), (b(K, 1), rows), (b(K, 1), None), (b(2, K + 1), None), (b(2 * K), None), (b(2, 2, K), rows)):
         with pytest.raises(binding.FireqError):
             binding._block_arguments("x", b(2, K), b(K), b(2, K), None, gate, gate_rows, 1.0, None)
-    for gate, gate_rows, gates in ((b(K), None, 1), (b(1, K), None, 1), (b(2, K), None, 2), (b(5, K), rows, 5)):
+    for gate, gate_rows, gates in ((b(K), None, 1), (b(1, K), None, 1), (b(1, 1, K), None, 1), (b(2, K), None, 2), (b(5, K), rows, 5)):
         assert binding._block_arguments("x", b(2, K), b(K), b(2, K), None, gate, gate_rows, 1.0, None)[2][4] == gates
+
+
+@pytest.mark.parametrize("rows", [None, torch.zeros(2, dtype=torch.int32)])
+def test_a_gate_of_no_rows(monkeypatch, rows):
+    """A table without a gate is refused, and not taken for no gate (its data are NULL)."""
+    monkeypatch.setattr(binding, "_dev", lambda t, dtype, name: t)
+    monkeypatch.setattr(binding, "_here", lambda *tensors: None)
+    x = torch.zeros((2, 16), dtype=torch.bfloat16)
+    with pytest.raises(binding.FireqError):
+        binding._block_arguments("x", x, x[0], x, None, x[:0], rows, 1.0, None)
