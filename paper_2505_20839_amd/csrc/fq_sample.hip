@@ -801,7 +801,15 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
             for (int i = t; i < find.n; i += FQS_T1) sh.list[i] = fqs_fetch(w.list + (size_t)b * FQS_LIST + i);
     }
     if (t == 0) sh.found = 0;
-    if (t < parts) part_mass[t] = listing ? fqs_fetch(w.sure + (size_t)b * parts + t) : fqs_scaled(w.total[(size_t)b * parts + t], fqs_factor(w.top[(size_t)b * parts + t], top, r.c));
+    if (t < parts) {
+        if (listing) {
+            part_mass[t] = fqs_fetch(w.sure + (size_t)b * parts + t);
+        } else {
+            // (min-p may end beyond the bins: of a part whose best lies below that nothing is kept, though its tokens may have a mass together)
+            const float best = w.top[(size_t)b * parts + t];
+            part_mass[t] = fqs_comp<WIDE>(best, 0) >= least ? fqs_scaled(w.total[(size_t)b * parts + t], fqs_factor(best, top, r.c)) : 0ull;
+        }
+    }
     __syncthreads();
     if (listing) least = find.least(*border);
     if (listing) {

@@ -1,0 +1,49 @@
+"""Sampling (fireq_sample.h) where a border, a sum or an exponential ends: tokens that the definition fixes without a tolerance."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def fq():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: torch.cuda.is_available() is False")
+    from paper_2505_20839_amd import binding
+    return binding
+
+
+def draw(fq, x, u, **filters):
+    """Tokens and log-probabilities by the C call, into outputs that hold a token that no row has; filters: a number for all rows."""
+    B, V = x.shape
+    t = {n: torch.full((B,), v, dtype=torch.int32 if n == "k" else torch.float32, device="cuda") for n, v in filters.items()}
+    uu = torch.tensor(u, dtype=torch.float32, device="cuda")
+    token, logprob = torch.full((B,), -7, dtype=torch.int32, device="cuda"), torch.full((B,), 7.0, device="cuda")
+    need = fq.fq_sample_workspace_bytes(B, V)
+    ws = torch.full((max(need, 16),), 0xA5, dtype=torch.uint8, device="cuda")
+    call = fq.lib().fq_sample_bf16_ws if x.dtype == torch.bfloat16 else fq.lib().fq_sample_fp32_ws
+    p = lambda n: t[n].data_ptr() if n in t else 0        # noqa: E731
+    rc = call(x.data_ptr(), x.stride(0), uu.data_ptr(), p("T"), p("k"), p("p"), p("m"), token.data_ptr(), logprob.data_ptr(), B, V, ws.data_ptr() if need else 0, need,
+              torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    torch.cuda.synchronize()
+    return token.tolist(), logprob.tolist()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [30000, 40000, 131072])
+@pytest.mark.parametrize("T", [1.0, 0.25])
+def test_min_p_beyond_the_masses(fq, dtype, V, T):
+    """min-p's border lies where a token has no mass of its own, but thousands of them have one together: those below it are not drawn all the same, and the
+    first token by index that is kept is, also with u = 0."""
+    x = torch.full((4, V), -28.0 * T, dtype=dtype, device="cuda")     # e^-28; the border is at log 1e-12 = -27.6
+    x[:, -1] = 0.0
+    x[2, V // 2:] = -29.0 * T
+    x[3, V // 3] = -1.0 * T
+    token, logprob = draw(fq, x, [0.0, 1e-9, 0.0, 0.0], T=T, m=1e-12)
+    assert token == [V - 1, V - 1, 0, V // 3]             # (the best of the third row is at -28 T: all its tokens are kept)
+    for b in range(4):
+        want = torch.log_softmax(x[b].double() / T, -1)[token[b]].item()
+        assert abs(logprob[b] - want) <= 2.0 ** -23 * abs(want) + 2.0 ** -16 + V * 2.0 ** -33      # (FP32 exponentials; 2^-33 a token)
