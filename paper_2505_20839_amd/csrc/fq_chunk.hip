@@ -265,10 +265,11 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const float f = SHAPED ? 1.0f : qs[r], half = fmaxf(top[r], __shfl_xor(top[r], 32, 64)), over = STEP == 16 ? fmaxf(half, __shfl_xor(half, 16, 64)) : half;
-            // (a row that is not past its slack keeps its reference, whatever the others do)
-            const float best = (over - m[r]) * f > FQA_SLACK ? over : m[r], x = __builtin_amdgcn_exp2f((m[r] - best) * f);
+            // (a row that is not past its slack keeps its reference and its term, whatever the others do)
+            const bool on = (over - m[r]) * f > FQA_SLACK;
+            const float best = on ? over : m[r], x = __builtin_amdgcn_exp2f((m[r] - best) * f);
             m[r] = best;
-            sub[r] = fmaf(best, -f, FQA_LIFT);
+            sub[r] = on ? fmaf(best, -f, FQA_LIFT) : sub[r];
             rescale(r, x);
         }
 #pragma unroll
@@ -370,7 +371,7 @@ __device__ __forceinline__ void fqc_begin(const fqa_queries<RT>& Q, fqa_state<RT
     for (int r = 0; r < RT; ++r) {
         // below every score (sums of 128 products of FP8 numbers and codes, at most 10^9; with a shape, FP32's own range)
         st.m[r] = CAP || BIAS ? FQA_LOWEST : -1.0e30f;
-        st.sub[r] = CAP || BIAS ? -FQA_LOWEST : fminf(1.0e30f * Q.qs[r], -FQA_LOWEST);
+        st.sub[r] = CAP || BIAS ? -FQA_LOWEST : fminf(fmaf(1.0e30f, Q.qs[r], FQA_LIFT), -FQA_LOWEST);   // (a factor of 1e-30 never passes the slack)
         st.l[r] = (fq_v4f){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 8; ++j) st.o[r][j] = (fq_v4f){0.f, 0.f, 0.f, 0.f};
@@ -761,7 +762,7 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
         }
         // (what the reference and its term begin with: fqc_begin)
         m[0] = CAP || BIAS ? FQA_LOWEST : -1.0e30f;
-        float sub[1] = {CAP || BIAS ? -FQA_LOWEST : fminf(1.0e30f * qs[0], -FQA_LOWEST)};
+        float sub[1] = {CAP || BIAS ? -FQA_LOWEST : fminf(fmaf(1.0e30f, qs[0], FQA_LIFT), -FQA_LOWEST)};
         mend(f);
         unpack(f, stage[0]);
         if (t0 + NT < t1) {
