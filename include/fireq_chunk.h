@@ -16,6 +16,7 @@
  *                      seen whole, or any range; a row with no token gets zeros.  A query row in no sequence (before starts[0], behind
  *                      starts[B]) is left as it was.  The products are those of fq_kv4_attention_ws with their error; tanh and the bias are FP32
  *                      (2^-19 of a score), a distance is counted from the row's nearest token on.
+ *                      Scores are below 10^7 in magnitude: a row with larger ones may be NaN, and no other is.
  *                      A key or value whose scale is NaN, or a page number outside the cache, gives NaN to the rows that attend to its tokens, and to no
  *                      other.  A sequence longer than max_len or than table_width * page gives NaN to its rows.
  *                      starts int32 [B + 1], not decreasing, 0 .. T (what lies outside is taken as the nearest of these, and rows of

@@ -23,3 +23,22 @@ def test_scales_next_to_zero_beside_rows_that_begin_later_and_earlier(fq, seqs, 
         out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, first=torch.as_tensor(first).cuda(), end=torch.as_tensor(end).cuda())
         assert torch.isfinite(out.float()).all()
         b.check(out, first=first, end=end, rows=rows)
+
+
+@pytest.mark.parametrize("seqs, Hq, Hkv", [([(4, 300)], 4, 2), ([(4, 1500), (3, 900)], 4, 1), ([(9, 300)], 4, 2), ([(70, 400)], 4, 2)])
+@pytest.mark.parametrize("at", [40, 100, 140, 200])
+@pytest.mark.parametrize("scale", [1e5, 1e7, 1e30])
+def test_rows_beside_those_whose_scores_pass_the_range(fq, seqs, Hq, Hkv, at, scale):  # noqa: F811
+    """Scores of 10^8 to 10^36: no other row of the wave is the worse for them."""
+    b = Batch(seqs, Hq, Hkv, 16, 83)
+    odd = np.arange(b.T) % 3 == 0
+    b.qs[odd] = scale
+    for early in (odd, ~odd):
+        first = np.where(early, 0, at).astype(np.int32)
+        end = np.concatenate([np.full(k, n) for k, n in seqs]).astype(np.int32)
+        rows = [i for i in range(b.T) if (i % 13 < 2 or i == b.T - 1) and not odd[i]]
+        for cap, bias in ((0.0, False), (1e20, False), (0.0, True), (1e10, True)):
+            slopes = np.linspace(0.5, 0.0, Hq).astype(np.float32) if bias else None
+            out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, first=torch.as_tensor(first).cuda(), end=torch.as_tensor(end).cuda(), cap=cap,
+                                            slopes=None if slopes is None else torch.as_tensor(slopes).cuda())
+            b.check(out, first=first, end=end, rows=rows, cap=cap, slopes=slopes)
