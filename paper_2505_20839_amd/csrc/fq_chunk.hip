@@ -480,7 +480,7 @@ __device__ __forceinline__ fqc_span fqc_take_rows(const fqc_args& a, const fqc_p
         const int i = first_row + 16 * r + n < at.nrows ? first_row + 16 * r + n : 0, t = at.token(i);
         const int pos = at.raw - at.count + t;
         int f = a.first ? a.first[at.start + t] : 0, e = a.end ? a.end[at.start + t] : pos + 1;
-        if (a.window > 0 && f < pos - a.window + 1) f = pos - a.window + 1;
+        if (a.window > 0 && pos >= a.window && f <= pos - a.window) f = pos - a.window + 1;   // (a shorter place leaves all; below 0 it would pass 32 bits)
         f = f < 0 ? 0 : f;
         e = e > at.len ? at.len : e;
         const bool none = f >= e, empty = none || first_row + 16 * r + n >= at.nrows;

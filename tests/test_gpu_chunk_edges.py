@@ -42,3 +42,14 @@ def test_rows_beside_those_whose_scores_pass_the_range(fq, seqs, Hq, Hkv, at, sc
             out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, first=torch.as_tensor(first).cuda(), end=torch.as_tensor(end).cuda(), cap=cap,
                                             slopes=None if slopes is None else torch.as_tensor(slopes).cuda())
             b.check(out, first=first, end=end, rows=rows, cap=cap, slopes=slopes)
+
+
+@pytest.mark.parametrize("seqs", [[(4, 1)], [(20, 9), (4, 1)], [(70, 30)]])
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 5, 2 ** 30])
+def test_the_longest_windows_of_rows_before_the_first_token(fq, seqs, window):  # noqa: F811
+    """Fewer cached than new tokens and an end of their own: rows whose place is negative see what a window leaves, which is all."""
+    b = Batch(seqs, 4, 2, 16, 89)
+    end = np.concatenate([np.full(k, n) for k, n in seqs]).astype(np.int32)
+    out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, end=torch.as_tensor(end).cuda(), window=window)
+    b.check(out, end=end, window=window)
+    b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, window=window), window=window)
