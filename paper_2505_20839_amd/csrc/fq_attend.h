@@ -127,7 +127,8 @@ __global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t
     constexpr int ROWS = 8 / GROUPS;                      // of a workgroup
     __shared__ float wm[GROUPS], wl[GROUPS];
     __shared__ fq_v4f wo[GROUPS][32];
-    const int c = threadIdx.x & 31, grp = (int)(threadIdx.x >> 5) % GROUPS, row = (int)blockIdx.x * ROWS + (int)(threadIdx.x >> 5) / GROUPS, n = parts.slots;
+    const int c = threadIdx.x & 31, grp = (int)(threadIdx.x >> 5) % GROUPS, n = parts.slots;
+    const int row = (int)(blockIdx.y * gridDim.x + blockIdx.x) * ROWS + (int)(threadIdx.x >> 5) / GROUPS;
     if (row >= rows) return;                              // (one row a workgroup where there is a barrier)
     if (starts && (row / Hq < starts[0] || row / Hq >= starts[B])) return;   // of no sequence: it has no parts
     const fq_v2f* ml = reinterpret_cast<const fq_v2f*>(parts.ml) + (size_t)row * n;
@@ -170,8 +171,9 @@ __global__ __launch_bounds__(256) void fqa_join_kernel(fqa_parts parts, uint16_t
 constexpr int FQA_JOIN_FEW = 8;
 // starts (or NULL): only the rows of sequences, tokens starts[0] .. starts[B] of Hq rows each.
 inline void fqa_join(const fqa_parts& parts, uint16_t* O, int rows, hipStream_t stream, const int* starts = nullptr, int B = 0, int Hq = 1) {
+    const int most = 1 << 23, high = (rows + most - 1) / most;   // (a grid has fewer than 2^32 threads in a dimension)
     if (parts.slots <= FQA_JOIN_FEW) hipLaunchKernelGGL(fqa_join_kernel<2>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, parts, O, rows, starts, B, Hq);
-    else hipLaunchKernelGGL(fqa_join_kernel<8>, dim3((unsigned)rows), dim3(256), 0, stream, parts, O, rows, starts, B, Hq);
+    else hipLaunchKernelGGL(fqa_join_kernel<8>, dim3((unsigned)((rows + high - 1) / high), (unsigned)high), dim3(256), 0, stream, parts, O, rows, starts, B, Hq);
 }
 
 // Tiles of a part, for `heads` (sequence, key/value head, 16 query rows) of up to `tiles` each; uneven: of several sequences, whose lengths

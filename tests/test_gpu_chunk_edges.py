@@ -53,3 +53,25 @@ def test_the_longest_windows_of_rows_before_the_first_token(fq, seqs, window):  
     out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, end=torch.as_tensor(end).cuda(), window=window)
     b.check(out, end=end, window=window)
     b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, window=window), window=window)
+
+
+def test_rows_past_the_threads_of_a_grid_in_parts(fq):  # noqa: F811
+    """2^24 rows, of which one sequence has a few, in more parts than a wave joins."""
+    b = Batch([(1, 2310)], 32, 1, 32, 101)
+    q, qs, cache, table, starts, lens = b.gpu()
+    want = fq.fq_kv4_attention_chunk(q, qs, cache, table, starts, lens, SCALE, max_new=1, max_len=2310)
+    T = 1 << 19
+    need = fq.fq_kv4_attention_chunk_workspace_bytes(T, 1, 32, 1, 1, 2310)
+    assert need // (T * 32 * 520) > 8
+    far = torch.empty((T, 32, 128), dtype=torch.uint8, device="cuda"), torch.empty((T, 32), device="cuda")
+    out = torch.full((T, 32, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    try:
+        for at in (0, 123457, T - 1):
+            far[0][at], far[1][at] = q[0], qs[0]
+            fq.fq_kv4_attention_chunk(*far, cache, table, starts + at, lens, SCALE, max_new=1, max_len=2310, out=out)
+            assert torch.equal(out[at].view(torch.int16), want[0].view(torch.int16))
+            out[at] = 7.0
+            assert all(bool((x == 7.0).all()) for x in out.split(1 << 17))   # rows of no sequence
+    finally:
+        del far, out
+        torch.cuda.empty_cache()
