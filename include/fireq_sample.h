@@ -9,8 +9,9 @@
  * token[b] is the first token, by index, at which the kept mass up to it passes u times the whole kept mass (u is taken as one of [0, 1 - 2^-24]), and
  * logprob[b] = log softmax(x / T)[token], over all V.  T = 0 takes the best token, and its log-probability at T = 1.
  *
- * -infinity is a token of no mass.  Exponentials are FP32 and sums those of whole numbers of 2^-32 of the largest of the row or of a part of it (the log-probability's may be FP32's): a token below 2^-33 of
- * the row's best may be taken as one of no mass.  Results do not depend on the order in which anything runs.
+ * -infinity is a token of no mass.  Exponentials are FP32 and sums those of whole numbers, of which the largest of the row, or of a part of it, has
+ * 2^32 - 2^8 (the log-probability's may be FP32's): a token below 2^-32 of the row's best may be taken as one of no mass.  Results do not depend on the
+ * order in which anything runs.
  * A row with a NaN or +infinity, with no token above -infinity, with T negative or not finite, or with u, p or m NaN, gives token -1 and
  * logprob NaN.
  *

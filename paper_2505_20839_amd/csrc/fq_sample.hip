@@ -3,8 +3,8 @@
 // min-p, top-k and top-p all keep a first run of the tokens in one order (larger logit first, lower index first among equals), so
 // what is kept is comp >= least for one number: comp = (ordered bits of the logit, inverted index).  It is found without sorting: of rows
 // of up to 32761 logits by a workgroup each (fqs_row_kernel), of longer ones by three kernels:
-//     parts    a row is cut into parts of up to 8192 logits.  Each finds its largest logit, takes e = exp((x - largest) / T) as a whole number of
-//              2^-32 (sums of whole numbers do not depend on their order; a token below 2^-33 of its part's best has no mass) and, where the row is
+//     parts    a row is cut into parts of up to 8192 logits.  Each finds its largest logit, takes e = exp((x - largest) / T) in whole numbers of
+//              2^-32 (fq_mass.h; their sums do not depend on their order, and a token below 2^-33 of its part's best has no mass) and, where the row is
 //              filtered at all, counts numbers and masses in FQS_BINS equal steps of x / T.  The steps lie on one grid for all parts.
 //     borders  a workgroup per row adds the parts' bins and finds the bin in which min-p or top-k end, and those in which top-p may.
 //     draw     the parts again: the tokens of those bins into a list.  The row's last workgroup selects among them, by number and then by mass, eight
@@ -16,13 +16,13 @@
 
 #include "fq_common.h"
 #include "fq_kernels.h"
+#include "fq_mass.h"
 
 namespace {
 
 typedef unsigned long long fqs_u64;
 
 constexpr int FQS_BINS = 512, FQS_LIST = 4096, FQS_ROW_LIST = 2048, FQS_T1 = 256, FQS_MOST_PARTS = 256;
-constexpr float FQS_UNIT = 0x1p32f;                       // masses in 2^-32 of the largest
 constexpr float FQS_SPAN = 23.0f;                         // nats that the bins cover: e^-23 is below 2^-33
 constexpr fqs_u64 FQS_MASS = (1ull << 50) - 1;            // a part's bin: number of tokens << 50 | mass (8192 * 2^32 at most)
 
@@ -84,7 +84,7 @@ __device__ __forceinline__ float fqs_line(float x, float steps) {
     return x > -__builtin_inff() ? y : x;
 }
 __device__ __forceinline__ fqs_u64 fqs_mass(float x, float top, float c) {
-    return (unsigned)rintf(__builtin_amdgcn_exp2f((x - top) * c) * FQS_UNIT);   // (the conversion ends at 2^32 - 1)
+    return fqs_units(__builtin_amdgcn_exp2f((x - top) * c));
 }
 
 // Bits that order as the numbers do (-0 as 0), 16 of bf16 and 32 of FP32, above the inverted index.
@@ -870,7 +870,7 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
                 }
             }
         a.token[b] = token;
-        if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)border->total * 0x1p-32));
+        if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)border->total / FQS_UNIT));
     }
 }
 
@@ -1007,7 +1007,7 @@ __global__ __launch_bounds__(1024) void fqs_row_kernel(fq_sample_args a) {
     const float u = fminf(fmaxf(a.u[b], 0.0f), 0x1.fffffep-1f);
     auto answer = [&](int token, float value) __attribute__((always_inline)) {
         a.token[b] = token;
-        if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)total * 0x1p-32));
+        if (a.logprob) a.logprob[b] = (float)(((double)value - (double)top) / r.T - log((double)total / FQS_UNIT));
     };
     if (r.k > 0 || r.p < 1.0f) {
         auto tokens = [&](auto f) __attribute__((always_inline)) {
@@ -1035,7 +1035,7 @@ __global__ __launch_bounds__(1024) void fqs_row_kernel(fq_sample_args a) {
                     const float v = x[e], weight = __builtin_amdgcn_exp2f((v - top) * r.c), d = line - fqs_line(v, r.steps);
                     if (v >= cut && weight >= lightest && d < (float)FQS_BINS) {
                         if (r.k > 0) atomicAdd(&count_of_bin[(int)d], 1u);
-                        if (r.p < 1.0f) atomicAdd(&mass_of_bin[(int)d], (fqs_u64)(unsigned)rintf(weight * FQS_UNIT));
+                        if (r.p < 1.0f) atomicAdd(&mass_of_bin[(int)d], (fqs_u64)fqs_units(weight));
                     }
                 }
             });

@@ -47,3 +47,19 @@ def test_min_p_beyond_the_masses(fq, dtype, V, T):
     for b in range(4):
         want = torch.log_softmax(x[b].double() / T, -1)[token[b]].item()
         assert abs(logprob[b] - want) <= 2.0 ** -23 * abs(want) + 2.0 ** -16 + V * 2.0 ** -33      # (FP32 exponentials; 2^-33 a token)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [3, 1000, 40000])
+def test_shares_that_add_up_to_one(fq, dtype, V):
+    """The best token and two of half its mass, or four of a quarter: the best alone has half of all."""
+    x = torch.full((2, V), -math.inf, dtype=dtype, device="cuda")
+    x[:, 0] = 0.0
+    x[0, -2:] = -1.0
+    x[1, -min(V - 1, 4):] = -2.0
+    T = 1.4426950216293335                                # log2 e in FP32, a little less: e^(-1/T) is 2^-1 (1 - 10^-8)
+    for k in (0, min(V, 30)):
+        token, _ = draw(fq, x, [0.9999, 0.9999], T=T, p=0.5, k=k)
+        assert token == [0, 0]
+        token, _ = draw(fq, x, [0.9999, 0.9999], T=T, p=0.6, k=k)
+        assert token[0] == V - 2                           # (three fifths need one more, the first by index)
