@@ -995,15 +995,26 @@ __global__ __launch_bounds__(1024) void fqs_row_kernel(fq_sample_args a) {
                 ++at;
             }
     };
-    // (its sum is FP32's: a thread's numbers in their order)
-    float sum = 0.f;
-    each(std::true_type(), [&](int c, const fqs_pack<WIDE>& x) __attribute__((always_inline)) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f((x[e] - top) * r.c);
-        if (listing) note(c, x, cut);
-    });
+    // the mass of all tokens: in whole numbers where top-p alone takes its part of it; otherwise it is the log-probability's, and FP32's (a thread's numbers in
+    // their order)
+    const bool by_mass_alone = r.p < 1.0f && r.k == 0 && !(r.low > 0.0f);
     fqs_u64 total;
-    fqs_scan<THREADS>((fqs_u64)(sum * FQS_UNIT), sh.scan, total);
+    if (by_mass_alone) {
+        fqs_u64 sum = 0;
+        each(std::true_type(), [&](int, const fqs_pack<WIDE>& x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += fqs_mass(x[e], top, r.c);
+        });
+        fqs_scan<THREADS>(sum, sh.scan, total);
+    } else {
+        float sum = 0.f;
+        each(std::true_type(), [&](int c, const fqs_pack<WIDE>& x) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += __builtin_amdgcn_exp2f((x[e] - top) * r.c);
+            if (listing) note(c, x, cut);
+        });
+        fqs_scan<THREADS>((fqs_u64)(sum * FQS_UNIT), sh.scan, total);
+    }
     const float u = fminf(fmaxf(a.u[b], 0.0f), 0x1.fffffep-1f);
     auto answer = [&](int token, float value) __attribute__((always_inline)) {
         a.token[b] = token;
@@ -1024,7 +1035,6 @@ __global__ __launch_bounds__(1024) void fqs_row_kernel(fq_sample_args a) {
             return;
         } else {
             // numbers and masses in bins.  top-p alone: tokens with less than half (1 - p) / V of the mass do not reach what it leaves out
-            const bool by_mass_alone = r.k == 0 && !(r.low > 0.0f);
             const float lightest = by_mass_alone ? 0.49f * (1.0f - fmaxf(r.p, 0.0f)) * ((float)total * (1.0f / FQS_UNIT)) / (float)a.V : 0.0f;
             __syncthreads();
             if (t == 0) listed = 0;

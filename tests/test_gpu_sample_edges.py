@@ -63,3 +63,27 @@ def test_shares_that_add_up_to_one(fq, dtype, V):
         assert token == [0, 0]
         token, _ = draw(fq, x, [0.9999, 0.9999], T=T, p=0.6, k=k)
         assert token[0] == V - 2                           # (three fifths need one more, the first by index)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [4, 8, 1000, 8192, 32760, 40000, 131072])
+@pytest.mark.parametrize("k", [0, -1])
+def test_top_p_of_equal_logits(fq, dtype, V, k):
+    """All alike: the first half of the tokens has half of the mass, and a quarter a quarter, in whole numbers."""
+    x = torch.full((3, V), 1.5, dtype=dtype, device="cuda")
+    for p, kept in ((0.5, V // 2), (0.25, V // 4), (0.75, 3 * V // 4)):
+        token, _ = draw(fq, x, [0.0, 0.5, 1 - 2.0 ** -24], p=p, k=k)
+        assert token == [0, kept // 2, kept - 1]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [20000, 32000, 32761, 40000])
+@pytest.mark.parametrize("p", [0.9995, 0.9999, 0.99999])
+def test_top_p_of_many_small_masses(fq, dtype, V, p):
+    """One token and thousands of 2^-25 of its mass: what top-p leaves out is counted in these, and none is lost beside the large one."""
+    x = torch.full((1, V), -25.0, dtype=dtype, device="cuda")
+    x[:, 0] = 0.0
+    p = torch.tensor(p, dtype=torch.float32).item()
+    kept = math.ceil((p * (1 + (V - 1) * 2.0 ** -25) - 1) * 2 ** 25)     # of the small ones, the first by index
+    token, _ = draw(fq, x, [1 - 2.0 ** -24], T=1.4426950216293335, p=p)
+    assert kept - 3 <= token[0] <= kept                    # (u leaves out two of them, and a small mass is 128 - 2^-17 of the units)
