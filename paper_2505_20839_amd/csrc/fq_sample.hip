@@ -970,7 +970,7 @@ __global__ __launch_bounds__(1024) void fqs_row_kernel(fq_sample_args a) {
         __syncthreads();
         if (sh.found < FQS_BINS) {
             const float x = (line - (float)sh.found) / r.steps;
-            cut = x - fabsf(x) * 0x1p-20f;                // (a number in that bin is not below)
+            cut = x - fmaxf(fabsf(x) * 0x1p-20f, 0x1p-149f / r.steps);   // (a number in that bin is not below, nor one whose steps underflow to it)
             listing = true;
         }
     }

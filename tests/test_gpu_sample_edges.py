@@ -87,3 +87,17 @@ def test_top_p_of_many_small_masses(fq, dtype, V, p):
     kept = math.ceil((p * (1 + (V - 1) * 2.0 ** -25) - 1) * 2 ** 25)     # of the small ones, the first by index
     token, _ = draw(fq, x, [1 - 2.0 ** -24], T=1.4426950216293335, p=p)
     assert kept - 3 <= token[0] <= kept                    # (u leaves out two of them, and a small mass is 128 - 2^-17 of the units)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [1000, 30000])
+@pytest.mark.parametrize("T", [1.0, 1e8, 1e30])
+def test_top_k_of_logits_next_to_zero(fq, dtype, V, T):
+    """Logits whose steps of x / T underflow: 0, then the others, of which the first by index is kept beside it."""
+    x = torch.full((3, V), -2.0 ** -133, dtype=dtype, device="cuda")
+    x[:, V // 2] = 0.0
+    x[2] *= 2.0
+    x[2, 7] = -2.0 ** -133
+    token, logprob = draw(fq, x, [0.2, 0.8, 0.2], T=T, k=2)
+    assert token == [0, V // 2, 7]
+    assert all(abs(v + math.log(V)) < 1e-4 for v in logprob)
