@@ -25,7 +25,7 @@
  *                      split, and max_new may be wrong at the cost of time alone.
  * Scratch: fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len) bytes (often 0), 16-byte aligned, under the rules of fireq_paged.h.
  *
- * window >= 0; cap >= 0 and finite, 0 or at least 2^-60; out_scale / cap finite; T < 2^23, T * Hq <= 2^25, B <= 65535, T * Hq / 16 + B * Hkv below 2^24, T * (Hq + 2 Hkv) below 2^28 - 16 (append); the other sizes, strides and alignments,
+ * window >= 0; cap >= 0 and finite, 0 or at least 2^-60 (one above 2^100 counts as 2^100); out_scale / cap finite; T < 2^23, T * Hq <= 2^25, B <= 65535, T * Hq / 16 + B * Hkv below 2^24, T * (Hq + 2 Hkv) below 2^28 - 16 (append); the other sizes, strides and alignments,
  * outputs that overlap nothing, and status codes as in fireq_paged.h.  T = 0 or B = 0 is a successful no-op.
  */
 #ifndef FIREQ_CHUNK_H

@@ -953,9 +953,10 @@ size_t fq_chunk_scratch_bytes(int T, int B, int Hq, int Hkv, int max_new, int ma
 
 void fq_launch_chunk(const fq_chunk_args& x, void* scratch, hipStream_t stream) {
     const fqc_plan p = fqc_choose(x);
+    const float cap = x.cap < 0x1p100f ? x.cap : 0x1p100f;   // (no score comes near it; twice a larger one, or its inverse, would leave FP32's normal numbers)
     fqc_args a = {x.Q, x.q_scale, x.c, x.table, x.starts, x.lens, x.first, x.end, x.slopes, x.width, x.window, x.T, x.B, x.Hq, x.Hkv, x.max_len, p.slots, p.chunk,
-                  x.out_scale, x.cap > 0.f ? 1.0f / x.cap : 0.f, {}, x.O};
-    const double c[5] = {0x1.fffffcp-1, -0x1.5551b8p-2, 0x1.107a08p-3, -0x1.a88656p-5, 0x1.ed307ap-7}, k1 = 1.44269504088896340736 * x.cap;
+                  x.out_scale, cap > 0.f ? 1.0f / cap : 0.f, {}, x.O};
+    const double c[5] = {0x1.fffffcp-1, -0x1.5551b8p-2, 0x1.107a08p-3, -0x1.a88656p-5, 0x1.ed307ap-7}, k1 = 1.44269504088896340736 * cap;
     const double t[3] = {0x1.ffffcep-1, -0x1.550db4p-2, 0x1.0193e6p-3};
     for (int i = 0; i < 5; ++i) a.shape.k[i] = (float)(k1 * c[i]);
     for (int i = 0; i < 3; ++i) a.shape.t[i] = (float)(k1 * t[i]);

@@ -75,3 +75,11 @@ def test_rows_past_the_threads_of_a_grid_in_parts(fq):  # noqa: F811
     finally:
         del far, out
         torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("seqs", [[(1, 60), (9, 120)], [(70, 150)]])
+@pytest.mark.parametrize("cap", [2.0 ** 99, 2.0 ** 100, 1e35, 1e38, 2e38, 3.4e38])
+def test_caps_up_to_the_largest_number(fq, seqs, cap):  # noqa: F811
+    b = Batch(seqs, 4, 2, 16, 97)
+    b.qs[::2] *= 1e-3
+    b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, cap=cap), cap=cap)
