@@ -7,7 +7,8 @@
  *     of these the first k                                  (k <= 0: all)
  *     of these the least first number whose mass, sum exp(x / T), is at least p times theirs   (p >= 1: all; p <= 0: the first)
  * token[b] is the first token, by index, at which the kept mass up to it passes u times the whole kept mass (u is taken as one of [0, 1 - 2^-24]), and
- * logprob[b] = log softmax(x / T)[token], over all V.  T = 0 takes the best token, and its log-probability at T = 1.
+ * logprob[b] = log softmax(x / T)[token], over all V.  T = 0 takes the best token, and its log-probability at T = 1.  Any other T counts as
+ * one of 2^-100 .. 2^100.
  *
  * -infinity is a token of no mass.  Exponentials are FP32 and sums those of whole numbers, of which the largest of the row, or of a part of it, has
  * 2^32 - 2^8 (the log-probability's may be FP32's): a token below 2^-32 of the row's best may be taken as one of no mass.  Results do not depend on the

@@ -101,3 +101,13 @@ def test_top_k_of_logits_next_to_zero(fq, dtype, V, T):
     token, logprob = draw(fq, x, [0.2, 0.8, 0.2], T=T, k=2)
     assert token == [0, V // 2, 7]
     assert all(abs(v + math.log(V)) < 1e-4 for v in logprob)
+
+
+@pytest.mark.parametrize("V", [3000, 40000])
+def test_temperatures_past_their_range(fq, V):
+    """A temperature outside 2^-100 .. 2^100 counts as the nearest of these."""
+    x = torch.zeros((2, V), device="cuda")
+    x[0, 1::2], x[1, 1::2] = -1.5 * 2.0 ** 100, -1.5 * 2.0 ** -100
+    for T, same in ((3e38, 2.0 ** 100), (2.0 ** 101, 2.0 ** 100), (1e-38, 2.0 ** -100), (2.0 ** -149, 2.0 ** -100)):
+        for u in (0.1, 0.93):
+            assert draw(fq, x, [u, u], T=T) == draw(fq, x, [u, u], T=same)
