@@ -12,8 +12,9 @@
  *   fq_rmsnorm_block           Y_bf16[m,k] = bf16(y)
  *   fq_rmsnorm_block_quant_ws  codes, row scales and (workspace != NULL) the prepared workspace of the next layer, as fq_rmsnorm_quant_ws
  *
- * A row of X with a number that is not finite, or whose squares pass FP32's range under a norm of its own, is NaN in H, and so is a row whose
- * gate lies outside the gates; what is NaN or infinite in H does to y, codes and scales what it does in fireq_norm.h.
+ * Under a norm of its own a row of X with a number that is not finite, or whose squares pass FP32's range, is NaN in H; without one (post_bf16 == NULL) such
+ * a number is what the formula makes of it, and the row's others are theirs.  A row whose gate lies outside the gates is NaN in H in either form.  What is
+ * NaN or infinite in H does to y, codes and scales what it does in fireq_norm.h.
  *
  *   X_bf16, R_bf16, H_bf16, Y_bf16 [M,K] and gate_bf16 [gates,K] row-major, w_bf16, post_bf16 [K], all 16-byte aligned; gate_rows int32 [M].
  *   eps > 0 and scale finite; K a positive multiple of 8; M < 2^22; 1 <= gates.  H_bf16 may be R_bf16 or X_bf16 itself, Y_bf16 X_bf16 or R_bf16; any
