@@ -896,11 +896,15 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
 // (a multiple of 4; more where that many parts would not hold a row's tokens).  `tokens` bounds those of a row.
 //     few      up to 32 rows of a head.  16 x 4000 tokens under 32 heads, 8 of keys: 4 new tokens each 24 us (40 by the kernel of many rows), 8 each 31 (41);
 //              for 16 rows the wider tile takes 28.  With 64 rows they meet: 54 and 61, two such sequences 23 and 20, one of 30000 35 and 30.
-//     parts    of many rows: one workgroup a compute unit, or two where that pays.  A step of 64 tokens takes about 1.8 us with one, 2.6 with two, so that half a
-//              microsecond a step is saved (nothing with a cap or a bias, whose vector instructions fill the time, unless there are several sequences, which
-//              differ: capped, 3 x up to 137 tokens at up to 5888 35 us with two, 46 with one; 7 x 92 at 1392 33, 41); a part adds 1040 bytes a row to
-//              what is joined, at 6 TB/s.  512 tokens at 4096: 4 parts 52 us, 2 parts 71; 33 at 30000: 32 parts 45, 16 52; 200 behind a window of 4096, capped:
-//              4 parts 41, 9 parts 45; 1000 behind a window of 1024: 1 part 32, 2 parts 41.
+//     parts    of many rows: one workgroup a compute unit, or two where that pays.  A step of 64 tokens takes about 1.2 us with one and 1.8 with two, 1.6 and
+//              2.5 with a cap or a bias; a part adds 1040 bytes a row to what is joined, at 6 TB/s, and with more than 8 a row takes a workgroup there
+//              (1.3 ns a row).  us by the parts, one sequence, the choice here first:
+//                  plain, half a microsecond a step saved: 500 tokens at 4000, 4 parts 46; 2 53     33 at 30000, 32 40; 16 47     640 at 4000, 3 54; 1 78
+//                  1000 at 1400, 1 32; 2 41     1000 behind a window of 1024, 1 32; 2 41     but 200 at 4096, 9 38; 8 28; 4 30 (its join)
+//                  capped, what its steps cost: 640 at 4000, 3 69; 1 107     640 at 1400, 3 35; 1 41     768 at 1400, 1 42; 2 44     1000 at 1400, 1 42; 2 50
+//                  1000 at 4000, 2 99; 1 107     256 at 4096, 8 36; 4 49     200 at 30000, 9 149; 4 204     64 at 30000, 32 57; 16 88     200 behind a window
+//                  of 4096, 4 38; 9 43     500 at 1400, 2 34; 4 33
+//                  several: 2 x 320 at 1400, 3 38; 1 41     5 x 128, 3 37; 1 41     but 7 x 92 at 1392, 3 48; 1 41     3 x 40 at 8000, 8 53; 16 49
 struct fqc_plan { int few, slots, chunk; };
 fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int tokens, bool shaped) {
     const int G = Hq / Hkv, cus = fq_device_cus();
@@ -913,8 +917,15 @@ fqc_plan fqc_choose(int T, int B, int Hq, int Hkv, int max_new, int tokens, bool
         p.slots = (tiles + p.chunk - 1) / p.chunk;
     } else {
         const long long one = cus / units > 1 ? cus / units : 1, room = tiles / 8;
-        const double part = (double)T * Hq * 1040 / 6.0e6, saved = shaped && B == 1 ? 0.0 : 0.5 * (tiles / 4) / one, joined = one > 1 ? one * part : 2.5 + 2 * part;   // us
-        const long long want = saved > joined ? 2 * cus / units : one, slots = want < room ? want : room;
+        const long long two = 2 * cus / units;
+        const double part = (double)T * Hq * 1040 / 6.0e6, steps = tiles / 4;   // us
+        double saved = 0.5 * steps / one, joined = one > 1 ? one * part : 2.5 + 2 * part;
+        if (shaped) {
+            saved = two > one ? 1.6 * steps * (1.0 / one - 1.53 / two) : 0.0;
+            joined = one > 1 ? (two - one) * part : 2.5 + two * part;
+            if (two > FQA_JOIN_FEW) joined += 1.3e-3 * T * Hq;
+        }
+        const long long want = saved > joined ? two : one, slots = want < room ? want : room;
         p.slots = (int)(slots < 1 ? 1 : slots > 64 ? 64 : slots);
     }
     return p;

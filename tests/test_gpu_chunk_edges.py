@@ -83,3 +83,26 @@ def test_caps_up_to_the_largest_number(fq, seqs, cap):  # noqa: F811
     b = Batch(seqs, 4, 2, 16, 97)
     b.qs[::2] *= 1e-3
     b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, cap=cap), cap=cap)
+
+
+@pytest.mark.parametrize("seqs, Hq, Hkv", [([(64, 2600)], 4, 1), ([(40, 1500)], 4, 2), ([(90, 1900), (45, 700)], 2, 1)])
+@pytest.mark.parametrize("cap, bias", [(25.0, False), (0.0, True), (25.0, True)])
+def test_capped_and_biased_chunks_in_parts(fq, seqs, Hq, Hkv, cap, bias):  # noqa: F811
+    """A few query tiles over some thousand tokens: as many parts as fill the device once or twice."""
+    b = Batch(seqs, Hq, Hkv, 32, 107)
+    slopes = np.linspace(0.3, 0.0, Hq).astype(np.float32) if bias else None
+    rows = [i for i in range(b.T) if i % 17 < 2 or i == b.T - 1]
+    for max_len in (max(n for _, n in seqs), 9000):
+        out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, max_new=max(k for k, _ in seqs), max_len=max_len, cap=cap, slopes=None if slopes is None else torch.as_tensor(slopes).cuda())
+        b.check(out, cap=cap, slopes=slopes, rows=rows)
+
+
+@pytest.mark.parametrize("cap, bias, window", [(0.0, False, 0), (20.0, False, 300), (0.0, True, 0)])
+def test_a_chunk_beside_single_tokens_of_long_caches(fq, cap, bias, window):  # noqa: F811
+    """One sequence brings more rows than a query tile holds, the others one token each at lengths from one to some thousand."""
+    b = Batch([(1, 2600), (200, 700), (1, 1), (1, 1300), (0, 500), (2, 1900)], 4, 2, 32, 103)
+    slopes = np.float32([0.5, 0.05, 0.005, 0.0]) if bias else None
+    rows = [i for i in range(b.T) if i % 29 < 2 or i > 200]
+    for kw in ({}, {"max_new": 200, "max_len": 2600}, {"max_new": 1}):
+        out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, cap=cap, window=window, slopes=None if slopes is None else torch.as_tensor(slopes).cuda(), **kw)
+        b.check(out, cap=cap, window=window, slopes=slopes, rows=rows)
