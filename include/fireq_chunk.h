@@ -22,11 +22,16 @@
  *                      starts int32 [B + 1], not decreasing, 0 .. T (what lies outside is taken as the nearest of these, and rows of
  *                      sequences that overlap are unspecified); first, end int32 [T]; slopes FP32 [Hq], finite (a negative one times any distance, too).
  *                      max_new and max_len are upper bounds of a sequence's rows and of seq_lens that the caller knows; both decide how the work is
- *                      split, and max_new may be wrong at the cost of time alone.
- * Scratch: fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len) bytes (often 0), 16-byte aligned, under the rules of fireq_paged.h.
+ *                      split.  max_new may be wrong: where it is below the truth, that costs time, and scratch for as many parts of T rows as few rows are cut in.
+ *                      One max_new chooses the kernel for all sequences: the single tokens of long caches beside a prompt's chunk are better given a call of
+ *                      their own (a chunk of 2048 and 40 tokens at up to 29251: 593 us in one call; 205 in two, with the first 41 starts and the last 2, of
+ *                      the same Q and O).
+ * Scratch: fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len) bytes (often 0), 16-byte aligned, under the rules of
+ * fireq_paged.h.
  *
- * window >= 0; cap >= 0 and finite, 0 or at least 2^-60 (one above 2^100 counts as 2^100); out_scale / cap finite; T < 2^23, T * Hq <= 2^25, B <= 65535, T * Hq / 16 + B * Hkv below 2^24, T * (Hq + 2 Hkv) below 2^28 - 16 (append); the other sizes, strides and alignments,
- * outputs that overlap nothing, and status codes as in fireq_paged.h.  T = 0 or B = 0 is a successful no-op.
+ * window >= 0; cap >= 0 and finite, 0 or at least 2^-60 (one above 2^100 counts as 2^100); out_scale / cap finite; T < 2^23, T * Hq <= 2^25,
+ * B <= 65535, T * Hq / 16 + B * Hkv below 2^24, T * (Hq + 2 Hkv) below 2^28 - 16 (append); the other sizes, strides and alignments, outputs that
+ * overlap nothing, and status codes as in fireq_paged.h.  T = 0 or B = 0 is a successful no-op.
  */
 #ifndef FIREQ_CHUNK_H
 #define FIREQ_CHUNK_H

@@ -17,8 +17,8 @@
  * logprob NaN.
  *
  * fq_sample_bf16_ws, fq_sample_fp32_ws   logits in bf16, in FP32; aligned to their size, ld >= V; logprob may be NULL.
- * Scratch: fq_sample_workspace_bytes(B, V) bytes (0 up to V = 32761), 16-byte aligned; it may be reused or freed once the work enqueued by the call has finished, and
- * calls that overlap in time need scratch of their own.
+ * Scratch: fq_sample_workspace_bytes(B, V) bytes (0 up to V = 32761), 16-byte aligned; it may be reused or freed once the work enqueued by the call
+ * has finished, and calls that overlap in time need scratch of their own.
  * 1 <= V <= 2^20, B <= 65535; outputs and scratch overlap neither each other nor an input (FQ_ERR_SHAPE).  Conventions and status codes are those of
  * fireq.h; B = 0 is a successful no-op.
  */

@@ -1053,8 +1053,10 @@ def fq_kv4_attention_chunk(Q: torch.Tensor, q_scale: torch.Tensor, cache: torch.
     `out` had them.
 
     `max_new`, `max_len`: upper bounds of a sequence's rows and of seq_lens that the host knows, by default T (1 where there are no more rows than
-    sequences: single tokens) and what the table has room for; both decide how the work is split, and a wrong max_new costs time alone;
-    `workspace` of fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len) bytes is allocated here when not given."""
+    sequences: single tokens) and what the table has room for; both decide how the work is split.  A wrong max_new costs time, and one below the truth
+    scratch.  The single tokens of long caches beside a prompt's chunk are faster in a call of their own (with their part of starts, seq_lens and the
+    table, the same Q and out).  `workspace` of fq_kv4_attention_chunk_workspace_bytes(T, B, Hq, Hkv, max_new, max_len) bytes is allocated here when
+    not given."""
     where = "fq_kv4_attention_chunk"
     r = (_marshal or marshal()).kv4_attention_chunk(Q, q_scale, cache, block_table, starts, seq_lens, out_scale, max_new, max_len, first, end, window, cap,
                                                     slopes, out, workspace)

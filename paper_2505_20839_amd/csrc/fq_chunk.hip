@@ -6,8 +6,8 @@
 //     ranges     a row's tokens are lo <= t < hi.  A wave takes the tiles that any of its rows has; where all of its rows have all of a step's
 //                tokens, no score is compared with a range.
 //     shape      x = cap tanh(out_scale q k / cap) - slope |pos - t|, in units of log2 e.  tanh(y) = y P(y^2) of three terms while every |y| is
-//                at most 5/16 (relative error 2^-19), of five up to 5/8 (2^-23), 1 - 2 / (1 + exp(2 y)) above.  A distance is counted from the row's nearest token: a constant less for
-//                all scores of a row, and exact in FP32 where it counts.
+//                at most 5/16 (relative error 2^-19), of five up to 5/8 (2^-23), 1 - 2 / (1 + exp(2 y)) above.  A distance is counted from the row's
+//                nearest token: a constant less for all scores of a row, and exact in FP32 where it counts.
 //     broken     a value whose scale is NaN must not reach the rows that do not see its token (0 * NaN): its NaN moves to the key's scale,
 //                which makes the probabilities NaN of those rows only that see it; so does a tile of a page outside the cache.
 #include <type_traits>
@@ -160,9 +160,10 @@ __device__ __forceinline__ void fqc_move_nans(fq_v2i& s) {
 }
 
 // Products c of a lane's RT rows and NT times 4 tokens (`first` + i * STEP + e), with the keys' sigmas ks -> probabilities, eight of them a lane's part of
-// the B operand of a product with values.  STEP 16: a row's tokens are shared out among four lanes, 16 apart, STEP 8: two, 32 apart; rescale(r, x) multiplies its sums.  whole: every row has all of the tokens; otherwise the others' scores become -infinity, whose probability is 0 beside any
-// finite reference (a row's before its first token too, and its factor is not 0).  The query tiles go through each stage together: one branch for all,
-// and each one's chain of instructions beside the others'.
+// the B operand of a product with values.  STEP 16: a row's tokens are shared out among four lanes, 16 apart, STEP 8: two, 32 apart; rescale(r, x)
+// multiplies its sums.  whole: every row has all of the tokens; otherwise the others' scores become -infinity, whose probability is 0 beside any finite
+// reference (a row's before its first token too, and its factor is not 0).  The query tiles go through each stage together: one branch for all, and each
+// one's chain of instructions beside the others'.
 template <int RT, int NT, int STEP, bool CAP, bool BIAS, class F>
 __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], const float (&ks)[NT][4], int first, const float (&qs)[RT],
                                                   const fqc_rows<RT>& rows, const fqc_shape& shape, float (&m)[RT], float (&sub)[RT], bool whole,
@@ -264,7 +265,8 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
     if (__any(past))
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            const float f = SHAPED ? 1.0f : qs[r], half = fmaxf(top[r], __shfl_xor(top[r], 32, 64)), over = STEP == 16 ? fmaxf(half, __shfl_xor(half, 16, 64)) : half;
+            const float f = SHAPED ? 1.0f : qs[r], half = fmaxf(top[r], __shfl_xor(top[r], 32, 64));
+            const float over = STEP == 16 ? fmaxf(half, __shfl_xor(half, 16, 64)) : half;
             // (a row that is not past its slack keeps its reference and its term, whatever the others do)
             const bool on = (over - m[r]) * f > FQA_SLACK;
             const float best = on ? over : m[r], x = __builtin_amdgcn_exp2f((m[r] - best) * f);
@@ -289,7 +291,8 @@ __device__ __forceinline__ void fqc_probabilities(const fq_v4f (&c)[RT][NT], con
 // one fused multiply-add with sigma / 16 and -72 sigma makes it sigma * (c - 8), exact (72 sigma has 8 bits and is at most 32256).
 __device__ __forceinline__ fqa_sigmas fqc_value_sigmas(int w) {
     fqa_sigmas s;
-    const fqa_v2h a = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, false), fqa_v2h), b = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, true), fqa_v2h);
+    const fqa_v2h a = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, false), fqa_v2h);
+    const fqa_v2h b = __builtin_convertvector(__builtin_amdgcn_cvt_pk_f32_fp8(w, true), fqa_v2h);
     s.s[0] = a * (fqa_v2h){(_Float16)0.0625f, (_Float16)0.0625f};
     s.s[1] = b * (fqa_v2h){(_Float16)0.0625f, (_Float16)0.0625f};
     s.n[0] = a * (fqa_v2h){(_Float16)-72.f, (_Float16)-72.f};
@@ -301,11 +304,15 @@ __device__ __forceinline__ fqa_sigmas fqc_value_sigmas(int w) {
 // Four tokens' values of a word: nibbles 0 and 2 (tokens 0, 1 and 2, 3 of one channel), 1 and 3 (of the channel 16 on).
 __device__ __forceinline__ void fqc_values4(int w, unsigned mask, unsigned base, const fqa_sigmas& a, fq_v2i& even, fq_v2i& odds) {
     const unsigned x = (unsigned)w;
-    even = (fq_v2i){__builtin_bit_cast(int, fqa_value_pair(x << 4, mask, base, a.s[0], a.n[0])), __builtin_bit_cast(int, fqa_value_pair(x >> 4, mask, base, a.s[1], a.n[1]))};
-    odds = (fq_v2i){__builtin_bit_cast(int, fqa_value_pair(x, mask, base, a.s[0], a.n[0])), __builtin_bit_cast(int, fqa_value_pair(x >> 8, mask, base, a.s[1], a.n[1]))};
+    even = (fq_v2i){__builtin_bit_cast(int, fqa_value_pair(x << 4, mask, base, a.s[0], a.n[0])),
+                    __builtin_bit_cast(int, fqa_value_pair(x >> 4, mask, base, a.s[1], a.n[1]))};
+    odds = (fq_v2i){__builtin_bit_cast(int, fqa_value_pair(x, mask, base, a.s[0], a.n[0])),
+                    __builtin_bit_cast(int, fqa_value_pair(x >> 8, mask, base, a.s[1], a.n[1]))};
 }
-// The lane's values for channels j and j + 1 of 16, j even: word w of each of two tiles (nibble 0: channel j of tokens 0, 1; 2: of tokens 2, 3; 1 and 3: j + 1).
-__device__ __forceinline__ void fqc_values(int w0, int w1, unsigned mask, unsigned base, const fqa_sigmas& a, const fqa_sigmas& b, fqa_v8h& even, fqa_v8h& odds) {
+// The lane's values for channels j and j + 1 of 16, j even: word w of each of two tiles (nibble 0: channel j of tokens 0, 1; 2: of tokens 2, 3; 1 and
+// 3: j + 1).
+__device__ __forceinline__ void fqc_values(int w0, int w1, unsigned mask, unsigned base, const fqa_sigmas& a, const fqa_sigmas& b, fqa_v8h& even,
+                                           fqa_v8h& odds) {
     const unsigned x = (unsigned)w0, y = (unsigned)w1;
     const fqa_v2h e0 = fqa_value_pair(x << 4, mask, base, a.s[0], a.n[0]), e1 = fqa_value_pair(x >> 4, mask, base, a.s[1], a.n[1]);
     const fqa_v2h e2 = fqa_value_pair(y << 4, mask, base, b.s[0], b.n[0]), e3 = fqa_value_pair(y >> 4, mask, base, b.s[1], b.n[1]);
@@ -319,8 +326,8 @@ __device__ __forceinline__ void fqc_values(int w0, int w1, unsigned mask, unsign
 
 // NT (even) tiles from tile tb on.
 template <int RT, int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], unsigned lost, int tb, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows, const fqc_shape& shape,
-                                         fqa_state<RT>& st, bool whole, unsigned mask, unsigned base, int g) {
+__device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], unsigned lost, int tb, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows,
+                                         const fqc_shape& shape, fqa_state<RT>& st, bool whole, unsigned mask, unsigned base, int g) {
     unsigned odd = 0u;
 #pragma unroll
     for (int i = 0; i < NT; ++i) odd |= ((unsigned)now[i].s[1] & 0x7F7F7F7Fu) + 0x01010101u;
@@ -342,11 +349,12 @@ __device__ __forceinline__ void fqc_step(fqa_tile (&now)[NT], unsigned lost, int
         ks[i][0] = s01[0]; ks[i][1] = s01[1]; ks[i][2] = s23[0]; ks[i][3] = s23[1];
     }
     fq_v4i pt[RT][NT / 2];
-    fqc_probabilities<RT, NT, 16, CAP, BIAS>(c, ks, 16 * tb + 4 * g, Q.qs, rows, shape, st.m, st.sub, whole, pt, [&](int r, float x) __attribute__((always_inline)) {
+    auto rescale = [&](int r, float x) __attribute__((always_inline)) {
         st.l[r] *= x;
 #pragma unroll
         for (int j = 0; j < 8; ++j) st.o[r][j] *= x;
-    });
+    };
+    fqc_probabilities<RT, NT, 16, CAP, BIAS>(c, ks, 16 * tb + 4 * g, Q.qs, rows, shape, st.m, st.sub, whole, pt, rescale);
 #pragma unroll
     for (int i = 0; i < NT / 2; ++i) {
         const fqa_sigmas sg[2] = {fqc_value_sigmas(now[2 * i].s[1]), fqc_value_sigmas(now[2 * i + 1].s[1])};
@@ -380,8 +388,8 @@ __device__ __forceinline__ void fqc_begin(const fqa_queries<RT>& Q, fqa_state<RT
 
 // Tiles t0 .. t1 for a wave's rows, the first ones' bytes in `a`; from token `whole0` to `whole1` all rows have all tokens.
 template <int RT, int NT, bool CAP, bool BIAS>
-__device__ __forceinline__ void fqc_range(fqc_cursor& cur, fqa_tile (&a)[NT], unsigned lost_a, int t0, int t1, int whole0, int whole1, const fqa_queries<RT>& Q, const fqc_rows<RT>& rows,
-                                          const fqc_shape& shape, fqa_state<RT>& st, int lane) {
+__device__ __forceinline__ void fqc_range(fqc_cursor& cur, fqa_tile (&a)[NT], unsigned lost_a, int t0, int t1, int whole0, int whole1,
+                                          const fqa_queries<RT>& Q, const fqc_rows<RT>& rows, const fqc_shape& shape, fqa_state<RT>& st, int lane) {
     const int g = lane >> 4;
     fqc_begin<RT, CAP, BIAS>(Q, st);
     unsigned mask = FQC_VALUE_MASK, base = FQC_VALUE_BASE;
@@ -428,8 +436,8 @@ __device__ __forceinline__ fqc_sequence fqc_sequence_of(const fqc_args& a, int k
         n = n - count * stride < stride ? n - count * stride : stride;
         if (stride > 1) continue;
         const int next = __builtin_amdgcn_readlane(first, count < 63 ? count + 1 : 63);
-        return {lo, __builtin_amdgcn_readlane(at, count), __builtin_amdgcn_readlane(first, count), count < 63 && count + 1 < __popcll(__ballot(in)) ? next : fqc_clamp(behind, a.T),
-                __builtin_amdgcn_readlane(len, count)};
+        return {lo, __builtin_amdgcn_readlane(at, count), __builtin_amdgcn_readlane(first, count),
+                count < 63 && count + 1 < __popcll(__ballot(in)) ? next : fqc_clamp(behind, a.T), __builtin_amdgcn_readlane(len, count)};
     }
 }
 
@@ -632,10 +640,9 @@ __global__ __launch_bounds__(64 * KVW, 2) void fqc_few_kernel(fqc_args a, fqa_pa
 // (lane % 32), the tokens 8 k + 4 h + e (h = lane / 32), and a tile's eight are its part of the B operand of a product with 32 channels, values in the same
 // order.  (A vector instruction costs half as much beside a product of 32 x 32 as beside one of 16 x 16, measured with two waves a SIMD.)  sum p: of the
 // rounded numbers, two to an instruction.
-// Bound by instructions: vector 76 %, matrix 28 % of the busy cycles.  8192 new tokens under 32 heads, 8 of keys: 515 to 528 us causal (1041 to 1067 TFLOP/s, at
-// the card's power: its clock falls to 2 GHz), 665 to 715 capped with a prefix seen whole (820 to 880); 4096 with a bias 204 (673); 2048 52 to 54; a
-// tile's own cost shows in 5000 tokens behind a window of one, 22 (60 MB).  Kept on the way there, on
-// the capped one: operands unpacked once a workgroup and not by each wave (1201 us from 2491), masks and tanh's ranges in branches (969, 773), three
+// Bound by instructions: vector 76 %, matrix 28 % of the busy cycles.  8192 new tokens under 32 heads, 8 of keys: 505 to 528 us causal (1041 to 1090
+// TFLOP/s, at the card's power: its clock falls to 2 GHz), 665 to 715 capped with a prefix seen whole (820 to 880); 4096 with a bias 190 to 204 (673);
+// 2048 49 to 52; a tile's own cost shows in 5000 tokens behind a window of one, 22 (60 MB).  Kept on the way there, on the capped one: operands unpacked once a workgroup and not by each wave (1201 us from 2491), masks and tanh's ranges in branches (969, 773), three
 // terms of tanh (719).  16 x 16 products took 696 and, causal, 530 to 558; 64 rows a wave spill.
 struct fqc_stage {
     fq_v4i k[2][2][2][64];                                // keys' bytes: pair of tiles, 64 dimensions, low and high nibbles, lane
@@ -804,11 +811,12 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
             if (now * 16 >= sp.tok1 || (now + NT) * 16 <= sp.tok0) return;   // (none of this wave's rows has any of the tokens)
             const bool whole = now * 16 >= whole0 && (now + NT) * 16 <= whole1;
             fq_v4i pt[1][NT];
-            fqc_probabilities<1, 2 * NT, 8, CAP, BIAS>(c, ks, 16 * now + 4 * h, qs, rows, a.shape, m, sub, whole, pt, [&](int, float x) __attribute__((always_inline)) {
+            auto rescale = [&](int, float x) __attribute__((always_inline)) {
                 l *= x;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) o[j] *= x;
-            });
+            };
+            fqc_probabilities<1, 2 * NT, 8, CAP, BIAS>(c, ks, 16 * now + 4 * h, qs, rows, a.shape, m, sub, whole, pt, rescale);
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
 #pragma unroll
@@ -851,7 +859,8 @@ __global__ __launch_bounds__(256, 2) void fqc_many_kernel(fqc_args a, fqa_parts 
             for (int i = 0; i < 4; ++i) {
                 const int r = 8 * i + (lane >> 3);
                 const size_t to = (size_t)(unsigned)__shfl((int)row, r, 64);
-                if (first_row + r < at.nrows) *reinterpret_cast<fq_v4i*>(dst + to * stride + 16 * (lane & 7)) = *reinterpret_cast<const fq_v4i*>(mine + r * PITCH + 16 * (lane & 7));
+                const fq_v4i x = *reinterpret_cast<const fq_v4i*>(mine + r * PITCH + 16 * (lane & 7));
+                if (first_row + r < at.nrows) *reinterpret_cast<fq_v4i*>(dst + to * stride + 16 * (lane & 7)) = x;
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();

@@ -7,9 +7,10 @@
 // Between two blocks with a norm on both sides (include/fireq_norm_block.h) the stream takes x by its own norm, a gate and a factor first:
 //     h = bf16(r + scale * gate * (x * post / sqrt(mean x^2 + eps)))
 // The same bytes and one more reduction over the row, which is in registers by then (in a second pass over rows that the registers do not hold).  The
-// norm's sums are added in the order of the other forms, so that it is that of the stream, bit for bit.  Measured, calls back to back: 8192 x 4096 to E4M3 45 us (235 MB,
-// 5.2 TB/s: the rate of a copy), 1000 x 5120 to bf16 with a gate row for each of 7 sequences 9.8 us (41 MB, 4.2 TB/s, vector instructions
-// nearly as busy), one row 3.6 us in a graph.
+// norm's sums are added in the order of the other forms, so that it is that of the stream, bit for bit.  Measured, calls back to back: 8192 x 4096 to
+// E4M3 45 us (235 MB, 5.2 TB/s: the rate of a copy), 1000 x 5120 to bf16 with a gate row for each of 7 sequences 9.8 us (41 MB, 4.2 TB/s, vector
+// instructions nearly as busy), one row 3.6 us in a graph.  With a prepared workspace, in a graph, without it in brackets: 100 x 4096 4.3 us (3.9),
+// 1000 x 5120 10.5 (9.8), 4096 x 4096 21.1 (20.6), 8192 x 4096 37.5 (36.2).
 #include <type_traits>
 #include "fq_common.h"
 #include "fq_kernels.h"

@@ -154,8 +154,9 @@ __device__ __forceinline__ int fqp_row_of(int i, int rows) {
 }
 
 // AXES: each pair takes its cosine by a position of its own; a position outside the table in any pair spoils the row.  A wave fetches a token's cosines
-// and sines once, a pair a lane, and they change lanes through its own LDS: 6001 tokens of 48 heads on three axes 28.5 us (4.3 TB/s; vector instructions
-// 80 % of the busy cycles).  Where all turn by one axis the other form is taken, in which every group of lanes fetches its own four pairs: 23.3, 27.0 here.
+// and sines once, a pair a lane, and they change lanes through its own LDS: 6001 tokens of 48 heads on three axes 28.5 to 31 us (4.3 TB/s; vector
+// instructions 80 % of the busy cycles).  Where all turn by one axis the other form is taken, in which every group of lanes fetches its own four pairs: 24, 27
+// here.
 struct fqp_one_axis {};
 template <bool INTERLEAVED, bool AXES>
 __global__ __launch_bounds__(512) void fqp_append_kernel(fqp_append_args a, std::conditional_t<AXES, fq_pair_axes, fqp_one_axis> axes) {

@@ -10,7 +10,7 @@
 //     draw     the parts again: the tokens of those bins into a list.  The row's last workgroup selects among them, by number and then by mass, eight
 //              bits of comp at a time (over the row again, where they are too many for its LDS), and finds the part, and in it the index, at which the
 //              kept mass in index order passes u times its sum.
-// 64 x 131072 of any filters 42 us in a graph: 12, 9 and 23 under a profiler, where reading the logits once takes 3.4; what is left are steps that wait for
+// 64 x 131072 of any filters 42 us in a graph (FP32 45; one row 35 and 33): 12, 9 and 23 under a profiler, where reading the logits once takes 3.4; what is left are steps that wait for
 // each other (67 % of the last kernel's time).  One workgroup a row behind the parts' took 56 (512 rows: 140 and not 178).
 #include <type_traits>
 
@@ -320,8 +320,8 @@ struct fqs_bin_ends {
     fqs_u64 counts[16], masses[16];                       // of waves
     fqs_u64 ends[3][2], at_end[2];                        // of three borders: bin, what lies before it; masses before and up to `end`
 };
-// The borders in o, whose top, line and total are there, from the number and mass of bin t of a thread (0 behind the bins).  whole: the mass of all tokens (0:
-// that of the bins).
+// The borders in o, whose top, line and total are there, from the number and mass of bin t of a thread (0 behind the bins).  whole: the mass of all tokens
+// (0: that of the bins).
 __device__ __forceinline__ void fqs_find_borders(fqs_border& o, const fqs_row& r, bool wide, unsigned count, fqs_u64 mass, fqs_u64 whole, float line, fqs_bin_ends& sh) {
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     fqs_u64 counts = fqs_wave_scan(count), masses = fqs_wave_scan(mass), all = 0;
@@ -874,8 +874,9 @@ __global__ __launch_bounds__(FQS_T1) void fqs_draw_kernel(fq_sample_args a, fqs_
     }
 }
 
-// A row for one workgroup: all of it in one kernel, without scratch.  Bound by one compute unit's vector instructions and by its steps' latency.  In a graph, against the
-// three kernels: 1 x 5000 11 us (28), 1 x 32000 14 (27), 64 rows of any filters 19 and 34 (32 and 35); 64 x 50000 would take 51 (37).
+// A row for one workgroup: all of it in one kernel, without scratch.  Bound by one compute unit's vector instructions and by its steps' latency.  In a
+// graph, against the three kernels: 1 x 5000 11 us (28), 1 x 32000 14.5 (27), 64 rows of any filters 19 and 35 (32 and 35); 64 x 50000 would take 51 (37).
+// FP32: 1 x 32000 14, 64 x 32000 34.
 // Where top-k, or min-p with top-p, leave at most 2048 tokens above a border known beforehand, these are listed in the pass that sums exponentials, and
 // nothing is binned: 1 x 32000 with top-k 50 and top-p 26 us before.  Otherwise the steps are those of the three kernels, with one unit for all masses.
 // Wave w has the chunks 64 n w .. 64 n (w + 1) - 1, n of a lane, 64 apart, and CHUNKS of all fit LDS.
@@ -995,8 +996,8 @@ __global__ __launch_bounds__(1024) void fqs_row_kernel(fq_sample_args a) {
                 ++at;
             }
     };
-    // the mass of all tokens: in whole numbers where top-p alone takes its part of it; otherwise it is the log-probability's, and FP32's (a thread's numbers in
-    // their order)
+    // the mass of all tokens: in whole numbers where top-p alone takes its part of it (8 x 32000 15.6 us for 15.2); otherwise it is the log-probability's,
+    // and FP32's (a thread's numbers in their order)
     const bool by_mass_alone = r.p < 1.0f && r.k == 0 && !(r.low > 0.0f);
     fqs_u64 total;
     if (by_mass_alone) {

@@ -103,6 +103,12 @@ def test_a_chunk_beside_single_tokens_of_long_caches(fq, cap, bias, window):  # 
     b = Batch([(1, 2600), (200, 700), (1, 1), (1, 1300), (0, 500), (2, 1900)], 4, 2, 32, 103)
     slopes = np.float32([0.5, 0.05, 0.005, 0.0]) if bias else None
     rows = [i for i in range(b.T) if i % 29 < 2 or i > 200]
+    shape = dict(cap=cap, window=window, slopes=None if slopes is None else torch.as_tensor(slopes).cuda())
     for kw in ({}, {"max_new": 200, "max_len": 2600}, {"max_new": 1}):
-        out = fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, cap=cap, window=window, slopes=None if slopes is None else torch.as_tensor(slopes).cuda(), **kw)
-        b.check(out, cap=cap, window=window, slopes=slopes, rows=rows)
+        b.check(fq.fq_kv4_attention_chunk(*b.gpu(), SCALE, **shape, **kw), cap=cap, window=window, slopes=slopes, rows=rows)
+    # a call for each run of sequences of one kind, into the same rows
+    q, qs, cache, table, starts, lens = b.gpu()
+    out = torch.full((b.T, 4, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    for lo, hi, new in ((0, 1, 1), (1, 2, 200), (2, 6, 1)):
+        fq.fq_kv4_attention_chunk(q, qs, cache, table[lo:hi], starts[lo:hi + 1], lens[lo:hi], SCALE, max_new=new, out=out, **shape)
+    b.check(out, cap=cap, window=window, slopes=slopes, rows=rows)
