@@ -1,5 +1,7 @@
 """Sampling (fireq_sample.h) where a border, a sum or an exponential ends: tokens that the definition fixes without a tolerance."""
 import math
+import random
+from fractions import Fraction
 
 import pytest
 import torch
@@ -111,3 +113,44 @@ def test_temperatures_past_their_range(fq, V):
     for T, same in ((3e38, 2.0 ** 100), (2.0 ** 101, 2.0 ** 100), (1e-38, 2.0 ** -100), (2.0 ** -149, 2.0 ** -100)):
         for u in (0.1, 0.93):
             assert draw(fq, x, [u, u], T=T) == draw(fq, x, [u, u], T=same)
+
+
+def expected(x, u, k, p, m):
+    """The definition in whole numbers, for whole logits at T = log2 e that lie up to 8 below the best: masses are 2^32 - 2^8 shifted right."""
+    top = max(x)
+    keep = sorted(range(len(x)), key=lambda i: (-x[i], i))
+    if m > 0:
+        keep = [i for i in keep if x[i] >= top + 1.4426950216293335 * math.log(m)]
+    keep = keep[:k] if 0 < k < len(x) else keep
+    mass = lambda i: (2 ** 32 - 2 ** 8) >> (top - x[i])   # noqa: E731
+    if p < 1:
+        want, n = Fraction(p) * sum(map(mass, keep)), 0
+        while n == 0 or sum(map(mass, keep[:n])) < want:
+            n += 1
+        keep = keep[:n]
+    want, c = Fraction(u) * sum(map(mass, keep)), 0
+    for i in sorted(keep):
+        c += mass(i)
+        if c > want:
+            return i
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [1, 5, 64, 300, 2500, 40000])
+def test_tokens_of_exact_masses(fq, dtype, V):
+    """Ties everywhere, borders of every filter on them: the very token of the definition."""
+    rng = random.Random(V)
+    f32 = lambda v: torch.tensor(v, dtype=torch.float32).item()     # noqa: E731
+    for depth in (0, 1, 2, 8):
+        # (long rows: a few tokens at the depths, the others have no mass)
+        some = rng.sample(range(V), min(V, 300))
+        x = torch.full((1, V), -math.inf)
+        x[0, some] = torch.tensor([float(-rng.randint(0, depth)) for _ in some])
+        x = x.to(dtype).cuda()
+        places = sorted(some)
+        y = [int(v) for v in x[0, places].tolist()]
+        for _ in range(12):
+            k, p, m = rng.choice([0, 1, 2, 7, 50, len(y) - 1]), f32(rng.choice([1.0, 0.5, 0.25, 0.0, 0.9, rng.random()])), f32(rng.choice([0.0, 0.0, 0.3, 0.1, 0.01]))
+            u = f32(rng.choice([0.0, 0.5, 1 - 2.0 ** -24, rng.random()]))
+            token, _ = draw(fq, x, [u], T=1.4426950216293335, k=k, p=p, m=m)
+            assert token[0] == places[expected(y, u, k if k < len(y) else 0, p, m)], (depth, k, p, m, u)
