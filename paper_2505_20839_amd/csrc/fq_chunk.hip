@@ -642,8 +642,9 @@ __global__ __launch_bounds__(64 * KVW, 2) void fqc_few_kernel(fqc_args a, fqa_pa
 // rounded numbers, two to an instruction.
 // Bound by instructions: vector 76 %, matrix 28 % of the busy cycles.  8192 new tokens under 32 heads, 8 of keys: 505 to 528 us causal (1041 to 1090
 // TFLOP/s, at the card's power: its clock falls to 2 GHz), 665 to 715 capped with a prefix seen whole (820 to 880); 4096 with a bias 190 to 204 (673);
-// 2048 49 to 52; a tile's own cost shows in 5000 tokens behind a window of one, 22 (60 MB).  Kept on the way there, on the capped one: operands unpacked once a workgroup and not by each wave (1201 us from 2491), masks and tanh's ranges in branches (969, 773), three
-// terms of tanh (719).  16 x 16 products took 696 and, causal, 530 to 558; 64 rows a wave spill.
+// 2048 49 to 52; a tile's own cost shows in 5000 tokens behind a window of one, 22 (60 MB).  Kept on the way there, on the capped one: operands unpacked
+// once a workgroup and not by each wave (1201 us from 2491), masks and tanh's ranges in branches (969, 773), three terms of tanh (719).  16 x 16
+// products took 696 and, causal, 530 to 558; 64 rows a wave spill.
 struct fqc_stage {
     fq_v4i k[2][2][2][64];                                // keys' bytes: pair of tiles, 64 dimensions, low and high nibbles, lane
     fq_v4i v[4][4][64];                                   // values in fp16: tile, 32 channels, lane
@@ -973,7 +974,7 @@ size_t fq_chunk_scratch_bytes(int T, int B, int Hq, int Hkv, int max_new, int ma
 
 void fq_launch_chunk(const fq_chunk_args& x, void* scratch, hipStream_t stream) {
     const fqc_plan p = fqc_choose(x);
-    const float cap = x.cap < 0x1p100f ? x.cap : 0x1p100f;   // (no score comes near it; twice a larger one, or its inverse, would leave FP32's normal numbers)
+    const float cap = x.cap < 0x1p100f ? x.cap : 0x1p100f;   // (no score comes near; a larger one's double or inverse would leave FP32's normal numbers)
     fqc_args a = {x.Q, x.q_scale, x.c, x.table, x.starts, x.lens, x.first, x.end, x.slopes, x.width, x.window, x.T, x.B, x.Hq, x.Hkv, x.max_len, p.slots, p.chunk,
                   x.out_scale, cap > 0.f ? 1.0f / cap : 0.f, {}, x.O};
     const double c[5] = {0x1.fffffcp-1, -0x1.5551b8p-2, 0x1.107a08p-3, -0x1.a88656p-5, 0x1.ed307ap-7}, k1 = 1.44269504088896340736 * cap;

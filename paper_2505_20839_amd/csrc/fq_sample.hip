@@ -10,8 +10,8 @@
 //     draw     the parts again: the tokens of those bins into a list.  The row's last workgroup selects among them, by number and then by mass, eight
 //              bits of comp at a time (over the row again, where they are too many for its LDS), and finds the part, and in it the index, at which the
 //              kept mass in index order passes u times its sum.
-// 64 x 131072 of any filters 42 us in a graph (FP32 45; one row 35 and 33): 12, 9 and 23 under a profiler, where reading the logits once takes 3.4; what is left are steps that wait for
-// each other (67 % of the last kernel's time).  One workgroup a row behind the parts' took 56 (512 rows: 140 and not 178).
+// 64 x 131072 of any filters 42 us in a graph (FP32 45; one row 35 and 33): 12, 9 and 23 under a profiler, where reading the logits once takes 3.4; what
+// is left are steps that wait for each other (67 % of the last kernel's time).  One workgroup a row behind the parts' took 56 (512 rows: 140 and not 178).
 #include <type_traits>
 
 #include "fq_common.h"
